@@ -534,6 +534,44 @@ us_status us_layer_norm_bwd_cast(const us_mat* X, const us_mat* w, const us_mat*
                                  float beta_wc, const us_mat* dX, const us_mat* dXq, const us_mat* dw, const us_mat* dc, void* ws,
                                  size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------ norms of queries and keys, with their rotation
+ *
+ * Root-mean-square norms of queries and keys, head by head, and the rotation of their features by the position of their row, in one
+ * pass (the paper's models have neither; the parts that decoder models put between the query / key projection and attention).  For
+ * the head_width features x of one head of one row:
+ *
+ *   us_qk_norm_fwd   xhat = x / sqrt(mean(x^2) + eps),  n = w * xhat,  y = R n
+ *   us_qk_norm_bwd   n' = R^T g,  u = w * n',  dX = beta_x (u - xhat mean(u * xhat)) / sqrt(mean(x^2) + eps),
+ *                    dw = beta_w * sum over rows and heads of n' * xhat
+ *
+ * R turns the pairs of the first 2 p features, p the pairs of a row of `table`: (a, b) -> (a c - b s, b c + a s) with pair i the features
+ * (i, i + p), or with neighbours = 1 (2 i, 2 i + 1); the other features are not turned.  table [positions x 2 p], F32: cosine c and
+ * sine s of each pair in turn (us_rotary_table).  NULL, ptr NULL or no columns: no rotation.  Row r is at position positions[r] (device
+ * array, one int32 a row), or where that is NULL at start + r % period (period 0: start + r), which must lie in the table
+ * (US_ERR_INVALID_ARG).  A position given on the device that does not lie in it makes what is turned of that row NaN.
+ * A norm gives unit scale and a rotation keeps it: alpha = 1, beta_x = 1; the weights are cut-edges, beta_w = (rows * heads)^-1/2.
+ *
+ * count (1..4) matrices with head_width columns a head -- queries and keys, of which there may be fewer heads -- are worked on by one
+ * launch; X, w, Y, G, dX, dw, beta_w: host arrays of count elements.  X, G: F32, BF16 or F16, any ld >= cols; Y, dX: any us_dtype; w
+ * (1 x head_width; ptr NULL, or the whole array NULL: ones): F32, BF16 or F16.  dw (the same shape and types; ptr NULL or NULL: not wanted) needs a w;
+ * beta_w NULL: ones.  Y may be X and dX may be X or G, with the same pitch and type.  1 <= head_width <= 1024 (US_ERR_UNSUPPORTED beyond).
+ * Pointers need the natural alignment of their elements; matrices of one input type with rows on 16-byte boundaries, heads of
+ * a multiple of 8 features up to 512 of which a multiple of 16 (neighbours: 8) is turned, and a table with rows on 16-byte boundaries take the fast kernels.
+ * Arithmetic in float32.  us_qk_norm_bwd: two launches where there is a dw, which then has a device workspace of us_qk_norm_bwd_workspace_bytes(head_width) bytes, 16-byte
+ * aligned, that no call at the same time uses (US_ERR_WORKSPACE if smaller); its size depends on the current device's SM count.  The sums are formed
+ * without atomics, in a fixed order.
+ *
+ * us_rotary_table: row r of table [positions x 2 p] (F32) receives cosine and sine of (first + r) * scale * base^(-i / p), i = 0 .. p - 1; the
+ * angles are formed in 64 bits, so that far positions keep all digits.  base and scale positive, first >= 0.
+ */
+us_status us_qk_norm_fwd(int count, const us_mat* X, const us_mat* w, const us_mat* Y, int64_t head_width, float eps, const us_mat* table,
+                         const int32_t* positions, int64_t start, int64_t period, int neighbours, void* stream);
+size_t us_qk_norm_bwd_workspace_bytes(int64_t head_width);
+us_status us_qk_norm_bwd(int count, const us_mat* X, const us_mat* w, const us_mat* G, const us_mat* dX, const us_mat* dw, const float* beta_w,
+                         int64_t head_width, float eps, float beta_x, const us_mat* table, const int32_t* positions, int64_t start,
+                         int64_t period, int neighbours, void* ws, size_t ws_bytes, void* stream);
+us_status us_rotary_table(const us_mat* table, double base, double scale, int64_t first, void* stream);
+
 /* ------------------------------------------------------------ quantisation diagnostics
  *
  * us_quant_stats: for v = scale * src (one float32 multiply per element) and a storage format fmt

@@ -251,6 +251,56 @@ def layer_norm_bwd(X, w, G, eps=0.0, beta_x=1.0, beta_wc=None):
 
 # --------------------------------------------------------------------------- storage rounding
 
+# --------------------------------------------------------------------------- norms of queries and keys, with their rotation
+
+def rotary_table(positions, rotated, base=10000.0, scale=1.0, first=0):
+    """[positions x rotated]: cosine and sine, in turn, of (first + r) scale base^(-2 i / rotated)."""
+    i = np.arange(rotated // 2)
+    a = (first + np.arange(positions))[:, None] * scale * base ** (-2.0 * i / max(1, rotated))
+    return np.stack([np.cos(a), np.sin(a)], -1).reshape(positions, rotated)
+
+
+def rotate(v, table, at, neighbours=False, back=False):
+    """Pairs of the first features of v [rows x heads x width] turned by the angles of positions `at`; a position outside the
+    table gives NaN there."""
+    v, table, at = np.asarray(v, np.float64), np.asarray(table, np.float64), np.asarray(at)
+    r = table.shape[1]
+    inside = (at >= 0) & (at < len(table))
+    t = np.where(inside[:, None], table[np.where(inside, at, 0)], np.nan)[:, None]
+    c, s = t[..., ::2], t[..., 1::2]
+    if back:
+        s = -s
+    ia = np.arange(0, r, 2) if neighbours else np.arange(r // 2)
+    ib = ia + 1 if neighbours else ia + r // 2
+    out = v.copy()
+    out[..., ia] = v[..., ia] * c - v[..., ib] * s
+    out[..., ib] = v[..., ib] * c + v[..., ia] * s
+    return out
+
+
+def _heads_of(X, width):
+    X = np.asarray(X, np.float64)
+    return X.reshape(X.shape[0], X.shape[1] // width, width)
+
+
+def qk_norm_fwd(X, w, width, eps, table=None, at=None, neighbours=False):
+    """y = R (w * x / sqrt(mean x^2 + eps)) for each head of `width` features of X [rows x heads * width]."""
+    x = _heads_of(X, width)
+    n = x / np.sqrt(np.mean(x * x, -1, keepdims=True) + _f32(eps)) * (1.0 if w is None else np.asarray(w, np.float64))
+    return (n if table is None else rotate(n, table, at, neighbours)).reshape(np.shape(X))
+
+
+def qk_norm_bwd(X, w, G, width, eps, beta_x=1.0, beta_w=1.0, table=None, at=None, neighbours=False):
+    """(dX, dw) for G = the gradient of qk_norm_fwd's result."""
+    x, n = _heads_of(X, width), _heads_of(G, width)
+    if table is not None:
+        n = rotate(n, table, at, neighbours, back=True)
+    size = np.sqrt(np.mean(x * x, -1, keepdims=True) + _f32(eps))
+    u, xhat = n * (1.0 if w is None else np.asarray(w, np.float64)), x / size
+    dX = _f32(beta_x) * (u - xhat * np.mean(u * xhat, -1, keepdims=True)) / size
+    return dX.reshape(np.shape(X)), _f32(beta_w) * np.sum(n * xhat, (0, 1))
+
+
 def store(v, dtype: str):
     """Round float64 values to a storage format; returns (values float64, codes or None)."""
     if dtype == "f64":          # no rounding: used by exact-arithmetic checks

@@ -42,8 +42,10 @@ int dtype_of(const at::Tensor& t) {
 }
 
 // A 2-D row-major tensor (last stride 1) as a us_mat; a single row has whatever pitch its stride says, but its length at least.
-us_mat describe(PyObject* o) {
+// vector: a 1-D tensor is taken as one row.
+us_mat describe(PyObject* o, bool vector = false) {
   const at::Tensor& t = THPVariable_Unpack(o);
+  if (vector && t.dim() == 1 && (t.size(0) < 2 || t.stride(0) == 1)) return us_mat{t.data_ptr(), dtype_of(t), 1, t.size(0), t.size(0)};
   if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) fail(PyExc_ValueError, "expected a 2-D tensor with unit column stride");
   const int64_t rows = t.size(0), cols = t.size(1), ld = t.stride(0);
   return us_mat{t.data_ptr(), dtype_of(t), rows, cols, rows > 1 ? ld : std::max(cols, ld)};
@@ -51,15 +53,43 @@ us_mat describe(PyObject* o) {
 
 // Argument conversion.  `mats` holds descriptions made for one immediate call.
 struct Args {
-  us_mat mats[16];
-  int used = 0;
+  us_mat mats[32];
+  float numbers[16];
+  int used = 0, numbers_used = 0;
   bool immediate;                                            // tensors are taken only by calls that are not kept
   explicit Args(bool now) : immediate(now) {}
   us_mat* add(PyObject* tensor) {
     if (!immediate) fail(PyExc_TypeError, "a prepared call takes structures");
-    if (used == 16) fail(PyExc_ValueError, "too many tensors");
+    if (used == 32) fail(PyExc_ValueError, "too many tensors");
     mats[used] = describe(tensor);
     return &mats[used++];
+  }
+  // `count` matrices given as a list or tuple of tensors (1-D ones are rows) and Nones
+  us_mat* add_all(PyObject* list, size_t count) {
+    if (!immediate) fail(PyExc_TypeError, "a prepared call takes structures");
+    const size_t n = (size_t)PySequence_Fast_GET_SIZE(list);
+    if (n < count) fail(PyExc_ValueError, "an array is shorter than the count");
+    if (used + n > 32) fail(PyExc_ValueError, "too many tensors");
+    us_mat* first = mats + used;
+    for (size_t i = 0; i < n; ++i) {
+      PyObject* o = PySequence_Fast_GET_ITEM(list, (Py_ssize_t)i);
+      if (o != Py_None && !THPVariable_Check(o)) fail(PyExc_TypeError, "expected tensors");
+      mats[used++] = o == Py_None ? us_mat{} : describe(o, true);
+    }
+    return first;
+  }
+  float* add_numbers(PyObject* list, size_t count) {
+    if (!immediate) fail(PyExc_TypeError, "a prepared call takes structures");
+    const size_t n = (size_t)PySequence_Fast_GET_SIZE(list);
+    if (n < count) fail(PyExc_ValueError, "an array is shorter than the count");
+    if (numbers_used + n > 16) fail(PyExc_ValueError, "too many numbers");
+    float* first = numbers + numbers_used;
+    for (size_t i = 0; i < n; ++i) {
+      const double v = PyFloat_AsDouble(PySequence_Fast_GET_ITEM(list, (Py_ssize_t)i));
+      if (v == -1.0 && PyErr_Occurred()) throw Failed();
+      numbers[numbers_used++] = (float)v;
+    }
+    return first;
   }
 };
 
@@ -95,12 +125,18 @@ constexpr bool kAddress = std::is_same_v<T, void*> || std::is_same_v<T, float*> 
 // ARRAY: a pointer to `count` elements in host memory.
 template <class T, bool ARRAY>
 T convert(PyObject* o, Args& a, size_t count) {
-  if constexpr (std::is_same_v<T, float>) {
+  if constexpr (std::is_floating_point_v<T>) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) throw Failed();
-    return (float)v;
+    return (T)v;
   } else if constexpr (std::is_pointer_v<T>) {
     if (o == Py_None) return nullptr;
+    if constexpr (ARRAY && (std::is_same_v<T, const us_mat*> || std::is_same_v<T, const float*>)) {
+      if (PyTuple_Check(o) || PyList_Check(o)) {
+        if constexpr (std::is_same_v<T, const us_mat*>) return a.add_all(o, count);
+        else return a.add_numbers(o, count);
+      }
+    }
     if constexpr (std::is_same_v<T, const us_mat*>) {
       if (THPVariable_Check(o) && count <= 1) return a.add(o);
     }
@@ -215,7 +251,7 @@ const Known kKnown[] = {
     US_ARRAYS(us_cast_multi, 3), US_ARRAYS(us_cast_multi_pitched, 3), US_CALL(us_residual_add), US_CALL(us_gelu_fwd), US_CALL(us_gelu_bwd), US_CALL(us_activation_fwd),
     US_CALL(us_activation_bwd), US_ARRAYS(us_weighted_add, 2), US_CALL(us_softmax_fwd), US_CALL(us_softmax_bwd), US_CALL(us_softmax_xent_fwd),
     US_CALL(us_softmax_xent_bwd), US_CALL(us_layer_norm_fwd), US_CALL(us_layer_norm_bwd), US_CALL(us_linear_fwd_cast), US_ARRAYS(us_linear_group_cast, 2),
-    US_CALL(us_layer_norm_fwd_cast), US_CALL(us_layer_norm_bwd_cast),
+    US_CALL(us_layer_norm_fwd_cast), US_CALL(us_layer_norm_bwd_cast), US_ARRAYS(us_qk_norm_fwd, 3), US_ARRAYS(us_qk_norm_bwd, 6), US_CALL(us_rotary_table),
 };
 constexpr size_t kCount = sizeof(kKnown) / sizeof(kKnown[0]);
 PyMethodDef g_calls[kCount];

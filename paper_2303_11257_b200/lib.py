@@ -150,6 +150,12 @@ def _load() -> C.CDLL:
     lib.us_layer_norm_fwd.restype = lib.us_layer_norm_bwd.restype = C.c_int
     lib.us_layer_norm_bwd_workspace_bytes.argtypes = [C.c_int64, C.c_int64]
     lib.us_layer_norm_bwd_workspace_bytes.restype = SZ
+    lib.us_qk_norm_fwd.argtypes = [C.c_int, MP, MP, MP, C.c_int64, F, MP, V, C.c_int64, C.c_int64, C.c_int, V]
+    lib.us_qk_norm_bwd.argtypes = [C.c_int, MP, MP, MP, MP, MP, C.POINTER(F), C.c_int64, F, F, MP, V, C.c_int64, C.c_int64, C.c_int, V, SZ, V]
+    lib.us_rotary_table.argtypes = [MP, C.c_double, C.c_double, C.c_int64, V]
+    lib.us_qk_norm_fwd.restype = lib.us_qk_norm_bwd.restype = lib.us_rotary_table.restype = C.c_int
+    lib.us_qk_norm_bwd_workspace_bytes.argtypes = [C.c_int64]
+    lib.us_qk_norm_bwd_workspace_bytes.restype = SZ
     lib.us_quant_stats_workspace_bytes.argtypes = []
     lib.us_quant_stats_workspace_bytes.restype = SZ
     lib.us_quant_stats.argtypes = [MP, F, C.c_int, C.c_int, C.c_int, V, V, V, SZ, V]
@@ -793,6 +799,49 @@ def us_layer_norm_bwd(X, w, G, eps, beta_x, beta_wc, dX, dw, dc, ws, stream=None
         X, w.view(1, -1), G, eps, beta_x, beta_wc, dX, dw.view(1, -1),
         dc.view(1, -1), ws, ws, _stream(stream)))
     return dX, dw, dc
+
+
+def us_rotary_table(table, base=10000.0, scale=1.0, first=0, stream=None):
+    """Fills table [positions x 2 pairs] (float32) with cosine and sine of each position's angles."""
+    _check("us_rotary_table", _entry("us_rotary_table")(table, base, scale, first, _stream(stream)))
+    return table
+
+
+def rotary_table(positions: int, rotated: int, base=10000.0, scale=1.0, device="cuda") -> torch.Tensor:
+    """A new table for us_qk_norm_fwd / bwd: angles of `rotated` features of a head at positions 0 .. positions - 1."""
+    return us_rotary_table(torch.empty((positions, rotated), dtype=torch.float32, device=device), base, scale)
+
+
+def us_qk_norm_fwd(X, w, Y, head_width, eps, table=None, positions=None, start=0, period=0, neighbours=False, stream=None):
+    """X, w, Y: lists of matrices [rows x heads * head_width] (queries and keys), norm weights [head_width] (or None) and outputs;
+    positions: int32 CUDA tensor [rows], or None for start + row % period."""
+    _check_positions(X, positions)
+    _check("us_qk_norm_fwd", _entry("us_qk_norm_fwd")(len(X), _of(X, X), _of(w, X), _of(Y, X), head_width, eps, table, positions, start, period, int(neighbours), _stream(stream)))
+    return Y
+
+
+def us_qk_norm_bwd_workspace_bytes(head_width: int) -> int:
+    return int(_lib.us_qk_norm_bwd_workspace_bytes(head_width))
+
+
+def us_qk_norm_bwd(X, w, G, dX, dw, head_width, eps, ws, beta_x=1.0, beta_w=None, table=None, positions=None, start=0, period=0, neighbours=False, stream=None):
+    """G, dX: lists of gradients of the outputs and of X; dw: list of weight gradients, or None; beta_w: list of their factors, or None
+    (ones); ws: a uint8 CUDA tensor of at least us_qk_norm_bwd_workspace_bytes(head_width) bytes, or None without dw."""
+    _check_positions(X, positions)
+    _check("us_qk_norm_bwd", _entry("us_qk_norm_bwd")(
+        len(X), _of(X, X), _of(w, X), _of(G, X), _of(dX, X), _of(dw, X), _of(beta_w, X), head_width, eps, beta_x, table, positions, start, period, int(neighbours),
+        ws, ws if ws is not None else 0, _stream(stream)))
+    return dX, dw
+
+
+def _of(parts, X):
+    if parts is not None and len(parts) != len(X):
+        raise ValueError("one entry per matrix is wanted")
+    return parts
+
+
+def _check_positions(X, positions):
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (X[0].shape[0],))
 
 
 def us_scales_linear(b: int, m: int, n: int, constrained: bool = False):
