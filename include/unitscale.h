@@ -313,7 +313,39 @@ us_status us_test_linear_tiling(int op, const us_mat* A, const us_mat* B, const 
                                 int* cols, int* ctas, int* shares);
 
 /* Activations of the table "Table of unit scaling factors", section Activations. */
-typedef enum { US_FN_GELU = 0, US_FN_RELU = 1, US_FN_TANH = 2, US_FN_SIGMOID = 3 } us_fn;
+typedef enum { US_FN_GELU = 0, US_FN_RELU = 1, US_FN_TANH = 2, US_FN_SIGMOID = 3, US_FN_SILU = 4 /* x / (1 + e^-x); not in the table, the usual gate */ } us_fn;
+
+/*
+ * us_ffn_gated_fwd / us_ffn_gated_bwd: the hidden layer of a gated FFN block, one kernel launch each way.
+ *
+ * The FFN of decoder models puts f(X Wg) * (X Wu) where the block of the figure "PyTorch examples" has gelu(X W1).  As scaled ops
+ * (section "Scaled ops"; matmuls as in section "Example"), for any us_fn f:
+ *
+ *   forward    h = alpha * X Wg,  u = alpha * X Wu        X [b x m], Wg, Wu [m x f]
+ *              A  = act_out_scale * f(act_in_scale * h) * u
+ *              H, U = h, u rounded to their format        (given both or neither: what the backward pass reads)
+ *   backward   dA = beta_x * G W2^T                       G [b x n], W2 [f x n]
+ *              dU = beta_u * f(act_in_scale * H) * dA
+ *              dH = beta_h * act_in_scale * f'(act_in_scale * H) * U * dA
+ *
+ * A is formed from the unrounded h and u; the gradients take H and U as stored, and dA is never rounded.  The unit-scaling values
+ * are act_out_scale = beta_u = 1 / rms f(Z) and beta_h = 1 / rms f'(Z) (us_scales_gated).  Wg and Wu may be the halves of one [m x 2 f] matrix, dH and dU those of one [b x 2 f]
+ * gradient: the rest of the backward pass is then us_linear_bwd_x and us_linear_bwd_w on these.
+ *
+ * X, Wg, Wu / G, W2: 8-bit (any mix of US_E4M3 / US_E5M2, but Wg and Wu alike), all BF16 or all F16.  A / dH, dU (alike): 8-bit for
+ * 8-bit operands (saturating), the operands' format for 16-bit ones.  H, U (alike): BF16, F16, or US_E4M3 -- activation checkpoints in 8 bits, which
+ * at unit scale need no factor (saturating at 448).  Any dimension >= 1; alignment, workspace, status word and errors as for us_linear_fwd.
+ * Outputs must not overlap one another or an input, except that dH may be H and dU may be U where their formats have one width (the same pointer and pitch).
+ */
+us_status us_ffn_gated_fwd(us_fn fn, const us_mat* X, const us_mat* Wg, const us_mat* Wu, float alpha, float act_in_scale, float act_out_scale,
+                           const us_mat* H, const us_mat* U, const us_mat* A, void* ws, size_t ws_bytes, void* stream);
+us_status us_ffn_gated_bwd(us_fn fn, const us_mat* G, const us_mat* W2, float beta_x, float act_in_scale, float beta_h, float beta_u, const us_mat* H,
+                           const us_mat* U, const us_mat* dH, const us_mat* dU, void* ws, size_t ws_bytes, void* stream);
+/* us_test_ffn_hidden_starved_cta for these kernels (all scales 1, US_FN_SILU). */
+us_status us_test_ffn_gated_fwd_starved(const us_mat* X, const us_mat* Wg, const us_mat* Wu, const us_mat* H, const us_mat* U, const us_mat* A, void* ws,
+                                        size_t ws_bytes, unsigned int wait_limit, int cta, int tiles, void* stream);
+us_status us_test_ffn_gated_bwd_starved(const us_mat* G, const us_mat* W2, const us_mat* H, const us_mat* U, const us_mat* dH, const us_mat* dU, void* ws,
+                                        size_t ws_bytes, unsigned int wait_limit, int cta, int tiles, void* stream);
 
 /* ------------------------------------------------------------ elementwise ops
  *
@@ -326,8 +358,8 @@ typedef enum { US_FN_GELU = 0, US_FN_RELU = 1, US_FN_TANH = 2, US_FN_SIGMOID = 3
  * us_residual_add  out = sqrt(1 - tau) * skip + sqrt(tau) * branch  (section "Weighted
  *                  addition", scheme fixed(tau)); serves the backward pass too: there
  *                  skip = incoming gradient, branch = gradient at the branch entry.
- * us_activation_fwd  A  = alpha * f(s_in * H) for f = relu(x) = max(x, 0), tanh, sigmoid(x) = (1 + e^-x)^-1
- *                  or gelu (table rows relu / gelu / tanh / sigmoid: alpha = 1 / std f(Z), Z ~ N(0,1));
+ * us_activation_fwd  A  = alpha * f(s_in * H) for f = relu(x) = max(x, 0), tanh, sigmoid(x) = (1 + e^-x)^-1,
+ *                  silu(x) = x sigmoid(x) or gelu (table rows relu / gelu / tanh / sigmoid: alpha = 1 / std f(Z), Z ~ N(0,1));
  * us_activation_bwd  dH = beta * s_in * f'(s_in * H) * dA (beta = 1 / rms f'(Z)); relu'(0) = 0.
  *                  US_FN_GELU gives the same values as us_gelu_fwd / us_gelu_bwd.
  * us_weighted_add  out = alpha * sum_i gamma_i * src_i over count (1..8) tensors of one shape (table row
@@ -600,6 +632,8 @@ us_status us_quant_stats(const us_mat* src, float scale, us_dtype fmt, int exp_l
  *   them as 1.701 / 1.481); constrained: both equal their geometric mean.
  * us_scales_activation: the same pair for any us_fn (relu: sqrt(2 / (1 - 1/pi)), sqrt 2; tanh
  *   1.593 / 1.467; sigmoid 4.802 / 4.722 as printed, carried here to float precision).
+ * us_scales_gated: factors of f(h) * u for independent h, u ~ N(0, 1) (us_ffn_gated_fwd / bwd): alpha = beta_u = 1 / rms f(Z) for the
+ *   product and the gradient of u, beta_h = 1 / rms f'(Z) for that of h; constrained: all three equal their geometric mean.
  * us_scales_residual: the coefficients of the fixed(tau) residual of section "Weighted addition",
  *   sqrt(1 - tau) for the skip connection and sqrt(tau) for the branch, 0 <= tau <= 1 (tau = 1 / (l + 1)
  *   gives the running-mean scheme for layer l).
@@ -615,6 +649,7 @@ us_status us_scales_linear(int64_t b, int64_t m, int64_t n, int constrained, flo
                            float* beta_x, float* beta_w);
 us_status us_scales_gelu(int constrained, float* alpha, float* beta);
 us_status us_scales_activation(us_fn fn, int constrained, float* alpha, float* beta);
+us_status us_scales_gated(us_fn fn, int constrained, float* alpha, float* beta_h, float* beta_u);
 us_status us_scales_residual(float tau, float* skip_coef, float* branch_coef);
 us_status us_scales_attention(int64_t s, int64_t d_head, int constrained, float* alpha_scores, float* beta_scores,
                               float* softmax_scale, float* alpha_context, float* beta_p, float* beta_v);

@@ -84,6 +84,9 @@ def _act(fn: str):
     if fn == "sigmoid":
         from scipy.special import expit                              # (1 + e^-z)^-1 without overflow
         return expit, (lambda z: expit(z) * expit(-z))
+    if fn == "silu":                                                 # not in the table: the usual gate of a gated FFN block
+        from scipy.special import expit
+        return (lambda z: z * expit(z)), (lambda z: expit(z) * (1.0 + z * expit(-z)))
     raise ValueError(fn)
 
 
@@ -98,6 +101,21 @@ def activation_bwd(fn, H, dA, s_in, beta):
     _, df = _act(fn)
     z = _f32(s_in) * np.asarray(H, np.float64)
     return _f32(beta) * _f32(s_in) * df(z) * np.asarray(dA, np.float64)
+
+
+# --------------------------------------------------------------------------- gated hidden layer
+
+def gated_fwd(fn, X, Wg, Wu, alpha, s_in, alpha_g):
+    """(A, h, u): h = alpha X Wg, u = alpha X Wu, A = alpha_g f(s_in h) u."""
+    h, u = linear_fwd(X, Wg, alpha), linear_fwd(X, Wu, alpha)
+    return activation_fwd(fn, h, s_in, alpha_g) * u, h, u
+
+
+def gated_bwd(fn, G, W2, beta_x, H, U, s_in, beta_h, beta_u):
+    """(dH, dU) from G = the gradient of the second layer's output: dA = beta_x G W2^T, dH = beta_h s_in f'(s_in H) U dA,
+    dU = beta_u f(s_in H) dA."""
+    dA = linear_bwd_x(G, W2, beta_x)
+    return activation_bwd(fn, H, np.asarray(U, np.float64) * dA, s_in, beta_h), activation_fwd(fn, H, s_in, beta_u) * dA
 
 
 # --------------------------------------------------------------------------- residual

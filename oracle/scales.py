@@ -94,6 +94,26 @@ def sigmoid_scales():
     return activation_scales(sg, lambda z: sg(z) * (1.0 - sg(z)))
 
 
+def silu(z):
+    return z * special.expit(z)
+
+
+def silu_grad(z):
+    return special.expit(z) * (1.0 + z * special.expit(-z))
+
+
+def silu_scales():
+    return activation_scales(silu, silu_grad)
+
+
+def gated_scales(f, df, constrained: bool = False):
+    """(alpha, beta_h, beta_u) of f(h) * u for independent unit-normal h, u: the product has mean zero and variance E[f(Z)^2], the gradient
+    of u variance E[f(Z)^2] and that of h variance E[f'(Z)^2]."""
+    a, b = (gaussian_expectation(lambda z, g=g: g(z) ** 2) ** -0.5 for g in (f, df))
+    factors = [a, b, a]
+    return tuple([geometric_mean(factors)] * 3 if constrained else factors)
+
+
 def residual_coefficients(tau: float):
     """(sqrt(1 - tau), sqrt(tau)) of the fixed(tau) residual scheme."""
     return math.sqrt(1.0 - tau), math.sqrt(tau)

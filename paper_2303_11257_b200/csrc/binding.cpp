@@ -252,6 +252,7 @@ const Known kKnown[] = {
     US_CALL(us_activation_bwd), US_ARRAYS(us_weighted_add, 2), US_CALL(us_softmax_fwd), US_CALL(us_softmax_bwd), US_CALL(us_softmax_xent_fwd),
     US_CALL(us_softmax_xent_bwd), US_CALL(us_layer_norm_fwd), US_CALL(us_layer_norm_bwd), US_CALL(us_linear_fwd_cast), US_ARRAYS(us_linear_group_cast, 2),
     US_CALL(us_layer_norm_fwd_cast), US_CALL(us_layer_norm_bwd_cast), US_ARRAYS(us_qk_norm_fwd, 3), US_ARRAYS(us_qk_norm_bwd, 6), US_CALL(us_rotary_table),
+    US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd),
 };
 constexpr size_t kCount = sizeof(kKnown) / sizeof(kKnown[0]);
 PyMethodDef g_calls[kCount];

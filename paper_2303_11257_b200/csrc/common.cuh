@@ -212,12 +212,14 @@ __device__ __forceinline__ float act_value(int fn, float z) {
   if (fn == US_FN_RELU) return fmaxf(z, 0.f);
   if (fn == US_FN_TANH) return 2.0f * sigmoid_f(2.0f * z) - 1.0f;
   if (fn == US_FN_SIGMOID) return sigmoid_f(z);
+  if (fn == US_FN_SILU) return z * sigmoid_f(z);
   return 0.f;   // gelu is dispatched before this point
 }
 __device__ __forceinline__ float act_slope(int fn, float z) {
   if (fn == US_FN_RELU) return z > 0.f ? 1.0f : 0.f;
   if (fn == US_FN_TANH) { const float s = sigmoid_f(2.0f * z), m = sigmoid_f(-2.0f * z); return 4.0f * s * m; }   // 1 - tanh^2
   if (fn == US_FN_SIGMOID) return sigmoid_f(z) * sigmoid_f(-z);
+  if (fn == US_FN_SILU) { const float s = sigmoid_f(z); return fmaf(z * s, sigmoid_f(-z), s); }
   return 0.f;
 }
 

@@ -451,7 +451,7 @@ extern "C" us_status us_gelu_bwd(const us_mat* H, const us_mat* dA, float s_in, 
 }
 
 extern "C" us_status us_activation_fwd(us_fn fn, const us_mat* H, float s_in, float alpha, const us_mat* A, void* stream) {
-  if (fn < US_FN_GELU || fn > US_FN_SIGMOID) return US_ERR_INVALID_ARG;
+  if (fn < US_FN_GELU || fn > US_FN_SILU) return US_ERR_INVALID_ARG;
   us_status s = check_ew(H, nullptr, A);
   if (s != US_OK) return s;
   if (fn == US_FN_GELU) return ew_launch<kGeluFwd>(H, nullptr, A, s_in, alpha, stream);
@@ -460,7 +460,7 @@ extern "C" us_status us_activation_fwd(us_fn fn, const us_mat* H, float s_in, fl
 
 extern "C" us_status us_activation_bwd(us_fn fn, const us_mat* H, const us_mat* dA, float s_in, float beta,
                                        const us_mat* dH, void* stream) {
-  if (fn < US_FN_GELU || fn > US_FN_SIGMOID || !dA) return US_ERR_INVALID_ARG;
+  if (fn < US_FN_GELU || fn > US_FN_SILU || !dA) return US_ERR_INVALID_ARG;
   us_status s = check_ew(H, dA, dH);
   if (s != US_OK) return s;
   if (fn == US_FN_GELU) return ew_launch<kGeluBwd>(H, dA, dH, s_in, beta, stream);

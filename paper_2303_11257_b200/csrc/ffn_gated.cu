@@ -1,0 +1,590 @@
+// us_ffn_gated_fwd / us_ffn_gated_bwd: the hidden layer of a gated FFN block, one launch each way.
+//
+//   forward    h = alpha X Wg,  u = alpha X Wu,  A = round(act_out * f(act_in * h) * u),  H, U = round(h), round(u)     (optional)
+//   backward   dA = beta_x G W2^T,  dU = round(beta_u * f(act_in * H) * dA),  dH = round(beta_h * act_in * f'(act_in * H) * U * dA)
+//
+// One warp-specialised persistent tcgen05 kernel for both: warp 0 fetches operand stages by TMA, one thread of warp 1 issues the MMAs,
+// the other warps turn finished accumulators into results, while the MMAs of the next tile run.  Forward, a tile is HC hidden columns of
+// both projections side by side in one accumulator: B is HC columns of Wg followed by HC columns of Wu, one MMA multiplies both by the same
+// A tile, and a lane finds h and u of the same element HC columns apart.  (Of a CTA pair the even CTA fetches Wg's half of B, the odd one
+// Wu's.)  Neither projection is written unless the caller wants the copies the backward pass reads; those are 16-bit or, at unit scale, E4M3
+// without a factor.  Backward, a tile is HC columns of dA, from which the epilogue makes both gradients with the copies it has fetched.
+//
+// Every wait is bounded as in the other GEMM kernels.
+#include <cuda.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "gemm_kernel.cuh"
+#include "host.h"
+
+namespace us {
+namespace {
+
+constexpr int kGatedEW = 8;
+constexpr int kRoom = 229376;                 // shared memory for stages
+constexpr int kMostStages = 16;
+
+struct GatedParams {
+  int M, N, K;                                // results are [M x N]; length of the contraction
+  int tiles_m, tiles_n;
+  FastDiv d_tiles_m;
+  uint32_t idesc;
+  float scale;                                // alpha / beta_x
+  float act_in, c0, c1;                       // c0: act_out / beta_u; c1: - / beta_h * act_in
+  int fn;
+  uint8_t *h, *u; long long h_ld, u_ld; int kept_dt, kept_sectors;     // the copies (forward: nullptr where not wanted)
+  uint8_t *o0, *o1; long long o0_ld, o1_ld; int out_dt, out_sectors;   // A / dH, dU
+  unsigned int* status;
+  uint32_t wait_limit;
+  uint32_t a_bytes; int stages;               // bytes of A in a stage (single CTAs: the rows that exist), and the stages that fit
+  int starved, served;                        // test hook (starved_cta)
+};
+
+template <bool BWD, int ES, int HC, int CG>
+struct GatedShape {
+  static constexpr int kN = BWD ? HC : 2 * HC;             // columns of an accumulator
+  static constexpr int kRowsB = kN / CG;                   // rows of B a CTA fetches
+  static constexpr int kBBytes = kRowsB * kStageKBytes;
+  static constexpr int kStageBytes = kBM * kStageKBytes + kBBytes;
+  static constexpr int kBarrierBytes = 512;
+  static constexpr int kTotal = kRoom + kBarrierBytes + 1024;
+  // Forward: B is N-major, in chunks of rows of K: 128 bytes wide, or the columns of one projection where they are fewer
+  static constexpr int kChunkRow = CG == 2 || HC * ES >= 128 ? 128 : HC * ES;
+  static constexpr int kChunkBytes = (kStageKBytes / ES) * kChunkRow;
+  static constexpr int kWarpCols = HC / (kGatedEW / 4);    // hidden columns of an epilogue warp, worked in slices
+  static constexpr int kSlice = kWarpCols < 32 ? kWarpCols : 32;
+};
+
+// ---------------------------------------------------------------- the gate
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// 1 / (1 + e^-z), relative error of a few 2^-22 and |z| 2^-23: far inside a step of the 16 and 8 bits that the results are rounded to.
+__device__ __forceinline__ float sigmoid_fast(float z) { return rcp_approx(1.0f + ex2_approx(-1.4426950408889634f * z)); }
+
+template <int FN>
+__device__ __forceinline__ float gate_value(float z) {
+  if (FN == US_FN_SILU) return z * sigmoid_fast(z);
+  if (FN == US_FN_SIGMOID) return sigmoid_fast(z);
+  if (FN == US_FN_GELU) return gelu_scaled(z, 1.f, 1.f);
+  return act_value(FN, z);
+}
+// f(z) and f'(z)
+template <int FN>
+__device__ __forceinline__ void gate_both(float z, float& f, float& df) {
+  if (FN == US_FN_SILU) {
+    const float s = sigmoid_fast(z);
+    f = z * s;
+    df = fmaf(f, 1.0f - s, s);
+  } else if (FN == US_FN_SIGMOID) {
+    f = sigmoid_fast(z);
+    df = f * (1.0f - f);
+  } else if (FN == US_FN_GELU) {
+    const float q = normal_tail(z), Phi = z >= 0.f ? 1.0f - q : q;
+    f = z * Phi;
+    df = fmaf(z * 0.39894228040143268f, ex2_approx((-0.72134752044448170f * z) * z), Phi);
+  } else {
+    f = act_value(FN, z);
+    df = act_slope(FN, z);
+  }
+}
+// Calls g with the launch's activation as a constant.
+template <class G>
+__device__ __forceinline__ void with_gate(int fn, G g) {
+  switch (fn) {
+    case US_FN_SILU: g(std::integral_constant<int, US_FN_SILU>()); break;
+    case US_FN_GELU: g(std::integral_constant<int, US_FN_GELU>()); break;
+    case US_FN_SIGMOID: g(std::integral_constant<int, US_FN_SIGMOID>()); break;
+    case US_FN_TANH: g(std::integral_constant<int, US_FN_TANH>()); break;
+    default: g(std::integral_constant<int, US_FN_RELU>()); break;
+  }
+}
+
+// ---------------------------------------------------------------- a lane's S columns of a row
+// S results rounded to dt, packed.
+template <int S>
+__device__ __forceinline__ void pack_row(int dt, const float (&y)[S], uint32_t (&w)[S / 2]) {
+  if (dt == US_BF16) {
+#pragma unroll
+    for (int i = 0; i < S / 2; ++i) w[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
+  } else if (dt == US_F16) {
+#pragma unroll
+    for (int i = 0; i < S / 2; ++i) w[i] = pack_f16x2(y[2 * i], y[2 * i + 1]);
+  } else if (dt == US_E4M3) {
+#pragma unroll
+    for (int i = 0; i < S / 4; ++i) w[i] = cvt_fp8x4<false>(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < S / 4; ++i) w[i] = cvt_fp8x4<true>(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+  }
+}
+// Those to memory; cols of them exist.  sectors: rows start on 32-byte boundaries (otherwise on 16-byte ones).
+template <int S>
+__device__ __forceinline__ void put_row(uint8_t* dst, int es, const uint32_t (&w)[S / 2], int cols, bool sectors) {
+  if (cols >= S) {
+    if (es == 2) {
+#pragma unroll
+      for (int i = 0; i < S / 16; ++i) {
+        if (sectors) {
+          ptx::stg256(dst + 32 * i, &w[8 * i]);
+        } else {
+          reinterpret_cast<uint4*>(dst)[2 * i] = make_uint4(w[8 * i], w[8 * i + 1], w[8 * i + 2], w[8 * i + 3]);
+          reinterpret_cast<uint4*>(dst)[2 * i + 1] = make_uint4(w[8 * i + 4], w[8 * i + 5], w[8 * i + 6], w[8 * i + 7]);
+        }
+      }
+    } else if (S == 32 && sectors) {
+      ptx::stg256(dst, w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < S / 16; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+      if (i < cols) {
+        if (es == 2) reinterpret_cast<uint16_t*>(dst)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        else if (i < 2 * S) dst[i] = (uint8_t)(w[(i >> 2) % (S / 2)] >> (8 * (i & 3)));
+      }
+  }
+}
+// The stored words of S columns; what does not exist is zero.
+template <int S>
+__device__ __forceinline__ void get_row(const uint8_t* src, int es, uint32_t (&w)[S / 2], int cols) {
+#pragma unroll
+  for (int i = 0; i < S / 2; ++i) w[i] = 0u;
+  if (cols >= S) {
+    const uint4* q = reinterpret_cast<const uint4*>(src);
+#pragma unroll
+    for (int i = 0; i < S / 8; ++i) {
+      if (es == 1 && i >= S / 16) break;
+      const uint4 v = __ldg(q + i);
+      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+      if (i < cols) {
+        if (es == 2) w[i >> 1] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(src) + i) << (16 * (i & 1));
+        else w[(i >> 2) % (S / 2)] |= (uint32_t)__ldg(src + i) << (8 * (i & 3));
+      }
+  }
+}
+template <int S>
+__device__ __forceinline__ void widen_row(int dt, const uint32_t (&w)[S / 2], float (&v)[S]) {
+  if (dt == US_E4M3) {
+#pragma unroll
+    for (int i = 0; i < S / 2; ++i) {
+      const float2 f = unpack_fp8x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))), false);
+      v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+  } else if (dt == US_BF16) {
+#pragma unroll
+    for (int i = 0; i < S / 2; ++i) { const float2 f = unpack_bf16x2(w[i]); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+  } else {
+#pragma unroll
+    for (int i = 0; i < S / 2; ++i) { const float2 f = unpack_f16x2(w[i]); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+  }
+}
+
+__device__ __forceinline__ uint64_t chunk_desc(uint32_t addr, int row_bytes, uint32_t lbo) {      // N-major B, swizzled by its row width
+  const uint64_t d = ptx::smem_desc_sw128(addr, lbo, 8u * row_bytes) & ~((uint64_t)7 << 61);
+  return d | ((uint64_t)(row_bytes == 128 ? 2 : row_bytes == 64 ? 4 : 6) << 61);
+}
+
+// ES: operand bytes per element (1 = FP8, 2 = BF16 / F16).  HC: hidden columns of a tile.  CG = 2: tiles of 256 rows by a CTA pair, 1: of 128 by a CTA.
+template <bool BWD, int ES, int HC, int CG>
+__global__ void __launch_bounds__(gemm_threads(kGatedEW), 1)
+gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0, const __grid_constant__ CUtensorMap tm_b1, const GatedParams p) {
+  using S = GatedShape<BWD, ES, HC, CG>;
+  constexpr int kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
+  constexpr uint32_t kTmemCols = 2 * kN;
+  const uint32_t a_bytes = CG == 2 ? (uint32_t)(kBM * kStageKBytes) : p.a_bytes, stage_bytes = a_bytes + S::kBBytes;
+  const int stages = CG == 2 ? kRoom / S::kStageBytes : p.stages;
+
+  ptx::grid_release_next();
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_addr(smem_raw));
+  const uint32_t bars = smem_base + kRoom;
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (kMostStages + s); };
+  auto acc_full_bar = [&](int a) { return bars + 8u * (2 * kMostStages + a); };
+  auto acc_empty_bar = [&](int a) { return bars + 8u * (2 * kMostStages + 2 + a); };
+  const uint32_t drained_bar = bars + 8u * (2 * kMostStages + 4);
+  static_assert(8 * (2 * kMostStages + 5) + 8 <= S::kBarrierBytes, "barrier area too small");
+  uint8_t* tail = smem_gen + kRoom + 8 * (2 * kMostStages + 5);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 4);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = CG == 2 ? (int)ptx::cluster_ctarank() : 0;
+  const int unit = blockIdx.x / CG, num_units = gridDim.x / CG;
+  const int num_tiles = p.tiles_m * p.tiles_n, num_kb = (p.K + kBK - 1) / kBK;
+  // column-major over the tiles: units that run side by side share a panel of weights
+  auto tile_mn2 = [&](int tile, int& tm, int& tn) { tn = p.d_tiles_m.div(tile); tm = tile - tn * p.tiles_m; };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) { ptx::mbar_init(full_bar(s), 1); ptx::mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full_bar(a), 1); ptx::mbar_init(acc_empty_bar(a), CG * kGatedEW); }
+    ptx::mbar_init(drained_bar, 1);
+    *abort_flag = 0;
+    ptx::mbar_init_fence();
+    ptx::prefetch_tensormap(&tm_a);
+    ptx::prefetch_tensormap(&tm_b0);
+    ptx::prefetch_tensormap(&tm_b1);
+  }
+  if (warp == 1) {
+    if (CG == 2) { ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), kTmemCols); ptx::tmem_relinquish_pair(); }
+    else { ptx::tmem_alloc(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), kTmemCols); ptx::tmem_relinquish(); }
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (CG == 2) ptx::cluster_meet();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer (every CTA)
+    if (ptx::elect_one()) {
+      uint32_t issued = 0;
+      int stage = 0; uint32_t phase = 0;
+      bool ok = true;
+      const int end = starved_cta(p.starved, rank) ? min(num_tiles, unit + p.served * num_units) : num_tiles;
+      for (int tile = unit; ok && tile < end; tile += num_units) {
+        int tm, tn;
+        tile_mn2(tile, tm, tn);
+        const int m0 = tm * kTileM + rank * kBM, n0 = tn * HC;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          ok = wait_bounded(empty_bar(stage), phase ^ 1u, abort_flag, p.status, p.wait_limit);
+          if (!ok) break;
+          const uint32_t a_dst = smem_base + stage * stage_bytes, b_dst = a_dst + a_bytes;
+          const int k0 = kb * kBK;
+          if (issued == 0) ptx::grid_wait_previous();       // coordinates and barriers are ready: only the loads wait
+          const uint32_t fb = CG == 2 ? ptx::in_even_cta(full_bar(stage)) : full_bar(stage);
+          if (rank == 0) ptx::mbar_expect_tx(full_bar(stage), CG * stage_bytes);
+          auto load = [&](uint32_t dst, const void* tmap, int x, int y) {
+            if (CG == 2) ptx::tma_load_2d_pair(dst, tmap, fb, x, y); else ptx::tma_load_2d(dst, tmap, fb, x, y);
+          };
+          load(a_dst, &tm_a, k0, m0);                                            // X / G [M x K], K-major
+          if (BWD) {
+            load(b_dst, &tm_b0, k0, n0 + rank * S::kRowsB);                      // W2 [N x K], K-major
+          } else if (CG == 2) {                                                  // Wg / Wu [K x N], N-major, 128 / ES columns per box
+#pragma unroll
+            for (int c = 0; c < ES; ++c) load(b_dst + c * S::kChunkBytes, rank == 0 ? &tm_b0 : &tm_b1, n0 + c * kBK, k0);
+          } else {
+            load(b_dst, &tm_b0, n0, k0);
+            load(b_dst + S::kChunkBytes, &tm_b1, n0, k0);
+          }
+          ++issued;
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (*abort_flag && rank == 0) {
+        // Let copies that are still in flight land before the CTA gives up its shared memory.
+        const uint32_t n = issued < (uint32_t)stages ? issued : (uint32_t)stages;
+        for (uint32_t i = 0; i < n; ++i) {
+          if (stage == 0) { stage = stages; phase ^= 1u; }
+          --stage;
+          for (uint32_t it = 0; it < p.wait_limit && !ptx::mbar_try_wait(full_bar(stage), phase); ++it) {}
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer (even CTA of a pair only)
+    if (ptx::elect_one() && rank == 0) {
+      ptx::grid_wait_previous();                       // no operand comes earlier: the bounded waits begin when the loads do
+      int stage = 0; uint32_t phase = 0, local = 0;
+      bool ok = true;
+      const uint32_t stage_step = stage_bytes >> 4;
+      const uint64_t a_desc = ptx::smem_desc_sw128(smem_base, 16, 1024);
+      const uint64_t b_desc = BWD ? ptx::smem_desc_sw128(smem_base + a_bytes, 16, 1024) : chunk_desc(smem_base + a_bytes, S::kChunkRow, S::kChunkBytes);
+      const uint32_t a_hi = (uint32_t)(a_desc >> 32), a_lo0 = (uint32_t)a_desc, b_hi = (uint32_t)(b_desc >> 32), b_lo0 = (uint32_t)b_desc;
+      constexpr uint32_t b_step = (BWD ? 32u : (uint32_t)S::kChunkBytes / kKSteps) >> 4;
+      for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
+        const uint32_t acc = local & 1u, acc_phase = (local >> 1) & 1u;
+        ok = wait_bounded(acc_empty_bar(acc), acc_phase ^ 1u, abort_flag, p.status, p.wait_limit);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        const uint32_t d_tmem = tmem_base + acc * kN;
+        uint32_t accumulate = 0;
+        for (int kb = 0; kb < num_kb; ++kb) {
+          if (!ptx::mbar_try_wait(full_bar(stage), phase)) {
+            ok = wait_bounded(full_bar(stage), phase, abort_flag, p.status, p.wait_limit);
+            if (!ok) break;
+          }
+          ptx::tc_fence_after_sync();
+          const uint32_t a_lo = a_lo0 + stage * stage_step, b_lo = b_lo0 + stage * stage_step;
+#pragma unroll
+          for (int k = 0; k < kKSteps; ++k) {
+            const uint64_t adesc = ((uint64_t)a_hi << 32) | (a_lo + k * 2u);
+            const uint64_t bdesc = ((uint64_t)b_hi << 32) | (b_lo + k * b_step);
+            if (CG == 2) ptx::mma_ss_pair<ES == 1>(d_tmem, adesc, bdesc, p.idesc, accumulate);
+            else ptx::mma_ss<ES == 1>(d_tmem, adesc, bdesc, p.idesc, accumulate);
+            accumulate = 1;
+          }
+          if (CG == 2) ptx::mma_commit_pair(empty_bar(stage), 3); else ptx::mma_commit(empty_bar(stage));
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) { if (CG == 2) ptx::mma_commit_pair(acc_full_bar(acc), 3); else ptx::mma_commit(acc_full_bar(acc)); }
+      }
+      if (*abort_flag) {
+        if (CG == 2) ptx::mma_commit_pair(drained_bar, 1); else ptx::mma_commit(drained_bar);
+        for (uint32_t it = 0; it < p.wait_limit && !ptx::mbar_try_wait(drained_bar, 0); ++it) {}
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue warps
+    ptx::grid_wait_previous();
+    // Warp (lane quarter q, part) owns 32 rows x kWarpCols hidden columns of the tile; a lane holds one row of them.
+    const int q = warp & 3, part = (warp - 2) >> 2;
+    const int out_es = dtype_size(p.out_dt), kept_es = dtype_size(p.kept_dt);
+    auto release_acc = [&](uint32_t a, int tile) {              // (where no later tile takes it nobody waits)
+      ptx::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0 && tile + 2 * num_units < num_tiles) {
+        if (CG == 2) ptx::mbar_arrive_cluster(ptx::in_even_cta(acc_empty_bar(a)));
+        else ptx::mbar_arrive(acc_empty_bar(a));
+      }
+    };
+    auto place = [&](int tile, int& row, int& col) {            // of this lane's first element
+      int tm, tn;
+      tile_mn2(tile, tm, tn);
+      row = tm * kTileM + rank * kBM + q * 32 + lane;
+      col = tn * HC + part * S::kWarpCols;
+    };
+    // Backward: the copies of the slice that comes next are on their way while one is worked on.
+    uint32_t rh[kSl / 2], ru[kSl / 2];
+    auto fetch = [&](int tile, int slice) {
+      if (tile >= num_tiles) return;
+      int row, col;
+      place(tile, row, col);
+      col += slice * kSl;
+      const int cols = row < p.M ? p.N - col : 0;
+      get_row<kSl>(p.h + (row * p.h_ld + col) * kept_es, kept_es, rh, cols);
+      get_row<kSl>(p.u + (row * p.u_ld + col) * kept_es, kept_es, ru, cols);
+    };
+    if (BWD) fetch(unit, 0);
+
+    uint32_t local = 0;
+    bool ok = true;
+    for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
+      int row, col0;
+      place(tile, row, col0);
+      const uint32_t acc = local & 1u, acc_phase = (local >> 1) & 1u;
+      ok = wait_bounded(acc_full_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      ptx::tc_fence_after_sync();
+      const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * kN + part * S::kWarpCols;
+#pragma unroll 1
+      for (int sl = 0; sl < kSlices; ++sl) {
+        const int col = col0 + sl * kSl, cols = row < p.M ? p.N - col : 0;
+        uint32_t r0[kSl], r1[BWD ? 1 : kSl];
+        if constexpr (kSl == 32) ptx::tmem_ld_32x32_issue(t_row + sl * kSl, r0); else ptx::tmem_ld_32x32_issue(t_row + sl * kSl, r0);
+        if constexpr (!BWD) ptx::tmem_ld_32x32_issue(t_row + HC + sl * kSl, r1);
+        float a[kSl], b[kSl];
+        if constexpr (BWD) {                                    // a, b: the kept projections, then dH, dU
+          widen_row<kSl>(p.kept_dt, rh, a);
+          widen_row<kSl>(p.kept_dt, ru, b);
+          if (sl + 1 < kSlices) fetch(tile, sl + 1); else fetch(tile + num_units, 0);
+        }
+        ptx::tmem_ld_fence(r0);
+        if constexpr (!BWD) ptx::tmem_ld_fence(r1);
+        if (sl + 1 == kSlices) release_acc(acc, tile);          // the values are in registers
+        uint32_t w[kSl / 2];
+        if constexpr (!BWD) {
+#pragma unroll
+          for (int i = 0; i < kSl; ++i) { a[i] = p.scale * __uint_as_float(r0[i]); b[i] = p.scale * __uint_as_float(r1[i]); }
+          if (p.h) {
+            pack_row<kSl>(p.kept_dt, a, w);
+            put_row<kSl>(p.h + (row * p.h_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
+            pack_row<kSl>(p.kept_dt, b, w);
+            put_row<kSl>(p.u + (row * p.u_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
+          }
+          with_gate(p.fn, [&](auto fn) {
+#pragma unroll
+            for (int i = 0; i < kSl; ++i) a[i] = p.c0 * gate_value<decltype(fn)::value>(p.act_in * a[i]) * b[i];
+          });
+          pack_row<kSl>(p.out_dt, a, w);
+          put_row<kSl>(p.o0 + (row * p.o0_ld + col) * out_es, out_es, w, cols, p.out_sectors);
+        } else {
+          with_gate(p.fn, [&](auto fn) {
+#pragma unroll
+            for (int i = 0; i < kSl; ++i) {
+              const float d = p.scale * __uint_as_float(r0[i]);
+              float f, df;
+              gate_both<decltype(fn)::value>(p.act_in * a[i], f, df);
+              a[i] = p.c1 * df * b[i] * d;
+              b[i] = p.c0 * f * d;
+            }
+          });
+          pack_row<kSl>(p.out_dt, a, w);
+          put_row<kSl>(p.o0 + (row * p.o0_ld + col) * out_es, out_es, w, cols, p.out_sectors);
+          pack_row<kSl>(p.out_dt, b, w);
+          put_row<kSl>(p.o1 + (row * p.o1_ld + col) * out_es, out_es, w, cols, p.out_sectors);
+        }
+      }
+    }
+    // Leaving (early too, when a wait ran out somewhere in the CTA): tensor-memory loads have landed.
+    ptx::tmem_ld_wait_all();
+  }
+
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (CG == 2) ptx::cluster_part(*abort_flag != 0);
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    if (CG == 2) ptx::tmem_dealloc_pair(tmem_base, kTmemCols); else ptx::tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------- host
+bool valid_mat(const us_mat* m) {
+  return m && m->ptr && m->rows >= 1 && m->cols >= 1 && m->ld >= m->cols && m->rows < (1ll << 31) && m->cols < (1ll << 31) && m->dtype >= US_F32 && m->dtype <= US_E5M2;
+}
+bool given(const us_mat* m) { return m && m->ptr; }
+bool aligned(const us_mat* m, int bytes) { return reinterpret_cast<uintptr_t>(m->ptr) % bytes == 0 && (m->ld * dtype_size(m->dtype)) % bytes == 0; }
+bool is_fp8(int dt) { return dt == US_E4M3 || dt == US_E5M2; }
+
+// host::make_tmap for boxes of 32 bytes a row that are multiplied as they are: swizzled with that width's pattern.
+bool make_chunk_tmap(CUtensorMap* tm, const us_mat* m, int es, int box_rows, int box_bytes) {
+  if (box_bytes != 32) return host::make_tmap(tm, m, es, box_rows, box_bytes);
+  host::EncodeTiledFn fn = host::encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)m->cols, (cuuint64_t)m->rows}, strides[1] = {(cuuint64_t)m->ld * es};
+  cuuint32_t box[2] = {(cuuint32_t)(box_bytes / es), (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  return fn(tm, es == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, m->ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool BWD, int ES, int HC, int CG>
+us_status launch_gated(const us_mat* A, const us_mat* B0, const us_mat* B1, GatedParams& p, int sms, cudaStream_t st) {
+  using S = GatedShape<BWD, ES, HC, CG>;
+  p.tiles_m = (p.M + kBM * CG - 1) / (kBM * CG);
+  p.tiles_n = (p.N + HC - 1) / HC;
+  if ((int64_t)p.tiles_m * p.tiles_n >= (1ll << 30)) return US_ERR_UNSUPPORTED;
+  p.d_tiles_m = make_fast_div(p.tiles_m);
+  const int one = ES == 1 ? US_E5M2 : US_BF16;
+  p.idesc = make_idesc(A->dtype == one, B0->dtype == one, false, !BWD, kBM * CG, S::kN);
+  // a short A: its rows in groups of eight.  The MMA still reads 128; what lies behind them ends up in rows that do not exist.
+  const int a_rows = CG == 1 && p.M < kBM ? (p.M + 7) / 8 * 8 : kBM;
+  p.a_bytes = (uint32_t)a_rows * kStageKBytes;
+  p.stages = std::min(kMostStages, (kRoom - kBM * kStageKBytes) / ((int)p.a_bytes + S::kBBytes));
+  CUtensorMap t[3];
+  constexpr int kBK = kStageKBytes / ES;
+  if (!host::make_tmap(&t[0], A, ES, a_rows, kStageKBytes)) return US_ERR_CUDA;
+  if (!(BWD ? host::make_tmap(&t[1], B0, ES, S::kRowsB, kStageKBytes) : make_chunk_tmap(&t[1], B0, ES, kBK, S::kChunkRow))) return US_ERR_CUDA;
+  if (BWD) t[2] = t[1];
+  else if (!make_chunk_tmap(&t[2], B1, ES, kBK, S::kChunkRow)) return US_ERR_CUDA;
+  const int tiles = p.tiles_m * p.tiles_n, most = sms / CG;
+  static std::atomic<uint64_t> smem_set{0};
+  return host::launch(gated_kernel<BWD, ES, HC, CG>, &smem_set, CG * (tiles < most ? tiles : most), gemm_threads(kGatedEW), S::kTotal, CG, st, t[0], t[1], t[2],
+                      static_cast<const GatedParams&>(p));
+}
+
+// Tiles of CTA pairs unless they would leave more than half of the pairs idle, else the widest of single CTAs, else, where the machine has
+// an SM for each of them, the narrow ones.
+template <bool BWD, int ES>
+us_status pick_gated(const us_mat* A, const us_mat* B0, const us_mat* B1, GatedParams& p, cudaStream_t st) {
+  const int sms = host::sm_count();
+  if (sms <= 0) return US_ERR_CUDA;
+  constexpr int kWide = BWD ? 256 : 128;
+  const int64_t M = p.M, N = p.N;
+  if (4 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) >= sms && M > kBM) return launch_gated<BWD, ES, kWide, 2>(A, B0, B1, p, sms, st);
+  const int64_t narrow = ((M + kBM - 1) / kBM) * ((N + kWide / 4 - 1) / (kWide / 4));
+  if (narrow <= sms) return launch_gated<BWD, ES, kWide / 4, 1>(A, B0, B1, p, sms, st);
+  return launch_gated<BWD, ES, kWide / 2, 1>(A, B0, B1, p, sms, st);
+}
+
+// The checks that both directions share: operands of one width (f8: 8-bit), workspace.
+us_status check_common(const us_mat* const* in, int n, const us_mat* const* out, int outs, const us_mat* H, const us_mat* U, const void* ws, size_t ws_bytes, bool& f8) {
+  if (!ws || ws_bytes < us_workspace_bytes()) return US_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(ws) % 16) return US_ERR_ALIGNMENT;
+  for (int i = 0; i < n; ++i) if (!aligned(in[i], 16)) return US_ERR_ALIGNMENT;
+  for (int i = 0; i < outs; ++i) if (!aligned(out[i], 16)) return US_ERR_ALIGNMENT;
+  if (given(H) && (!aligned(H, 16) || !aligned(U, 16))) return US_ERR_ALIGNMENT;
+  f8 = is_fp8(in[0]->dtype);
+  const bool h16 = in[0]->dtype == US_BF16 || in[0]->dtype == US_F16;
+  if (!f8 && !h16) return US_ERR_UNSUPPORTED;
+  for (int i = 1; i < n; ++i) if (f8 ? !is_fp8(in[i]->dtype) : in[i]->dtype != in[0]->dtype) return US_ERR_UNSUPPORTED;
+  for (int i = 0; i < outs; ++i) if (f8 ? !is_fp8(out[i]->dtype) : out[i]->dtype != in[0]->dtype) return US_ERR_UNSUPPORTED;
+  if (given(H) && H->dtype != US_BF16 && H->dtype != US_F16 && H->dtype != US_E4M3) return US_ERR_UNSUPPORTED;
+  return US_OK;
+}
+
+us_status gated_fwd(int fn, const us_mat* X, const us_mat* Wg, const us_mat* Wu, float alpha, float act_in, float act_out, const us_mat* H, const us_mat* U,
+                    const us_mat* A, void* ws, size_t ws_bytes, void* stream, uint32_t wait_limit, int starved, int served) {
+  if (fn < US_FN_GELU || fn > US_FN_SILU || !valid_mat(X) || !valid_mat(Wg) || !valid_mat(Wu) || !valid_mat(A)) return US_ERR_INVALID_ARG;
+  const int64_t M = X->rows, K = X->cols, N = Wg->cols;
+  if (Wg->rows != K || Wu->rows != K || Wu->cols != N || Wu->dtype != Wg->dtype || A->rows != M || A->cols != N) return US_ERR_INVALID_ARG;
+  if (given(H) != given(U)) return US_ERR_INVALID_ARG;
+  if (given(H) && (!valid_mat(H) || !valid_mat(U) || H->rows != M || H->cols != N || U->rows != M || U->cols != N || U->dtype != H->dtype)) return US_ERR_INVALID_ARG;
+  const us_mat *in[3] = {X, Wg, Wu}, *out[1] = {A};
+  bool f8;
+  const us_status s = check_common(in, 3, out, 1, H, U, ws, ws_bytes, f8);
+  if (s != US_OK) return s;
+  GatedParams p{};
+  p.M = (int)M; p.N = (int)N; p.K = (int)K;
+  p.scale = alpha; p.act_in = act_in; p.c0 = act_out; p.fn = fn;
+  p.kept_dt = US_BF16;
+  if (given(H)) {
+    p.h = static_cast<uint8_t*>(H->ptr); p.h_ld = H->ld; p.u = static_cast<uint8_t*>(U->ptr); p.u_ld = U->ld;
+    p.kept_dt = H->dtype; p.kept_sectors = aligned(H, 32) && aligned(U, 32);
+  }
+  p.o0 = static_cast<uint8_t*>(A->ptr); p.o0_ld = A->ld; p.out_dt = A->dtype; p.out_sectors = aligned(A, 32);
+  p.status = static_cast<unsigned int*>(ws); p.wait_limit = wait_limit; p.starved = starved; p.served = served;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return f8 ? pick_gated<false, 1>(X, Wg, Wu, p, st) : pick_gated<false, 2>(X, Wg, Wu, p, st);
+}
+
+us_status gated_bwd(int fn, const us_mat* G, const us_mat* W2, float beta_x, float act_in, float beta_h, float beta_u, const us_mat* H, const us_mat* U,
+                    const us_mat* dH, const us_mat* dU, void* ws, size_t ws_bytes, void* stream, uint32_t wait_limit, int starved, int served) {
+  if (fn < US_FN_GELU || fn > US_FN_SILU || !valid_mat(G) || !valid_mat(W2) || !valid_mat(H) || !valid_mat(U) || !valid_mat(dH) || !valid_mat(dU)) return US_ERR_INVALID_ARG;
+  const int64_t M = G->rows, K = G->cols, N = W2->rows;
+  if (W2->cols != K) return US_ERR_INVALID_ARG;
+  const us_mat* same[4] = {H, U, dH, dU};
+  for (const us_mat* m : same) if (m->rows != M || m->cols != N) return US_ERR_INVALID_ARG;
+  if (U->dtype != H->dtype || dU->dtype != dH->dtype) return US_ERR_INVALID_ARG;
+  const us_mat *in[2] = {G, W2}, *out[2] = {dH, dU};
+  bool f8;
+  const us_status s = check_common(in, 2, out, 2, H, U, ws, ws_bytes, f8);
+  if (s != US_OK) return s;
+  GatedParams p{};
+  p.M = (int)M; p.N = (int)N; p.K = (int)K;
+  p.scale = beta_x; p.act_in = act_in; p.c0 = beta_u; p.c1 = beta_h * act_in; p.fn = fn;
+  p.h = static_cast<uint8_t*>(H->ptr); p.h_ld = H->ld; p.u = static_cast<uint8_t*>(U->ptr); p.u_ld = U->ld; p.kept_dt = H->dtype;
+  p.o0 = static_cast<uint8_t*>(dH->ptr); p.o0_ld = dH->ld; p.o1 = static_cast<uint8_t*>(dU->ptr); p.o1_ld = dU->ld;
+  p.out_dt = dH->dtype; p.out_sectors = aligned(dH, 32) && aligned(dU, 32);
+  p.status = static_cast<unsigned int*>(ws); p.wait_limit = wait_limit; p.starved = starved; p.served = served;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return f8 ? pick_gated<true, 1>(G, W2, W2, p, st) : pick_gated<true, 2>(G, W2, W2, p, st);
+}
+
+// Test hook: of a CTA pair only the odd one may starve alone (the even one waits for its copies; nobody would wait for those of the odd one).
+bool bad_hook(uint32_t wait_limit, int cta, int tiles) { return wait_limit == 0 || wait_limit > (1u << 16) || cta < -1 || cta > 1 || tiles < 0 || tiles > 1024; }
+
+}  // namespace
+}  // namespace us
+
+extern "C" us_status us_ffn_gated_fwd(us_fn fn, const us_mat* X, const us_mat* Wg, const us_mat* Wu, float alpha, float act_in_scale, float act_out_scale,
+                                      const us_mat* H, const us_mat* U, const us_mat* A, void* ws, size_t ws_bytes, void* stream) {
+  return us::gated_fwd(fn, X, Wg, Wu, alpha, act_in_scale, act_out_scale, H, U, A, ws, ws_bytes, stream, us::kWaitLimit, 0, 0);
+}
+extern "C" us_status us_ffn_gated_bwd(us_fn fn, const us_mat* G, const us_mat* W2, float beta_x, float act_in_scale, float beta_h, float beta_u, const us_mat* H,
+                                      const us_mat* U, const us_mat* dH, const us_mat* dU, void* ws, size_t ws_bytes, void* stream) {
+  return us::gated_bwd(fn, G, W2, beta_x, act_in_scale, beta_h, beta_u, H, U, dH, dU, ws, ws_bytes, stream, us::kWaitLimit, 0, 0);
+}
+extern "C" us_status us_test_ffn_gated_fwd_starved(const us_mat* X, const us_mat* Wg, const us_mat* Wu, const us_mat* H, const us_mat* U, const us_mat* A, void* ws,
+                                                   size_t ws_bytes, uint32_t wait_limit, int cta, int tiles, void* stream) {
+  if (us::bad_hook(wait_limit, cta, tiles)) return US_ERR_INVALID_ARG;
+  return us::gated_fwd(US_FN_SILU, X, Wg, Wu, 1.f, 1.f, 1.f, H, U, A, ws, ws_bytes, stream, wait_limit, cta + 2, tiles);
+}
+extern "C" us_status us_test_ffn_gated_bwd_starved(const us_mat* G, const us_mat* W2, const us_mat* H, const us_mat* U, const us_mat* dH, const us_mat* dU, void* ws,
+                                                   size_t ws_bytes, uint32_t wait_limit, int cta, int tiles, void* stream) {
+  if (us::bad_hook(wait_limit, cta, tiles)) return US_ERR_INVALID_ARG;
+  return us::gated_bwd(US_FN_SILU, G, W2, 1.f, 1.f, 1.f, 1.f, H, U, dH, dU, ws, ws_bytes, stream, wait_limit, cta + 2, tiles);
+}

@@ -101,11 +101,33 @@ extern "C" us_status us_scales_activation(us_fn fn, int constrained, float* alph
     case US_FN_RELU: a = 1.7128585504496627; b = 1.4142135623730951; break;
     case US_FN_TANH: a = 1.5925374197228314; b = 1.4674135916307951; break;
     case US_FN_SIGMOID: a = 4.8013133720399622; b = 4.7226460859379743; break;
+    case US_FN_SILU: a = 1.7871872221004417; b = 1.6233202579524972; break;
     default: return US_ERR_INVALID_ARG;
   }
   if (constrained) a = b = sqrt(a * b);
   *alpha = (float)a;
   *beta = (float)b;
+  return US_OK;
+}
+
+extern "C" us_status us_scales_gated(us_fn fn, int constrained, float* alpha, float* beta_h, float* beta_u) {
+  if (!alpha || !beta_h || !beta_u) return US_ERR_INVALID_ARG;
+  // 1 / rms f(Z) and 1 / rms f'(Z) for Z ~ N(0, 1), relu in closed form, the others by numerical integration: the other factor of the product
+  // has mean zero, so that the rms of f(h), mean included, is the product's standard deviation.
+  double a, b;
+  switch (fn) {
+    case US_FN_GELU: a = 1.5335304411955353; b = kGeluBeta; break;
+    case US_FN_RELU: a = 1.4142135623730951; b = 1.4142135623730951; break;
+    case US_FN_TANH: a = 1.5925374197228314; b = 1.4674135916307951; break;
+    case US_FN_SIGMOID: a = 1.8462285453386056; b = 4.7226460859379743; break;
+    case US_FN_SILU: a = 1.676532470331091; b = 1.6233202579524972; break;
+    default: return US_ERR_INVALID_ARG;
+  }
+  double u = a;
+  if (constrained) a = b = u = cbrt(a * a * b);
+  *alpha = (float)a;
+  *beta_h = (float)b;
+  *beta_u = (float)u;
   return US_OK;
 }
 

@@ -18,8 +18,8 @@ STATUS_NAMES = {
 }
 US_F32, US_BF16, US_F16, US_E4M3, US_E5M2 = range(5)
 US_ACT_NONE, US_ACT_GELU, US_ACT_GELU_GRAD, US_ACT_RELU, US_ACT_RELU_GRAD, US_ACT_TANH, US_ACT_TANH_GRAD, US_ACT_SIGMOID, US_ACT_SIGMOID_GRAD = range(9)
-US_FN_GELU, US_FN_RELU, US_FN_TANH, US_FN_SIGMOID = range(4)
-FN_BY_NAME = {"gelu": US_FN_GELU, "relu": US_FN_RELU, "tanh": US_FN_TANH, "sigmoid": US_FN_SIGMOID}
+US_FN_GELU, US_FN_RELU, US_FN_TANH, US_FN_SIGMOID, US_FN_SILU = range(5)
+FN_BY_NAME = {"gelu": US_FN_GELU, "relu": US_FN_RELU, "tanh": US_FN_TANH, "sigmoid": US_FN_SIGMOID, "silu": US_FN_SILU}
 
 _TORCH_DTYPES = {
     torch.float32: US_F32, torch.bfloat16: US_BF16, torch.float16: US_F16,
@@ -150,6 +150,12 @@ def _load() -> C.CDLL:
     lib.us_layer_norm_fwd.restype = lib.us_layer_norm_bwd.restype = C.c_int
     lib.us_layer_norm_bwd_workspace_bytes.argtypes = [C.c_int64, C.c_int64]
     lib.us_layer_norm_bwd_workspace_bytes.restype = SZ
+    lib.us_ffn_gated_fwd.argtypes = [C.c_int, MP, MP, MP, F, F, F, MP, MP, MP, V, SZ, V]
+    lib.us_ffn_gated_bwd.argtypes = [C.c_int, MP, MP, F, F, F, F, MP, MP, MP, MP, V, SZ, V]
+    lib.us_test_ffn_gated_fwd_starved.argtypes = lib.us_test_ffn_gated_bwd_starved.argtypes = [MP] * 6 + [V, SZ, C.c_uint, C.c_int, C.c_int, V]
+    lib.us_ffn_gated_fwd.restype = lib.us_ffn_gated_bwd.restype = lib.us_test_ffn_gated_fwd_starved.restype = lib.us_test_ffn_gated_bwd_starved.restype = C.c_int
+    lib.us_scales_gated.argtypes = [C.c_int, C.c_int] + [C.POINTER(C.c_float)] * 3
+    lib.us_scales_gated.restype = C.c_int
     lib.us_qk_norm_fwd.argtypes = [C.c_int, MP, MP, MP, C.c_int64, F, MP, V, C.c_int64, C.c_int64, C.c_int, V]
     lib.us_qk_norm_bwd.argtypes = [C.c_int, MP, MP, MP, MP, MP, C.POINTER(F), C.c_int64, F, F, MP, V, C.c_int64, C.c_int64, C.c_int, V, SZ, V]
     lib.us_rotary_table.argtypes = [MP, C.c_double, C.c_double, C.c_int64, V]
@@ -633,6 +639,31 @@ def us_test_ffn_hidden_starved(X, W1, G, W2, A, dH, ws, wait_limit: int, stream=
                                            ws.numel() * ws.element_size(), wait_limit, _stream(stream)))
 
 
+def us_ffn_gated_fwd(fn, X, Wg, Wu, alpha, A, ws, H=None, U=None, act_in_scale=1.0, act_out_scale=1.0, stream=None):
+    """Hidden layer of a gated FFN block in one launch: A = act_out_scale f(act_in_scale h) u with h = alpha X Wg, u = alpha X Wu; H and U (both
+    or neither) receive h and u as the backward pass reads them."""
+    _check("us_ffn_gated_fwd", _entry("us_ffn_gated_fwd")(FN_BY_NAME.get(fn, fn), X, Wg, Wu, alpha, act_in_scale, act_out_scale, H, U, A, ws, ws, _stream(stream)))
+    return A
+
+
+def us_ffn_gated_bwd(fn, G, W2, beta_x, H, U, dH, dU, ws, act_in_scale=1.0, beta_h=1.0, beta_u=1.0, stream=None):
+    """Its backward pass down to both projections: dH and dU from G = the gradient of the second layer's output, W2 and the stored H, U."""
+    _check("us_ffn_gated_bwd", _entry("us_ffn_gated_bwd")(FN_BY_NAME.get(fn, fn), G, W2, beta_x, act_in_scale, beta_h, beta_u, H, U, dH, dU, ws, ws, _stream(stream)))
+    return dH, dU
+
+
+def us_test_ffn_gated_fwd_starved(X, Wg, Wu, H, U, A, ws, wait_limit: int, cta: int, tiles: int, stream=None):
+    """us_test_linear_fwd_starved_cta for the kernel of us_ffn_gated_fwd."""
+    _check("us_test_ffn_gated_fwd_starved", _lib.us_test_ffn_gated_fwd_starved(*(C.byref(mat(t)) if t is not None else None for t in (X, Wg, Wu, H, U, A)), ws.data_ptr(),
+                                                                               ws.numel(), wait_limit, cta, tiles, _stream(stream)))
+
+
+def us_test_ffn_gated_bwd_starved(G, W2, H, U, dH, dU, ws, wait_limit: int, cta: int, tiles: int, stream=None):
+    """us_test_linear_fwd_starved_cta for the kernel of us_ffn_gated_bwd."""
+    _check("us_test_ffn_gated_bwd_starved", _lib.us_test_ffn_gated_bwd_starved(*(C.byref(mat(t)) for t in (G, W2, H, U, dH, dU)), ws.data_ptr(), ws.numel(), wait_limit, cta,
+                                                                               tiles, _stream(stream)))
+
+
 def us_test_linear_fwd_starved_cta(X, W, alpha, Y, ws, wait_limit: int, cta: int, tiles: int, stream=None):
     """us_test_linear_fwd_starved with loads withheld from one CTA of each cluster (-1: every CTA) after its first `tiles` tiles."""
     _check("us_test_linear_fwd_starved_cta",
@@ -689,6 +720,13 @@ def us_scales_activation(fn, constrained: bool = False):
     a, b = C.c_float(), C.c_float()
     _check("us_scales_activation", _lib.us_scales_activation(FN_BY_NAME.get(fn, fn), int(constrained), C.byref(a), C.byref(b)))
     return a.value, b.value
+
+
+def us_scales_gated(fn, constrained: bool = False):
+    """(alpha, beta_h, beta_u) of a gated product."""
+    v = [C.c_float() for _ in range(3)]
+    _check("us_scales_gated", _lib.us_scales_gated(FN_BY_NAME.get(fn, fn), int(constrained), *(C.byref(x) for x in v)))
+    return tuple(x.value for x in v)
 
 
 def us_residual_add(skip, branch, tau, out, stream=None):
