@@ -23,8 +23,10 @@ namespace us {
 namespace {
 
 constexpr int kGatedEW = 8;
-constexpr int kRoom = 229376;                 // shared memory for stages
+constexpr int kRoom = 229376;                 // shared memory for stages and the epilogue's boxes
 constexpr int kMostStages = 16;
+// Backward, an epilogue warp has boxes of 32 rows x up to 64 bytes: two pairs that the copies of h and u arrive in, one that dH and dU leave from.
+constexpr int kBoxBytes = 2048, kEpiWarpBytes = 6 * kBoxBytes;
 
 struct GatedParams {
   int M, N, K;                                // results are [M x N]; length of the contraction
@@ -34,8 +36,9 @@ struct GatedParams {
   float scale;                                // alpha / beta_x
   float act_in, c0, c1;                       // c0: act_out / beta_u; c1: - / beta_h * act_in
   int fn;
-  uint8_t *h, *u; long long h_ld, u_ld; int kept_dt, kept_sectors;     // the copies (forward: nullptr where not wanted)
-  uint8_t *o0, *o1; long long o0_ld, o1_ld; int out_dt, out_sectors;   // A / dH, dU
+  int kept_dt, out_dt;                        // types of the copies of h and u, and of the results
+  uint8_t *h, *u, *o0; long long h_ld, u_ld, o0_ld; int kept_sectors, out_sectors;     // forward: the copies (nullptr: not wanted) and A
+  int unit_cols;                              // backward: columns of a box (32, or 64 of 8 bits)
   unsigned int* status;
   uint32_t wait_limit;
   uint32_t a_bytes; int stages;               // bytes of A in a stage (single CTAs: the rows that exist), and the stages that fit
@@ -48,6 +51,8 @@ struct GatedShape {
   static constexpr int kRowsB = kN / CG;                   // rows of B a CTA fetches
   static constexpr int kBBytes = kRowsB * kStageKBytes;
   static constexpr int kStageBytes = kBM * kStageKBytes + kBBytes;
+  static constexpr int kEpiBytes = BWD ? kGatedEW * kEpiWarpBytes : 0;
+  static constexpr int kStages = (kRoom - kEpiBytes) / kStageBytes;
   static constexpr int kBarrierBytes = 512;
   static constexpr int kTotal = kRoom + kBarrierBytes + 1024;
   // Forward: B is N-major, in chunks of rows of K: 128 bytes wide, or the columns of one projection where they are fewer
@@ -151,28 +156,6 @@ __device__ __forceinline__ void put_row(uint8_t* dst, int es, const uint32_t (&w
       }
   }
 }
-// The stored words of S columns; what does not exist is zero.
-template <int S>
-__device__ __forceinline__ void get_row(const uint8_t* src, int es, uint32_t (&w)[S / 2], int cols) {
-#pragma unroll
-  for (int i = 0; i < S / 2; ++i) w[i] = 0u;
-  if (cols >= S) {
-    const uint4* q = reinterpret_cast<const uint4*>(src);
-#pragma unroll
-    for (int i = 0; i < S / 8; ++i) {
-      if (es == 1 && i >= S / 16) break;
-      const uint4 v = __ldg(q + i);
-      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < S; ++i)
-      if (i < cols) {
-        if (es == 2) w[i >> 1] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(src) + i) << (16 * (i & 1));
-        else w[(i >> 2) % (S / 2)] |= (uint32_t)__ldg(src + i) << (8 * (i & 3));
-      }
-  }
-}
 template <int S>
 __device__ __forceinline__ void widen_row(int dt, const uint32_t (&w)[S / 2], float (&v)[S]) {
   if (dt == US_E4M3) {
@@ -198,12 +181,14 @@ __device__ __forceinline__ uint64_t chunk_desc(uint32_t addr, int row_bytes, uin
 // ES: operand bytes per element (1 = FP8, 2 = BF16 / F16).  HC: hidden columns of a tile.  CG = 2: tiles of 256 rows by a CTA pair, 1: of 128 by a CTA.
 template <bool BWD, int ES, int HC, int CG>
 __global__ void __launch_bounds__(gemm_threads(kGatedEW), 1)
-gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0, const __grid_constant__ CUtensorMap tm_b1, const GatedParams p) {
+gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0, const __grid_constant__ CUtensorMap tm_b1,
+             const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_dh,
+             const __grid_constant__ CUtensorMap tm_du, const GatedParams p) {
   using S = GatedShape<BWD, ES, HC, CG>;
   constexpr int kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
   constexpr uint32_t kTmemCols = 2 * kN;
   const uint32_t a_bytes = CG == 2 ? (uint32_t)(kBM * kStageKBytes) : p.a_bytes, stage_bytes = a_bytes + S::kBBytes;
-  const int stages = CG == 2 ? kRoom / S::kStageBytes : p.stages;
+  const int stages = CG == 2 ? S::kStages : p.stages;
 
   ptx::grid_release_next();
   extern __shared__ uint8_t smem_raw[];
@@ -215,8 +200,10 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
   auto acc_full_bar = [&](int a) { return bars + 8u * (2 * kMostStages + a); };
   auto acc_empty_bar = [&](int a) { return bars + 8u * (2 * kMostStages + 2 + a); };
   const uint32_t drained_bar = bars + 8u * (2 * kMostStages + 4);
-  static_assert(8 * (2 * kMostStages + 5) + 8 <= S::kBarrierBytes, "barrier area too small");
-  uint8_t* tail = smem_gen + kRoom + 8 * (2 * kMostStages + 5);
+  auto in_bar = [&](int w, int s) { return bars + 8u * (2 * kMostStages + 5 + 2 * w + s); };
+  constexpr int kBars = 2 * kMostStages + 5 + 2 * kGatedEW;
+  static_assert(8 * kBars + 8 <= S::kBarrierBytes, "barrier area too small");
+  uint8_t* tail = smem_gen + kRoom + 8 * kBars;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 4);
 
@@ -231,6 +218,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
     for (int s = 0; s < stages; ++s) { ptx::mbar_init(full_bar(s), 1); ptx::mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full_bar(a), 1); ptx::mbar_init(acc_empty_bar(a), CG * kGatedEW); }
     ptx::mbar_init(drained_bar, 1);
+    if (BWD) for (int w = 0; w < kGatedEW; ++w) { ptx::mbar_init(in_bar(w, 0), 1); ptx::mbar_init(in_bar(w, 1), 1); }
     *abort_flag = 0;
     ptx::mbar_init_fence();
     ptx::prefetch_tensormap(&tm_a);
@@ -356,47 +344,29 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
       row = tm * kTileM + rank * kBM + q * 32 + lane;
       col = tn * HC + part * S::kWarpCols;
     };
-    // Backward: the copies of the slice that comes next are on their way while one is worked on.
-    uint32_t rh[kSl / 2], ru[kSl / 2];
-    auto fetch = [&](int tile, int slice) {
-      if (tile >= num_tiles) return;
-      int row, col;
-      place(tile, row, col);
-      col += slice * kSl;
-      const int cols = row < p.M ? p.N - col : 0;
-      get_row<kSl>(p.h + (row * p.h_ld + col) * kept_es, kept_es, rh, cols);
-      get_row<kSl>(p.u + (row * p.u_ld + col) * kept_es, kept_es, ru, cols);
-    };
-    if (BWD) fetch(unit, 0);
-
     uint32_t local = 0;
     bool ok = true;
-    for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
-      int row, col0;
-      place(tile, row, col0);
-      const uint32_t acc = local & 1u, acc_phase = (local >> 1) & 1u;
-      ok = wait_bounded(acc_full_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      ptx::tc_fence_after_sync();
-      const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * kN + part * S::kWarpCols;
+    if constexpr (!BWD) {
+      for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
+        int row, col0;
+        place(tile, row, col0);
+        const uint32_t acc = local & 1u, acc_phase = (local >> 1) & 1u;
+        ok = wait_bounded(acc_full_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * kN + part * S::kWarpCols;
 #pragma unroll 1
-      for (int sl = 0; sl < kSlices; ++sl) {
-        const int col = col0 + sl * kSl, cols = row < p.M ? p.N - col : 0;
-        uint32_t r0[kSl], r1[BWD ? 1 : kSl];
-        if constexpr (kSl == 32) ptx::tmem_ld_32x32_issue(t_row + sl * kSl, r0); else ptx::tmem_ld_32x32_issue(t_row + sl * kSl, r0);
-        if constexpr (!BWD) ptx::tmem_ld_32x32_issue(t_row + HC + sl * kSl, r1);
-        float a[kSl], b[kSl];
-        if constexpr (BWD) {                                    // a, b: the kept projections, then dH, dU
-          widen_row<kSl>(p.kept_dt, rh, a);
-          widen_row<kSl>(p.kept_dt, ru, b);
-          if (sl + 1 < kSlices) fetch(tile, sl + 1); else fetch(tile + num_units, 0);
-        }
-        ptx::tmem_ld_fence(r0);
-        if constexpr (!BWD) ptx::tmem_ld_fence(r1);
-        if (sl + 1 == kSlices) release_acc(acc, tile);          // the values are in registers
-        uint32_t w[kSl / 2];
-        if constexpr (!BWD) {
+        for (int sl = 0; sl < kSlices; ++sl) {
+          const int col = col0 + sl * kSl, cols = row < p.M ? p.N - col : 0;
+          uint32_t r0[kSl], r1[kSl];
+          ptx::tmem_ld_32x32_issue(t_row + sl * kSl, r0);
+          ptx::tmem_ld_32x32_issue(t_row + HC + sl * kSl, r1);
+          ptx::tmem_ld_fence(r0);
+          ptx::tmem_ld_fence(r1);
+          if (sl + 1 == kSlices) release_acc(acc, tile);          // the values are in registers
+          float a[kSl], b[kSl];
+          uint32_t w[kSl / 2];
 #pragma unroll
           for (int i = 0; i < kSl; ++i) { a[i] = p.scale * __uint_as_float(r0[i]); b[i] = p.scale * __uint_as_float(r1[i]); }
           if (p.h) {
@@ -411,10 +381,81 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
           });
           pack_row<kSl>(p.out_dt, a, w);
           put_row<kSl>(p.o0 + (row * p.o0_ld + col) * out_es, out_es, w, cols, p.out_sectors);
-        } else {
+        }
+      }
+    } else {
+      // Units of unit_cols columns: the copies of two are on their way while one is worked on.  A lane's row of a box is read and written by that
+      // lane, 16-byte chunk c at c ^ the pattern of its row (64-byte rows swizzled, 32-byte ones not).
+      const int ew = warp - 2, uc = p.unit_cols;
+      const uint32_t boxes = smem_base + (uint32_t)(kRoom - S::kEpiBytes + ew * kEpiWarpBytes), box_out = boxes + 4 * kBoxBytes;
+      const int in_row = uc * kept_es, out_row = uc * out_es;
+      const uint32_t in_sw = in_row == 64 ? (uint32_t)((lane >> 1) & 3) : 0u, out_sw = out_row == 64 ? (uint32_t)((lane >> 1) & 3) : 0u;
+      uint32_t issued = 0, used = 0;
+      int next_tile = unit, next_col = 0;                        // the unit whose copies are fetched next: columns from the warp's first on
+      auto fetch = [&]() {
+        int row = 0, col = 0;
+        for (; next_tile < num_tiles; next_tile += num_units, next_col = 0) {
+          place(next_tile, row, col);
+          if (next_col < S::kWarpCols && col + next_col < p.N) break;
+        }
+        if (next_tile >= num_tiles) return;
+        if (ptx::elect_one()) {
+          const uint32_t bar = in_bar(ew, issued & 1u), dst = boxes + (issued & 1u) * 2 * kBoxBytes;
+          ptx::mbar_expect_tx(bar, 64u * in_row);
+          ptx::tma_load_2d(dst, &tm_h, bar, col + next_col, row - lane);
+          ptx::tma_load_2d(dst + kBoxBytes, &tm_u, bar, col + next_col, row - lane);
+        }
+        ++issued;
+        next_col += uc;
+      };
+      fetch();
+      fetch();
+      for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
+        int row, col0;
+        place(tile, row, col0);
+        const uint32_t acc = local & 1u, acc_phase = (local >> 1) & 1u;
+        ok = wait_bounded(acc_full_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * kN + part * S::kWarpCols;
+        const int end = min(S::kWarpCols, p.N - col0);           // columns of this warp that exist
+        if (end <= 0) release_acc(acc, tile);
+#pragma unroll 1
+        for (int at = 0; at < end; at += 32) {
+          const int off = at & (uc - 1);
+          const bool last_of_unit = off + 32 == uc || at + 32 >= end;
+          uint32_t r0[32];
+          ptx::tmem_ld_32x32_issue(t_row + at, r0);
+          if (off == 0) {
+            ok = wait_bounded(in_bar(ew, used & 1u), (used >> 1) & 1u, abort_flag, p.status, p.wait_limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+          }
+          uint32_t rh[16], ru[16];
+          {
+            const uint32_t src = boxes + (used & 1u) * 2 * kBoxBytes + (uint32_t)(lane * in_row), c0 = (uint32_t)(off * kept_es) >> 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (k >= 2 && kept_es == 1) break;
+              const uint4 vh = ptx::lds128(src + (((c0 + k) ^ in_sw) << 4)), vu = ptx::lds128(src + kBoxBytes + (((c0 + k) ^ in_sw) << 4));
+              rh[4 * k] = vh.x; rh[4 * k + 1] = vh.y; rh[4 * k + 2] = vh.z; rh[4 * k + 3] = vh.w;
+              ru[4 * k] = vu.x; ru[4 * k + 1] = vu.y; ru[4 * k + 2] = vu.z; ru[4 * k + 3] = vu.w;
+            }
+          }
+          if (last_of_unit) {
+            ++used;
+            __syncwarp();
+            fetch();
+          }
+          float a[32], b[32];                                    // the kept projections, then dH, dU
+          widen_row<32>(p.kept_dt, rh, a);
+          widen_row<32>(p.kept_dt, ru, b);
+          ptx::tmem_ld_fence(r0);
+          if (at + 32 >= end) release_acc(acc, tile);            // the values are in registers
           with_gate(p.fn, [&](auto fn) {
 #pragma unroll
-            for (int i = 0; i < kSl; ++i) {
+            for (int i = 0; i < 32; ++i) {
               const float d = p.scale * __uint_as_float(r0[i]);
               float f, df;
               gate_both<decltype(fn)::value>(p.act_in * a[i], f, df);
@@ -422,12 +463,39 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
               b[i] = p.c0 * f * d;
             }
           });
-          pack_row<kSl>(p.out_dt, a, w);
-          put_row<kSl>(p.o0 + (row * p.o0_ld + col) * out_es, out_es, w, cols, p.out_sectors);
-          pack_row<kSl>(p.out_dt, b, w);
-          put_row<kSl>(p.o1 + (row * p.o1_ld + col) * out_es, out_es, w, cols, p.out_sectors);
+          if (off == 0) {                                        // the stores of the unit before have read the boxes
+            if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
+            __syncwarp();
+          }
+          const uint32_t dst = box_out + (uint32_t)(lane * out_row), c0 = (uint32_t)(off * out_es) >> 4;
+          uint32_t w[16];
+          auto stage = [&](uint32_t to) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (k >= 2 && out_es == 1) break;
+              ptx::sts128(to + (((c0 + k) ^ out_sw) << 4), make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]));
+            }
+          };
+          pack_row<32>(p.out_dt, a, w);
+          stage(dst);
+          pack_row<32>(p.out_dt, b, w);
+          stage(dst + kBoxBytes);
+          if (last_of_unit) {
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (ptx::elect_one()) {
+              ptx::tma_store_2d(&tm_dh, box_out, col0 + at - off, row - lane);
+              ptx::tma_store_2d(&tm_du, box_out + kBoxBytes, col0 + at - off, row - lane);
+              ptx::bulk_commit_group();
+            }
+          }
         }
       }
+      // Copies that are still in flight after a wait that ran out land, and stores have read their boxes, before the CTA gives up its shared memory.
+      for (; used < issued; ++used)
+        for (uint32_t it = 0; it < p.wait_limit && !ptx::mbar_try_wait(in_bar(ew, used & 1u), (used >> 1) & 1u); ++it) {}
+      if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
+      __syncwarp();
     }
     // Leaving (early too, when a wait ran out somewhere in the CTA): tensor-memory loads have landed.
     ptx::tmem_ld_wait_all();
@@ -461,8 +529,11 @@ bool make_chunk_tmap(CUtensorMap* tm, const us_mat* m, int es, int box_rows, int
             CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+struct GatedMats { const us_mat *a, *b0, *b1, *h, *u, *dh, *du; };       // forward: h .. du not used
+
 template <bool BWD, int ES, int HC, int CG>
-us_status launch_gated(const us_mat* A, const us_mat* B0, const us_mat* B1, GatedParams& p, int sms, cudaStream_t st) {
+us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t st) {
+  const us_mat *A = m.a, *B0 = m.b0, *B1 = m.b1;
   using S = GatedShape<BWD, ES, HC, CG>;
   p.tiles_m = (p.M + kBM * CG - 1) / (kBM * CG);
   p.tiles_n = (p.N + HC - 1) / HC;
@@ -473,31 +544,40 @@ us_status launch_gated(const us_mat* A, const us_mat* B0, const us_mat* B1, Gate
   // a short A: its rows in groups of eight.  The MMA still reads 128; what lies behind them ends up in rows that do not exist.
   const int a_rows = CG == 1 && p.M < kBM ? (p.M + 7) / 8 * 8 : kBM;
   p.a_bytes = (uint32_t)a_rows * kStageKBytes;
-  p.stages = std::min(kMostStages, (kRoom - kBM * kStageKBytes) / ((int)p.a_bytes + S::kBBytes));
-  CUtensorMap t[3];
+  p.stages = std::min(kMostStages, (kRoom - std::max(S::kEpiBytes, kBM * kStageKBytes)) / ((int)p.a_bytes + S::kBBytes));
+  CUtensorMap t[7];
   constexpr int kBK = kStageKBytes / ES;
   if (!host::make_tmap(&t[0], A, ES, a_rows, kStageKBytes)) return US_ERR_CUDA;
   if (!(BWD ? host::make_tmap(&t[1], B0, ES, S::kRowsB, kStageKBytes) : make_chunk_tmap(&t[1], B0, ES, kBK, S::kChunkRow))) return US_ERR_CUDA;
   if (BWD) t[2] = t[1];
   else if (!make_chunk_tmap(&t[2], B1, ES, kBK, S::kChunkRow)) return US_ERR_CUDA;
+  if (BWD) {
+    const int kept_es = dtype_size(m.h->dtype), out_es = dtype_size(m.dh->dtype);
+    p.unit_cols = kept_es == 1 && out_es == 1 && S::kWarpCols >= 64 ? 64 : 32;
+    if (!host::make_tmap(&t[3], m.h, kept_es, 32, p.unit_cols * kept_es) || !host::make_tmap(&t[4], m.u, kept_es, 32, p.unit_cols * kept_es) ||
+        !host::make_tmap(&t[5], m.dh, out_es, 32, p.unit_cols * out_es) || !host::make_tmap(&t[6], m.du, out_es, 32, p.unit_cols * out_es))
+      return US_ERR_CUDA;
+  } else {
+    t[3] = t[4] = t[5] = t[6] = t[0];
+  }
   const int tiles = p.tiles_m * p.tiles_n, most = sms / CG;
   static std::atomic<uint64_t> smem_set{0};
-  return host::launch(gated_kernel<BWD, ES, HC, CG>, &smem_set, CG * (tiles < most ? tiles : most), gemm_threads(kGatedEW), S::kTotal, CG, st, t[0], t[1], t[2],
-                      static_cast<const GatedParams&>(p));
+  return host::launch(gated_kernel<BWD, ES, HC, CG>, &smem_set, CG * (tiles < most ? tiles : most), gemm_threads(kGatedEW), S::kTotal, CG, st, t[0], t[1], t[2], t[3],
+                      t[4], t[5], t[6], static_cast<const GatedParams&>(p));
 }
 
 // Tiles of CTA pairs unless they would leave more than half of the pairs idle, else the widest of single CTAs, else, where the machine has
 // an SM for each of them, the narrow ones.
 template <bool BWD, int ES>
-us_status pick_gated(const us_mat* A, const us_mat* B0, const us_mat* B1, GatedParams& p, cudaStream_t st) {
+us_status pick_gated(const GatedMats& m, GatedParams& p, cudaStream_t st) {
   const int sms = host::sm_count();
   if (sms <= 0) return US_ERR_CUDA;
   constexpr int kWide = BWD ? 256 : 128;
   const int64_t M = p.M, N = p.N;
-  if (4 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) >= sms && M > kBM) return launch_gated<BWD, ES, kWide, 2>(A, B0, B1, p, sms, st);
+  if (4 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) >= sms && M > kBM) return launch_gated<BWD, ES, kWide, 2>(m, p, sms, st);
   const int64_t narrow = ((M + kBM - 1) / kBM) * ((N + kWide / 4 - 1) / (kWide / 4));
-  if (narrow <= sms) return launch_gated<BWD, ES, kWide / 4, 1>(A, B0, B1, p, sms, st);
-  return launch_gated<BWD, ES, kWide / 2, 1>(A, B0, B1, p, sms, st);
+  if (narrow <= sms) return launch_gated<BWD, ES, kWide / 4, 1>(m, p, sms, st);
+  return launch_gated<BWD, ES, kWide / 2, 1>(m, p, sms, st);
 }
 
 // The checks that both directions share: operands of one width (f8: 8-bit), workspace.
@@ -538,7 +618,8 @@ us_status gated_fwd(int fn, const us_mat* X, const us_mat* Wg, const us_mat* Wu,
   p.o0 = static_cast<uint8_t*>(A->ptr); p.o0_ld = A->ld; p.out_dt = A->dtype; p.out_sectors = aligned(A, 32);
   p.status = static_cast<unsigned int*>(ws); p.wait_limit = wait_limit; p.starved = starved; p.served = served;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return f8 ? pick_gated<false, 1>(X, Wg, Wu, p, st) : pick_gated<false, 2>(X, Wg, Wu, p, st);
+  const GatedMats m{X, Wg, Wu, nullptr, nullptr, nullptr, nullptr};
+  return f8 ? pick_gated<false, 1>(m, p, st) : pick_gated<false, 2>(m, p, st);
 }
 
 us_status gated_bwd(int fn, const us_mat* G, const us_mat* W2, float beta_x, float act_in, float beta_h, float beta_u, const us_mat* H, const us_mat* U,
@@ -556,12 +637,11 @@ us_status gated_bwd(int fn, const us_mat* G, const us_mat* W2, float beta_x, flo
   GatedParams p{};
   p.M = (int)M; p.N = (int)N; p.K = (int)K;
   p.scale = beta_x; p.act_in = act_in; p.c0 = beta_u; p.c1 = beta_h * act_in; p.fn = fn;
-  p.h = static_cast<uint8_t*>(H->ptr); p.h_ld = H->ld; p.u = static_cast<uint8_t*>(U->ptr); p.u_ld = U->ld; p.kept_dt = H->dtype;
-  p.o0 = static_cast<uint8_t*>(dH->ptr); p.o0_ld = dH->ld; p.o1 = static_cast<uint8_t*>(dU->ptr); p.o1_ld = dU->ld;
-  p.out_dt = dH->dtype; p.out_sectors = aligned(dH, 32) && aligned(dU, 32);
+  p.kept_dt = H->dtype; p.out_dt = dH->dtype;
   p.status = static_cast<unsigned int*>(ws); p.wait_limit = wait_limit; p.starved = starved; p.served = served;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return f8 ? pick_gated<true, 1>(G, W2, W2, p, st) : pick_gated<true, 2>(G, W2, W2, p, st);
+  const GatedMats m{G, W2, W2, H, U, dH, dU};
+  return f8 ? pick_gated<true, 1>(m, p, st) : pick_gated<true, 2>(m, p, st);
 }
 
 // Test hook: of a CTA pair only the odd one may starve alone (the even one waits for its copies; nobody would wait for those of the odd one).
