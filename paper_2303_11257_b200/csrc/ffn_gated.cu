@@ -22,16 +22,20 @@
 namespace us {
 namespace {
 
-constexpr int kGatedEW = 8;
+// Epilogue warps.  Of a CTA pair's tiles sixteen a CTA, whose arithmetic is the longest part of an FP8 tile; backward with 16-bit operands, where the MMAs
+// take twice as long, eight with two slots each.  (8192 x 1024 x 4096 backward, us, sixteen with one slot / eight with two: FP8 54.0 / 57.5, BF16 90.9 / 88.3.)
+__host__ __device__ constexpr bool gated_few(bool bwd, int es, int cg) { return cg == 1 || (bwd && es == 2); }
+__host__ __device__ constexpr int gated_ew(bool bwd, int es, int cg) { return gated_few(bwd, es, cg) ? 8 : 16; }
 constexpr int kRoom = 229376;                 // shared memory for stages and the epilogue's boxes
 constexpr int kMostStages = 16;
-// Backward, an epilogue warp has boxes of 32 rows x up to 64 bytes: two pairs that the copies of h and u arrive in, one that dH and dU leave from.
-constexpr int kBoxBytes = 2048, kEpiWarpBytes = 6 * kBoxBytes;
+// Backward, an epilogue warp has one or two slots for the copies of h and u that arrive and the dH and dU that leave, in boxes of 32 rows x up to 64 bytes.
+constexpr int kSlotBytes = 6144;
 
 struct GatedParams {
   int M, N, K;                                // results are [M x N]; length of the contraction
   int tiles_m, tiles_n;
-  FastDiv d_tiles_m;
+  int band_m, full_bands;                     // tile rows of a band of the tile order, and the bands that have as many
+  FastDiv d_band, d_rows, d_rows_last;        // by band_m * tiles_n, band_m, tiles_m % band_m
   uint32_t idesc;
   float scale;                                // alpha / beta_x
   float act_in, c0, c1;                       // c0: act_out / beta_u; c1: - / beta_h * act_in
@@ -48,17 +52,18 @@ struct GatedParams {
 template <bool BWD, int ES, int HC, int CG>
 struct GatedShape {
   static constexpr int kN = BWD ? HC : 2 * HC;             // columns of an accumulator
+  static constexpr int kEW = gated_ew(BWD, ES, CG), kSlots = gated_few(BWD, ES, CG) ? 2 : 1;   // warps and slots of the epilogue
   static constexpr int kRowsB = kN / CG;                   // rows of B a CTA fetches
   static constexpr int kBBytes = kRowsB * kStageKBytes;
   static constexpr int kStageBytes = kBM * kStageKBytes + kBBytes;
-  static constexpr int kEpiBytes = BWD ? kGatedEW * kEpiWarpBytes : 0;
+  static constexpr int kEpiBytes = BWD ? kEW * kSlots * kSlotBytes : 0;
   static constexpr int kStages = (kRoom - kEpiBytes) / kStageBytes;
-  static constexpr int kBarrierBytes = 512;
+  static constexpr int kBarrierBytes = 1024;
   static constexpr int kTotal = kRoom + kBarrierBytes + 1024;
   // Forward: B is N-major, in chunks of rows of K: 128 bytes wide, or the columns of one projection where they are fewer
   static constexpr int kChunkRow = CG == 2 || HC * ES >= 128 ? 128 : HC * ES;
   static constexpr int kChunkBytes = (kStageKBytes / ES) * kChunkRow;
-  static constexpr int kWarpCols = HC / (kGatedEW / 4);    // hidden columns of an epilogue warp, worked in slices
+  static constexpr int kWarpCols = HC / (kEW / 4);    // hidden columns of an epilogue warp, worked in slices
   static constexpr int kSlice = kWarpCols < 32 ? kWarpCols : 32;
 };
 
@@ -68,47 +73,93 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// 1 / (1 + e^-z), relative error of a few 2^-22 and |z| 2^-23: far inside a step of the 16 and 8 bits that the results are rounded to.
-__device__ __forceinline__ float sigmoid_fast(float z) { return rcp_approx(1.0f + ex2_approx(-1.4426950408889634f * z)); }
-
-template <int FN>
-__device__ __forceinline__ float gate_value(float z) {
-  if (FN == US_FN_SILU) return z * sigmoid_fast(z);
-  if (FN == US_FN_SIGMOID) return sigmoid_fast(z);
-  if (FN == US_FN_GELU) return gelu_scaled(z, 1.f, 1.f);
-  return act_value(FN, z);
+// Two values at a time (packed float32 arithmetic): x holds pre-activations, in2 = splat(act_in), nl2 = splat(-act_in log2 e).
+// sigmoid(act_in x) = 1 / (1 + e^-z): relative error of a few 2^-22 and |z| 2^-23, far inside a step of the 16 and 8 bits that results are rounded to.
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 x, f32x2 nl2) {
+  float p0, p1;
+  unpack2(mul2(x, nl2), p0, p1);
+  unpack2(add2(pack2(ex2_approx(p0), ex2_approx(p1)), splat2(1.0f)), p0, p1);
+  return pack2(rcp_approx(p0), rcp_approx(p1));
 }
-// f(z) and f'(z)
+__device__ __forceinline__ f32x2 normal_cdf2(f32x2 z) {
+  float z0, z1, q0, q1;
+  unpack2(z, z0, z1);
+  normal_tail2(sat_mul_abs(z0, 1.0f / kTailRange), sat_mul_abs(z1, 1.0f / kTailRange), q0, q1);
+  return pack2(z0 >= 0.f ? 1.0f - q0 : q0, z1 >= 0.f ? 1.0f - q1 : q1);
+}
+// f(act_in x)
 template <int FN>
-__device__ __forceinline__ void gate_both(float z, float& f, float& df) {
-  if (FN == US_FN_SILU) {
-    const float s = sigmoid_fast(z);
-    f = z * s;
-    df = fmaf(f, 1.0f - s, s);
-  } else if (FN == US_FN_SIGMOID) {
-    f = sigmoid_fast(z);
-    df = f * (1.0f - f);
-  } else if (FN == US_FN_GELU) {
-    const float q = normal_tail(z), Phi = z >= 0.f ? 1.0f - q : q;
-    f = z * Phi;
-    df = fmaf(z * 0.39894228040143268f, ex2_approx((-0.72134752044448170f * z) * z), Phi);
+__device__ __forceinline__ f32x2 gate_value2(f32x2 x, f32x2 in2, f32x2 nl2) {
+  if (FN == US_FN_SILU) return mul2(mul2(x, in2), sigmoid2(x, nl2));
+  if (FN == US_FN_SIGMOID) return sigmoid2(x, nl2);
+  if (FN == US_FN_TANH) return fma2(sigmoid2(x, add2(nl2, nl2)), splat2(2.0f), splat2(-1.0f));      // tanh z = 2 sigmoid(2 z) - 1
+  const f32x2 z = mul2(x, in2);
+  if (FN == US_FN_GELU) return mul2(z, normal_cdf2(z));
+  float z0, z1;
+  unpack2(z, z0, z1);
+  return pack2(act_value(US_FN_RELU, z0), act_value(US_FN_RELU, z1));
+}
+// Both gradients of a product: yh = c1 f'(act_in x) u d, yu = c0 f(act_in x) d; c0, c1 splat.
+template <int FN>
+__device__ __forceinline__ void gate_grads2(f32x2 x, f32x2 u, f32x2 d, float act_in, f32x2 nl2, f32x2 c0, f32x2 c1, f32x2& yh, f32x2& yu) {
+  const f32x2 one = splat2(1.0f), in2 = splat2(act_in);
+  f32x2 f, df;
+  if (FN == US_FN_SILU) {                                 // f' = s (1 + z (1 - s)), f = z s; c0 holds act_in, too
+    const f32x2 s = sigmoid2(x, nl2), g = mul2(s, d);
+    yu = mul2(mul2(g, x), c0);
+    yh = mul2(mul2(mul2(g, fma2(x, fma2(s, splat2(-act_in), in2), one)), u), c1);
+    return;
+  }
+  if (FN == US_FN_SIGMOID) {
+    f = sigmoid2(x, nl2);
+    df = mul2(f, fma2(f, splat2(-1.0f), one));
+  } else if (FN == US_FN_TANH) {
+    const f32x2 s = sigmoid2(x, add2(nl2, nl2));
+    f = fma2(s, splat2(2.0f), splat2(-1.0f));
+    df = mul2(mul2(s, splat2(4.0f)), fma2(s, splat2(-1.0f), one));
   } else {
-    f = act_value(FN, z);
-    df = act_slope(FN, z);
+    const f32x2 z = mul2(x, in2);
+    float z0, z1;
+    if (FN == US_FN_GELU) {
+      const f32x2 Phi = normal_cdf2(z);
+      unpack2(mul2(mul2(splat2(-0.72134752044448170f), z), z), z0, z1);
+      f = mul2(z, Phi);
+      df = fma2(mul2(z, splat2(0.39894228040143268f)), pack2(ex2_approx(z0), ex2_approx(z1)), Phi);
+    } else {
+      unpack2(z, z0, z1);
+      f = pack2(act_value(US_FN_RELU, z0), act_value(US_FN_RELU, z1));
+      df = pack2(act_slope(US_FN_RELU, z0), act_slope(US_FN_RELU, z1));
+    }
+  }
+  yh = mul2(mul2(mul2(c1, df), u), d);
+  yu = mul2(mul2(c0, f), d);
+}
+
+// What is computed from v[FROM .. FROM + COUNT - 1] is computed behind this, and behind the stores before it: a slice is worked on in groups of
+// columns, because all of it at once does not fit the registers.
+template <int FROM, int COUNT, class T, int N>
+__device__ __forceinline__ void from_here(T (&v)[N]) {
+#pragma unroll
+  for (int i = FROM; i < FROM + COUNT; ++i) {
+    if constexpr (std::is_same_v<T, float>) asm volatile("" : "+f"(v[i])); else asm volatile("" : "+r"(v[i]));
+  }
+}
+template <int N, class G>
+__device__ __forceinline__ void unrolled(G g) {              // g(0) .. g(N - 1), the argument as a constant
+  if constexpr (N > 0) {
+    unrolled<N - 1>(g);
+    g(std::integral_constant<int, N - 1>());
   }
 }
 // Calls g with the launch's activation as a constant.
 template <class G>
 __device__ __forceinline__ void with_gate(int fn, G g) {
-  switch (fn) {
-    case US_FN_SILU: g(std::integral_constant<int, US_FN_SILU>()); break;
-    case US_FN_GELU: g(std::integral_constant<int, US_FN_GELU>()); break;
-    case US_FN_SIGMOID: g(std::integral_constant<int, US_FN_SIGMOID>()); break;
-    case US_FN_TANH: g(std::integral_constant<int, US_FN_TANH>()); break;
-    default: g(std::integral_constant<int, US_FN_RELU>()); break;
-  }
+  if (fn == US_FN_SILU) g(std::integral_constant<int, US_FN_SILU>());
+  else if (fn == US_FN_SIGMOID) g(std::integral_constant<int, US_FN_SIGMOID>());
+  else if (fn == US_FN_TANH) g(std::integral_constant<int, US_FN_TANH>());
+  else if (fn == US_FN_GELU) g(std::integral_constant<int, US_FN_GELU>());
+  else g(std::integral_constant<int, US_FN_RELU>());
 }
-
 // ---------------------------------------------------------------- a lane's S columns of a row
 // S results rounded to dt, packed.
 template <int S>
@@ -156,21 +207,35 @@ __device__ __forceinline__ void put_row(uint8_t* dst, int es, const uint32_t (&w
       }
   }
 }
-template <int S>
-__device__ __forceinline__ void widen_row(int dt, const uint32_t (&w)[S / 2], float (&v)[S]) {
-  if (dt == US_E4M3) {
+// Columns 2 i and 2 i + 1 of a row of stored words of type KEPT.
+template <int KEPT, int N>
+__device__ __forceinline__ f32x2 widen2(const uint32_t (&w)[N], int i) {
+  const float2 v = KEPT == US_E4M3 ? unpack_fp8x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))), false) : KEPT == US_BF16 ? unpack_bf16x2(w[i]) : unpack_f16x2(w[i]);
+  return pack2(v.x, v.y);
+}
+// Sixteen results rounded to type DT, packed: four words of 8-bit ones, eight of 16-bit ones.
+template <int DT>
+__device__ __forceinline__ void pack16(const f32x2 (&y)[8], uint32_t (&w)[8]) {
+  float v[16];
 #pragma unroll
-    for (int i = 0; i < S / 2; ++i) {
-      const float2 f = unpack_fp8x2((uint16_t)(w[i >> 1] >> (16 * (i & 1))), false);
-      v[2 * i] = f.x; v[2 * i + 1] = f.y;
-    }
-  } else if (dt == US_BF16) {
+  for (int i = 0; i < 8; ++i) unpack2(y[i], v[2 * i], v[2 * i + 1]);
 #pragma unroll
-    for (int i = 0; i < S / 2; ++i) { const float2 f = unpack_bf16x2(w[i]); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
-  } else {
-#pragma unroll
-    for (int i = 0; i < S / 2; ++i) { const float2 f = unpack_f16x2(w[i]); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+  for (int i = 0; i < 8; ++i) {
+    if (DT == US_BF16) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    else if (DT == US_F16) w[i] = pack_f16x2(v[2 * i], v[2 * i + 1]);
+    else if (i < 4) w[i] = cvt_fp8x4<DT == US_E5M2>(v[(4 * i) & 15], v[(4 * i + 1) & 15], v[(4 * i + 2) & 15], v[(4 * i + 3) & 15]);
   }
+}
+// Calls g with the types of the copies and of the results (of operands of ES bytes) as constants.
+template <int ES, class G>
+__device__ __forceinline__ void with_formats(int kept, int out, G g) {
+  auto with_out = [&](auto k) {
+    constexpr int kOne = ES == 1 ? US_E5M2 : US_BF16, kOther = ES == 1 ? US_E4M3 : US_F16;
+    if (out == kOne) g(k, std::integral_constant<int, kOne>()); else g(k, std::integral_constant<int, kOther>());
+  };
+  if (kept == US_E4M3) with_out(std::integral_constant<int, US_E4M3>());
+  else if (kept == US_BF16) with_out(std::integral_constant<int, US_BF16>());
+  else with_out(std::integral_constant<int, US_F16>());
 }
 
 __device__ __forceinline__ uint64_t chunk_desc(uint32_t addr, int row_bytes, uint32_t lbo) {      // N-major B, swizzled by its row width
@@ -180,12 +245,12 @@ __device__ __forceinline__ uint64_t chunk_desc(uint32_t addr, int row_bytes, uin
 
 // ES: operand bytes per element (1 = FP8, 2 = BF16 / F16).  HC: hidden columns of a tile.  CG = 2: tiles of 256 rows by a CTA pair, 1: of 128 by a CTA.
 template <bool BWD, int ES, int HC, int CG>
-__global__ void __launch_bounds__(gemm_threads(kGatedEW), 1)
+__global__ void __launch_bounds__(gemm_threads(gated_ew(BWD, ES, CG)), 1)
 gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0, const __grid_constant__ CUtensorMap tm_b1,
              const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_dh,
              const __grid_constant__ CUtensorMap tm_du, const GatedParams p) {
   using S = GatedShape<BWD, ES, HC, CG>;
-  constexpr int kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
+  constexpr int kEW = S::kEW, kSlots = S::kSlots, kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
   constexpr uint32_t kTmemCols = 2 * kN;
   const uint32_t a_bytes = CG == 2 ? (uint32_t)(kBM * kStageKBytes) : p.a_bytes, stage_bytes = a_bytes + S::kBBytes;
   const int stages = CG == 2 ? S::kStages : p.stages;
@@ -200,8 +265,8 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
   auto acc_full_bar = [&](int a) { return bars + 8u * (2 * kMostStages + a); };
   auto acc_empty_bar = [&](int a) { return bars + 8u * (2 * kMostStages + 2 + a); };
   const uint32_t drained_bar = bars + 8u * (2 * kMostStages + 4);
-  auto in_bar = [&](int w, int s) { return bars + 8u * (2 * kMostStages + 5 + 2 * w + s); };
-  constexpr int kBars = 2 * kMostStages + 5 + 2 * kGatedEW;
+  auto in_bar = [&](int w, int s) { return bars + 8u * (2 * kMostStages + 5 + kSlots * w + s); };
+  constexpr int kBars = 2 * kMostStages + 5 + kSlots * kEW;
   static_assert(8 * kBars + 8 <= S::kBarrierBytes, "barrier area too small");
   uint8_t* tail = smem_gen + kRoom + 8 * kBars;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
@@ -211,14 +276,19 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
   const int rank = CG == 2 ? (int)ptx::cluster_ctarank() : 0;
   const int unit = blockIdx.x / CG, num_units = gridDim.x / CG;
   const int num_tiles = p.tiles_m * p.tiles_n, num_kb = (p.K + kBK - 1) / kBK;
-  // column-major over the tiles: units that run side by side share a panel of weights
-  auto tile_mn2 = [&](int tile, int& tm, int& tn) { tn = p.d_tiles_m.div(tile); tm = tile - tn * p.tiles_m; };
+  // in bands of band_m tile rows, down a band first and then across: what runs together covers whole rows of the results
+  auto tile_mn2 = [&](int tile, int& tm, int& tn) {
+    const int band = p.d_band.div(tile), first = band * p.band_m, r = tile - first * p.tiles_n;
+    const bool last = band >= p.full_bands;
+    tn = last ? p.d_rows_last.div(r) : p.d_rows.div(r);
+    tm = first + r - tn * (last ? p.tiles_m - first : p.band_m);
+  };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) { ptx::mbar_init(full_bar(s), 1); ptx::mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full_bar(a), 1); ptx::mbar_init(acc_empty_bar(a), CG * kGatedEW); }
+    for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full_bar(a), 1); ptx::mbar_init(acc_empty_bar(a), CG * kEW); }
     ptx::mbar_init(drained_bar, 1);
-    if (BWD) for (int w = 0; w < kGatedEW; ++w) { ptx::mbar_init(in_bar(w, 0), 1); ptx::mbar_init(in_bar(w, 1), 1); }
+    if (BWD) for (int w = 0; w < kSlots * kEW; ++w) ptx::mbar_init(in_bar(0, w), 1);
     *abort_flag = 0;
     ptx::mbar_init_fence();
     ptx::prefetch_tensormap(&tm_a);
@@ -330,6 +400,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
     // Warp (lane quarter q, part) owns 32 rows x kWarpCols hidden columns of the tile; a lane holds one row of them.
     const int q = warp & 3, part = (warp - 2) >> 2;
     const int out_es = dtype_size(p.out_dt), kept_es = dtype_size(p.kept_dt);
+    const f32x2 scale2 = splat2(p.scale), in2 = splat2(p.act_in), nl2 = splat2(-1.4426950408889634f * p.act_in), c0 = splat2(!BWD ? p.c0 : p.fn == US_FN_SILU ? p.c0 * p.scale * p.act_in : p.c0 * p.scale), c1 = splat2(p.c1 * p.scale);
     auto release_acc = [&](uint32_t a, int tile) {              // (where no later tile takes it nobody waits)
       ptx::tc_fence_before_sync();
       __syncwarp();
@@ -368,29 +439,38 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
           float a[kSl], b[kSl];
           uint32_t w[kSl / 2];
 #pragma unroll
-          for (int i = 0; i < kSl; ++i) { a[i] = p.scale * __uint_as_float(r0[i]); b[i] = p.scale * __uint_as_float(r1[i]); }
+          for (int i = 0; i < kSl; i += 2) {
+            unpack2(mul2(scale2, pack2(__uint_as_float(r0[i]), __uint_as_float(r0[i + 1]))), a[i], a[i + 1]);
+            unpack2(mul2(scale2, pack2(__uint_as_float(r1[i]), __uint_as_float(r1[i + 1]))), b[i], b[i + 1]);
+          }
           if (p.h) {
             pack_row<kSl>(p.kept_dt, a, w);
             put_row<kSl>(p.h + (row * p.h_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
             pack_row<kSl>(p.kept_dt, b, w);
             put_row<kSl>(p.u + (row * p.u_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
           }
+          float y[kSl];
           with_gate(p.fn, [&](auto fn) {
 #pragma unroll
-            for (int i = 0; i < kSl; ++i) a[i] = p.c0 * gate_value<decltype(fn)::value>(p.act_in * a[i]) * b[i];
+            for (int i = 0; i < kSl; i += 2)
+              unpack2(mul2(mul2(gate_value2<decltype(fn)::value>(pack2(a[i], a[i + 1]), in2, nl2), c0), pack2(b[i], b[i + 1])), y[i], y[i + 1]);
           });
-          pack_row<kSl>(p.out_dt, a, w);
+          pack_row<kSl>(p.out_dt, y, w);
           put_row<kSl>(p.o0 + (row * p.o0_ld + col) * out_es, out_es, w, cols, p.out_sectors);
         }
       }
     } else {
-      // Units of unit_cols columns: the copies of two are on their way while one is worked on.  A lane's row of a box is read and written by that
-      // lane, 16-byte chunk c at c ^ the pattern of its row (64-byte rows swizzled, 32-byte ones not).
+      // Units of unit_cols columns, whose copies arrive in a pair of boxes ahead of the accumulator and whose gradients leave from it.  A lane's row of a
+      // box is read and written by that lane, 16-byte chunk c at c ^ the pattern of its row (64-byte rows swizzled, 32-byte ones not).
       const int ew = warp - 2, uc = p.unit_cols;
-      const uint32_t boxes = smem_base + (uint32_t)(kRoom - S::kEpiBytes + ew * kEpiWarpBytes), box_out = boxes + 4 * kBoxBytes;
+      const uint32_t boxes = smem_base + (uint32_t)(kRoom - S::kEpiBytes + ew * kSlots * kSlotBytes);
       const int in_row = uc * kept_es, out_row = uc * out_es;
+      // where copies and gradients have one width a gradient takes the place of its copy
+      const uint32_t in_box = 32u * in_row, out_box = 32u * out_row, box_out = kept_es == out_es ? 0u : 2u * in_box;
       const uint32_t in_sw = in_row == 64 ? (uint32_t)((lane >> 1) & 3) : 0u, out_sw = out_row == 64 ? (uint32_t)((lane >> 1) & 3) : 0u;
       uint32_t issued = 0, used = 0;
+      auto slot_of = [&](uint32_t k) { return kSlots == 1 ? 0u : k & 1u; };
+      auto phase_of = [&](uint32_t k) { return kSlots == 1 ? k & 1u : (k >> 1) & 1u; };
       int next_tile = unit, next_col = 0;                        // the unit whose copies are fetched next: columns from the warp's first on
       auto fetch = [&]() {
         int row = 0, col = 0;
@@ -400,16 +480,16 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
         }
         if (next_tile >= num_tiles) return;
         if (ptx::elect_one()) {
-          const uint32_t bar = in_bar(ew, issued & 1u), dst = boxes + (issued & 1u) * 2 * kBoxBytes;
-          ptx::mbar_expect_tx(bar, 64u * in_row);
+          ptx::bulk_wait_group_read<kSlots - 1>();               // the stores that left from these boxes have read them
+          const uint32_t bar = in_bar(ew, slot_of(issued)), dst = boxes + slot_of(issued) * kSlotBytes;
+          ptx::mbar_expect_tx(bar, 2 * in_box);
           ptx::tma_load_2d(dst, &tm_h, bar, col + next_col, row - lane);
-          ptx::tma_load_2d(dst + kBoxBytes, &tm_u, bar, col + next_col, row - lane);
+          ptx::tma_load_2d(dst + in_box, &tm_u, bar, col + next_col, row - lane);
         }
         ++issued;
         next_col += uc;
       };
-      fetch();
-      fetch();
+      for (int k = 0; k < kSlots; ++k) fetch();
       for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
         int row, col0;
         place(tile, row, col0);
@@ -425,75 +505,61 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
         for (int at = 0; at < end; at += 32) {
           const int off = at & (uc - 1);
           const bool last_of_unit = off + 32 == uc || at + 32 >= end;
-          uint32_t r0[32];
-          ptx::tmem_ld_32x32_issue(t_row + at, r0);
           if (off == 0) {
-            ok = wait_bounded(in_bar(ew, used & 1u), (used >> 1) & 1u, abort_flag, p.status, p.wait_limit);
+            ok = wait_bounded(in_bar(ew, slot_of(used)), phase_of(used), abort_flag, p.status, p.wait_limit);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
           }
-          uint32_t rh[16], ru[16];
-          {
-            const uint32_t src = boxes + (used & 1u) * 2 * kBoxBytes + (uint32_t)(lane * in_row), c0 = (uint32_t)(off * kept_es) >> 4;
+          const uint32_t slot = boxes + slot_of(used) * kSlotBytes, src = slot + (uint32_t)(lane * in_row), dst = slot + box_out + (uint32_t)(lane * out_row);
+          const uint32_t in_chunk = (uint32_t)(off * kept_es) >> 4, out_chunk = (uint32_t)(off * out_es) >> 4;
+          with_formats<ES>(p.kept_dt, p.out_dt, [&](auto kept, auto out) {
+            with_gate(p.fn, [&](auto fn) {
+              constexpr int kWords = decltype(kept)::value == US_E4M3 ? 4 : 8;         // of sixteen kept values
+              unrolled<2>([&](auto half) {                       // sixteen columns
+                uint32_t r0[16], rh[kWords], ru[kWords], wh[8], wu[8];
+                ptx::tmem_ld_32x32_issue(t_row + at + 16 * decltype(half)::value, r0);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (k >= 2 && kept_es == 1) break;
-              const uint4 vh = ptx::lds128(src + (((c0 + k) ^ in_sw) << 4)), vu = ptx::lds128(src + kBoxBytes + (((c0 + k) ^ in_sw) << 4));
-              rh[4 * k] = vh.x; rh[4 * k + 1] = vh.y; rh[4 * k + 2] = vh.z; rh[4 * k + 3] = vh.w;
-              ru[4 * k] = vu.x; ru[4 * k + 1] = vu.y; ru[4 * k + 2] = vu.z; ru[4 * k + 3] = vu.w;
-            }
-          }
-          if (last_of_unit) {
-            ++used;
-            __syncwarp();
-            fetch();
-          }
-          float a[32], b[32];                                    // the kept projections, then dH, dU
-          widen_row<32>(p.kept_dt, rh, a);
-          widen_row<32>(p.kept_dt, ru, b);
-          ptx::tmem_ld_fence(r0);
-          if (at + 32 >= end) release_acc(acc, tile);            // the values are in registers
-          with_gate(p.fn, [&](auto fn) {
+                for (int k = 0; k < kWords / 4; ++k) {
+                  const uint32_t chunk = ((in_chunk + decltype(half)::value * (kWords / 4) + k) ^ in_sw) << 4;
+                  const uint4 vh = ptx::lds128(src + chunk), vu = ptx::lds128(src + in_box + chunk);
+                  rh[4 * k] = vh.x; rh[4 * k + 1] = vh.y; rh[4 * k + 2] = vh.z; rh[4 * k + 3] = vh.w;
+                  ru[4 * k] = vu.x; ru[4 * k + 1] = vu.y; ru[4 * k + 2] = vu.z; ru[4 * k + 3] = vu.w;
+                }
+                ptx::tmem_ld_fence(r0);
+                if (decltype(half)::value == 1 && at + 32 >= end) release_acc(acc, tile);            // the values are in registers
+                f32x2 yh[8], yu[8];
+                from_here<0, 16>(r0);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float d = p.scale * __uint_as_float(r0[i]);
-              float f, df;
-              gate_both<decltype(fn)::value>(p.act_in * a[i], f, df);
-              a[i] = p.c1 * df * b[i] * d;
-              b[i] = p.c0 * f * d;
-            }
+                for (int i = 0; i < 8; ++i)
+                  gate_grads2<decltype(fn)::value>(widen2<decltype(kept)::value>(rh, i), widen2<decltype(kept)::value>(ru, i),
+                                                   pack2(__uint_as_float(r0[2 * i]), __uint_as_float(r0[2 * i + 1])), p.act_in, nl2, c0, c1, yh[i], yu[i]);
+                pack16<decltype(out)::value>(yh, wh);
+                pack16<decltype(out)::value>(yu, wu);
+#pragma unroll
+                for (int k = 0; k < ES; ++k) {          // one chunk of 8-bit results, two of 16-bit ones
+                  const uint32_t chunk = ((out_chunk + decltype(half)::value * ES + k) ^ out_sw) << 4;
+                  ptx::sts128(dst + chunk, make_uint4(wh[4 * k], wh[4 * k + 1], wh[4 * k + 2], wh[4 * k + 3]));
+                  ptx::sts128(dst + out_box + chunk, make_uint4(wu[4 * k], wu[4 * k + 1], wu[4 * k + 2], wu[4 * k + 3]));
+                }
+              });
+            });
           });
-          if (off == 0) {                                        // the stores of the unit before have read the boxes
-            if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
-            __syncwarp();
-          }
-          const uint32_t dst = box_out + (uint32_t)(lane * out_row), c0 = (uint32_t)(off * out_es) >> 4;
-          uint32_t w[16];
-          auto stage = [&](uint32_t to) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (k >= 2 && out_es == 1) break;
-              ptx::sts128(to + (((c0 + k) ^ out_sw) << 4), make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]));
-            }
-          };
-          pack_row<32>(p.out_dt, a, w);
-          stage(dst);
-          pack_row<32>(p.out_dt, b, w);
-          stage(dst + kBoxBytes);
           if (last_of_unit) {
             ptx::fence_proxy_async_smem();
             __syncwarp();
             if (ptx::elect_one()) {
-              ptx::tma_store_2d(&tm_dh, box_out, col0 + at - off, row - lane);
-              ptx::tma_store_2d(&tm_du, box_out + kBoxBytes, col0 + at - off, row - lane);
+              ptx::tma_store_2d(&tm_dh, slot + box_out, col0 + at - off, row - lane);
+              ptx::tma_store_2d(&tm_du, slot + box_out + out_box, col0 + at - off, row - lane);
               ptx::bulk_commit_group();
             }
+            ++used;
+            fetch();
           }
         }
       }
       // Copies that are still in flight after a wait that ran out land, and stores have read their boxes, before the CTA gives up its shared memory.
       for (; used < issued; ++used)
-        for (uint32_t it = 0; it < p.wait_limit && !ptx::mbar_try_wait(in_bar(ew, used & 1u), (used >> 1) & 1u); ++it) {}
+        for (uint32_t it = 0; it < p.wait_limit && !ptx::mbar_try_wait(in_bar(ew, slot_of(used)), phase_of(used)); ++it) {}
       if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
       __syncwarp();
     }
@@ -538,7 +604,14 @@ us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t
   p.tiles_m = (p.M + kBM * CG - 1) / (kBM * CG);
   p.tiles_n = (p.N + HC - 1) / HC;
   if ((int64_t)p.tiles_m * p.tiles_n >= (1ll << 30)) return US_ERR_UNSUPPORTED;
-  p.d_tiles_m = make_fast_div(p.tiles_m);
+  // Whole rows of the results one after another while the weights stay in L2, else bands of 1024 tokens or so, which read them once each (us, bands of 1 / 4 / 8
+  // tile rows / all: forward FP8 16384 x 2048 x 8192 443 / 449 / 463 / 471, BF16 8192 x 1024 x 4096 126 / 127 / 128 / 130, its backward pass 90 / 91 / 92 / 96).
+  const bool resident = (int64_t)p.K * p.N * ES * (BWD ? 1 : 2) <= (64ll << 20);
+  p.band_m = std::min(p.tiles_m, resident ? 1 : 8 / CG);
+  p.full_bands = p.tiles_m / p.band_m;
+  p.d_band = make_fast_div(p.band_m * p.tiles_n);
+  p.d_rows = make_fast_div(p.band_m);
+  p.d_rows_last = make_fast_div(p.tiles_m % p.band_m ? p.tiles_m % p.band_m : 1);
   const int one = ES == 1 ? US_E5M2 : US_BF16;
   p.idesc = make_idesc(A->dtype == one, B0->dtype == one, false, !BWD, kBM * CG, S::kN);
   // a short A: its rows in groups of eight.  The MMA still reads 128; what lies behind them ends up in rows that do not exist.
@@ -562,7 +635,7 @@ us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t
   }
   const int tiles = p.tiles_m * p.tiles_n, most = sms / CG;
   static std::atomic<uint64_t> smem_set{0};
-  return host::launch(gated_kernel<BWD, ES, HC, CG>, &smem_set, CG * (tiles < most ? tiles : most), gemm_threads(kGatedEW), S::kTotal, CG, st, t[0], t[1], t[2], t[3],
+  return host::launch(gated_kernel<BWD, ES, HC, CG>, &smem_set, CG * (tiles < most ? tiles : most), gemm_threads(S::kEW), S::kTotal, CG, st, t[0], t[1], t[2], t[3],
                       t[4], t[5], t[6], static_cast<const GatedParams&>(p));
 }
 
