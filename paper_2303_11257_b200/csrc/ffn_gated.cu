@@ -49,14 +49,14 @@ struct GatedParams {
   int starved, served;                        // test hook (starved_cta)
 };
 
-template <bool BWD, int ES, int HC, int CG>
+template <bool BWD, int ES, int HC, int CG, bool BOXED = false>
 struct GatedShape {
   static constexpr int kN = BWD ? HC : 2 * HC;             // columns of an accumulator
   static constexpr int kEW = gated_ew(BWD, ES, CG), kSlots = gated_few(BWD, ES, CG) ? 2 : 1;   // warps and slots of the epilogue
   static constexpr int kRowsB = kN / CG;                   // rows of B a CTA fetches
   static constexpr int kBBytes = kRowsB * kStageKBytes;
   static constexpr int kStageBytes = kBM * kStageKBytes + kBBytes;
-  static constexpr int kEpiBytes = BWD ? kEW * kSlots * kSlotBytes : 0;
+  static constexpr int kEpiBytes = BWD ? kEW * kSlots * kSlotBytes : BOXED ? kEW * 3 * 2048 : 0;
   static constexpr int kStages = (kRoom - kEpiBytes) / kStageBytes;
   static constexpr int kBarrierBytes = 1024;
   static constexpr int kTotal = kRoom + kBarrierBytes + 1024;
@@ -226,6 +226,12 @@ __device__ __forceinline__ void pack16(const f32x2 (&y)[8], uint32_t (&w)[8]) {
     else if (i < 4) w[i] = cvt_fp8x4<DT == US_E5M2>(v[(4 * i) & 15], v[(4 * i + 1) & 15], v[(4 * i + 2) & 15], v[(4 * i + 3) & 15]);
   }
 }
+__device__ __forceinline__ void pack16(int dt, const f32x2 (&y)[8], uint32_t (&w)[8]) {
+  if (dt == US_BF16) pack16<US_BF16>(y, w);
+  else if (dt == US_F16) pack16<US_F16>(y, w);
+  else if (dt == US_E4M3) pack16<US_E4M3>(y, w);
+  else pack16<US_E5M2>(y, w);
+}
 // Calls g with the types of the copies and of the results (of operands of ES bytes) as constants.
 template <int ES, class G>
 __device__ __forceinline__ void with_formats(int kept, int out, G g) {
@@ -243,13 +249,15 @@ __device__ __forceinline__ uint64_t chunk_desc(uint32_t addr, int row_bytes, uin
   return d | ((uint64_t)(row_bytes == 128 ? 2 : row_bytes == 64 ? 4 : 6) << 61);
 }
 
-// ES: operand bytes per element (1 = FP8, 2 = BF16 / F16).  HC: hidden columns of a tile.  CG = 2: tiles of 256 rows by a CTA pair, 1: of 128 by a CTA.
-template <bool BWD, int ES, int HC, int CG>
+// ES: operand bytes per element (1 = FP8, 2 = BF16 / F16).  HC: hidden columns of a tile.  CG = 2: tiles of 256 rows by a CTA pair, 1: of 128 by a CTA.  BOXED (forward,
+// pairs): results leave by TMA, where no unit has a second tile whose MMAs the stores could hide behind.  (us, stored by the lanes / boxed: 1000 x 528 x 2096 F16 13.3 / 9.4; several
+// tiles each: 8192 x 1024 x 4096 BF16 125 / 130, 16384 x 2048 x 8192 FP8 443 / 474, half of which is the stages that the boxes take.)
+template <bool BWD, int ES, int HC, int CG, bool BOXED>
 __global__ void __launch_bounds__(gemm_threads(gated_ew(BWD, ES, CG)), 1)
 gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0, const __grid_constant__ CUtensorMap tm_b1,
              const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_dh,
              const __grid_constant__ CUtensorMap tm_du, const GatedParams p) {
-  using S = GatedShape<BWD, ES, HC, CG>;
+  using S = GatedShape<BWD, ES, HC, CG, BOXED>;
   constexpr int kEW = S::kEW, kSlots = S::kSlots, kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
   constexpr uint32_t kTmemCols = 2 * kN;
   const uint32_t a_bytes = CG == 2 ? (uint32_t)(kBM * kStageKBytes) : p.a_bytes, stage_bytes = a_bytes + S::kBBytes;
@@ -417,7 +425,73 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
     };
     uint32_t local = 0;
     bool ok = true;
-    if constexpr (!BWD) {
+    if constexpr (BOXED) {
+      // A warp has 32 hidden columns of a tile; A and the copies leave through a box each.
+      const uint32_t box_a = smem_base + (uint32_t)(kRoom - S::kEpiBytes + (warp - 2) * S::kEpiBytes / kEW), box_h = box_a + 1024u * out_es, box_u = box_h + 1024u * kept_es;
+      const uint32_t out_sw = out_es == 2 ? (uint32_t)((lane >> 1) & 3) : 0u, kept_sw = kept_es == 2 ? (uint32_t)((lane >> 1) & 3) : 0u;
+      for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
+        int row, col;
+        place(tile, row, col);
+        const uint32_t acc = local & 1u, acc_phase = (local >> 1) & 1u;
+        ok = wait_bounded(acc_full_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        if (col >= p.N) {                                        // (the same for all lanes)
+          release_acc(acc, tile);
+          continue;
+        }
+        const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * kN + part * S::kWarpCols;
+        if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();    // the last tile's stores have read the boxes
+        __syncwarp();
+        unrolled<2>([&](auto half) {                             // sixteen columns
+          constexpr int k = decltype(half)::value;
+          uint32_t r0[16], r1[16], w[8];
+          ptx::tmem_ld_32x32_issue(t_row + 16 * k, r0);
+          ptx::tmem_ld_32x32_issue(t_row + HC + 16 * k, r1);
+          ptx::tmem_ld_fence(r0);
+          ptx::tmem_ld_fence(r1);
+          if (k == 1) release_acc(acc, tile);                    // the values are in registers
+          f32x2 h[8], u[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            h[i] = mul2(scale2, pack2(__uint_as_float(r0[2 * i]), __uint_as_float(r0[2 * i + 1])));
+            u[i] = mul2(scale2, pack2(__uint_as_float(r1[2 * i]), __uint_as_float(r1[2 * i + 1])));
+          }
+          auto stage = [&](uint32_t box, int es, uint32_t sw) {  // a 16-byte chunk of 8-bit values, two of 16-bit ones
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              if (c == 1 && es == 1) break;
+              ptx::sts128(box + (uint32_t)(lane * 32 * es) + (((uint32_t)(k * es + c) ^ sw) << 4), make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
+            }
+          };
+          if (p.h) {
+            pack16(p.kept_dt, h, w);
+            stage(box_h, kept_es, kept_sw);
+            pack16(p.kept_dt, u, w);
+            stage(box_u, kept_es, kept_sw);
+          }
+          with_gate(p.fn, [&](auto fn) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = mul2(mul2(gate_value2<decltype(fn)::value>(h[i], in2, nl2), c0), u[i]);
+          });
+          pack16(p.out_dt, h, w);
+          stage(box_a, out_es, out_sw);
+        });
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (ptx::elect_one()) {
+          ptx::tma_store_2d(&tm_dh, box_a, col, row - lane);
+          if (p.h) {
+            ptx::tma_store_2d(&tm_h, box_h, col, row - lane);
+            ptx::tma_store_2d(&tm_u, box_u, col, row - lane);
+          }
+          ptx::bulk_commit_group();
+        }
+      }
+      if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
+      __syncwarp();
+    } else if constexpr (!BWD) {
       for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
         int row, col0;
         place(tile, row, col0);
@@ -595,12 +669,12 @@ bool make_chunk_tmap(CUtensorMap* tm, const us_mat* m, int es, int box_rows, int
             CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-struct GatedMats { const us_mat *a, *b0, *b1, *h, *u, *dh, *du; };       // forward: h .. du not used
+struct GatedMats { const us_mat *a, *b0, *b1, *h, *u, *dh, *du; };       // forward: dh is A, du not used
 
-template <bool BWD, int ES, int HC, int CG>
+template <bool BWD, int ES, int HC, int CG, bool BOXED = false>
 us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t st) {
   const us_mat *A = m.a, *B0 = m.b0, *B1 = m.b1;
-  using S = GatedShape<BWD, ES, HC, CG>;
+  using S = GatedShape<BWD, ES, HC, CG, BOXED>;
   p.tiles_m = (p.M + kBM * CG - 1) / (kBM * CG);
   p.tiles_n = (p.N + HC - 1) / HC;
   if ((int64_t)p.tiles_m * p.tiles_n >= (1ll << 30)) return US_ERR_UNSUPPORTED;
@@ -632,10 +706,14 @@ us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t
       return US_ERR_CUDA;
   } else {
     t[3] = t[4] = t[5] = t[6] = t[0];
+    const int kept_es = dtype_size(p.kept_dt), out_es = dtype_size(p.out_dt);
+    if (BOXED && (!host::make_tmap(&t[5], m.dh, out_es, 32, 32 * out_es) || (p.h && (!host::make_tmap(&t[3], m.h, kept_es, 32, 32 * kept_es) ||
+                                                                                      !host::make_tmap(&t[4], m.u, kept_es, 32, 32 * kept_es)))))
+      return US_ERR_CUDA;
   }
   const int tiles = p.tiles_m * p.tiles_n, most = sms / CG;
   static std::atomic<uint64_t> smem_set{0};
-  return host::launch(gated_kernel<BWD, ES, HC, CG>, &smem_set, CG * (tiles < most ? tiles : most), gemm_threads(S::kEW), S::kTotal, CG, st, t[0], t[1], t[2], t[3],
+  return host::launch(gated_kernel<BWD, ES, HC, CG, BOXED>, &smem_set, CG * (tiles < most ? tiles : most), gemm_threads(S::kEW), S::kTotal, CG, st, t[0], t[1], t[2], t[3],
                       t[4], t[5], t[6], static_cast<const GatedParams&>(p));
 }
 
@@ -647,7 +725,12 @@ us_status pick_gated(const GatedMats& m, GatedParams& p, cudaStream_t st) {
   if (sms <= 0) return US_ERR_CUDA;
   constexpr int kWide = BWD ? 256 : 128;
   const int64_t M = p.M, N = p.N;
-  if (4 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) >= sms && M > kBM) return launch_gated<BWD, ES, kWide, 2>(m, p, sms, st);
+  if (4 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) >= sms && M > kBM) {
+    if constexpr (!BWD) {
+      if (2 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) <= sms) return launch_gated<BWD, ES, kWide, 2, true>(m, p, sms, st);
+    }
+    return launch_gated<BWD, ES, kWide, 2>(m, p, sms, st);
+  }
   const int64_t narrow = ((M + kBM - 1) / kBM) * ((N + kWide / 4 - 1) / (kWide / 4));
   if (narrow <= sms) return launch_gated<BWD, ES, kWide / 4, 1>(m, p, sms, st);
   return launch_gated<BWD, ES, kWide / 2, 1>(m, p, sms, st);
@@ -691,7 +774,7 @@ us_status gated_fwd(int fn, const us_mat* X, const us_mat* Wg, const us_mat* Wu,
   p.o0 = static_cast<uint8_t*>(A->ptr); p.o0_ld = A->ld; p.out_dt = A->dtype; p.out_sectors = aligned(A, 32);
   p.status = static_cast<unsigned int*>(ws); p.wait_limit = wait_limit; p.starved = starved; p.served = served;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const GatedMats m{X, Wg, Wu, nullptr, nullptr, nullptr, nullptr};
+  const GatedMats m{X, Wg, Wu, H, U, A, nullptr};
   return f8 ? pick_gated<false, 1>(m, p, st) : pick_gated<false, 2>(m, p, st);
 }
 
