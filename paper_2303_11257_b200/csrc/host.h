@@ -17,6 +17,18 @@ inline us_status failed() {
   return US_ERR_CUDA;
 }
 
+// Lets a kernel take up to `bytes` of dynamic shared memory on the current device.  set: one static word per kernel, a bit per device on which that has been done.
+template <class... P>
+bool allow_smem(void (*kern)(P...), std::atomic<uint64_t>& set, size_t bytes) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (set.load(std::memory_order_relaxed) & bit) return true;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+  set.fetch_or(bit, std::memory_order_relaxed);
+  return true;
+}
+
 // Launches a kernel that calls ptx::grid_wait_previous (programmatic dependent launch): its CTAs may take their
 // places and set up barriers and tensor memory while the previous kernel of the stream still drains, and wait there
 // for that kernel's completion before they touch memory.  In such a kernel at least one thread of every CTA waits, so that
@@ -24,18 +36,11 @@ inline us_status failed() {
 // waits (whose limit is then not spent on the predecessor).  Worth its while where the grid is resident at once (the three launches of a
 // 256 x 128 x 512 step 18.4 -> 16.4 us, of a 8192 x 1024 x 4096 one 199 -> 193 us); a grid of many waves pays for the wait
 // in every CTA (cross-entropy rows, 2048 CTAs: 39 -> 44 us) and is launched plainly.  cluster: CTAs per cluster (1: none).
-// smem_set: one static word per kernel, a bit per device on which its dynamic shared memory limit is set (nullptr: within 48 KB).
+// smem_set: allow_smem's static word (nullptr: within 48 KB, or allowed before).
 template <class... P, class... A>
 us_status launch(void (*kern)(P...), std::atomic<uint64_t>* smem_set, int grid, int threads, size_t smem, int cluster,
                  cudaStream_t stream, const A&... args) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return failed();
-  const uint64_t bit = 1ull << (dev & 63);
-  const bool known = !smem_set || (smem_set->load(std::memory_order_relaxed) & bit);
-  if (!known) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return failed();
-    smem_set->fetch_or(bit, std::memory_order_relaxed);
-  }
+  if (smem_set && !allow_smem(kern, *smem_set, smem)) return failed();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)threads);
@@ -72,13 +77,7 @@ bool make_tmap(CUtensorMap* tm, const us_mat* m, int es, int box_rows, int box_b
 template <class... P, class... A>
 us_status launch_plain(void (*kern)(P...), std::atomic<uint64_t>* smem_set, int grid, int threads, int max_smem, size_t smem,
                        cudaStream_t stream, const A&... args) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return failed();
-  const uint64_t bit = 1ull << (dev & 63);
-  if (!(smem_set->load(std::memory_order_relaxed) & bit)) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem) != cudaSuccess) return failed();
-    smem_set->fetch_or(bit, std::memory_order_relaxed);
-  }
+  if (!allow_smem(kern, *smem_set, (size_t)max_smem)) return failed();
   kern<<<(unsigned)grid, (unsigned)threads, smem, stream>>>(P(args)...);
   return cudaGetLastError() == cudaSuccess ? US_OK : US_ERR_CUDA;
 }

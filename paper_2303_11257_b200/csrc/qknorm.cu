@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kMostParts = 4, kMostWidth = 1024, kMostVecWidth = 512;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kBwdCtasPerSm = 2, kFwdCtasPerSm = 4;
+constexpr int kBwdCtasPerSm = 2, kFwdCtasPerSm = 3;
 
 struct QkPart {
   const void *x, *g, *w;
@@ -34,7 +34,7 @@ struct QkPart {
   int64_t x_ld, g_ld, y_ld;
   int x_dt, g_dt, w_dt, y_dt, dw_dt;
   int heads, blocks;           // heads, and warp units per row
-  FastDiv d_blocks;            // by blocks
+  uint32_t step_rows, step_blocks, step_position;      // of the units of a warp: rows, blocks beyond them, rows modulo the period
   int first_cta, ctas;         // CTAs that work for this part
   float beta_w;
 };
@@ -50,14 +50,12 @@ struct QkArgs {
   int lanes, group;            // vector kernels: lanes of a group that hold features, and the group's size
 };
 
-// The table row of a matrix row, nullptr where its position is not in the table.
-__device__ __forceinline__ const float* angles_of(const QkArgs& p, int64_t row) {
-  const int64_t at = p.positions ? (int64_t)__ldg(p.positions + row) : p.start + (p.period ? (int64_t)((uint32_t)row % p.period) : row);
-  return at >= 0 && at < p.table_rows ? p.table + at * p.table_ld : nullptr;
+__device__ __forceinline__ int64_t position_of(const QkArgs& p, int64_t row) {
+  return p.positions ? (int64_t)__ldg(p.positions + row) : p.start + (p.period ? (int64_t)((uint32_t)row % p.period) : row);
 }
-
-__device__ __forceinline__ int64_t row_of(const QkPart& q, int64_t unit) {
-  return q.blocks == 1 ? unit : unit < (1ll << 31) ? (int64_t)q.d_blocks.div((int)unit) : unit / q.blocks;
+// The table row of a position, nullptr where it is not in the table.
+__device__ __forceinline__ const float* angles_at(const QkArgs& p, int64_t at) {
+  return at >= 0 && at < p.table_rows ? p.table + at * p.table_ld : nullptr;
 }
 
 __device__ __forceinline__ float group_sum(float v, int group) {
@@ -65,29 +63,50 @@ __device__ __forceinline__ float group_sum(float v, int group) {
   return v;
 }
 
-// Eight features: as they are stored (one register for two 16-bit ones), and as float32.
-template <int DT> struct Chunk { uint4 r; };
-template <> struct Chunk<US_F32> { float4 a, b; };
+// Sixteen bytes to this lane's place in shared memory, asynchronously; waiting until at most N groups of them are under way.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A chunk of eight features in shared memory, 512 bytes of a warp (float32: twice that) in pieces of sixteen bytes a lane.  Widened to pairs of neighbours, for arithmetic
+// on two values at a time.
 template <int DT>
-__device__ __forceinline__ void fetch(Chunk<DT>& c, const void* base, int64_t at) {
-  if constexpr (DT == US_F32) {
-    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-    c.a = __ldg(q); c.b = __ldg(q + 1);
-  } else {
-    c.r = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at));
-  }
+constexpr int kChunkBytes = DT == US_F32 ? 1024 : 512;
+template <int DT>
+__device__ __forceinline__ void fetch(uint32_t to, const char* from) {
+  copy16(to, from);
+  if (DT == US_F32) copy16(to + 512u, from + 16);
 }
 template <int DT>
-__device__ __forceinline__ void clear(Chunk<DT>& c) {
-  if constexpr (DT == US_F32) c.a = c.b = make_float4(0.f, 0.f, 0.f, 0.f); else c.r = make_uint4(0u, 0u, 0u, 0u);
-}
-template <int DT>
-__device__ __forceinline__ void widen(const Chunk<DT>& c, float (&v)[8]) {
+__device__ __forceinline__ void widen(uint32_t from, f32x2 (&v)[4]) {
+  const uint4 r = ptx::lds128(from);
   if constexpr (DT == US_F32) {
-    v[0] = c.a.x; v[1] = c.a.y; v[2] = c.a.z; v[3] = c.a.w; v[4] = c.b.x; v[5] = c.b.y; v[6] = c.b.z; v[7] = c.b.w;
+    const uint4 s = ptx::lds128(from + 512u);
+    v[0] = pack2(__uint_as_float(r.x), __uint_as_float(r.y)); v[1] = pack2(__uint_as_float(r.z), __uint_as_float(r.w));
+    v[2] = pack2(__uint_as_float(s.x), __uint_as_float(s.y)); v[3] = pack2(__uint_as_float(s.z), __uint_as_float(s.w));
   } else {
-    unpack16x8(c.r, DT, v);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = DT == US_BF16 ? unpack_bf16x2(w[i]) : unpack_f16x2(w[i]);
+      v[i] = pack2(f.x, f.y);
+    }
   }
+}
+__device__ __forceinline__ float halves_sum(f32x2 v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
+}
+// Eight features rounded to dt, to an address with the chunk's alignment.
+__device__ __forceinline__ void put(char* to, int dt, const f32x2 (&y)[4]) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack2(y[i], v[2 * i], v[2 * i + 1]);
+  store8(to, dt, 0, 0, 8, true, v);
 }
 
 // Which features a lane has, and which of them are rotated.
@@ -95,9 +114,17 @@ struct Lane {
   int a, b;                    // first feature of each chunk
   bool has_a, has_b, rot_a, rot_b;
 };
-template <bool NEIGHBOURS>
+// FULL: every lane of a group has two chunks and every feature is rotated (widths of 16 to 512 that are a power of two), known when compiled: tests of a lane's share
+// become selections between registers in the arithmetic, twice as many instructions in all.
+template <bool NEIGHBOURS, bool FULL>
 __device__ __forceinline__ Lane lane_of(const QkArgs& p, int j) {
   Lane l;
+  if (FULL) {
+    l.a = NEIGHBOURS ? 16 * j : 8 * j;
+    l.b = NEIGHBOURS ? l.a + 8 : l.a + p.width / 2;
+    l.has_a = l.has_b = l.rot_a = l.rot_b = true;
+    return l;
+  }
   if (NEIGHBOURS) {
     l.a = 16 * j; l.b = 16 * j + 8;
     l.rot_a = l.a < p.rotated; l.rot_b = l.b < p.rotated;
@@ -112,34 +139,49 @@ __device__ __forceinline__ Lane lane_of(const QkArgs& p, int j) {
   l.rot_a = l.rot_a && l.has_a; l.rot_b = l.rot_b && l.has_b;
   return l;
 }
-// Cosines and sines of a lane's pairs: eight pairs from pair 8 j on.
-__device__ __forceinline__ void fetch_angles(const QkArgs& p, int64_t row, int j, const Lane& l, float (&cs)[16]) {
+// Cosines and sines of a lane's pairs, eight from pair 8 j on, as a turn needs them.  Chunk a of a half turn: cos[0 .. 3] its cosines, two each, sin[0 .. 3] the sines.
+// Neighbours: for pair i of chunk a (b: i + 4) cos[i] = (c, c), sin[i] = (-s, s).
+template <bool NEIGHBOURS>
+struct Turn { f32x2 cos[NEIGHBOURS ? 8 : 4], sin[NEIGHBOURS ? 8 : 4]; };
+// from: this lane's 64 bytes of the table's row.  inside: whether there is one; otherwise what is turned becomes NaN.
+template <bool NEIGHBOURS, bool BACK>
+__device__ __forceinline__ void read_turn(uint32_t from, bool inside, const Lane& l, Turn<NEIGHBOURS>& t) {
   if (!(l.rot_a || l.rot_b)) return;
-  const float* t = angles_of(p, row);
+  const uint32_t none = 0x7fffffffu;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool there = i < 2 ? l.rot_a : l.rot_b;
-    const float4 v = there && t ? __ldg(reinterpret_cast<const float4*>(t + 16 * j) + i)
-                                : make_float4(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff), __int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
-    cs[4 * i] = v.x; cs[4 * i + 1] = v.y; cs[4 * i + 2] = v.z; cs[4 * i + 3] = v.w;
+  for (int i = 0; i < 4; ++i) {                                // two pairs
+    const uint4 r = inside ? ptx::lds128(from + 16u * i) : make_uint4(none, none, none, none);
+    float4 v = make_float4(__uint_as_float(r.x), __uint_as_float(r.y), __uint_as_float(r.z), __uint_as_float(r.w));
+    if (BACK) { v.y = -v.y; v.w = -v.w; }
+    if constexpr (NEIGHBOURS) {
+      t.cos[2 * i] = pack2(v.x, v.x); t.cos[2 * i + 1] = pack2(v.z, v.z);
+      t.sin[2 * i] = pack2(-v.y, v.y); t.sin[2 * i + 1] = pack2(-v.w, v.w);
+    } else {
+      t.cos[i] = pack2(v.x, v.z); t.sin[i] = pack2(v.y, v.w);
+    }
   }
 }
-__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
-  const float t = a * c - b * s;
-  b = b * c + a * s;
-  a = t;
+__device__ __forceinline__ f32x2 swapped(f32x2 v) {
+  float a, b;
+  unpack2(v, a, b);
+  return pack2(b, a);
 }
-template <bool NEIGHBOURS, bool BACK>
-__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&cs)[16], const Lane& l) {
-  if (NEIGHBOURS) {
+__device__ __forceinline__ f32x2 negated(f32x2 v) { return v ^ 0x8000000080000000ull; }
+template <bool NEIGHBOURS>
+__device__ __forceinline__ void rotate(f32x2 (&a)[4], f32x2 (&b)[4], const Turn<NEIGHBOURS>& t, const Lane& l) {
+  if constexpr (NEIGHBOURS) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (l.rot_a) turn(a[2 * i], a[2 * i + 1], cs[2 * i], BACK ? -cs[2 * i + 1] : cs[2 * i + 1]);
-      if (l.rot_b) turn(b[2 * i], b[2 * i + 1], cs[8 + 2 * i], BACK ? -cs[8 + 2 * i + 1] : cs[8 + 2 * i + 1]);
+      if (l.rot_a) a[i] = fma2(swapped(a[i]), t.sin[i], mul2(a[i], t.cos[i]));
+      if (l.rot_b) b[i] = fma2(swapped(b[i]), t.sin[4 + i], mul2(b[i], t.cos[4 + i]));
     }
   } else if (l.rot_a) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(a[i], b[i], cs[2 * i], BACK ? -cs[2 * i + 1] : cs[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) {
+      const f32x2 ya = fma2(negated(b[i]), t.sin[i], mul2(a[i], t.cos[i]));
+      b[i] = fma2(a[i], t.sin[i], mul2(b[i], t.cos[i]));
+      a[i] = ya;
+    }
   }
 }
 
@@ -148,112 +190,184 @@ __device__ __forceinline__ int part_of(const QkArgs& p, int cta) {
   while (k + 1 < p.count && cta >= p.part[k + 1].first_cta) ++k;
   return k;
 }
-__device__ __forceinline__ void load_weight(const QkPart& q, const Lane& l, float (&wa)[8], float (&wb)[8]) {
+__device__ __forceinline__ void load_weight(const QkPart& q, const Lane& l, f32x2 (&wa)[4], f32x2 (&wb)[4]) {
+  auto at = [&](bool has, int i) { return has ? (q.w ? load_one(q.w, q.w_dt, i) : 1.f) : 0.f; };
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    wa[i] = l.has_a ? (q.w ? load_one(q.w, q.w_dt, l.a + i) : 1.f) : 0.f;
-    wb[i] = l.has_b ? (q.w ? load_one(q.w, q.w_dt, l.b + i) : 1.f) : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    wa[i] = pack2(at(l.has_a, l.a + 2 * i), at(l.has_a, l.a + 2 * i + 1));
+    wb[i] = pack2(at(l.has_b, l.b + 2 * i), at(l.has_b, l.b + 2 * i + 1));
   }
 }
 
-// DT: type of the inputs.  ITER: steps of 32 / G heads whose loads are in flight together.
-template <int DT, int ITER, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads) qk_fwd_kernel(const __grid_constant__ QkArgs p) {
-  const int zero = ptx::grid_wait_previous();
-  const QkPart& q = p.part[part_of(p, blockIdx.x)];
-  const int lane = threadIdx.x & 31, j = lane & (p.group - 1), per = 32 / p.group;
-  const Lane l = lane_of<NEIGHBOURS>(p, j);
-  float wa[8], wb[8];
-  load_weight(q, l, wa, wb);
-  const int64_t units = p.rows * q.blocks, step = (int64_t)q.ctas * kWarps;
-  for (int64_t u = (int64_t)(blockIdx.x - q.first_cta) * kWarps + (threadIdx.x >> 5) + zero; u < units; u += step) {
-    const int64_t row = row_of(q, u);
-    const int head0 = (int)(u - row * q.blocks) * (per * ITER) + lane / p.group;
-    Chunk<DT> ca[ITER], cb[ITER];
-#pragma unroll
-    for (int k = 0; k < ITER; ++k) {
-      const int head = head0 + k * per;
-      const int64_t at = row * q.x_ld + (int64_t)head * p.width;
-      if (head < q.heads && l.has_a) fetch(ca[k], q.x, at + l.a); else clear(ca[k]);
-      if (head < q.heads && l.has_b) fetch(cb[k], q.x, at + l.b); else clear(cb[k]);
-    }
-    float cs[16];
-    if (p.table) fetch_angles(p, row, j, l, cs);
-#pragma unroll
-    for (int k = 0; k < ITER; ++k) {
-      const int head = head0 + k * per;
-      float a[8], b[8], ss = 0.f;
-      widen(ca[k], a); widen(cb[k], b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-      const float r = rsqrtf(fmaf(group_sum(ss, p.group), p.inv_width, p.eps));
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { a[i] *= r * wa[i]; b[i] *= r * wb[i]; }
-      if (p.table) rotate<NEIGHBOURS, false>(a, b, cs, l);
-      const int64_t at = row * q.y_ld + (int64_t)head * p.width;
-      if (head < q.heads && l.has_a) store8(q.y, q.y_dt, at, l.a, p.width, true, a);
-      if (head < q.heads && l.has_b) store8(q.y, q.y_dt, at, l.b, p.width, true, b);
-    }
-  }
-}
+// The vector kernels' walk over the units of a warp: kSteps steps of 32 / G heads of one row, which arrive in a ring of kStages slots of the warp's own in shared memory, two units
+// ahead of the one that is worked on.  (With the loads of one unit in registers and none ahead, 8192 tokens of 16 + 16 heads of 64 took 20.7 us forward and 29.4 backward, 16384
+// tokens of 32 + 8 heads of 128 into E4M3 91 to 107: latency.)
+template <int DT>
+constexpr int kSteps = DT == US_F32 ? 1 : 2;
+constexpr int kStages = 3;
+// Bytes of a slot: both chunks of a step, of x and backward of the gradient, and the row of the table.
+template <bool BWD, int DT>
+__host__ __device__ constexpr int slot_bytes(int group) { return kSteps<DT> * (BWD ? 4 : 2) * kChunkBytes<DT> + 64 * group; }
 
-template <int DT, int ITER, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kThreads, 2) qk_bwd_kernel(const __grid_constant__ QkArgs p) {
-  __shared__ float sums[kWarps][kMostVecWidth];
-  const int zero = ptx::grid_wait_previous();
-  const QkPart& q = p.part[part_of(p, blockIdx.x)];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane & (p.group - 1), per = 32 / p.group;
-  const Lane l = lane_of<NEIGHBOURS>(p, j);
-  float wa[8], wb[8], da[8], db[8];
-  load_weight(q, l, wa, wb);
+// A unit of a warp, and its position where all rows' follow from their number.  Advanced by additions: 64-bit products and divisions for each unit were most of what
+// the kernels issued (21 to 26 instructions a value).
+struct Unit { uint32_t row, block, position; };
+__device__ __forceinline__ Unit first_unit(const QkArgs& p, const QkPart& q, uint32_t number) {
+  const uint32_t row = number / (uint32_t)q.blocks;
+  return Unit{row, number - row * q.blocks, p.period ? row % p.period : row};
+}
+__device__ __forceinline__ void advance(const QkArgs& p, const QkPart& q, Unit& u) {
+  const uint32_t carry = u.block + q.step_blocks >= (uint32_t)q.blocks;
+  u.block += q.step_blocks - (carry ? q.blocks : 0);
+  u.row += q.step_rows + carry;
+  u.position += q.step_position + carry;
+  if (p.period && u.position >= p.period) u.position -= p.period;
+}
+__device__ __forceinline__ int64_t position_of(const QkArgs& p, const Unit& u) { return p.positions ? (int64_t)__ldg(p.positions + u.row) : p.start + (int64_t)u.position; }
+// Bytes from a matrix to a lane's first feature of a unit: row, and heads of the unit and before the lane's.
+__device__ __forceinline__ int64_t offset(const Unit& u, uint32_t row_bytes, uint32_t block_bytes) { return (int64_t)((uint64_t)u.row * row_bytes + (uint64_t)u.block * block_bytes); }
+
+template <bool BWD, int DT, class G>
+__device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lane& l, uint32_t ring, int zero, G work) {
+  constexpr int kC = kChunkBytes<DT>, kStep = (BWD ? 4 : 2) * kC, kEs = DT == US_F32 ? 4 : 2;
+  const int lane = threadIdx.x & 31, j = lane & (p.group - 1), per = 32 / p.group, slot = slot_bytes<BWD, DT>(p.group);
+  const uint32_t rows = (uint32_t)p.rows, x_row = (uint32_t)(q.x_ld * kEs), g_row = BWD ? (uint32_t)(q.g_ld * kEs) : 0u;
+  const uint32_t step_bytes = (uint32_t)(per * p.width * kEs), block_bytes = step_bytes * kSteps<DT>;
+  const int place = (lane / p.group) * p.width;                 // this lane's head among those of a step
+  const char *xa = static_cast<const char*>(q.x) + (place + l.a) * kEs, *ga = static_cast<const char*>(q.g) + (place + l.a) * kEs;
+  const int b_minus_a = (l.b - l.a) * kEs;
+  const bool turns = p.table != nullptr;
+  const float* table = p.table + 16 * j;
+  Unit now = first_unit(p, q, (blockIdx.x - q.first_cta) * kWarps + (threadIdx.x >> 5) + zero), next = now;
+  // positions are read one unit before the copy of their angles is issued; inside: a bit per slot, whether its position is in the table
+  int64_t position = turns && next.row < rows ? position_of(p, next) : 0;
+  uint32_t inside = 0u;
+  auto issue = [&](int s) {
+    if (next.row < rows) {
+      const uint32_t to = ring + s * slot + lane * 16u;
+      const char *x = xa + offset(next, x_row, block_bytes), *g = BWD ? ga + offset(next, g_row, block_bytes) : nullptr;
+      const int heads = q.heads - (int)next.block * (per * kSteps<DT>) - lane / p.group;        // left from this lane's first on
 #pragma unroll
-  for (int i = 0; i < 8; ++i) da[i] = db[i] = 0.f;
-  const int64_t units = p.rows * q.blocks, step = (int64_t)q.ctas * kWarps;
-  for (int64_t u = (int64_t)(blockIdx.x - q.first_cta) * kWarps + warp + zero; u < units; u += step) {
-    const int64_t row = row_of(q, u);
-    const int head0 = (int)(u - row * q.blocks) * (per * ITER) + lane / p.group;
-    Chunk<DT> ca[ITER], cb[ITER], ga[ITER], gb[ITER];
-#pragma unroll
-    for (int k = 0; k < ITER; ++k) {
-      const int head = head0 + k * per;
-      const int64_t at = row * q.x_ld + (int64_t)head * p.width, ag = row * q.g_ld + (int64_t)head * p.width;
-      if (head < q.heads && l.has_a) { fetch(ca[k], q.x, at + l.a); fetch(ga[k], q.g, ag + l.a); } else { clear(ca[k]); clear(ga[k]); }
-      if (head < q.heads && l.has_b) { fetch(cb[k], q.x, at + l.b); fetch(gb[k], q.g, ag + l.b); } else { clear(cb[k]); clear(gb[k]); }
-    }
-    float cs[16];
-    if (p.table) fetch_angles(p, row, j, l, cs);
-#pragma unroll
-    for (int k = 0; k < ITER; ++k) {
-      const int head = head0 + k * per;
-      float a[8], b[8], na[8], nb[8], ss = 0.f, dot = 0.f;
-      widen(ca[k], a); widen(cb[k], b);
-      widen(ga[k], na); widen(gb[k], nb);
-      if (p.table) rotate<NEIGHBOURS, true>(na, nb, cs, l);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-        dot = fmaf(na[i] * wa[i], a[i], fmaf(nb[i] * wb[i], b[i], dot));
+      for (int k = 0; k < kSteps<DT>; ++k) {
+        if (k * per >= heads) break;
+        if (l.has_a) { fetch<DT>(to + k * kStep, x + k * step_bytes); if (BWD) fetch<DT>(to + k * kStep + 2 * kC, g + k * step_bytes); }
+        if (l.has_b) { fetch<DT>(to + k * kStep + kC, x + k * step_bytes + b_minus_a); if (BWD) fetch<DT>(to + k * kStep + 3 * kC, g + k * step_bytes + b_minus_a); }
       }
+      const int64_t at = position;
+      advance(p, q, next);
+      if (turns) {
+        const bool in = at >= 0 && at < p.table_rows;
+        inside = (inside & ~(1u << s)) | ((uint32_t)in << s);
+        if (in && lane < p.group) {
+          const float* t = table + at * p.table_ld;
+          const uint32_t angles = ring + s * slot + kSteps<DT> * kStep + 64u * j;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < 2 ? l.rot_a : l.rot_b) copy16(angles + 16u * i, t + 4 * i);
+        }
+        if (next.row < rows) position = position_of(p, next);
+      }
+    }
+    copies_commit();
+  };
+  for (int s = 0; s < kStages - 1; ++s) issue(s);
+  const int y_es = dtype_size(q.y_dt);
+  const uint32_t y_row = (uint32_t)(q.y_ld * y_es), y_step = (uint32_t)(per * p.width * y_es);
+  char* y = static_cast<char*>(q.y) + (place + l.a) * y_es;
+  const int y_b = (l.b - l.a) * y_es;
+  for (int s = 0; now.row < rows; advance(p, q, now)) {
+    copies_wait<kStages - 2>();
+    __syncwarp();
+    issue(s == 0 ? kStages - 1 : s - 1);                        // the slot that the last unit was read from
+    const uint32_t from = ring + s * slot;
+    const int heads = q.heads - (int)now.block * (per * kSteps<DT>) - lane / p.group;
+    work(heads, from + lane * 16u, from + kSteps<DT> * kStep + 64u * j, (inside >> s & 1u) != 0u, y + offset(now, y_row, y_step * kSteps<DT>), y_step, y_b);
+    if (++s == kStages) s = 0;
+  }
+  copies_wait<0>();
+}
+
+// DT: type of the inputs.
+template <int DT, bool NEIGHBOURS, bool FULL>
+__global__ void __launch_bounds__(kThreads, kFwdCtasPerSm) qk_fwd_kernel(const __grid_constant__ QkArgs p) {
+  extern __shared__ __align__(16) float smem[];
+  const int zero = ptx::grid_wait_previous();
+  const QkPart& q = p.part[part_of(p, blockIdx.x)];
+  const int lane = threadIdx.x & 31, per = 32 / p.group;
+  const Lane l = lane_of<NEIGHBOURS, FULL>(p, lane & (p.group - 1));
+  f32x2 wa[4], wb[4];
+  load_weight(q, l, wa, wb);
+  const uint32_t ring = ptx::smem_addr(smem) + (threadIdx.x >> 5) * kStages * slot_bytes<false, DT>(p.group);
+  walk<false, DT>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, bool inside, char* y, uint32_t y_step, int y_b) {
+    Turn<NEIGHBOURS> turn;
+    if (FULL || p.table) read_turn<NEIGHBOURS, false>(angles, inside, l, turn);
+#pragma unroll
+    for (int k = 0; k < kSteps<DT>; ++k) {
+      const uint32_t from = data + k * 2 * kChunkBytes<DT>;
+      f32x2 a[4] = {}, b[4] = {}, ss = 0ull;
+      if (l.has_a) widen<DT>(from, a);
+      if (l.has_b) widen<DT>(from + kChunkBytes<DT>, b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ss = fma2(a[i], a[i], fma2(b[i], b[i], ss));
+      const f32x2 r = splat2(rsqrtf(fmaf(group_sum(halves_sum(ss), p.group), p.inv_width, p.eps)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { a[i] = mul2(mul2(a[i], r), wa[i]); b[i] = mul2(mul2(b[i], r), wb[i]); }
+      if (FULL || p.table) rotate<NEIGHBOURS>(a, b, turn, l);
+      if (k * per < heads && l.has_a) put(y + k * y_step, q.y_dt, a);
+      if (k * per < heads && l.has_b) put(y + k * y_step + y_b, q.y_dt, b);
+    }
+  });
+}
+
+template <int DT, bool NEIGHBOURS, bool FULL>
+__global__ void __launch_bounds__(kThreads, kBwdCtasPerSm) qk_bwd_kernel(const __grid_constant__ QkArgs p) {
+  extern __shared__ __align__(16) float smem[];
+  const int zero = ptx::grid_wait_previous();
+  const QkPart& q = p.part[part_of(p, blockIdx.x)];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 32 / p.group;
+  const Lane l = lane_of<NEIGHBOURS, FULL>(p, lane & (p.group - 1));
+  f32x2 wa[4], wb[4], da2[4] = {}, db2[4] = {};
+  load_weight(q, l, wa, wb);
+  const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * slot_bytes<true, DT>(p.group);
+  walk<true, DT>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, bool inside, char* y, uint32_t y_step, int y_b) {
+    Turn<NEIGHBOURS> turn;
+    if (FULL || p.table) read_turn<NEIGHBOURS, true>(angles, inside, l, turn);
+#pragma unroll
+    for (int k = 0; k < kSteps<DT>; ++k) {
+      const uint32_t from = data + k * 4 * kChunkBytes<DT>;
+      f32x2 a[4] = {}, b[4] = {}, na[4] = {}, nb[4] = {}, ss2 = 0ull, dot2 = 0ull;
+      if (l.has_a) { widen<DT>(from, a); widen<DT>(from + 2 * kChunkBytes<DT>, na); }
+      if (l.has_b) { widen<DT>(from + kChunkBytes<DT>, b); widen<DT>(from + 3 * kChunkBytes<DT>, nb); }
+      if (FULL || p.table) rotate<NEIGHBOURS>(na, nb, turn, l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ss2 = fma2(a[i], a[i], fma2(b[i], b[i], ss2));
+        dot2 = fma2(mul2(na[i], wa[i]), a[i], fma2(mul2(nb[i], wb[i]), b[i], dot2));
+      }
+      float ss = halves_sum(ss2), dot = halves_sum(dot2);
       for (int o = p.group >> 1; o > 0; o >>= 1) {
         ss += __shfl_xor_sync(0xffffffffu, ss, o);
         dot += __shfl_xor_sync(0xffffffffu, dot, o);
       }
-      if (head >= q.heads) continue;                      // (its chunks are zero, but 1 / sigma of nothing may not be finite)
+      if (k * per >= heads) continue;                     // (what its slots hold is not of this unit)
       const float r = rsqrtf(fmaf(ss, p.inv_width, p.eps));
-      const float m = dot * r * r * p.inv_width, br = p.beta_x * r;       // mean(u xhat) = r dot / width, times xhat = x r
+      // mean(u xhat) = r dot / width, times xhat = x r
+      const f32x2 m = splat2(-dot * r * r * p.inv_width), br = splat2(p.beta_x * r), r2 = splat2(r);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        da[i] = fmaf(na[i], a[i] * r, da[i]);
-        db[i] = fmaf(nb[i], b[i] * r, db[i]);
-        a[i] = br * fmaf(-a[i], m, na[i] * wa[i]);
-        b[i] = br * fmaf(-b[i], m, nb[i] * wb[i]);
+      for (int i = 0; i < 4; ++i) {
+        da2[i] = fma2(na[i], mul2(a[i], r2), da2[i]);
+        db2[i] = fma2(nb[i], mul2(b[i], r2), db2[i]);
+        a[i] = mul2(br, fma2(a[i], m, mul2(na[i], wa[i])));
+        b[i] = mul2(br, fma2(b[i], m, mul2(nb[i], wb[i])));
       }
-      const int64_t at = row * q.y_ld + (int64_t)head * p.width;
-      if (l.has_a) store8(q.y, q.y_dt, at, l.a, p.width, true, a);
-      if (l.has_b) store8(q.y, q.y_dt, at, l.b, p.width, true, b);
+      if (l.has_a) put(y + k * y_step, q.y_dt, a);
+      if (l.has_b) put(y + k * y_step + y_b, q.y_dt, b);
     }
-  }
+  });
   if (!q.dw) return;
+  float da[8], db[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { unpack2(da2[i], da[2 * i], da[2 * i + 1]); unpack2(db2[i], db[2 * i], db[2 * i + 1]); }
   for (int o = p.group; o < 32; o <<= 1) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -261,18 +375,19 @@ __global__ void __launch_bounds__(kThreads, 2) qk_bwd_kernel(const __grid_consta
       db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
     }
   }
+  __syncthreads();                                        // every warp is through with its ring, which the sums take the place of
   if (lane < p.group) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (l.has_a) sums[warp][l.a + i] = da[i];
-      if (l.has_b) sums[warp][l.b + i] = db[i];
+      if (l.has_a) smem[warp * p.width + l.a + i] = da[i];
+      if (l.has_b) smem[warp * p.width + l.b + i] = db[i];
     }
   }
   __syncthreads();
   for (int c = threadIdx.x; c < p.width; c += kThreads) {
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) v += sums[k][c];
+    for (int k = 0; k < kWarps; ++k) v += smem[k * p.width + c];
     p.partial[(int64_t)blockIdx.x * p.width + c] = v;
   }
 }
@@ -311,7 +426,7 @@ __global__ void __launch_bounds__(kThreads) qk_general_kernel(const __grid_const
     }
     __syncwarp();
     const float r = rsqrtf(fmaf(warp_sum(ss), p.inv_width, p.eps));
-    const float* t = p.table ? angles_of(p, row) : nullptr;
+    const float* t = p.table ? angles_at(p, position_of(p, row)) : nullptr;
     auto weight = [&](int e) { return q.w ? load_one(q.w, q.w_dt, e) : 1.f; };
     // feature e of v turned (BACK: back)
     auto turned = [&](const float* v, int e, bool weighted) {
@@ -446,7 +561,7 @@ us_status prepare(Call& c, int count, const us_mat* X, const us_mat* w, const us
     // the vector kernels take parts of one input type (its gradients too)
     if (c.dt < 0) c.dt = q.x_dt;
     c.vec = c.vec && q.x_dt == c.dt && aligned(X[k], 16) && aligned(Y[k], dtype_size(Y[k].dtype) == 1 ? 8 : 16) &&
-            (!G || (q.g_dt == c.dt && aligned(G[k], 16)));
+            (!G || (q.g_dt == c.dt && aligned(G[k], 16))) && X[k].ld < (1ll << 29) && Y[k].ld < (1ll << 29) && (!G || G[k].ld < (1ll << 29));   // (pitches in bytes within 32 bits)
   }
   c.empty = !any || (a.rows == 0 && !dw);
   return US_OK;
@@ -457,8 +572,7 @@ int deal(QkArgs& a, int per_block, int most) {
   int64_t all = 0;
   for (int k = 0; k < a.count; ++k) {
     QkPart& q = a.part[k];
-    q.blocks = (q.heads + per_block - 1) / per_block;
-    q.d_blocks = make_fast_div(std::max(1, q.blocks));
+    q.blocks = std::max(1, (q.heads + per_block - 1) / per_block);
     all += a.rows * q.heads;
   }
   int grid = 0;
@@ -469,28 +583,32 @@ int deal(QkArgs& a, int per_block, int most) {
     q.first_cta = grid;
     q.ctas = (int)std::max<int64_t>(1, std::min(want, share));
     grid += q.ctas;
+    const int64_t step = (int64_t)q.ctas * kWarps, blocks = q.blocks;
+    q.step_rows = (uint32_t)(step / blocks); q.step_blocks = (uint32_t)(step % blocks);
+    q.step_position = a.period ? q.step_rows % a.period : q.step_rows;
   }
   return grid;
 }
 
-template <bool BWD, int DT, int ITER>
-us_status launch_vec(const Call& c, int neighbours, int grid, cudaStream_t st) {
-  if constexpr (BWD)
-    return neighbours ? host::launch(qk_bwd_kernel<DT, ITER, true>, nullptr, grid, kThreads, 0, 1, st, c.a)
-                      : host::launch(qk_bwd_kernel<DT, ITER, false>, nullptr, grid, kThreads, 0, 1, st, c.a);
-  else
-    return neighbours ? host::launch(qk_fwd_kernel<DT, ITER, true>, nullptr, grid, kThreads, 0, 1, st, c.a)
-                      : host::launch(qk_fwd_kernel<DT, ITER, false>, nullptr, grid, kThreads, 0, 1, st, c.a);
-}
 template <bool BWD, int DT>
-us_status pick_iter(const Call& c, int iter, int neighbours, int grid, cudaStream_t st) {
-  if constexpr (!BWD) {
-    if (iter >= 4) return launch_vec<BWD, DT, 4>(c, neighbours, grid, st);
+us_status launch_vec(Call& c, int neighbours, int sms, cudaStream_t st) {
+  // as many CTAs an SM as their rings leave room for, and no more
+  const size_t smem = (size_t)kWarps * kStages * slot_bytes<BWD, DT>(c.a.group);
+  constexpr size_t most = (size_t)kWarps * kStages * slot_bytes<BWD, DT>(32);
+  const int grid = deal(c.a, 32 / c.a.group * kSteps<DT>, sms * std::min(BWD ? kBwdCtasPerSm : kFwdCtasPerSm, (int)((227 << 10) / (smem + 1024))));
+  const bool full = c.a.table && c.a.rotated == c.a.width && c.a.group * 16 == c.a.width;
+  static std::atomic<uint64_t> smem_set[4];
+  auto go = [&](auto kern) {
+    if (!host::allow_smem(kern, smem_set[2 * full + neighbours], most)) return host::failed();
+    return host::launch(kern, nullptr, grid, kThreads, smem, 1, st, c.a);
+  };
+  if constexpr (BWD) {
+    if (full) return neighbours ? go(qk_bwd_kernel<DT, true, true>) : go(qk_bwd_kernel<DT, false, true>);
+    return neighbours ? go(qk_bwd_kernel<DT, true, false>) : go(qk_bwd_kernel<DT, false, false>);
+  } else {
+    if (full) return neighbours ? go(qk_fwd_kernel<DT, true, true>) : go(qk_fwd_kernel<DT, false, true>);
+    return neighbours ? go(qk_fwd_kernel<DT, true, false>) : go(qk_fwd_kernel<DT, false, false>);
   }
-  if constexpr (!BWD || DT != US_F32) {
-    if (iter >= 2) return launch_vec<BWD, DT, 2>(c, neighbours, grid, st);
-  }
-  return launch_vec<BWD, DT, 1>(c, neighbours, grid, st);
 }
 
 template <bool BWD>
@@ -509,16 +627,8 @@ us_status issue(Call& c, int neighbours, cudaStream_t st) {
   const int chunks = a.width / 8;
   a.lanes = neighbours ? (chunks + 1) / 2 : a.rotated / 16 + (chunks - a.rotated / 8 + 1) / 2;
   for (a.group = 1; a.group < a.lanes; a.group *= 2) {}
-  const int per = 32 / a.group;
-  int heads = 1;
-  for (int k = 0; k < a.count; ++k) heads = std::max(heads, a.part[k].heads);
-  const int steps = (heads + per - 1) / per, most_iter = !BWD ? 4 : c.dt == US_F32 ? 1 : 2;       // (what the registers hold)
-  int iter = steps >= most_iter ? most_iter : steps >= 2 ? 2 : 1;
-  // few tokens: a step to a warp, so that all of them are under way at once
-  while (iter > 1 && a.rows * ((steps + iter - 1) / iter) < (int64_t)sms * kWarps) iter /= 2;
-  const int grid = deal(a, per * iter, sms * (BWD ? kBwdCtasPerSm : kFwdCtasPerSm));
-  if (c.dt == US_F32) return pick_iter<BWD, US_F32>(c, iter, neighbours, grid, st);
-  return c.dt == US_BF16 ? pick_iter<BWD, US_BF16>(c, iter, neighbours, grid, st) : pick_iter<BWD, US_F16>(c, iter, neighbours, grid, st);
+  if (c.dt == US_F32) return launch_vec<BWD, US_F32>(c, neighbours, sms, st);
+  return c.dt == US_BF16 ? launch_vec<BWD, US_BF16>(c, neighbours, sms, st) : launch_vec<BWD, US_F16>(c, neighbours, sms, st);
 }
 
 }  // namespace
