@@ -14,6 +14,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "host.h"
@@ -25,7 +26,7 @@ namespace {
 
 constexpr int kMostParts = 4, kMostWidth = 1024, kMostVecWidth = 512;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kBwdCtasPerSm = 2, kFwdCtasPerSm = 3;
+constexpr int kBwdCtasPerSm = 2, kFwdCtasPerSm = 2;
 
 struct QkPart {
   const void *x, *g, *w;
@@ -101,12 +102,39 @@ __device__ __forceinline__ float halves_sum(f32x2 v) {
   unpack2(v, a, b);
   return a + b;
 }
-// Eight features rounded to dt, to an address with the chunk's alignment.
-__device__ __forceinline__ void put(char* to, int dt, const f32x2 (&y)[4]) {
+// Eight features rounded to type DT, to an address with the chunk's alignment.
+template <int DT>
+__device__ __forceinline__ void put(char* to, const f32x2 (&y)[4]) {
   float v[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) unpack2(y[i], v[2 * i], v[2 * i + 1]);
-  store8(to, dt, 0, 0, 8, true, v);
+  if (DT == US_F32) {
+    reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else if (DT == US_BF16) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  } else if (DT == US_F16) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3]), pack_f16x2(v[4], v[5]), pack_f16x2(v[6], v[7]));
+  } else {
+    *reinterpret_cast<uint2*>(to) = make_uint2(cvt_fp8x4<DT == US_E5M2>(v[0], v[1], v[2], v[3]), cvt_fp8x4<DT == US_E5M2>(v[4], v[5], v[6], v[7]));
+  }
+}
+// Calls g with the type of a part's results as a constant.
+template <class G>
+__device__ __forceinline__ void with_output(int dt, G g) {
+  switch (dt) {
+    case US_F32: g(std::integral_constant<int, US_F32>()); break;
+    case US_BF16: g(std::integral_constant<int, US_BF16>()); break;
+    case US_F16: g(std::integral_constant<int, US_F16>()); break;
+    case US_E4M3: g(std::integral_constant<int, US_E4M3>()); break;
+    default: g(std::integral_constant<int, US_E5M2>()); break;
+  }
+}
+// 1 / sqrt(x), within 2 steps; of nothing infinite.
+__device__ __forceinline__ float rsqrt_approx(float x) {
+  float r;
+  asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // Which features a lane has, and which of them are rotated.
@@ -139,25 +167,24 @@ __device__ __forceinline__ Lane lane_of(const QkArgs& p, int j) {
   l.rot_a = l.rot_a && l.has_a; l.rot_b = l.rot_b && l.has_b;
   return l;
 }
-// Cosines and sines of a lane's pairs, eight from pair 8 j on, as a turn needs them.  Chunk a of a half turn: cos[0 .. 3] its cosines, two each, sin[0 .. 3] the sines.
+// Cosines and sines of a lane's pairs, eight from pair 8 j on, as a turn needs them.  Chunk a of a half turn: cos[0 .. 3] its cosines, two each, sin and minus the sines and their negatives.
 // Neighbours: for pair i of chunk a (b: i + 4) cos[i] = (c, c), sin[i] = (-s, s).
 template <bool NEIGHBOURS>
-struct Turn { f32x2 cos[NEIGHBOURS ? 8 : 4], sin[NEIGHBOURS ? 8 : 4]; };
-// from: this lane's 64 bytes of the table's row.  inside: whether there is one; otherwise what is turned becomes NaN.
+struct Turn { f32x2 cos[NEIGHBOURS ? 8 : 4], sin[NEIGHBOURS ? 8 : 4], minus[NEIGHBOURS ? 1 : 4]; };
+// from: this lane's 64 bytes of the table's row
 template <bool NEIGHBOURS, bool BACK>
-__device__ __forceinline__ void read_turn(uint32_t from, bool inside, const Lane& l, Turn<NEIGHBOURS>& t) {
+__device__ __forceinline__ void read_turn(uint32_t from, const Lane& l, Turn<NEIGHBOURS>& t) {
   if (!(l.rot_a || l.rot_b)) return;
-  const uint32_t none = 0x7fffffffu;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {                                // two pairs
-    const uint4 r = inside ? ptx::lds128(from + 16u * i) : make_uint4(none, none, none, none);
+    const uint4 r = ptx::lds128(from + 16u * i);
     float4 v = make_float4(__uint_as_float(r.x), __uint_as_float(r.y), __uint_as_float(r.z), __uint_as_float(r.w));
     if (BACK) { v.y = -v.y; v.w = -v.w; }
     if constexpr (NEIGHBOURS) {
       t.cos[2 * i] = pack2(v.x, v.x); t.cos[2 * i + 1] = pack2(v.z, v.z);
       t.sin[2 * i] = pack2(-v.y, v.y); t.sin[2 * i + 1] = pack2(-v.w, v.w);
     } else {
-      t.cos[i] = pack2(v.x, v.z); t.sin[i] = pack2(v.y, v.w);
+      t.cos[i] = pack2(v.x, v.z); t.sin[i] = pack2(v.y, v.w); t.minus[i] = pack2(-v.y, -v.w);
     }
   }
 }
@@ -166,7 +193,6 @@ __device__ __forceinline__ f32x2 swapped(f32x2 v) {
   unpack2(v, a, b);
   return pack2(b, a);
 }
-__device__ __forceinline__ f32x2 negated(f32x2 v) { return v ^ 0x8000000080000000ull; }
 template <bool NEIGHBOURS>
 __device__ __forceinline__ void rotate(f32x2 (&a)[4], f32x2 (&b)[4], const Turn<NEIGHBOURS>& t, const Lane& l) {
   if constexpr (NEIGHBOURS) {
@@ -178,7 +204,7 @@ __device__ __forceinline__ void rotate(f32x2 (&a)[4], f32x2 (&b)[4], const Turn<
   } else if (l.rot_a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const f32x2 ya = fma2(negated(b[i]), t.sin[i], mul2(a[i], t.cos[i]));
+      const f32x2 ya = fma2(b[i], t.minus[i], mul2(a[i], t.cos[i]));
       b[i] = fma2(a[i], t.sin[i], mul2(b[i], t.cos[i]));
       a[i] = ya;
     }
@@ -199,15 +225,13 @@ __device__ __forceinline__ void load_weight(const QkPart& q, const Lane& l, f32x
   }
 }
 
-// The vector kernels' walk over the units of a warp: kSteps steps of 32 / G heads of one row, which arrive in a ring of kStages slots of the warp's own in shared memory, two units
+// The vector kernels' walk over the units of a warp: STEPS steps of 32 / G heads of one row, which arrive in a ring of kStages slots of the warp's own in shared memory, two units
 // ahead of the one that is worked on.  (With the loads of one unit in registers and none ahead, 8192 tokens of 16 + 16 heads of 64 took 20.7 us forward and 29.4 backward, 16384
 // tokens of 32 + 8 heads of 128 into E4M3 91 to 107: latency.)
-template <int DT>
-constexpr int kSteps = DT == US_F32 ? 1 : 2;
 constexpr int kStages = 3;
 // Bytes of a slot: both chunks of a step, of x and backward of the gradient, and the row of the table.
-template <bool BWD, int DT>
-__host__ __device__ constexpr int slot_bytes(int group) { return kSteps<DT> * (BWD ? 4 : 2) * kChunkBytes<DT> + 64 * group; }
+template <bool BWD, int DT, int STEPS>
+__host__ __device__ constexpr int slot_bytes(int group) { return STEPS * (BWD ? 4 : 2) * kChunkBytes<DT> + 64 * group; }
 
 // A unit of a warp, and its position where all rows' follow from their number.  Advanced by additions: 64-bit products and divisions for each unit were most of what
 // the kernels issued (21 to 26 instructions a value).
@@ -216,54 +240,73 @@ __device__ __forceinline__ Unit first_unit(const QkArgs& p, const QkPart& q, uin
   const uint32_t row = number / (uint32_t)q.blocks;
   return Unit{row, number - row * q.blocks, p.period ? row % p.period : row};
 }
-__device__ __forceinline__ void advance(const QkArgs& p, const QkPart& q, Unit& u) {
+__device__ __forceinline__ bool advance(const QkArgs& p, const QkPart& q, Unit& u) {            // whether the blocks of a row were through
   const uint32_t carry = u.block + q.step_blocks >= (uint32_t)q.blocks;
   u.block += q.step_blocks - (carry ? q.blocks : 0);
   u.row += q.step_rows + carry;
   u.position += q.step_position + carry;
   if (p.period && u.position >= p.period) u.position -= p.period;
+  return carry;
 }
-__device__ __forceinline__ int64_t position_of(const QkArgs& p, const Unit& u) { return p.positions ? (int64_t)__ldg(p.positions + u.row) : p.start + (int64_t)u.position; }
-// Bytes from a matrix to a lane's first feature of a unit: row, and heads of the unit and before the lane's.
-__device__ __forceinline__ int64_t offset(const Unit& u, uint32_t row_bytes, uint32_t block_bytes) { return (int64_t)((uint64_t)u.row * row_bytes + (uint64_t)u.block * block_bytes); }
+// (what is not in the table, negative ones too, is not below its number of rows, which are fewer than 2^31 here)
+__device__ __forceinline__ uint32_t position_of(const QkArgs& p, const Unit& u) { return p.positions ? (uint32_t)__ldg(p.positions + u.row) : (uint32_t)p.start + u.position; }
+// A lane's place in a matrix.  STEPPED: it goes from unit to unit by additions (forward; backward, where registers are short, by a product).
+template <bool STEPPED>
+struct Place {
+  char* base;
+  int64_t row_bytes, carried;                                   // STEPPED: bytes from unit to unit, and what is added where the blocks of a row are through
+  int block_bytes;
+  __device__ __forceinline__ Place(const void* to, const Unit& u, const QkPart& q, int64_t pitch, int block) : base(static_cast<char*>(const_cast<void*>(to))), row_bytes(pitch), block_bytes(block) {
+    if (STEPPED) {
+      base += u.row * pitch + (int64_t)u.block * block;
+      row_bytes = q.step_rows * pitch + (int64_t)q.step_blocks * block;
+      carried = pitch - (int64_t)q.blocks * block;
+    }
+  }
+  __device__ __forceinline__ char* at(const Unit& u) const { return STEPPED ? base : base + u.row * row_bytes + (int64_t)u.block * block_bytes; }
+  __device__ __forceinline__ void advance(bool carry) { if (STEPPED) { base += row_bytes; if (carry) base += carried; } }
+};
 
-template <bool BWD, int DT, class G>
+template <bool BWD, int DT, int STEPS, class G>
 __device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lane& l, uint32_t ring, int zero, G work) {
   constexpr int kC = kChunkBytes<DT>, kStep = (BWD ? 4 : 2) * kC, kEs = DT == US_F32 ? 4 : 2;
-  const int lane = threadIdx.x & 31, j = lane & (p.group - 1), per = 32 / p.group, slot = slot_bytes<BWD, DT>(p.group);
-  const uint32_t rows = (uint32_t)p.rows, x_row = (uint32_t)(q.x_ld * kEs), g_row = BWD ? (uint32_t)(q.g_ld * kEs) : 0u;
-  const uint32_t step_bytes = (uint32_t)(per * p.width * kEs), block_bytes = step_bytes * kSteps<DT>;
-  const int place = (lane / p.group) * p.width;                 // this lane's head among those of a step
-  const char *xa = static_cast<const char*>(q.x) + (place + l.a) * kEs, *ga = static_cast<const char*>(q.g) + (place + l.a) * kEs;
-  const int b_minus_a = (l.b - l.a) * kEs;
+  const int lane = threadIdx.x & 31, j = lane & (p.group - 1), per = 32 / p.group, slot = slot_bytes<BWD, DT, STEPS>(p.group);
+  const uint32_t rows = (uint32_t)p.rows;
+  const int step_bytes = per * p.width * kEs, b_minus_a = (l.b - l.a) * kEs;
+  const int first = lane / p.group * p.width + l.a;             // this lane's first feature among those of a step
   const bool turns = p.table != nullptr;
   const float* table = p.table + 16 * j;
   Unit now = first_unit(p, q, (blockIdx.x - q.first_cta) * kWarps + (threadIdx.x >> 5) + zero), next = now;
-  // positions are read one unit before the copy of their angles is issued; inside: a bit per slot, whether its position is in the table
-  int64_t position = turns && next.row < rows ? position_of(p, next) : 0;
-  uint32_t inside = 0u;
+  Place<!BWD> x(static_cast<const char*>(q.x) + first * kEs, next, q, q.x_ld * kEs, step_bytes * STEPS), g(BWD ? static_cast<const char*>(q.g) + first * kEs : nullptr, next, q, q.g_ld * kEs, step_bytes * STEPS);
+  // positions are read one unit before the copy of their angles is issued; one that is not in the table has NaN for angles
+  uint32_t position = turns && next.row < rows ? position_of(p, next) : 0;
   auto issue = [&](int s) {
     if (next.row < rows) {
       const uint32_t to = ring + s * slot + lane * 16u;
-      const char *x = xa + offset(next, x_row, block_bytes), *g = BWD ? ga + offset(next, g_row, block_bytes) : nullptr;
-      const int heads = q.heads - (int)next.block * (per * kSteps<DT>) - lane / p.group;        // left from this lane's first on
+      const char *px = x.at(next), *pg = BWD ? g.at(next) : nullptr;
+      const int heads = q.heads - (int)next.block * (per * STEPS) - lane / p.group;        // left from this lane's first on
 #pragma unroll
-      for (int k = 0; k < kSteps<DT>; ++k) {
+      for (int k = 0; k < STEPS; ++k) {
         if (k * per >= heads) break;
-        if (l.has_a) { fetch<DT>(to + k * kStep, x + k * step_bytes); if (BWD) fetch<DT>(to + k * kStep + 2 * kC, g + k * step_bytes); }
-        if (l.has_b) { fetch<DT>(to + k * kStep + kC, x + k * step_bytes + b_minus_a); if (BWD) fetch<DT>(to + k * kStep + 3 * kC, g + k * step_bytes + b_minus_a); }
+        if (l.has_a) { fetch<DT>(to + k * kStep, px + k * step_bytes); if (BWD) fetch<DT>(to + k * kStep + 2 * kC, pg + k * step_bytes); }
+        if (l.has_b) { fetch<DT>(to + k * kStep + kC, px + k * step_bytes + b_minus_a); if (BWD) fetch<DT>(to + k * kStep + 3 * kC, pg + k * step_bytes + b_minus_a); }
       }
-      const int64_t at = position;
-      advance(p, q, next);
+      const uint32_t at = position;
+      const bool carry = advance(p, q, next);
+      x.advance(carry);
+      if (BWD) g.advance(carry);
       if (turns) {
-        const bool in = at >= 0 && at < p.table_rows;
-        inside = (inside & ~(1u << s)) | ((uint32_t)in << s);
-        if (in && lane < p.group) {
-          const float* t = table + at * p.table_ld;
-          const uint32_t angles = ring + s * slot + kSteps<DT> * kStep + 64u * j;
+        if (lane < p.group) {
+          const uint32_t angles = ring + s * slot + STEPS * kStep + 64u * j, none = 0x7fffffffu;
+          if (at < (uint32_t)p.table_rows) {
+            const float* t = table + (uint64_t)at * (uint32_t)p.table_ld;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i < 2 ? l.rot_a : l.rot_b) copy16(angles + 16u * i, t + 4 * i);
+            for (int i = 0; i < 4; ++i)
+              if (i < 2 ? l.rot_a : l.rot_b) copy16(angles + 16u * i, t + 4 * i);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ptx::sts128(angles + 16u * i, make_uint4(none, none, none, none));
+          }
         }
         if (next.row < rows) position = position_of(p, next);
       }
@@ -272,54 +315,55 @@ __device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lan
   };
   for (int s = 0; s < kStages - 1; ++s) issue(s);
   const int y_es = dtype_size(q.y_dt);
-  const uint32_t y_row = (uint32_t)(q.y_ld * y_es), y_step = (uint32_t)(per * p.width * y_es);
-  char* y = static_cast<char*>(q.y) + (place + l.a) * y_es;
-  const int y_b = (l.b - l.a) * y_es;
-  for (int s = 0; now.row < rows; advance(p, q, now)) {
+  const int y_step = per * p.width * y_es, y_b = (l.b - l.a) * y_es;
+  Place<!BWD> y(static_cast<char*>(q.y) + first * y_es, now, q, q.y_ld * y_es, y_step * STEPS);
+  for (int s = 0; now.row < rows; y.advance(advance(p, q, now))) {
     copies_wait<kStages - 2>();
     __syncwarp();
     issue(s == 0 ? kStages - 1 : s - 1);                        // the slot that the last unit was read from
     const uint32_t from = ring + s * slot;
-    const int heads = q.heads - (int)now.block * (per * kSteps<DT>) - lane / p.group;
-    work(heads, from + lane * 16u, from + kSteps<DT> * kStep + 64u * j, (inside >> s & 1u) != 0u, y + offset(now, y_row, y_step * kSteps<DT>), y_step, y_b);
+    const int heads = q.heads - (int)now.block * (per * STEPS) - lane / p.group;
+    work(heads, from + lane * 16u, from + STEPS * kStep + 64u * j, y.at(now), y_step, y_b);
     if (++s == kStages) s = 0;
   }
   copies_wait<0>();
 }
 
 // DT: type of the inputs.
-template <int DT, bool NEIGHBOURS, bool FULL>
+template <int DT, int STEPS, bool NEIGHBOURS, bool FULL>
 __global__ void __launch_bounds__(kThreads, kFwdCtasPerSm) qk_fwd_kernel(const __grid_constant__ QkArgs p) {
   extern __shared__ __align__(16) float smem[];
   const int zero = ptx::grid_wait_previous();
   const QkPart& q = p.part[part_of(p, blockIdx.x)];
+  with_output(q.y_dt, [&](auto y_dt) {
   const int lane = threadIdx.x & 31, per = 32 / p.group;
   const Lane l = lane_of<NEIGHBOURS, FULL>(p, lane & (p.group - 1));
   f32x2 wa[4], wb[4];
   load_weight(q, l, wa, wb);
-  const uint32_t ring = ptx::smem_addr(smem) + (threadIdx.x >> 5) * kStages * slot_bytes<false, DT>(p.group);
-  walk<false, DT>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, bool inside, char* y, uint32_t y_step, int y_b) {
+  const uint32_t ring = ptx::smem_addr(smem) + (threadIdx.x >> 5) * kStages * slot_bytes<false, DT, STEPS>(p.group);
+  walk<false, DT, STEPS>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, char* y, int y_step, int y_b) {
     Turn<NEIGHBOURS> turn;
-    if (FULL || p.table) read_turn<NEIGHBOURS, false>(angles, inside, l, turn);
+    if (FULL || p.table) read_turn<NEIGHBOURS, false>(angles, l, turn);
 #pragma unroll
-    for (int k = 0; k < kSteps<DT>; ++k) {
+    for (int k = 0; k < STEPS; ++k) {
       const uint32_t from = data + k * 2 * kChunkBytes<DT>;
       f32x2 a[4] = {}, b[4] = {}, ss = 0ull;
       if (l.has_a) widen<DT>(from, a);
       if (l.has_b) widen<DT>(from + kChunkBytes<DT>, b);
 #pragma unroll
       for (int i = 0; i < 4; ++i) ss = fma2(a[i], a[i], fma2(b[i], b[i], ss));
-      const f32x2 r = splat2(rsqrtf(fmaf(group_sum(halves_sum(ss), p.group), p.inv_width, p.eps)));
+      const f32x2 r = splat2(rsqrt_approx(fmaf(group_sum(halves_sum(ss), p.group), p.inv_width, p.eps)));
 #pragma unroll
       for (int i = 0; i < 4; ++i) { a[i] = mul2(mul2(a[i], r), wa[i]); b[i] = mul2(mul2(b[i], r), wb[i]); }
       if (FULL || p.table) rotate<NEIGHBOURS>(a, b, turn, l);
-      if (k * per < heads && l.has_a) put(y + k * y_step, q.y_dt, a);
-      if (k * per < heads && l.has_b) put(y + k * y_step + y_b, q.y_dt, b);
+      if (k * per < heads && l.has_a) put<decltype(y_dt)::value>(y + k * y_step, a);
+      if (k * per < heads && l.has_b) put<decltype(y_dt)::value>(y + k * y_step + y_b, b);
     }
+  });
   });
 }
 
-template <int DT, bool NEIGHBOURS, bool FULL>
+template <int DT, int STEPS, bool NEIGHBOURS, bool FULL>
 __global__ void __launch_bounds__(kThreads, kBwdCtasPerSm) qk_bwd_kernel(const __grid_constant__ QkArgs p) {
   extern __shared__ __align__(16) float smem[];
   const int zero = ptx::grid_wait_previous();
@@ -328,12 +372,13 @@ __global__ void __launch_bounds__(kThreads, kBwdCtasPerSm) qk_bwd_kernel(const _
   const Lane l = lane_of<NEIGHBOURS, FULL>(p, lane & (p.group - 1));
   f32x2 wa[4], wb[4], da2[4] = {}, db2[4] = {};
   load_weight(q, l, wa, wb);
-  const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * slot_bytes<true, DT>(p.group);
-  walk<true, DT>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, bool inside, char* y, uint32_t y_step, int y_b) {
+  const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * slot_bytes<true, DT, STEPS>(p.group);
+  with_output(q.y_dt, [&](auto y_dt) {
+  walk<true, DT, STEPS>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, char* y, int y_step, int y_b) {
     Turn<NEIGHBOURS> turn;
-    if (FULL || p.table) read_turn<NEIGHBOURS, true>(angles, inside, l, turn);
+    if (FULL || p.table) read_turn<NEIGHBOURS, true>(angles, l, turn);
 #pragma unroll
-    for (int k = 0; k < kSteps<DT>; ++k) {
+    for (int k = 0; k < STEPS; ++k) {
       const uint32_t from = data + k * 4 * kChunkBytes<DT>;
       f32x2 a[4] = {}, b[4] = {}, na[4] = {}, nb[4] = {}, ss2 = 0ull, dot2 = 0ull;
       if (l.has_a) { widen<DT>(from, a); widen<DT>(from + 2 * kChunkBytes<DT>, na); }
@@ -350,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtasPerSm) qk_bwd_kernel(const _
         dot += __shfl_xor_sync(0xffffffffu, dot, o);
       }
       if (k * per >= heads) continue;                     // (what its slots hold is not of this unit)
-      const float r = rsqrtf(fmaf(ss, p.inv_width, p.eps));
+      const float r = rsqrt_approx(fmaf(ss, p.inv_width, p.eps));
       // mean(u xhat) = r dot / width, times xhat = x r
       const f32x2 m = splat2(-dot * r * r * p.inv_width), br = splat2(p.beta_x * r), r2 = splat2(r);
 #pragma unroll
@@ -360,9 +405,10 @@ __global__ void __launch_bounds__(kThreads, kBwdCtasPerSm) qk_bwd_kernel(const _
         a[i] = mul2(br, fma2(a[i], m, mul2(na[i], wa[i])));
         b[i] = mul2(br, fma2(b[i], m, mul2(nb[i], wb[i])));
       }
-      if (l.has_a) put(y + k * y_step, q.y_dt, a);
-      if (l.has_b) put(y + k * y_step + y_b, q.y_dt, b);
+      if (l.has_a) put<decltype(y_dt)::value>(y + k * y_step, a);
+      if (l.has_b) put<decltype(y_dt)::value>(y + k * y_step + y_b, b);
     }
+  });
   });
   if (!q.dw) return;
   float da[8], db[8];
@@ -531,7 +577,7 @@ us_status prepare(Call& c, int count, const us_mat* X, const us_mat* w, const us
     if (positions && reinterpret_cast<uintptr_t>(positions) % 4) return US_ERR_ALIGNMENT;
     a.table = static_cast<const float*>(table->ptr); a.table_ld = table->ld; a.table_rows = table->rows;
     a.positions = positions; a.start = start; a.period = period < a.rows ? (uint32_t)period : 0; a.rotated = (int)table->cols;
-    c.vec = c.vec && aligned(*table, 16) && a.rotated % (neighbours ? 8 : 16) == 0;
+    c.vec = c.vec && table->rows < (1ll << 31) && aligned(*table, 16) && a.rotated % (neighbours ? 8 : 16) == 0;
   }
   c.vec = c.vec && width % 8 == 0 && width <= kMostVecWidth;
   bool any = false;
@@ -561,7 +607,7 @@ us_status prepare(Call& c, int count, const us_mat* X, const us_mat* w, const us
     // the vector kernels take parts of one input type (its gradients too)
     if (c.dt < 0) c.dt = q.x_dt;
     c.vec = c.vec && q.x_dt == c.dt && aligned(X[k], 16) && aligned(Y[k], dtype_size(Y[k].dtype) == 1 ? 8 : 16) &&
-            (!G || (q.g_dt == c.dt && aligned(G[k], 16))) && X[k].ld < (1ll << 29) && Y[k].ld < (1ll << 29) && (!G || G[k].ld < (1ll << 29));   // (pitches in bytes within 32 bits)
+            (!G || (q.g_dt == c.dt && aligned(G[k], 16)));
   }
   c.empty = !any || (a.rows == 0 && !dw);
   return US_OK;
@@ -590,12 +636,12 @@ int deal(QkArgs& a, int per_block, int most) {
   return grid;
 }
 
-template <bool BWD, int DT>
+template <bool BWD, int DT, int STEPS>
 us_status launch_vec(Call& c, int neighbours, int sms, cudaStream_t st) {
   // as many CTAs an SM as their rings leave room for, and no more
-  const size_t smem = (size_t)kWarps * kStages * slot_bytes<BWD, DT>(c.a.group);
-  constexpr size_t most = (size_t)kWarps * kStages * slot_bytes<BWD, DT>(32);
-  const int grid = deal(c.a, 32 / c.a.group * kSteps<DT>, sms * std::min(BWD ? kBwdCtasPerSm : kFwdCtasPerSm, (int)((227 << 10) / (smem + 1024))));
+  const size_t smem = (size_t)kWarps * kStages * slot_bytes<BWD, DT, STEPS>(c.a.group);
+  constexpr size_t most = (size_t)kWarps * kStages * slot_bytes<BWD, DT, STEPS>(32);
+  const int grid = deal(c.a, 32 / c.a.group * STEPS, sms * std::min(BWD ? kBwdCtasPerSm : kFwdCtasPerSm, (int)((227 << 10) / (smem + 1024))));
   const bool full = c.a.table && c.a.rotated == c.a.width && c.a.group * 16 == c.a.width;
   static std::atomic<uint64_t> smem_set[4];
   auto go = [&](auto kern) {
@@ -603,11 +649,11 @@ us_status launch_vec(Call& c, int neighbours, int sms, cudaStream_t st) {
     return host::launch(kern, nullptr, grid, kThreads, smem, 1, st, c.a);
   };
   if constexpr (BWD) {
-    if (full) return neighbours ? go(qk_bwd_kernel<DT, true, true>) : go(qk_bwd_kernel<DT, false, true>);
-    return neighbours ? go(qk_bwd_kernel<DT, true, false>) : go(qk_bwd_kernel<DT, false, false>);
+    if (full) return neighbours ? go(qk_bwd_kernel<DT, STEPS, true, true>) : go(qk_bwd_kernel<DT, STEPS, false, true>);
+    return neighbours ? go(qk_bwd_kernel<DT, STEPS, true, false>) : go(qk_bwd_kernel<DT, STEPS, false, false>);
   } else {
-    if (full) return neighbours ? go(qk_fwd_kernel<DT, true, true>) : go(qk_fwd_kernel<DT, false, true>);
-    return neighbours ? go(qk_fwd_kernel<DT, true, false>) : go(qk_fwd_kernel<DT, false, false>);
+    if (full) return neighbours ? go(qk_fwd_kernel<DT, STEPS, true, true>) : go(qk_fwd_kernel<DT, STEPS, false, true>);
+    return neighbours ? go(qk_fwd_kernel<DT, STEPS, true, false>) : go(qk_fwd_kernel<DT, STEPS, false, false>);
   }
 }
 
@@ -627,8 +673,8 @@ us_status issue(Call& c, int neighbours, cudaStream_t st) {
   const int chunks = a.width / 8;
   a.lanes = neighbours ? (chunks + 1) / 2 : a.rotated / 16 + (chunks - a.rotated / 8 + 1) / 2;
   for (a.group = 1; a.group < a.lanes; a.group *= 2) {}
-  if (c.dt == US_F32) return launch_vec<BWD, US_F32>(c, neighbours, sms, st);
-  return c.dt == US_BF16 ? launch_vec<BWD, US_BF16>(c, neighbours, sms, st) : launch_vec<BWD, US_F16>(c, neighbours, sms, st);
+  if (c.dt == US_F32) return launch_vec<BWD, US_F32, 1>(c, neighbours, sms, st);
+  return c.dt == US_BF16 ? launch_vec<BWD, US_BF16, 2>(c, neighbours, sms, st) : launch_vec<BWD, US_F16, 2>(c, neighbours, sms, st);
 }
 
 }  // namespace
