@@ -462,3 +462,31 @@ def ffn_block(X, W1, W2, G, sc: FFNScales, *, operand: str = "fp8",
 def ffn_flops(T: int, d: int, f: int) -> float:
     """Matmul FLOPs of one FFN block, forward + backward: two linear layers x 6 b m n."""
     return 2 * 6.0 * T * d * f
+
+
+def gated_ffn_block(X, W1, W2, G, gate: str, tau: float = 0.5, operand: str = "fp8", kept: str = "bf16", io_dtype: str = "bf16") -> FFNResult:
+    """An FFN block with hidden layer f(X Wg) * (X Wu), W1 = [Wg Wu], unconstrained factors; r.H = [H U] and r.dHq = [dH dU] as
+    stored, the rest as for ffn_block."""
+    T, d = np.shape(X)
+    f = W1.shape[1] // 2
+    act_fmt, grad_fmt = ("e4m3", "e5m2") if operand == "fp8" else (operand, operand)
+    fn, dfn = _act(gate)
+    ag, bh, bu = S.gated_scales(fn, dfn)
+    r = FFNResult()
+    r.Xq, _ = store(np.asarray(X), act_fmt)
+    r.W1q, _ = store(np.asarray(W1), act_fmt)
+    r.W2q, _ = store(np.asarray(W2), act_fmt)
+    r.Gq, _ = store(np.asarray(G), grad_fmt)
+    c_skip, c_branch = S.residual_coefficients(tau)
+    A, h, u = gated_fwd(gate, r.Xq, r.W1q[:, :f], r.W1q[:, f:], d ** -0.5, 1.0, ag)
+    r.Aq, r.Aq_codes = store(A, act_fmt)
+    r.H, _ = store(np.concatenate([h, u], 1), kept)
+    ep2 = Epilogue(skip=np.asarray(X, np.float64), skip_coef=c_skip, out_coef=c_branch)
+    r.R, _, _ = apply_epilogue(linear_fwd(r.Aq, r.W2q, f ** -0.5), ep2, io_dtype)
+    r.dA = linear_bwd_x(r.Gq, r.W2q, d ** -0.5)
+    r.dHq, r.dHq_codes = store(np.concatenate(gated_bwd(gate, r.Gq, r.W2q, d ** -0.5, r.H[:, :f], r.H[:, f:], 1.0, bh, bu), 1), grad_fmt)
+    r.dW2, _, _ = apply_epilogue(linear_bwd_w(r.Aq, r.Gq, T ** -0.5), None, "f32")
+    ep5 = Epilogue(skip=np.asarray(G, np.float64), skip_coef=c_skip, out_coef=c_branch)
+    r.dX, _, _ = apply_epilogue(linear_bwd_x(r.dHq, r.W1q, (2 * f) ** -0.5), ep5, io_dtype)
+    r.dW1, _, _ = apply_epilogue(linear_bwd_w(r.Xq, r.dHq, T ** -0.5), None, "f32")
+    return r

@@ -23,6 +23,10 @@ FP8 operands like the projections (section "Experiments": all matmul inputs are 
 GEMM writes Q, K, V as E4M3, the softmax writes P as E4M3, the gradients dC and dS are written as E5M2
 and the batched GEMMs write dQ, dK, dV straight into the E5M2 operand of the QKV backward GEMMs (one
 cast launch fewer); S and dP, which feed no matmul, stay in BF16.
+
+gate = "silu" (or another activation): the FFN block is gated (ffn.UnitScaledGatedFFN; W1 is [d x 2 d_ff]), its pre-activations kept in the type `kept`.
+qk_norm: queries and keys pass through a root-mean-square norm of each head on their way to the scores, and with rotary = base through the rotation by
+their position in the sequence (us_qk_norm_fwd / bwd, one launch for both); the norms' weights are step()'s qk = (wq, wk), their gradients dqk.
 """
 from __future__ import annotations
 
@@ -64,8 +68,8 @@ def backward_in_one_launch(problems: int, slen: int, fp8: bool) -> bool:
 class UnitScaledEncoderLayer:
     def __init__(self, nseq: int, slen: int, d: int, nhead: int, d_ff: int, tau: float = 0.5,
                  attention: str = "bf16", norm: str | None = None, eps: float = 1e-5, device="cuda",
-                 fused_attention: bool = False):
-        assert d % nhead == 0 and norm in (None, "post")
+                 fused_attention: bool = False, gate: str | None = None, kept: str = "bf16", qk_norm: bool = False, rotary: float | None = None):
+        assert d % nhead == 0 and norm in (None, "post") and (qk_norm or rotary is None)
         self.attention, self.norm, self.eps = attention, norm, eps
         # fused_attention: scores, scaled softmax and context of the forward pass as one us_attention_fwd launch, and the
         # whole backward pass as one us_attention_bwd_all launch, or dP, the softmax gradient and dQ as one us_attention_bwd
@@ -82,12 +86,17 @@ class UnitScaledEncoderLayer:
         T = self.T = nseq * slen
         e = lambda r, c, dt: torch.empty((r, c), dtype=dt, device=device)
         self.Xq, self.Wqkv_q, self.Wo_q = e(T, d, E4), e(d, 3 * d, E4), e(d, d, E4)
-        self.QKV = e(T, 3 * d, act_dt)
+        # with norms of queries and keys the projection's outputs are 16-bit; QKn, and with FP8 operands Vq, are what attention reads
+        self.QKV = e(T, 3 * d, wide_dt if qk_norm else act_dt)
         self.S = None if fused_attention else e(nseq * nhead * slen, slen, wide_dt)
         self.P = e(nseq * nhead * slen, slen, act_dt)
         self.Cq = e(T, d, E4)
         self.R1 = e(T, d, torch.bfloat16)
-        self.ffn = F.UnitScaledFFN(T, d, d_ff, scales=F.FFNScales.unit(T, d, d_ff, tau), device=device)
+        self.gate, self.qk_norm = gate, qk_norm
+        if gate is None:
+            self.ffn = F.UnitScaledFFN(T, d, d_ff, scales=F.FFNScales.unit(T, d, d_ff, tau), device=device)
+        else:
+            self.ffn = F.UnitScaledGatedFFN(T, d, d_ff, gate=gate, kept=kept, tau=tau, device=device)
         self.g1q = e(T, d, E5)
         self.dC = e(T, d, grad_dt)
         self.dP = None if fused_attention else e(nseq * nhead * slen, slen, wide_dt)
@@ -95,7 +104,14 @@ class UnitScaledEncoderLayer:
         self.dQKVq = e(T, 3 * d, E5)
         # dQ, dK, dV are consumed only as the E5M2 operand of the QKV projection's backward GEMMs: with FP8 attention
         # operands, and with the fused attention kernels, their producers write that format directly (no cast launch)
-        self.dQKV = self.dQKVq if (attention == "fp8" or fused_attention) else e(T, 3 * d, grad_dt)
+        self.dQKV = self.dQKVq if (attention == "fp8" or fused_attention or qk_norm) else e(T, 3 * d, grad_dt)
+        if qk_norm:
+            self.QKn, self.dQKn = e(T, 2 * d, act_dt), e(T, 2 * d, wide_dt)
+            self.Vq = e(T, d, act_dt) if attention == "fp8" else None
+            self.rotary = L.rotary_table(slen, self.hd // 2 * 2, rotary, device=device) if rotary is not None else None
+            self.dqk = [torch.empty(self.hd, dtype=torch.float32, device=device) for _ in range(2)]
+            self.qk_ws = torch.empty(L.us_qk_norm_bwd_workspace_bytes(self.hd), dtype=torch.uint8, device=device)
+            self.beta_qk = L.us_scales_linear(T * nhead, 1, 1)[2]      # b^-1/2 with b = all heads of all tokens
         self.dX = e(T, d, torch.bfloat16)
         self.dWqkv, self.dWo = e(d, 3 * d, torch.float32), e(d, d, torch.float32)
         self.ws = L.new_workspace(device)
@@ -113,16 +129,20 @@ class UnitScaledEncoderLayer:
         a_o, b_o, _ = L.us_scales_linear(T, d, d)
         self.sc = dict(alpha_qkv=a_qkv, beta_qkv=b_qkv, alpha_o=a_o, beta_o=b_o, beta_w=b_w, **L.us_scales_attention(s, hd))
         qkv = (slen * 3 * d, hd)          # (outer, inner) strides of a head slice of a [T x 3d] matrix
+        qk = (slen * 2 * d, hd) if qk_norm else qkv
+        v = (slen * d, hd) if qk_norm and attention == "fp8" else qkv
         sq = (nhead * slen * slen, slen * slen)
         td = (slen * d, hd)               # head slice of a [T x d] matrix
         n = (nseq, nhead)
-        self.bt = dict(scores=L.batch(n, qkv, qkv, sq), ctx=L.batch(n, sq, qkv, td), dP=L.batch(n, td, qkv, sq),
-                       dV=L.batch(n, sq, td, qkv), dQ=L.batch(n, sq, qkv, qkv), dK=L.batch(n, sq, qkv, qkv))
+        self.bt = dict(scores=L.batch(n, qk, qk, sq), ctx=L.batch(n, sq, v, td), dP=L.batch(n, td, v, sq),
+                       dV=L.batch(n, sq, td, qkv), dQ=L.batch(n, sq, qk, qk), dK=L.batch(n, sq, qk, qk))
         # fused cast, attention forward, FFN forward + backward, attention backward (one cast fewer with FP8 attention)
-        self._launches = 1 + (3 if fused_attention else 5) + 7 + ((10 if (attention == "fp8" or fused_attention) else 11) - (2 if fused_attention else 0)) + (7 if norm == "post" else 0)
-        self.bt_fused = L.attention_batch(n, qkv, qkv, qkv, td, sq)
-        self.bt_fused_bwd = L.attention_bwd_batch(n, td, sq, qkv, qkv, sq, qkv)
-        self.bt_fused_all = L.attention_bwd_all_batch(n, td, sq, qkv, qkv, qkv, sq, qkv, qkv, qkv)
+        self._launches = 1 + (3 if fused_attention else 5) + 7 + ((10 if self.dQKV is self.dQKVq else 11) - (2 if fused_attention else 0)) + (7 if norm == "post" else 0)
+        if qk_norm:
+            self._launches += 3 + (attention == "fp8")                 # norms forward; backward, with the sums of their weights' gradients; the values' cast
+        self.bt_fused = L.attention_batch(n, qk, qk, v, td, sq)
+        self.bt_fused_bwd = L.attention_bwd_batch(n, td, sq, qk, v, sq, qk)
+        self.bt_fused_all = L.attention_bwd_all_batch(n, td, sq, qk, qk, v, sq, qk, qk, qkv)
         self._whole = backward_in_one_launch(nseq * nhead, slen, attention == "fp8")
 
     @property
@@ -163,6 +183,27 @@ class UnitScaledEncoderLayer:
         o = which * self.d
         return M[: self.slen, o:o + self.hd]
 
+    def _operands(self):
+        """Problem (0, 0) of the queries, keys and values that attention reads, and of their gradients that it writes."""
+        if not self.qk_norm:
+            return [self._heads(self.QKV, i) for i in range(3)], [self._heads(self.dQKV, i) for i in range(3)]
+        V = self._heads(self.QKV, 2) if self.Vq is None else self._heads(self.Vq, 0)
+        return [self._heads(self.QKn, 0), self._heads(self.QKn, 1), V], [self._heads(self.dQKn, 0), self._heads(self.dQKn, 1), self._heads(self.dQKVq, 2)]
+
+    def _plan_qk(self, p, backward: bool):
+        """The launch that norms (and rotates) queries and keys, or takes their gradients back."""
+        d = self.d
+        pair = lambda M: (L.us_mat * 2)(p.mat(M[:, :d]), p.mat(M[:, d:2 * d]))
+        w = (L.us_mat * 2)()
+        p.slot("wq", w[0])
+        p.slot("wk", w[1])
+        place = (p.mat(self.rotary) if self.rotary is not None else None, None, 0, self.slen, 0)
+        if not backward:
+            return L.Call("us_qk_norm_fwd", 2, pair(self.QKV), w, pair(self.QKn), self.hd, self.eps, *place)
+        dw = (L.us_mat * 2)(*(L._vec(t) for t in self.dqk))
+        return L.Call("us_qk_norm_bwd", 2, pair(self.QKV), w, pair(self.dQKn), pair(self.dQKVq), dw, (L.C.c_float * 2)(self.beta_qk, self.beta_qk), self.hd, self.eps, 1.0,
+                      *place, self.qk_ws.data_ptr(), self.qk_ws.numel())
+
     # ---- a step as calls laid out once over the layer's buffers (L.Plan), the same ones as _step_each, as (where, call) pairs
     MAIN, SIDE, JOIN = L.Plan.MAIN, L.Plan.SIDE, L.Plan.JOIN
 
@@ -173,6 +214,8 @@ class UnitScaledEncoderLayer:
             own += (self.S, self.dP)
         if self.norm == "post":
             own += (self.U1, self.R2, self.dU1, self.dU2, self.ln_ws, *self.dln)
+        if self.qk_norm:
+            own += (self.QKn, self.dQKn, self.qk_ws, *self.dqk) + tuple(t for t in (self.Vq, self.rotary) if t is not None)
         return own
 
     def _state(self):
@@ -194,7 +237,11 @@ class UnitScaledEncoderLayer:
         yield MAIN, p.cast_multi(["Wqkv", "Wo", "X", "W1", "W2"] + ([] if post else ["G"]),
                                  [self.Wqkv_q, self.Wo_q, self.Xq, f.W1q, f.W2q] + ([] if post else [f.Gq]))
         yield MAIN, p.linear("us_linear_fwd", self.Xq, self.Wqkv_q, sc["alpha_qkv"], self.QKV, ws)
-        Q, K, V = (self._heads(self.QKV, i) for i in range(3))
+        (Q, K, V), (dQ, dK, dV) = self._operands()
+        if self.qk_norm:
+            yield MAIN, self._plan_qk(p, backward=False)
+            if self.Vq is not None:
+                yield MAIN, L.Call("us_cast_fp8", p.mat(self.QKV[:, 2 * self.d:]), 1.0, p.mat(self.Vq))
         P, C_h = self.P[:s], self.Cq[:s, : self.hd]
         tail = (ws.data_ptr(), ws.numel())
         if fused:
@@ -223,7 +270,6 @@ class UnitScaledEncoderLayer:
             g1 = f.dX
         yield MAIN, p.group([(L.US_OP_BWD_W, self.Cq, self.g1q, sc["beta_w"], self.dWo, None, None),
                              (L.US_OP_BWD_X, self.g1q, self.Wo_q, sc["beta_o"], self.dC, None, None)], ws)
-        dQ, dK, dV = (self._heads(self.dQKV, i) for i in range(3))
         dS, dC_h = self.dS[:s], self.dC[:s, : self.hd]
         if self.whole_bwd:
             # dS is read by no later launch; it is stored (7 us of 8192 tokens of 16 heads and 512 keys at 16 bits) because self.dS holds
@@ -243,6 +289,8 @@ class UnitScaledEncoderLayer:
                 yield self.SIDE, gemm_dk
                 yield MAIN, p.batched("us_linear_fwd_batched", dS, K, sc["beta_Q"], dQ, self.bt["dQ"], ws)
             yield self.JOIN, None                                   # dQ, dK, dV all written
+        if self.qk_norm:
+            yield MAIN, self._plan_qk(p, backward=True)
         if self.dQKV is not self.dQKVq:
             yield MAIN, L.Call("us_cast_fp8", p.mat(self.dQKV), 1.0, p.mat(self.dQKVq))
         yield MAIN, p.group([(L.US_OP_BWD_W, self.Xq, self.dQKVq, sc["beta_w"], self.dWqkv, None, None),
@@ -267,17 +315,20 @@ class UnitScaledEncoderLayer:
                 e.record(cur)                                       # an event has a handle once it has been recorded
         p.issue(self._lay_out, inputs, cur.cuda_stream, (self.ffn._side_streams()[0], *self._events))
 
-    def step(self, X, Wqkv, Wo, W1, W2, G, stream=None, ln=None):
+    def step(self, X, Wqkv, Wo, W1, W2, G, stream=None, ln=None, qk=None):
         """One forward + backward pass.  G is the gradient of the layer output; with norm = "post",
-        ln = (w1, c1, w2, c2) are the weights and biases of the two layer norms ([d] each)."""
-        if self.ffn.grouped and self.ffn.fused_hidden:
+        ln = (w1, c1, w2, c2) are the weights and biases of the two layer norms ([d] each); with qk_norm, qk = (wq, wk) are
+        the weights of the norms of queries and keys ([d / nhead] each)."""
+        if self.qk_norm or (self.ffn.grouped and self.ffn.fused_hidden):
             norm = dict(zip(("w1", "c1", "w2", "c2"), (t.view(1, -1) for t in ln))) if self.norm == "post" else {}
+            if self.qk_norm:
+                norm |= dict(zip(("wq", "wk"), (t.view(1, -1) for t in qk)))
             self._run(stream, X=X, Wqkv=Wqkv, Wo=Wo, W1=W1, W2=W2, G=G, **norm)
             return self.dX
         return self._step_each(X, Wqkv, Wo, W1, W2, G, stream, ln)
 
     def _step_each(self, X, Wqkv, Wo, W1, W2, G, stream, ln):
-        """step() call by call, for an FFN block whose grouped forms are switched off."""
+        """step() call by call, for an FFN block whose grouped forms are switched off (neither gated nor with norms of queries and keys)."""
         sc, ws, s = self.sc, self.ws, self.slen
         post = self.norm == "post"
         # ---- forward
@@ -367,4 +418,4 @@ class UnitScaledEncoderLayer:
         T, d, f, s, hd = self.T, self.d, self.d_ff, self.slen, self.hd
         proj = 6.0 * T * d * 3 * d + 6.0 * T * d * d
         att = 2 * 6.0 * (self.nseq * self.nhead) * s * s * hd
-        return proj + att + 12.0 * T * d * f
+        return proj + att + self.ffn.flops(T, d, f)

@@ -413,3 +413,138 @@ class UnitScaledFFN:
     def flops(T: int, d: int, f: int) -> float:
         """Matmul FLOPs, forward + backward: 2 linear layers x 3 GEMMs x 2 T d f."""
         return 12.0 * T * d * f
+
+
+@dataclass
+class GatedScales:
+    alpha1: float
+    alpha2: float
+    beta_x1: float
+    beta_x2: float
+    beta_w: float
+    alpha_g: float
+    beta_h: float
+    beta_u: float
+    s_in: float = 1.0
+    tau: float = 0.5
+
+    @staticmethod
+    def unit(T: int, d: int, f: int, gate: str = "silu", tau: float = 0.5, constrained: bool = False, dp_world: int = 1) -> "GatedScales":
+        """dp_world: as for FFNScales.unit.  The first layer has d inputs for each of its 2 f outputs, whose gradients all end in an input's."""
+        a1, _, bw = L.us_scales_linear(T * dp_world, d, f)
+        _, bx1, _ = L.us_scales_linear(T, d, 2 * f)
+        a2, bx2, _ = L.us_scales_linear(T, f, d, constrained)
+        if constrained:
+            a1 = bx1 = (a1 * bx1) ** 0.5
+        ag, bh, bu = L.us_scales_gated(gate, constrained)
+        return GatedScales(a1, a2, bx1, bx2, bw, ag, bh, bu, 1.0, tau)
+
+
+class UnitScaledGatedFFN(UnitScaledFFN):
+    """An FFN block whose hidden layer is f(X Wg) * (X Wu), f = gate (gelu, relu, tanh, sigmoid, silu):
+
+        h = alpha1 q(X) q(Wg) ; u = alpha1 q(X) q(Wu) ; A = q(alpha_g f(s_in h) u), h and u kept    us_ffn_gated_fwd
+        R = sqrt(1-tau) X + sqrt(tau) alpha2 A W2q                                                  us_linear_fwd + residual epilogue
+        dH = q(beta_h s_in f'(s_in h) u dA), dU = q(beta_u f(s_in h) dA), dA = beta_x2 Gq W2q^T     us_ffn_gated_bwd
+        dW2 = beta_w A^T Gq ; dW1 = beta_w Xq^T [dH dU] ; dX = sqrt(1-tau) G + sqrt(tau) beta_x1 [dH dU] W1q^T
+
+    W1 = [Wg Wu] is one [d x 2 f] matrix, and dW1 its gradient.  kept: the type in which h and u wait for the backward pass, "bf16",
+    "fp16", or "e4m3": checkpoints of 8 bits, half the bytes, which at unit scale need no factor.  f must be a multiple of 16.  step(), forward() and
+    backward() are used as those of UnitScaledFFN; a step is four launches (three GEMMs of the second layer and the first layer's gradients are one)."""
+
+    def __init__(self, T: int, d: int, f: int, scales: GatedScales | None = None, operand: str = "fp8", gate: str = "silu", kept: str = "bf16",
+                 io_dtype=torch.bfloat16, device="cuda", tau: float = 0.5):
+        if f % 16 or gate not in L.FN_BY_NAME:
+            raise ValueError("a gated block needs a hidden width that is a multiple of 16 and one of the activations " + ", ".join(L.FN_BY_NAME))
+        self.T, self.d, self.f = T, d, f
+        self.sc = scales or GatedScales.unit(T, d, f, gate, tau)
+        self.operand, self.gate = operand, L.FN_BY_NAME[gate]
+        act_dt, grad_dt = _OPERAND[operand]
+        e = lambda r, c, dt: torch.empty((r, c), dtype=dt, device=device)
+        op = lambda r, c, dt: L.operand(r, c, dt, device)
+        self.Xq, self.W1q, self.W2q, self.Gq = op(T, d, act_dt), op(d, 2 * f, act_dt), op(f, d, act_dt), op(T, d, grad_dt)
+        self.HU = op(T, 2 * f, {"bf16": torch.bfloat16, "fp16": torch.float16, "e4m3": torch.float8_e4m3fn}[kept])
+        self.Aq, self.dHUq = op(T, f, act_dt), op(T, 2 * f, grad_dt)
+        self.R, self.dX = e(T, d, io_dtype), e(T, d, io_dtype)
+        self.dW1, self.dW2 = e(d, 2 * f, torch.float32), e(f, d, torch.float32)
+        self.ws = L.new_workspace(device)
+        self._c = L.us_scales_residual(self.sc.tau)
+        # step() of the plain block chooses among its launches by these; here there is one way.  (An encoder layer asks.)
+        self.fused_casts = self.grouped = self.fused_hidden = True
+        self.concurrent = operand == "fp8"
+        self._side, self._plans = None, {}
+
+    def _owned(self):
+        return (self.Xq, self.W1q, self.W2q, self.Gq, self.HU, self.Aq, self.dHUq, self.R, self.dX, self.dW1, self.dW2, self.ws)
+
+    def _state(self):
+        sc = self.sc
+        return (sc.alpha1, sc.alpha2, sc.beta_x1, sc.beta_x2, sc.beta_w, sc.alpha_g, sc.beta_h, sc.beta_u, sc.s_in, self._c, self.operand, self.gate)
+
+    def _halves(self, p, m):
+        return p.mat(m[:, :self.f]), p.mat(m[:, self.f:])
+
+    def _plan_hidden_fwd(self, p):
+        sc = self.sc
+        return L.Call("us_ffn_gated_fwd", self.gate, p.mat(self.Xq), *self._halves(p, self.W1q), sc.alpha1, sc.s_in, sc.alpha_g, *self._halves(p, self.HU), p.mat(self.Aq),
+                      self.ws.data_ptr(), self.ws.numel())
+
+    def _plan_hidden_bwd(self, p):
+        sc = self.sc
+        return L.Call("us_ffn_gated_bwd", self.gate, p.mat(self.Gq), p.mat(self.W2q), sc.beta_x2, sc.s_in, sc.beta_h, sc.beta_u, *self._halves(p, self.HU),
+                      *self._halves(p, self.dHUq), self.ws.data_ptr(), self.ws.numel())
+
+    def plan_gemms(self, p, X, G, dX_copy=None):
+        yield self._plan_hidden_fwd(p)
+        yield self._plan_hidden_bwd(p)
+        w2, w1, x1 = self._plan_backward_entries(G)
+        yield p.group([w2, w1, (L.US_OP_FWD, self.Aq, self.W2q, self.sc.alpha2, self.R, X, self._c), x1], self.ws, {3: dX_copy} if dX_copy is not None else None)
+
+    def plan_forward(self, p, X, cast_x=True):
+        if cast_x:
+            yield self._plan_cast(p, X, self.Xq)
+        yield self._plan_hidden_fwd(p)
+        yield p.linear("us_linear_fwd", self.Aq, self.W2q, self.sc.alpha2, self.R, self.ws, p.residual(X, self._c))
+
+    def plan_backward(self, p, G, cast_g=True):
+        if cast_g:
+            yield self._plan_cast(p, G, self.Gq)
+        yield self._plan_hidden_bwd(p)
+        yield p.group(self._plan_backward_entries(G), self.ws)
+
+    def _plan_backward_entries(self, G):
+        sc = self.sc
+        return [(L.US_OP_BWD_W, self.Aq, self.Gq, sc.beta_w, self.dW2, None, None),
+                (L.US_OP_BWD_W, self.Xq, self.dHUq, sc.beta_w, self.dW1, None, None),
+                (L.US_OP_BWD_X, self.dHUq, self.W1q, sc.beta_x1, self.dX, G, self._c)]
+
+    @property
+    def gemm_launches(self) -> int:
+        """Launches of the GEMMs of a step: forward and backward hidden layer, and the grouped launch (two where it shares contractions)."""
+        return 2 + self._group_launches(forward=True)
+
+    def _group_launches(self, forward: bool) -> int:
+        calls = [L.linear_call(op, a, b, scale, out) for op, a, b, scale, out, _, _ in self._plan_backward_entries(None)]
+        return L.us_linear_group_launches(calls + ([L.linear_call(L.US_OP_FWD, self.Aq, self.W2q, self.sc.alpha2, self.R)] if forward else []))
+
+    @property
+    def launches_per_step(self) -> int:
+        return 1 + self.gemm_launches
+
+    def backward(self, G, stream=None, cast_g: bool = True):
+        self._run("backward" if cast_g else "backward_from_cast", stream, G=G)
+        return self.dX, self.dW1, self.dW2
+
+    def step(self, X, W1, W2, G, stream=None):
+        self._run("step", stream, X=X, W1=W1, W2=W2, G=G)
+        return self.dX, self.dW1, self.dW2
+
+    def stages(self, *args, **kwargs):
+        raise NotImplementedError("a gated block has no unfused launches")
+
+    step_launches = step_from_casts = group_calls = backward_calls = stages
+
+    @staticmethod
+    def flops(T: int, d: int, f: int) -> float:
+        """Matmul FLOPs, forward + backward: three matrices x 3 GEMMs x 2 T d f."""
+        return 18.0 * T * d * f

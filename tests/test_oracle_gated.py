@@ -56,3 +56,26 @@ def test_host_helpers():
             L.us_scales_gated(bad)
         with pytest.raises(L.UnitScaleError):
             L.us_scales_activation(bad)
+
+
+@pytest.mark.parametrize("gate", ["silu", "gelu"])
+def test_block_gradients_are_finite_differences_times_constants(gate):
+    """Weight gradients of the block without roundings: the true gradients of sum(G R) times the ratio of the factors."""
+    T, d, f = 5, 4, 6
+    X, W1, W2, G = (RNG.standard_normal(s) for s in ((T, d), (d, 2 * f), (f, d), (T, d)))
+    run = lambda W1_, W2_: O.gated_ffn_block(X, W1_, W2_, G, gate, operand="f64", kept="f64", io_dtype="f64")
+    r, loss = run(W1, W2), lambda W1_, W2_: (G * run(W1_, W2_).R).sum()
+    a, bh, bu = S.gated_scales(*FNS[gate])
+    c, e = 0.5 ** 0.5, 1e-5
+    up = (T ** -0.5 * d ** -0.5) / (d ** -0.5 * a * c * f ** -0.5)              # of dW1, but for its beta_h or beta_u
+    for i in range(d):
+        for j in range(2 * f):
+            E = np.zeros_like(W1)
+            E[i, j] = e
+            true = (loss(W1 + E, W2) - loss(W1 - E, W2)) / (2 * e)
+            assert abs(true * up * (bh if j < f else bu) - r.dW1[i, j]) < 1e-6
+    for i in range(f):
+        for j in range(d):
+            E = np.zeros_like(W2)
+            E[i, j] = e
+            assert abs((loss(W1, W2 + E) - loss(W1, W2 - E)) / (2 * e) * T ** -0.5 / (c * f ** -0.5) - r.dW2[i, j]) < 1e-6
