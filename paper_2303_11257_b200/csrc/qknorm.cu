@@ -267,8 +267,8 @@ struct Place {
   __device__ __forceinline__ void advance(bool carry) { if (STEPPED) { base += row_bytes; if (carry) base += carried; } }
 };
 
-template <bool BWD, int DT, int STEPS, class G>
-__device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lane& l, uint32_t ring, int zero, G work) {
+template <bool BWD, int DT, int STEPS, class B, class G>
+__device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lane& l, uint32_t ring, int zero, B begin, G work) {
   constexpr int kC = kChunkBytes<DT>, kStep = (BWD ? 4 : 2) * kC, kEs = DT == US_F32 ? 4 : 2;
   const int lane = threadIdx.x & 31, j = lane & (p.group - 1), per = 32 / p.group, slot = slot_bytes<BWD, DT, STEPS>(p.group);
   const uint32_t rows = (uint32_t)p.rows;
@@ -314,6 +314,7 @@ __device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lan
     copies_commit();
   };
   for (int s = 0; s < kStages - 1; ++s) issue(s);
+  begin();                                                      // what else has to be fetched, while those are on their way
   const int y_es = dtype_size(q.y_dt);
   const int y_step = per * p.width * y_es, y_b = (l.b - l.a) * y_es;
   Place<!BWD> y(static_cast<char*>(q.y) + first * y_es, now, q, q.y_ld * y_es, y_step * STEPS);
@@ -339,9 +340,8 @@ __global__ void __launch_bounds__(kThreads, kFwdCtasPerSm) qk_fwd_kernel(const _
   const int lane = threadIdx.x & 31, per = 32 / p.group;
   const Lane l = lane_of<NEIGHBOURS, FULL>(p, lane & (p.group - 1));
   f32x2 wa[4], wb[4];
-  load_weight(q, l, wa, wb);
   const uint32_t ring = ptx::smem_addr(smem) + (threadIdx.x >> 5) * kStages * slot_bytes<false, DT, STEPS>(p.group);
-  walk<false, DT, STEPS>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, char* y, int y_step, int y_b) {
+  walk<false, DT, STEPS>(p, q, l, ring, zero, [&] { load_weight(q, l, wa, wb); }, [&](int heads, uint32_t data, uint32_t angles, char* y, int y_step, int y_b) {
     Turn<NEIGHBOURS> turn;
     if (FULL || p.table) read_turn<NEIGHBOURS, false>(angles, l, turn);
 #pragma unroll
@@ -371,10 +371,9 @@ __global__ void __launch_bounds__(kThreads, kBwdCtasPerSm) qk_bwd_kernel(const _
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 32 / p.group;
   const Lane l = lane_of<NEIGHBOURS, FULL>(p, lane & (p.group - 1));
   f32x2 wa[4], wb[4], da2[4] = {}, db2[4] = {};
-  load_weight(q, l, wa, wb);
   const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * slot_bytes<true, DT, STEPS>(p.group);
   with_output(q.y_dt, [&](auto y_dt) {
-  walk<true, DT, STEPS>(p, q, l, ring, zero, [&](int heads, uint32_t data, uint32_t angles, char* y, int y_step, int y_b) {
+  walk<true, DT, STEPS>(p, q, l, ring, zero, [&] { load_weight(q, l, wa, wb); }, [&](int heads, uint32_t data, uint32_t angles, char* y, int y_step, int y_b) {
     Turn<NEIGHBOURS> turn;
     if (FULL || p.table) read_turn<NEIGHBOURS, true>(angles, l, turn);
 #pragma unroll

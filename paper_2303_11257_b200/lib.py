@@ -853,8 +853,9 @@ def rotary_table(positions: int, rotated: int, base=10000.0, scale=1.0, device="
 def us_qk_norm_fwd(X, w, Y, head_width, eps, table=None, positions=None, start=0, period=0, neighbours=False, stream=None):
     """X, w, Y: lists of matrices [rows x heads * head_width] (queries and keys), norm weights [head_width] (or None) and outputs;
     positions: int32 CUDA tensor [rows], or None for start + row % period."""
-    _check_positions(X, positions)
-    _check("us_qk_norm_fwd", _entry("us_qk_norm_fwd")(len(X), _of(X, X), _of(w, X), _of(Y, X), head_width, eps, table, positions, start, period, int(neighbours), _stream(stream)))
+    n = len(X)
+    _check_lists(n, X, positions, w, Y)
+    _check("us_qk_norm_fwd", _entry("us_qk_norm_fwd")(n, X, w, Y, head_width, eps, table, positions, start, period, neighbours, _stream(stream)))
     return Y
 
 
@@ -865,21 +866,18 @@ def us_qk_norm_bwd_workspace_bytes(head_width: int) -> int:
 def us_qk_norm_bwd(X, w, G, dX, dw, head_width, eps, ws, beta_x=1.0, beta_w=None, table=None, positions=None, start=0, period=0, neighbours=False, stream=None):
     """G, dX: lists of gradients of the outputs and of X; dw: list of weight gradients, or None; beta_w: list of their factors, or None
     (ones); ws: a uint8 CUDA tensor of at least us_qk_norm_bwd_workspace_bytes(head_width) bytes, or None without dw."""
-    _check_positions(X, positions)
+    n = len(X)
+    _check_lists(n, X, positions, w, G, dX, dw, beta_w)
     _check("us_qk_norm_bwd", _entry("us_qk_norm_bwd")(
-        len(X), _of(X, X), _of(w, X), _of(G, X), _of(dX, X), _of(dw, X), _of(beta_w, X), head_width, eps, beta_x, table, positions, start, period, int(neighbours),
-        ws, ws if ws is not None else 0, _stream(stream)))
+        n, X, w, G, dX, dw, beta_w, head_width, eps, beta_x, table, positions, start, period, neighbours, ws, ws if ws is not None else 0, _stream(stream)))
     return dX, dw
 
 
-def _of(parts, X):
-    if parts is not None and len(parts) != len(X):
-        raise ValueError("one entry per matrix is wanted")
-    return parts
-
-
-def _check_positions(X, positions):
-    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (X[0].shape[0],))
+def _check_lists(n, X, positions, *lists):
+    for v in lists:
+        if v is not None and len(v) != n:
+            raise ValueError("one entry per matrix is wanted")
+    assert positions is None or (positions.dtype is torch.int32 and positions.dim() == 1 and positions.is_contiguous() and positions.numel() == X[0].size(0))
 
 
 def us_scales_linear(b: int, m: int, n: int, constrained: bool = False):
