@@ -333,7 +333,7 @@ typedef enum { US_FN_GELU = 0, US_FN_RELU = 1, US_FN_TANH = 2, US_FN_SIGMOID = 3
  * gradient: the rest of the backward pass is then us_linear_bwd_x and us_linear_bwd_w on these.
  *
  * X, Wg, Wu / G, W2: 8-bit (any mix of US_E4M3 / US_E5M2, but Wg and Wu alike), all BF16 or all F16.  A / dH, dU (alike): 8-bit for
- * 8-bit operands (saturating), the operands' format for 16-bit ones.  H, U (alike): BF16, F16, or US_E4M3 -- activation checkpoints in 8 bits, which
+ * 8-bit operands (saturating), the operands' format for 16-bit ones (other combinations, and sizes beyond 2^31 - 256: US_ERR_UNSUPPORTED).  H, U (alike): BF16, F16, or US_E4M3 -- activation checkpoints in 8 bits, which
  * at unit scale need no factor (saturating at 448).  Any dimension >= 1; alignment, workspace, status word and errors as for us_linear_fwd.
  * Outputs must not overlap one another or an input, except that dH may be H and dU may be U where their formats have one width (the same pointer and pitch).
  */
@@ -586,7 +586,8 @@ us_status us_layer_norm_bwd_cast(const us_mat* X, const us_mat* w, const us_mat*
  * count (1..4) matrices with head_width columns a head -- queries and keys, of which there may be fewer heads -- are worked on by one
  * launch; X, w, Y, G, dX, dw, beta_w: host arrays of count elements.  X, G: F32, BF16 or F16, any ld >= cols; Y, dX: any us_dtype; w
  * (1 x head_width; ptr NULL, or the whole array NULL: ones): F32, BF16 or F16.  dw (the same shape and types; ptr NULL or NULL: not wanted) needs a w;
- * beta_w NULL: ones.  Y may be X and dX may be X or G, with the same pitch and type.  1 <= head_width <= 1024 (US_ERR_UNSUPPORTED beyond).
+ * beta_w NULL: ones.  Y may be X and dX may be X or G, with the same pitch and type.  1 <= head_width <= 1024 (US_ERR_UNSUPPORTED beyond), fewer
+ * than 2^31 rows.
  * Pointers need the natural alignment of their elements; matrices of one input type with rows on 16-byte boundaries, heads of
  * a multiple of 8 features up to 512 of which a multiple of 16 (neighbours: 8) is turned, and a table with rows on 16-byte boundaries take the fast kernels.
  * Arithmetic in float32.  us_qk_norm_bwd: two launches where there is a dw, which then has a device workspace of us_qk_norm_bwd_workspace_bytes(head_width) bytes, 16-byte

@@ -737,12 +737,14 @@ us_status pick_gated(const GatedMats& m, GatedParams& p, cudaStream_t st) {
 }
 
 // The checks that both directions share: operands of one width (f8: 8-bit), workspace.
+constexpr int64_t kMostSize = 0x7fffff00;        // rows, columns and contraction: the coordinates of a tile that ends behind them are 32-bit numbers
 us_status check_common(const us_mat* const* in, int n, const us_mat* const* out, int outs, const us_mat* H, const us_mat* U, const void* ws, size_t ws_bytes, bool& f8) {
   if (!ws || ws_bytes < us_workspace_bytes()) return US_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(ws) % 16) return US_ERR_ALIGNMENT;
   for (int i = 0; i < n; ++i) if (!aligned(in[i], 16)) return US_ERR_ALIGNMENT;
   for (int i = 0; i < outs; ++i) if (!aligned(out[i], 16)) return US_ERR_ALIGNMENT;
   if (given(H) && (!aligned(H, 16) || !aligned(U, 16))) return US_ERR_ALIGNMENT;
+  for (int i = 0; i < n; ++i) if (in[i]->rows > kMostSize || in[i]->cols > kMostSize) return US_ERR_UNSUPPORTED;
   f8 = is_fp8(in[0]->dtype);
   const bool h16 = in[0]->dtype == US_BF16 || in[0]->dtype == US_F16;
   if (!f8 && !h16) return US_ERR_UNSUPPORTED;

@@ -51,6 +51,8 @@ def test_forward():
     for bad in (dict(dt=F32), dict(A=M(BF, 300, 208)), dict(X=M(BF, 300, 64)), dict(dt=BF, A=M(F16, 300, 208)), dict(dt=BF, A=M(E4, 300, 208)), dict(dt=BF, X=M(F16, 300, 64)),
                 dict(H=M(F32, 300, 208), U=M(F32, 300, 208)), dict(H=M(E5, 300, 208), U=M(E5, 300, 208))):
         assert fwd(**bad) == 2, bad
+    huge = (1 << 31) - 1
+    assert fwd(X=M(E4, huge, 64), A=M(E4, huge, 208)) == 2 and fwd(X=M(E4, 300, huge, 1 << 31), Wg=M(E4, huge, 208), Wu=M(E4, huge, 208)) == 2
     for bad in (dict(X=M(E4, 300, 64, 72)), dict(Wu=M(E4, 64, 208, addr=0x10008)), dict(A=M(E4, 300, 208, 216)), dict(H=K, U=M(BF, 300, 208, 212)), dict(ws=0x20008)):
         assert fwd(**bad) == 3, bad
     assert fwd(ws=None) == 4 and fwd(size=L.us_workspace_bytes() - 1) == 4

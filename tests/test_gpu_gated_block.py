@@ -105,3 +105,24 @@ def test_layer_against_the_oracle(attention, fused, norm, gate, rotary):
     graph.replay()
     layer.check()
     assert all(torch.equal(a, b) for a, b in zip(want, (layer.dX, layer.dWqkv, layer.ffn.dW1, *layer.dqk)))
+
+
+@pytest.mark.parametrize("T,d,f,operand,kept", [(256, 128, 512, "fp8", "e4m3"), (16000, 128, 400, "fp8", "bf16"), (1000, 528, 2096, "bf16", "e4m3")])
+def test_launches_of_a_gated_step(T, d, f, operand, kept):
+    from paper_2303_11257_b200 import ffn
+    from tests.test_gpu_launch_counts import _kernels
+    block = ffn.UnitScaledGatedFFN(T, d, f, operand=operand, kept=kept)
+    x = [torch.zeros(s, device="cuda") for s in ((T, d), (d, 2 * f), (f, d), (T, d))]
+    assert _kernels(lambda: block.step(*x)) == block.launches_per_step
+
+
+@pytest.mark.parametrize("attention,norm,fused,gate", [("bf16", None, True, "silu"), ("fp8", "post", True, "silu"), ("fp16", None, False, None), ("fp8", None, False, "gelu")])
+def test_launches_of_a_layer_step(attention, norm, fused, gate):
+    from paper_2303_11257_b200 import encoder
+    from tests.test_gpu_launch_counts import _kernels
+    nseq, slen, nhead = 4, 256, 2
+    T, d, f = nseq * slen, 64 * nhead, 256 * nhead
+    layer = encoder.UnitScaledEncoderLayer(nseq, slen, d, nhead, f, attention=attention, fused_attention=fused, norm=norm, gate=gate, qk_norm=True, rotary=10000.0)
+    t = [torch.zeros(s, device="cuda") for s in ((T, d), (d, 3 * d), (d, d), (d, 2 * f if gate else f), (f, d), (T, d))]
+    ln, qk = ([torch.ones(d, device="cuda") for _ in range(4)] if norm else None), [torch.ones(64, device="cuda") for _ in range(2)]
+    assert _kernels(lambda: layer.step(*t, ln=ln, qk=qk)) == layer.kernel_launches
