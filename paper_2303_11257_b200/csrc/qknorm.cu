@@ -313,6 +313,13 @@ __device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lan
     }
     copies_commit();
   };
+  if (!(l.has_a && l.has_b)) {                                  // chunks that a lane has not are zeros, which are never copied over
+    for (uint32_t at = ring + lane * 16u; at < ring + kStages * slot; at += slot) {
+#pragma unroll
+      for (int c = 0; c < STEPS * kStep / 512; ++c)
+        if (!(c / (kC / 512) & 1 ? l.has_b : l.has_a)) ptx::sts128(at + 512u * c, make_uint4(0u, 0u, 0u, 0u));
+    }
+  }
   for (int s = 0; s < kStages - 1; ++s) issue(s);
   begin();                                                      // what else has to be fetched, while those are on their way
   const int y_es = dtype_size(q.y_dt);
@@ -347,9 +354,9 @@ __global__ void __launch_bounds__(kThreads, kFwdCtasPerSm) qk_fwd_kernel(const _
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
       const uint32_t from = data + k * 2 * kChunkBytes<DT>;
-      f32x2 a[4] = {}, b[4] = {}, ss = 0ull;
-      if (l.has_a) widen<DT>(from, a);
-      if (l.has_b) widen<DT>(from + kChunkBytes<DT>, b);
+      f32x2 a[4], b[4], ss = 0ull;
+      widen<DT>(from, a);
+      widen<DT>(from + kChunkBytes<DT>, b);
 #pragma unroll
       for (int i = 0; i < 4; ++i) ss = fma2(a[i], a[i], fma2(b[i], b[i], ss));
       const f32x2 r = splat2(rsqrt_approx(fmaf(group_sum(halves_sum(ss), p.group), p.inv_width, p.eps)));
@@ -379,9 +386,11 @@ __global__ void __launch_bounds__(kThreads, kBwdCtasPerSm) qk_bwd_kernel(const _
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) {
       const uint32_t from = data + k * 4 * kChunkBytes<DT>;
-      f32x2 a[4] = {}, b[4] = {}, na[4] = {}, nb[4] = {}, ss2 = 0ull, dot2 = 0ull;
-      if (l.has_a) { widen<DT>(from, a); widen<DT>(from + 2 * kChunkBytes<DT>, na); }
-      if (l.has_b) { widen<DT>(from + kChunkBytes<DT>, b); widen<DT>(from + 3 * kChunkBytes<DT>, nb); }
+      f32x2 a[4], b[4], na[4], nb[4], ss2 = 0ull, dot2 = 0ull;
+      widen<DT>(from, a);
+      widen<DT>(from + kChunkBytes<DT>, b);
+      widen<DT>(from + 2 * kChunkBytes<DT>, na);
+      widen<DT>(from + 3 * kChunkBytes<DT>, nb);
       if (FULL || p.table) rotate<NEIGHBOURS>(na, nb, turn, l);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
