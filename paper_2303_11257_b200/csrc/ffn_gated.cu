@@ -10,6 +10,10 @@
 // Wu's.)  Neither projection is written unless the caller wants the copies the backward pass reads; those are 16-bit or, at unit scale, E4M3
 // without a factor.  Backward, a tile is HC columns of dA, from which the epilogue makes both gradients with the copies it has fetched.
 //
+// Bound: forward the tensor pipe and, over seconds, power: 8192 x 1024 x 4096 BF16 with copies 125 us (1.10 PFLOP/s; 98 in a burst), 16384 x 2048 x 8192 FP8 with E4M3
+// copies 440 us (2.5 PFLOP/s).  Backward, BF16 88 us (268 MB of copies and gradients beside 69 GFLOP: the SM's memory path), FP8 from E4M3 copies 54 us (the epilogue's
+// instructions).  One token of 1024 x 4096 in BF16 5.4 us.
+//
 // Every wait is bounded as in the other GEMM kernels.
 #include <cuda.h>
 
@@ -675,6 +679,7 @@ template <bool BWD, int ES, int HC, int CG, bool BOXED = false>
 us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t st) {
   const us_mat *A = m.a, *B0 = m.b0, *B1 = m.b1;
   using S = GatedShape<BWD, ES, HC, CG, BOXED>;
+  if (CG == 2 && p.starved == 2) return US_ERR_INVALID_ARG;        // test hook: of a pair only the odd CTA may starve alone (nobody would wait for its copies)
   p.tiles_m = (p.M + kBM * CG - 1) / (kBM * CG);
   p.tiles_n = (p.N + HC - 1) / HC;
   if ((int64_t)p.tiles_m * p.tiles_n >= (1ll << 30)) return US_ERR_UNSUPPORTED;
@@ -802,7 +807,6 @@ us_status gated_bwd(int fn, const us_mat* G, const us_mat* W2, float beta_x, flo
   return f8 ? pick_gated<true, 1>(m, p, st) : pick_gated<true, 2>(m, p, st);
 }
 
-// Test hook: of a CTA pair only the odd one may starve alone (the even one waits for its copies; nobody would wait for those of the odd one).
 bool bad_hook(uint32_t wait_limit, int cta, int tiles) { return wait_limit == 0 || wait_limit > (1u << 16) || cta < -1 || cta > 1 || tiles < 0 || tiles > 1024; }
 
 }  // namespace

@@ -4,12 +4,13 @@
 //   forward    r = 1 / sqrt(mean x^2 + eps),  n = w x r,  y = R n          R: each pair (a, b) of the rotated features -> (a c - b s, b c + a s)
 //   backward   n' = R^T g,  u = w n',  dx = beta_x r (u - x r mean(u x r)),  dw = beta_w sum n' x r
 //
-// Bound by HBM: every element is read once and written once.  A head is held by a group of G lanes (a power of two), each with two chunks of
-// eight features that hold whole pairs -- features i .. i + 7 and their partners half a rotation further, or sixteen neighbours -- so that the
-// rotation needs no exchange and one group sum (forward) or two (backward) are all that lanes tell one another.  A warp takes 32 / G heads at
-// once and kIter such steps of one token, whose cosines and sines it holds in registers over all of them; the norm's weight it holds for the
-// whole launch, since a CTA works for one part (queries or keys) only.  Weight gradients are summed in the registers of the lane that has
-// the feature, then over groups, warps and, in a second launch, CTAs, in a fixed order without atomics.
+// Every element is read once and written once; the kernels are bound by the instructions they issue before they are by HBM (11 to 14 a value).  8192 tokens of 16 + 16 heads of 64
+// in BF16: forward 13.7 us (4.9 TB/s), backward 23.0 (4.4 TB/s); 16384 tokens of 32 + 8 heads of 128 into E4M3 58 us (4.5 TB/s).
+// A head is held by a group of G lanes (a power of two), each with two chunks of eight features that hold whole pairs -- features i .. i + 7 and their partners half a
+// rotation further, or sixteen neighbours -- so that the rotation needs no exchange and one group sum (forward) or two (backward) are all that lanes tell one another.  A warp's
+// unit is some steps of 32 / G heads of one row, whose cosines and sines it holds in registers over all of them; the norm's weight it holds for the whole launch,
+// since a CTA works for one part (queries or keys) only.  Weight gradients are summed in the registers of the lane that has the feature, then over groups, warps and, in a second
+// launch, CTAs, in a fixed order without atomics.
 // Rows that are not on 16-byte boundaries, and widths that are no multiple of eight, take the general kernels: a warp a head, through shared memory.
 #include <cuda.h>
 

@@ -241,6 +241,19 @@ def test_starved_launches_time_out_and_the_next_call_is_correct(shape):
             assert all(torch.equal(a, b) for a, b in zip(run(), want))
 
 
+def test_the_even_cta_of_a_pair_does_not_starve_alone():
+    """Nobody would wait for the copies of the odd one: the hook refuses it where tiles are a pair's."""
+    L, _ = _lib()
+    b, m, f, n = SHAPES["pair"]
+    X, Wg, Wu, A, ws = U.empty(b, 272, "e4m3"), U.empty(m, f, "e4m3"), U.empty(m, f, "e4m3"), U.empty(b, f, "e4m3"), L.new_workspace()
+    with pytest.raises(L.UnitScaleError) as e:
+        L.us_test_ffn_gated_fwd_starved(X, Wg, Wu, None, None, A, ws, 2000, 0, 0)
+    assert e.value.status == 1
+    with pytest.raises(L.UnitScaleError) as e:
+        L.us_test_ffn_gated_bwd_starved(U.empty(b, n, "e4m3"), U.empty(f, n, "e4m3"), A, A, U.empty(b, f, "e4m3"), U.empty(b, f, "e4m3"), ws, 2000, 0, 0)
+    assert e.value.status == 1 and L.us_workspace_status(ws) == 0
+
+
 def test_silu_as_an_elementwise_op():
     """us_activation_fwd / bwd: float32 results within 4e-7 of the definition, relative to 1 + |z|."""
     L, _ = _lib()
