@@ -27,13 +27,16 @@ namespace us {
 namespace {
 
 // Epilogue warps.  Of a CTA pair's tiles sixteen a CTA, whose arithmetic is the longest part of an FP8 tile; backward with 16-bit operands, where the MMAs
-// take twice as long, eight with two slots each.  (8192 x 1024 x 4096 backward, us, sixteen with one slot / eight with two: FP8 54.0 / 57.5, BF16 90.9 / 88.3.)
+// take twice as long, eight.  (8192 x 1024 x 4096 backward, us, sixteen / eight: FP8 54.0 / 57.5, BF16 90.9 / 88.3.)
 __host__ __device__ constexpr bool gated_few(bool bwd, int es, int cg) { return cg == 1 || (bwd && es == 2); }
 __host__ __device__ constexpr int gated_ew(bool bwd, int es, int cg) { return gated_few(bwd, es, cg) ? 8 : 16; }
 constexpr int kRoom = 229376;                 // shared memory for stages and the epilogue's boxes
 constexpr int kMostStages = 16;
-// Backward, an epilogue warp has one or two slots for the copies of h and u that arrive and the dH and dU that leave, in boxes of 32 rows x up to 64 bytes.
-constexpr int kSlotBytes = 6144;
+// Backward, an epilogue warp has slots for the copies of h and u that arrive and the dH and dU that leave, in boxes of 32 rows x 32 columns.  Where copies and gradients have one
+// width a gradient leaves from the box of its copy, and there are three slots: a store has a unit's time to read one before it is filled again.  Elsewhere a slot has
+// boxes for both (6144 bytes), in as many slots as fit.
+constexpr int kMostSlots = 3;
+__host__ __device__ constexpr int epi_room(int ew) { return ew == 16 ? 6144 : 12288; }      // bytes of a warp
 
 struct GatedParams {
   int M, N, K;                                // results are [M x N]; length of the contraction
@@ -46,7 +49,7 @@ struct GatedParams {
   int fn;
   int kept_dt, out_dt;                        // types of the copies of h and u, and of the results
   uint8_t *h, *u, *o0; long long h_ld, u_ld, o0_ld; int kept_sectors, out_sectors;     // forward: the copies (nullptr: not wanted) and A
-  int unit_cols;                              // backward: columns of a box (32, or 64 of 8 bits)
+  int slots;                                  // backward: slots of an epilogue warp
   unsigned int* status;
   uint32_t wait_limit;
   uint32_t a_bytes; int stages;               // bytes of A in a stage (single CTAs: the rows that exist), and the stages that fit
@@ -56,11 +59,11 @@ struct GatedParams {
 template <bool BWD, int ES, int HC, int CG, bool BOXED = false>
 struct GatedShape {
   static constexpr int kN = BWD ? HC : 2 * HC;             // columns of an accumulator
-  static constexpr int kEW = gated_ew(BWD, ES, CG), kSlots = gated_few(BWD, ES, CG) ? 2 : 1;   // warps and slots of the epilogue
+  static constexpr int kEW = gated_ew(BWD, ES, CG);         // epilogue warps
   static constexpr int kRowsB = kN / CG;                   // rows of B a CTA fetches
   static constexpr int kBBytes = kRowsB * kStageKBytes;
   static constexpr int kStageBytes = kBM * kStageKBytes + kBBytes;
-  static constexpr int kEpiBytes = BWD ? kEW * kSlots * kSlotBytes : BOXED ? kEW * 3 * 2048 : 0;
+  static constexpr int kEpiBytes = BWD ? kEW * epi_room(kEW) : BOXED ? kEW * 3 * 2048 : 0;
   static constexpr int kStages = (kRoom - kEpiBytes) / kStageBytes;
   static constexpr int kBarrierBytes = 1024;
   static constexpr int kTotal = kRoom + kBarrierBytes + 1024;
@@ -262,7 +265,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
              const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_dh,
              const __grid_constant__ CUtensorMap tm_du, const GatedParams p) {
   using S = GatedShape<BWD, ES, HC, CG, BOXED>;
-  constexpr int kEW = S::kEW, kSlots = S::kSlots, kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
+  constexpr int kEW = S::kEW, kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
   constexpr uint32_t kTmemCols = 2 * kN;
   const uint32_t a_bytes = CG == 2 ? (uint32_t)(kBM * kStageKBytes) : p.a_bytes, stage_bytes = a_bytes + S::kBBytes;
   const int stages = CG == 2 ? S::kStages : p.stages;
@@ -277,8 +280,8 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
   auto acc_full_bar = [&](int a) { return bars + 8u * (2 * kMostStages + a); };
   auto acc_empty_bar = [&](int a) { return bars + 8u * (2 * kMostStages + 2 + a); };
   const uint32_t drained_bar = bars + 8u * (2 * kMostStages + 4);
-  auto in_bar = [&](int w, int s) { return bars + 8u * (2 * kMostStages + 5 + kSlots * w + s); };
-  constexpr int kBars = 2 * kMostStages + 5 + kSlots * kEW;
+  auto in_bar = [&](int w, int s) { return bars + 8u * (2 * kMostStages + 5 + kMostSlots * w + s); };
+  constexpr int kBars = 2 * kMostStages + 5 + kMostSlots * kEW;
   static_assert(8 * kBars + 8 <= S::kBarrierBytes, "barrier area too small");
   uint8_t* tail = smem_gen + kRoom + 8 * kBars;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
@@ -300,7 +303,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
     for (int s = 0; s < stages; ++s) { ptx::mbar_init(full_bar(s), 1); ptx::mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { ptx::mbar_init(acc_full_bar(a), 1); ptx::mbar_init(acc_empty_bar(a), CG * kEW); }
     ptx::mbar_init(drained_bar, 1);
-    if (BWD) for (int w = 0; w < kSlots * kEW; ++w) ptx::mbar_init(in_bar(0, w), 1);
+    if (BWD) for (int w = 0; w < kMostSlots * kEW; ++w) ptx::mbar_init(in_bar(0, w), 1);
     *abort_flag = 0;
     ptx::mbar_init_fence();
     ptx::prefetch_tensormap(&tm_a);
@@ -538,18 +541,17 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
         }
       }
     } else {
-      // Units of unit_cols columns, whose copies arrive in a pair of boxes ahead of the accumulator and whose gradients leave from it.  A lane's row of a
-      // box is read and written by that lane, 16-byte chunk c at c ^ the pattern of its row (64-byte rows swizzled, 32-byte ones not).
-      const int ew = warp - 2, uc = p.unit_cols;
-      const uint32_t boxes = smem_base + (uint32_t)(kRoom - S::kEpiBytes + ew * kSlots * kSlotBytes);
-      const int in_row = uc * kept_es, out_row = uc * out_es;
-      // where copies and gradients have one width a gradient takes the place of its copy
-      const uint32_t in_box = 32u * in_row, out_box = 32u * out_row, box_out = kept_es == out_es ? 0u : 2u * in_box;
+      // Units of 32 columns, whose copies arrive in a slot's boxes ahead of the accumulator.  A lane's row of a box is read and written by that lane, 16-byte chunk c at c ^ the
+      // pattern of its row (64-byte rows swizzled, 32-byte ones not).
+      const int ew = warp - 2;
+      const bool in_place = kept_es == out_es;
+      const uint32_t boxes = smem_base + (uint32_t)(kRoom - S::kEpiBytes + ew * epi_room(kEW)), in_row = 32u * kept_es, out_row = 32u * out_es;
+      const uint32_t in_box = 32u * in_row, out_box = 32u * out_row, box_out = in_place ? 0u : 2u * in_box, slot_bytes = box_out + 2u * out_box;
       const uint32_t in_sw = in_row == 64 ? (uint32_t)((lane >> 1) & 3) : 0u, out_sw = out_row == 64 ? (uint32_t)((lane >> 1) & 3) : 0u;
-      uint32_t issued = 0, used = 0;
-      auto slot_of = [&](uint32_t k) { return kSlots == 1 ? 0u : k & 1u; };
-      auto phase_of = [&](uint32_t k) { return kSlots == 1 ? k & 1u : (k >> 1) & 1u; };
+      int pending = 0, fetch_slot = 0, slot = 0;                 // units whose copies have been asked for, the slot of the next one, and that of the unit that is worked on next
+      uint32_t slot_phase = 0;
       int next_tile = unit, next_col = 0;                        // the unit whose copies are fetched next: columns from the warp's first on
+      // In place: called once a unit has been stored, it fills the slot of the unit before, whose store is the last but one.
       auto fetch = [&]() {
         int row = 0, col = 0;
         for (; next_tile < num_tiles; next_tile += num_units, next_col = 0) {
@@ -558,16 +560,21 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
         }
         if (next_tile >= num_tiles) return;
         if (ptx::elect_one()) {
-          ptx::bulk_wait_group_read<kSlots - 1>();               // the stores that left from these boxes have read them
-          const uint32_t bar = in_bar(ew, slot_of(issued)), dst = boxes + slot_of(issued) * kSlotBytes;
+          if (in_place) ptx::bulk_wait_group_read<1>();
+          const uint32_t bar = in_bar(ew, fetch_slot), to = boxes + fetch_slot * slot_bytes;
           ptx::mbar_expect_tx(bar, 2 * in_box);
-          ptx::tma_load_2d(dst, &tm_h, bar, col + next_col, row - lane);
-          ptx::tma_load_2d(dst + in_box, &tm_u, bar, col + next_col, row - lane);
+          ptx::tma_load_2d(to, &tm_h, bar, col + next_col, row - lane);
+          ptx::tma_load_2d(to + in_box, &tm_u, bar, col + next_col, row - lane);
         }
-        ++issued;
-        next_col += uc;
+        if (++fetch_slot == p.slots) fetch_slot = 0;
+        ++pending;
+        next_col += 32;
       };
-      for (int k = 0; k < kSlots; ++k) fetch();
+      auto next_slot = [&]() {
+        if (++slot == p.slots) { slot = 0; slot_phase ^= 1u; }
+        --pending;
+      };
+      for (int k = in_place ? 1 : 0; k < p.slots; ++k) fetch();
       for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
         int row, col0;
         place(tile, row, col0);
@@ -581,15 +588,14 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
         if (end <= 0) release_acc(acc, tile);
 #pragma unroll 1
         for (int at = 0; at < end; at += 32) {
-          const int off = at & (uc - 1);
-          const bool last_of_unit = off + 32 == uc || at + 32 >= end;
-          if (off == 0) {
-            ok = wait_bounded(in_bar(ew, slot_of(used)), phase_of(used), abort_flag, p.status, p.wait_limit);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
+          ok = wait_bounded(in_bar(ew, slot), slot_phase, abort_flag, p.status, p.wait_limit);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (!in_place) {                                       // the boxes that gradients leave from have been read by the stores before
+            if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
+            __syncwarp();
           }
-          const uint32_t slot = boxes + slot_of(used) * kSlotBytes, src = slot + (uint32_t)(lane * in_row), dst = slot + box_out + (uint32_t)(lane * out_row);
-          const uint32_t in_chunk = (uint32_t)(off * kept_es) >> 4, out_chunk = (uint32_t)(off * out_es) >> 4;
+          const uint32_t box = boxes + slot * slot_bytes, src = box + lane * in_row, dst = box + box_out + lane * out_row;
           with_formats<ES>(p.kept_dt, p.out_dt, [&](auto kept, auto out) {
             with_gate(p.fn, [&](auto fn) {
               constexpr int kWords = decltype(kept)::value == US_E4M3 ? 4 : 8;         // of sixteen kept values
@@ -598,7 +604,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
                 ptx::tmem_ld_32x32_issue(t_row + at + 16 * decltype(half)::value, r0);
 #pragma unroll
                 for (int k = 0; k < kWords / 4; ++k) {
-                  const uint32_t chunk = ((in_chunk + decltype(half)::value * (kWords / 4) + k) ^ in_sw) << 4;
+                  const uint32_t chunk = ((decltype(half)::value * (kWords / 4) + k) ^ in_sw) << 4;
                   const uint4 vh = ptx::lds128(src + chunk), vu = ptx::lds128(src + in_box + chunk);
                   rh[4 * k] = vh.x; rh[4 * k + 1] = vh.y; rh[4 * k + 2] = vh.z; rh[4 * k + 3] = vh.w;
                   ru[4 * k] = vu.x; ru[4 * k + 1] = vu.y; ru[4 * k + 2] = vu.z; ru[4 * k + 3] = vu.w;
@@ -615,29 +621,27 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
                 pack16<decltype(out)::value>(yu, wu);
 #pragma unroll
                 for (int k = 0; k < ES; ++k) {          // one chunk of 8-bit results, two of 16-bit ones
-                  const uint32_t chunk = ((out_chunk + decltype(half)::value * ES + k) ^ out_sw) << 4;
+                  const uint32_t chunk = ((decltype(half)::value * ES + k) ^ out_sw) << 4;
                   ptx::sts128(dst + chunk, make_uint4(wh[4 * k], wh[4 * k + 1], wh[4 * k + 2], wh[4 * k + 3]));
                   ptx::sts128(dst + out_box + chunk, make_uint4(wu[4 * k], wu[4 * k + 1], wu[4 * k + 2], wu[4 * k + 3]));
                 }
               });
             });
           });
-          if (last_of_unit) {
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (ptx::elect_one()) {
-              ptx::tma_store_2d(&tm_dh, slot + box_out, col0 + at - off, row - lane);
-              ptx::tma_store_2d(&tm_du, slot + box_out + out_box, col0 + at - off, row - lane);
-              ptx::bulk_commit_group();
-            }
-            ++used;
-            fetch();
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (ptx::elect_one()) {
+            ptx::tma_store_2d(&tm_dh, box + box_out, col0 + at, row - lane);
+            ptx::tma_store_2d(&tm_du, box + box_out + out_box, col0 + at, row - lane);
+            ptx::bulk_commit_group();
           }
+          next_slot();
+          fetch();
         }
       }
       // Copies that are still in flight after a wait that ran out land, and stores have read their boxes, before the CTA gives up its shared memory.
-      for (; used < issued; ++used)
-        for (uint32_t it = 0; it < p.wait_limit && !ptx::mbar_try_wait(in_bar(ew, slot_of(used)), phase_of(used)); ++it) {}
+      for (; pending > 0; next_slot())
+        for (uint32_t it = 0; it < p.wait_limit && !ptx::mbar_try_wait(in_bar(ew, slot), slot_phase); ++it) {}
       if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
       __syncwarp();
     }
@@ -705,9 +709,9 @@ us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t
   else if (!make_chunk_tmap(&t[2], B1, ES, kBK, S::kChunkRow)) return US_ERR_CUDA;
   if (BWD) {
     const int kept_es = dtype_size(m.h->dtype), out_es = dtype_size(m.dh->dtype);
-    p.unit_cols = kept_es == 1 && out_es == 1 && S::kWarpCols >= 64 ? 64 : 32;
-    if (!host::make_tmap(&t[3], m.h, kept_es, 32, p.unit_cols * kept_es) || !host::make_tmap(&t[4], m.u, kept_es, 32, p.unit_cols * kept_es) ||
-        !host::make_tmap(&t[5], m.dh, out_es, 32, p.unit_cols * out_es) || !host::make_tmap(&t[6], m.du, out_es, 32, p.unit_cols * out_es))
+    p.slots = kept_es == out_es ? kMostSlots : epi_room(S::kEW) / (2048 * (kept_es + out_es));
+    if (!host::make_tmap(&t[3], m.h, kept_es, 32, 32 * kept_es) || !host::make_tmap(&t[4], m.u, kept_es, 32, 32 * kept_es) ||
+        !host::make_tmap(&t[5], m.dh, out_es, 32, 32 * out_es) || !host::make_tmap(&t[6], m.du, out_es, 32, 32 * out_es))
       return US_ERR_CUDA;
   } else {
     t[3] = t[4] = t[5] = t[6] = t[0];
