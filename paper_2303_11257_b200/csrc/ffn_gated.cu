@@ -11,7 +11,7 @@
 // without a factor.  Backward, a tile is HC columns of dA, from which the epilogue makes both gradients with the copies it has fetched.
 //
 // Bound: forward the tensor pipe and, over seconds, power: 8192 x 1024 x 4096 BF16 with copies 125 us (1.10 PFLOP/s; 98 in a burst), 16384 x 2048 x 8192 FP8 with E4M3
-// copies 440 us (2.5 PFLOP/s).  Backward, BF16 88 us (268 MB of copies and gradients beside 69 GFLOP: the SM's memory path), FP8 from E4M3 copies 54 us (the epilogue's
+// copies 440 us (2.5 PFLOP/s).  Backward, BF16 85 us (268 MB of copies and gradients beside 69 GFLOP: the SM's memory path), FP8 from E4M3 copies 53 us (the epilogue's
 // instructions).  One token of 1024 x 4096 in BF16 5.4 us.
 //
 // Every wait is bounded as in the other GEMM kernels.
@@ -33,7 +33,8 @@ __host__ __device__ constexpr int gated_ew(bool bwd, int es, int cg) { return ga
 constexpr int kRoom = 229376;                 // shared memory for stages and the epilogue's boxes
 constexpr int kMostStages = 16;
 // Backward, an epilogue warp has slots for the copies of h and u that arrive and the dH and dU that leave, in boxes of 32 rows x 32 columns.  Where copies and gradients have one
-// width a gradient leaves from the box of its copy, and there are three slots: a store has a unit's time to read one before it is filled again.  Elsewhere a slot has
+// width a gradient leaves from the box of its copy, and there are three slots: a store has a unit's time to read one before it is filled again (8192 x 1024 x 4096, two / three / four slots, the last in a stage's room:
+// BF16 92.7 / 84.7 / 91.8 us, FP8 56.8 / 53.3 / 54.8).  Elsewhere a slot has
 // boxes for both (6144 bytes), in as many slots as fit.
 constexpr int kMostSlots = 3;
 __host__ __device__ constexpr int epi_room(int ew) { return ew == 16 ? 6144 : 12288; }      // bytes of a warp

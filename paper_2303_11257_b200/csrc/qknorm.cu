@@ -5,7 +5,7 @@
 //   backward   n' = R^T g,  u = w n',  dx = beta_x r (u - x r mean(u x r)),  dw = beta_w sum n' x r
 //
 // Every element is read once and written once; the kernels are bound by the instructions they issue before they are by HBM (11 to 14 a value).  8192 tokens of 16 + 16 heads of 64
-// in BF16: forward 13.7 us (4.9 TB/s), backward 23.0 (4.4 TB/s); 16384 tokens of 32 + 8 heads of 128 into E4M3 58 us (4.5 TB/s).
+// in BF16: forward 13.5 us (5.0 TB/s), backward 22.0 (4.6 TB/s); 16384 tokens of 32 + 8 heads of 128 into E4M3 58 us (4.5 TB/s).
 // A head is held by a group of G lanes (a power of two), each with two chunks of eight features that hold whole pairs -- features i .. i + 7 and their partners half a
 // rotation further, or sixteen neighbours -- so that the rotation needs no exchange and one group sum (forward) or two (backward) are all that lanes tell one another.  A warp's
 // unit is some steps of 32 / G heads of one row, whose cosines and sines it holds in registers over all of them; the norm's weight it holds for the whole launch,
@@ -226,10 +226,10 @@ __device__ __forceinline__ void load_weight(const QkPart& q, const Lane& l, f32x
   }
 }
 
-// The vector kernels' walk over the units of a warp: STEPS steps of 32 / G heads of one row, which arrive in a ring of kStages slots of the warp's own in shared memory, two units
-// ahead of the one that is worked on.  (With the loads of one unit in registers and none ahead, 8192 tokens of 16 + 16 heads of 64 took 20.7 us forward and 29.4 backward, 16384
-// tokens of 32 + 8 heads of 128 into E4M3 91 to 107: latency.)
-constexpr int kStages = 3;
+// The vector kernels' walk over the units of a warp: STEPS steps of 32 / G heads of one row, which arrive in a ring of kStages slots of the warp's own in shared memory, ahead of the
+// one that is worked on.  (us, 8192 tokens of 16 + 16 heads of 64 forward and backward, 16384 of 32 + 8 heads of 128 into E4M3; rings of two / three slots: 13.5 / 13.7, 22.0 / 23.0, 57.6 / 58.2;
+// units of one step 14.4, 22.7, 69; of four 72 for the last.)
+constexpr int kStages = 2;
 // Bytes of a slot: both chunks of a step, of x and backward of the gradient, and the row of the table.
 template <bool BWD, int DT, int STEPS>
 __host__ __device__ constexpr int slot_bytes(int group) { return STEPS * (BWD ? 4 : 2) * kChunkBytes<DT> + 64 * group; }
