@@ -854,7 +854,10 @@ def us_qk_norm_fwd(X, w, Y, head_width, eps, table=None, positions=None, start=0
     """X, w, Y: lists of matrices [rows x heads * head_width] (queries and keys), norm weights [head_width] (or None) and outputs;
     positions: int32 CUDA tensor [rows], or None for start + row % period."""
     n = len(X)
-    _check_lists(n, X, positions, w, Y)
+    if len(Y) != n or (w is not None and len(w) != n):
+        raise ValueError("one entry per matrix is wanted")
+    if positions is not None:
+        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == X[0].size(0)
     _check("us_qk_norm_fwd", _entry("us_qk_norm_fwd")(n, X, w, Y, head_width, eps, table, positions, start, period, neighbours, _stream(stream)))
     return Y
 
@@ -867,17 +870,13 @@ def us_qk_norm_bwd(X, w, G, dX, dw, head_width, eps, ws, beta_x=1.0, beta_w=None
     """G, dX: lists of gradients of the outputs and of X; dw: list of weight gradients, or None; beta_w: list of their factors, or None
     (ones); ws: a uint8 CUDA tensor of at least us_qk_norm_bwd_workspace_bytes(head_width) bytes, or None without dw."""
     n = len(X)
-    _check_lists(n, X, positions, w, G, dX, dw, beta_w)
+    if len(G) != n or len(dX) != n or (w is not None and len(w) != n) or (dw is not None and len(dw) != n) or (beta_w is not None and len(beta_w) != n):
+        raise ValueError("one entry per matrix is wanted")
+    if positions is not None:
+        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == X[0].size(0)
     _check("us_qk_norm_bwd", _entry("us_qk_norm_bwd")(
         n, X, w, G, dX, dw, beta_w, head_width, eps, beta_x, table, positions, start, period, neighbours, ws, ws if ws is not None else 0, _stream(stream)))
     return dX, dw
-
-
-def _check_lists(n, X, positions, *lists):
-    for v in lists:
-        if v is not None and len(v) != n:
-            raise ValueError("one entry per matrix is wanted")
-    assert positions is None or (positions.dtype is torch.int32 and positions.dim() == 1 and positions.is_contiguous() and positions.numel() == X[0].size(0))
 
 
 def us_scales_linear(b: int, m: int, n: int, constrained: bool = False):
