@@ -211,7 +211,7 @@ __device__ __forceinline__ void put_row(uint8_t* dst, int es, const uint32_t (&w
     for (int i = 0; i < S; ++i)
       if (i < cols) {
         if (es == 2) reinterpret_cast<uint16_t*>(dst)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-        else if (i < 2 * S) dst[i] = (uint8_t)(w[(i >> 2) % (S / 2)] >> (8 * (i & 3)));
+        else dst[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
       }
   }
 }

@@ -223,6 +223,40 @@ def test_captured_and_replayed_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(got, (Y, dX, dw)))
 
 
+@pytest.mark.parametrize("x_fmt,g_fmt", [("bf16", "bf16"), ("f32", "bf16"), ("fp16", "f32")])
+@pytest.mark.parametrize("place", [dict(start=17), dict(start=5, period=1), dict(period=200), dict(period=41, start=2)])
+def test_matrices_of_their_own_pitches_and_types(x_fmt, g_fmt, place):
+    """Queries of one type and keys of another, gradients with other pitches and types, every way to say where rows are."""
+    L = _lib()
+    rng = np.random.default_rng(11)
+    rows, width, heads, eps = 83, 64, (5, 2), 1e-5
+    table_h = np.float32(O.rotary_table(120, width))
+    table = torch.from_numpy(table_h).cuda()
+    at = place.get("start", 0) + (np.arange(rows) % place["period"] if place.get("period") else np.arange(rows))
+    x_fmts = (x_fmt, "bf16")
+    Xh, Gh = ([rng.standard_normal((rows, h * width)).astype(np.float32) for h in heads] for _ in range(2))
+    X = [U.to_device(x, f, ld=x.shape[1] + 8 * (k + 1)) for k, (x, f) in enumerate(zip(Xh, x_fmts))]
+    G = [U.to_device(g, g_fmt, ld=g.shape[1] + 24) for g in Gh]
+    w = [torch.ones(width, device="cuda") * (1 + k) for k in range(2)]
+    Y, dX, dw = [torch.empty_like(x, dtype=torch.float32) for x in _f32_like(X)], [torch.empty_like(x, dtype=torch.float32) for x in _f32_like(X)], [torch.empty(width, device="cuda") for _ in range(2)]
+    ws = torch.empty(L.us_qk_norm_bwd_workspace_bytes(width), dtype=torch.uint8, device="cuda")
+    L.us_qk_norm_fwd(X, w, Y, width, eps, table=table, **place)
+    L.us_qk_norm_bwd(X, w, G, dX, dw, width, eps, ws, table=table, **place)
+    for k in range(2):
+        x, g = U.values_of(Xh[k], x_fmts[k]), U.values_of(Gh[k], g_fmt)
+        n = O.qk_norm_fwd(x, [1.0 + k] * width, width, eps).reshape(rows, heads[k], width)
+        _check(Y[k], O.qk_norm_fwd(x, [1.0 + k] * width, width, eps, table_h, at), 1.5e-6 * _magnitude(n, width, False).reshape(rows, -1), "f32", "Y")
+        ref, dwr = O.qk_norm_bwd(x, [1.0 + k] * width, g, width, eps, 1.0, 1.0, table_h, at)
+        xv, m = x.reshape(rows, heads[k], width), _magnitude(g.reshape(rows, heads[k], width), width, False) * (1.0 + k)
+        size = np.sqrt((xv * xv).mean(-1, keepdims=True) + eps)
+        _check(dX[k], ref, (5e-6 / size * (m + np.abs(xv / size) * (m * np.abs(xv / size)).mean(-1, keepdims=True))).reshape(rows, -1), "f32", "dX")
+        assert (np.abs(dw[k].double().cpu().numpy() - dwr) <= 4e-6 * (m / (1.0 + k) * np.abs(xv / size)).sum((0, 1))).all()
+
+
+def _f32_like(X):
+    return [torch.empty(x.shape, device="cuda") for x in X]
+
+
 def test_many_rows_and_offsets_beyond_32_bits():
     """Rows 1.6 million elements apart: the last one starts 4.6e9 elements into its buffer."""
     L = _lib()
