@@ -701,7 +701,7 @@ us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t
   // a short A: its rows in groups of eight.  The MMA still reads 128; what lies behind them ends up in rows that do not exist.
   const int a_rows = CG == 1 && p.M < kBM ? (p.M + 7) / 8 * 8 : kBM;
   p.a_bytes = (uint32_t)a_rows * kStageKBytes;
-  p.stages = std::min(kMostStages, (kRoom - std::max(S::kEpiBytes, kBM * kStageKBytes)) / ((int)p.a_bytes + S::kBBytes));
+  p.stages = std::min(kMostStages, (kRoom - std::max((int)S::kEpiBytes, kBM * kStageKBytes)) / ((int)p.a_bytes + S::kBBytes));
   CUtensorMap t[7];
   constexpr int kBK = kStageKBytes / ES;
   if (!host::make_tmap(&t[0], A, ES, a_rows, kStageKBytes)) return US_ERR_CUDA;
@@ -743,7 +743,7 @@ us_status pick_gated(const GatedMats& m, GatedParams& p, cudaStream_t st) {
   }
   const int64_t narrow = ((M + kBM - 1) / kBM) * ((N + kWide / 4 - 1) / (kWide / 4));
   if (narrow <= sms) return launch_gated<BWD, ES, kWide / 4, 1>(m, p, sms, st);
-  return launch_gated<BWD, ES, kWide / 2, 1>(m, p, sms, st);
+  return launch_gated<BWD, ES, kWide / 2, 1, !BWD>(m, p, sms, st);
 }
 
 // The checks that both directions share: operands of one width (f8: 8-bit), workspace.
