@@ -257,9 +257,10 @@ __device__ __forceinline__ uint64_t chunk_desc(uint32_t addr, int row_bytes, uin
   return d | ((uint64_t)(row_bytes == 128 ? 2 : row_bytes == 64 ? 4 : 6) << 61);
 }
 
-// ES: operand bytes per element (1 = FP8, 2 = BF16 / F16).  HC: hidden columns of a tile.  CG = 2: tiles of 256 rows by a CTA pair, 1: of 128 by a CTA.  BOXED (forward,
-// pairs): results leave by TMA, where no unit has a second tile whose MMAs the stores could hide behind.  (us, stored by the lanes / boxed: 1000 x 528 x 2096 F16 13.3 / 9.4; several
-// tiles each: 8192 x 1024 x 4096 BF16 125 / 130, 16384 x 2048 x 8192 FP8 443 / 474, half of which is the stages that the boxes take.)
+// ES: operand bytes per element (1 = FP8, 2 = BF16 / F16).  HC: hidden columns of a tile.  CG = 2: tiles of 256 rows by a CTA pair, 1: of 128 by a CTA.  BOXED (forward):
+// results leave by TMA, not by the lanes; the boxes take a stage or two.  That pays where the stores are not hidden behind the MMAs of a unit's next tile (boxed_pairs; single
+// CTAs of 64 hidden columns, always).  (us, lanes / boxes.  One tile a unit: 1000 x 528 x 2096 F16 13.3 / 9.4; 700 x 2048 x 1500 FP8 20.4 / 9.5, BF16 26 / 13;
+// 1000 x 1024 x 1024 FP8 5.8 / 6.2.)
 template <bool BWD, int ES, int HC, int CG, bool BOXED>
 __global__ void __launch_bounds__(gemm_threads(gated_ew(BWD, ES, CG)), 1)
 gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0, const __grid_constant__ CUtensorMap tm_b1,
@@ -727,6 +728,11 @@ us_status launch_gated(const GatedMats& m, GatedParams& p, int sms, cudaStream_t
                       t[4], t[5], t[6], static_cast<const GatedParams&>(p));
 }
 
+// Boxes for CTA pairs: no unit has a second tile, or the contraction is too short (nine stages) to hide the stores.  (us, lanes / boxes, copies of h and u in BF16:
+// 2048 x 528 x 2096 BF16 17.5 / 12.7, FP8 16.4 / 11.1; 8192 x 1024 x 4096 FP8 82 / 72, BF16 121 / 126; 4096 x K x 4096 BF16, K = 576: 55 / 48, 640: 47.6 / 46.7,
+// 768: 51.8 / 53.5; FP8, K = 1152: 50 / 45, 1536: 49.8 / 52.5; 16384 x 2048 x 8192 FP8 with copies in E4M3 443 / 474.)
+inline bool boxed_pairs(int64_t tiles, int64_t k_bytes, int sms) { return 2 * tiles <= sms || k_bytes <= 9 * kStageKBytes; }
+
 // Tiles of CTA pairs unless they would leave more than half of the pairs idle, else the widest of single CTAs, else, where the machine has
 // an SM for each of them, the narrow ones.
 template <bool BWD, int ES>
@@ -737,7 +743,7 @@ us_status pick_gated(const GatedMats& m, GatedParams& p, cudaStream_t st) {
   const int64_t M = p.M, N = p.N;
   if (4 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) >= sms && M > kBM) {
     if constexpr (!BWD) {
-      if (2 * ((M + 255) / 256) * ((N + kWide - 1) / kWide) <= sms) return launch_gated<BWD, ES, kWide, 2, true>(m, p, sms, st);
+      if (boxed_pairs(((M + 255) / 256) * ((N + kWide - 1) / kWide), (int64_t)p.K * ES, sms)) return launch_gated<BWD, ES, kWide, 2, true>(m, p, sms, st);
     }
     return launch_gated<BWD, ES, kWide, 2>(m, p, sms, st);
   }

@@ -17,9 +17,9 @@ from tests import util as U
 pytestmark = pytest.mark.gpu
 US_ERR_TIMEOUT = 6
 # One shape per form of the launch on 148 SMs, ragged in every dimension: narrow tiles, wide ones of single CTAs, tiles of CTA pairs (one and
-# several each), both directions; single rows; a contraction longer than the ring of stages; the smallest matrices.
+# several each, of short and of long contractions), both directions; single rows; a contraction longer than the ring of stages; the smallest matrices.
 SHAPES = {"one": (1, 1, 1, 1), "token": (1, 520, 1104, 304), "few": (37, 144, 336, 208), "narrow": (300, 80, 1000, 144), "wide": (600, 272, 1500, 96), "wider": (600, 272, 2100, 96), "pair": (1300, 272, 1808, 400),
-          "pairs": (2300, 96, 4870, 64), "long": (130, 3000, 90, 2500), "tall": (5000, 33, 70, 65)}
+          "pairs": (2300, 96, 4870, 64), "deep": (1300, 1168, 1700, 64), "long": (130, 3000, 90, 2500), "tall": (5000, 33, 70, 65)}
 
 
 def _lib():
