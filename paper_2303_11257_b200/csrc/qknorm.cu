@@ -300,7 +300,7 @@ __device__ __forceinline__ void walk(const QkArgs& p, const QkPart& q, const Lan
         if (lane < p.group) {
           const uint32_t angles = ring + s * slot + STEPS * kStep + 64u * j, none = 0x7fffffffu;
           if (at < (uint32_t)p.table_rows) {
-            const float* t = table + (uint64_t)at * (uint32_t)p.table_ld;
+            const float* t = table + (int64_t)at * p.table_ld;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (i < 2 ? l.rot_a : l.rot_b) copy16(angles + 16u * i, t + 4 * i);

@@ -281,3 +281,26 @@ def test_table():
         L.us_rotary_table(t, base, scale, first)
         ref = O.rotary_table(rows, rotated, base, scale, first)
         assert np.all(np.abs(t.double().cpu().numpy() - ref) <= 2.0 ** -25 + 2e-9)
+
+
+def test_table_rows_more_than_32_bits_apart():
+    """A table whose rows lie 2^32 and more elements apart turns as the same table in one piece does."""
+    L = _lib()
+    rows, width = 5, 64
+    X = torch.randn(rows, 4 * width, device="cuda").to(torch.bfloat16)
+    at = torch.tensor([1, 0, 1, 1, 0], dtype=torch.int32, device="cuda")
+    near = L.rotary_table(64, width)[[7, 40]]
+    ws, w = torch.empty(L.us_qk_norm_bwd_workspace_bytes(width), dtype=torch.uint8, device="cuda"), torch.ones(width, device="cuda")
+
+    def both(table):
+        Y, dX, dw = torch.empty_like(X), torch.empty_like(X), torch.empty(width, device="cuda")
+        L.us_qk_norm_fwd([X], [w], [Y], width, 1e-6, table=table, positions=at)
+        L.us_qk_norm_bwd([X], [w], [X], [dX], [dw], width, 1e-6, ws, table=table, positions=at)
+        return Y, dX, dw
+    want = both(near)
+    for pitch in (2 ** 32, 2 ** 32 + 64):
+        buf = torch.zeros(pitch + width, device="cuda")
+        far = torch.as_strided(buf, (2, width), (pitch, 1))
+        far.copy_(near)
+        assert all(torch.equal(a, b) for a, b in zip(both(far), want)), pitch
+        del buf, far
