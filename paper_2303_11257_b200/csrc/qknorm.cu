@@ -582,7 +582,8 @@ us_status prepare(Call& c, int count, const us_mat* X, const us_mat* w, const us
     if (table->dtype != US_F32) return US_ERR_UNSUPPORTED;
     if (table->rows < 1 || table->cols % 2 || table->cols > width) return US_ERR_INVALID_ARG;
     // positions on the host's side of the call are known to be in the table; those on the device are checked there
-    if (!positions && a.rows > 0 && start + (period ? std::min(period, a.rows) : a.rows) > table->rows) return US_ERR_INVALID_ARG;
+    const int64_t span = period ? std::min(period, a.rows) : a.rows;                // (start + span may pass 2^63)
+    if (!positions && a.rows > 0 && (span > table->rows || start > table->rows - span)) return US_ERR_INVALID_ARG;
     if (positions && reinterpret_cast<uintptr_t>(positions) % 4) return US_ERR_ALIGNMENT;
     a.table = static_cast<const float*>(table->ptr); a.table_ld = table->ld; a.table_rows = table->rows;
     a.positions = positions; a.start = start; a.period = period < a.rows ? (uint32_t)period : 0; a.rotated = (int)table->cols;

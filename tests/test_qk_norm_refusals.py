@@ -87,3 +87,13 @@ def test_lists_of_tensors_are_described_by_the_binding():
         L.us_qk_norm_fwd([x, x], [w], [x, x], 64, 0.0, stream=0)
     with pytest.raises(AssertionError):
         L.us_qk_norm_fwd([x], None, [x], 64, 0.0, positions=torch.zeros(4), stream=0)
+
+
+def test_starts_near_the_end_of_64_bits():
+    """start + rows is not formed where it would pass 2^63."""
+    last = 2 ** 63 - 1
+    for start in (last, last - 3, last - 7, 2 ** 62, 2 ** 32, 2 ** 32 + 3):
+        assert fwd(start=start) == 1 and fwd(start=start, period=4) == 1 and fwd(start=start, period=1) == 1, start
+    assert fwd(period=last) == 5 and fwd(period=last, start=24) == 5 and fwd(period=last, start=25) == 1
+    # where the positions are on the device, or nothing is turned, start is not read
+    assert fwd(start=last, pos=0x40000) == 5 and fwd(start=last, table=None) == 5
