@@ -219,7 +219,7 @@ class UnitScaledEncoderLayer:
         return own
 
     def _state(self):
-        return (*self.sc.values(), self.c_skip, self.c_branch, self.eps, self.beta_ln if self.norm else 0.0) + self.ffn._state()
+        return (*self.sc.values(), self.c_skip, self.c_branch, self.eps, self.beta_ln if self.norm else 0.0, self.beta_qk if self.qk_norm else 0.0) + self.ffn._state()
 
     def _lay_out(self, p):
         sc, ws, s, f = self.sc, self.ws, self.slen, self.ffn

@@ -92,3 +92,23 @@ def test_factors():
     c = ffn.GatedScales.unit(64, 32, 48, "gelu", constrained=True)
     assert c.alpha1 == c.beta_x1 and c.alpha_g == c.beta_h == c.beta_u and c.alpha2 == c.beta_x2
     assert abs(ffn.GatedScales.unit(64, 32, 48, dp_world=4).beta_w - 256 ** -0.5) < 1e-7
+
+
+def test_a_changed_factor_of_the_norms_weights_is_used(monkeypatch):
+    """beta_qk belongs to what a step was laid out for, as beta_ln does."""
+    layer, x = _layer(qk_norm=True, norm="post")
+    rec = _Recorder()
+    monkeypatch.setattr(L, "_lib", rec)
+    ln = [torch.ones(128)] * 4
+
+    def factors():
+        rec.calls = []
+        layer.step(*x, stream=0, qk=[torch.ones(64)] * 2, ln=ln)
+        (args,) = [a for n, a in rec.calls if n == "us_qk_norm_bwd"]
+        return [float(v) for v in args[6]], {float(a[5]) for n, a in rec.calls if n == "us_layer_norm_bwd_cast"}
+    first, _ = factors()
+    assert first == [layer.beta_qk] * 2
+    layer.beta_qk = 0.25
+    assert factors() == ([0.25, 0.25], {layer.beta_ln})
+    layer.beta_ln = 0.125
+    assert factors() == ([0.25, 0.25], {0.125})
