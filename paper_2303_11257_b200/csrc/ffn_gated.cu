@@ -89,6 +89,22 @@ __device__ __forceinline__ f32x2 sigmoid2(f32x2 x, f32x2 nl2) {
   unpack2(add2(pack2(ex2_approx(p0), ex2_approx(p1)), splat2(1.0f)), p0, p1);
   return pack2(rcp_approx(p0), rcp_approx(p1));
 }
+// min(x, m), or x where that is NaN.
+__device__ __forceinline__ float min_nan(float x, float m) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(m));
+  return r;
+}
+// s = sigmoid(z) and c = 1 - s = e^-z s, z = act_in x.  (1 - s itself cancels where s is close to 1: the slope s c would be 1 % off at z = 12, and nothing from 17 on.)
+// e^-z is kept finite, so that c stays a number where s is nothing.
+__device__ __forceinline__ void sigmoid_both2(f32x2 x, f32x2 nl2, f32x2& s, f32x2& c) {
+  float p0, p1;
+  unpack2(mul2(x, nl2), p0, p1);
+  const f32x2 e = pack2(ex2_approx(min_nan(p0, 127.f)), ex2_approx(min_nan(p1, 127.f)));
+  unpack2(add2(e, splat2(1.0f)), p0, p1);
+  s = pack2(rcp_approx(p0), rcp_approx(p1));
+  c = mul2(e, s);
+}
 __device__ __forceinline__ f32x2 normal_cdf2(f32x2 z) {
   float z0, z1, q0, q1;
   unpack2(z, z0, z1);
@@ -119,12 +135,14 @@ __device__ __forceinline__ void gate_grads2(f32x2 x, f32x2 u, f32x2 d, float act
     return;
   }
   if (FN == US_FN_SIGMOID) {
-    f = sigmoid2(x, nl2);
-    df = mul2(f, fma2(f, splat2(-1.0f), one));
-  } else if (FN == US_FN_TANH) {
-    const f32x2 s = sigmoid2(x, add2(nl2, nl2));
+    f32x2 c;
+    sigmoid_both2(x, nl2, f, c);
+    df = mul2(f, c);
+  } else if (FN == US_FN_TANH) {                          // tanh z = 2 sigmoid(2 z) - 1
+    f32x2 s, c;
+    sigmoid_both2(x, add2(nl2, nl2), s, c);
     f = fma2(s, splat2(2.0f), splat2(-1.0f));
-    df = mul2(mul2(s, splat2(4.0f)), fma2(s, splat2(-1.0f), one));
+    df = mul2(mul2(s, splat2(4.0f)), c);
   } else {
     const f32x2 z = mul2(x, in2);
     float z0, z1;

@@ -265,3 +265,39 @@ def test_silu_as_an_elementwise_op():
     assert np.all(np.abs(A.double().cpu().numpy() - O.activation_fwd("silu", h, 0.75, 1.5)) <= 1.5 * 4e-7 * (1 + np.abs(h)))
     assert np.all(np.abs(dH.double().cpu().numpy() - O.activation_bwd("silu", h, 0.5, 0.75, 1.25)) <= 4e-7 * (1 + np.abs(h)))
     assert all(abs(a - b) < 1e-6 for a, b in zip(L.us_scales_activation("silu"), S.silu_scales()))
+
+
+def _gate_and_slope(fn, z):
+    """f and f' for sigmoid and tanh, in closed forms without cancellation."""
+    if fn == "sigmoid":
+        e = np.exp(-np.abs(z))
+        return np.where(z >= 0, 1.0, e) / (1 + e), e / (1 + e) ** 2
+    return np.tanh(z), np.cosh(z) ** -2.0
+
+
+def _gradients_of_both_signs(b, f, act, grad, kept, s_in, fn):
+    """(z, dH, dU) for arguments from 2^-12 to 15 in the left half of the columns and their negatives in the right one; u = dA = 1 exactly."""
+    L, _ = _lib()
+    v = np.float32(2.0 ** np.linspace(-12, np.log2(15), b * (f // 2))).reshape(b, -1)
+    h = U.values_of(np.concatenate([v, -v], 1), kept)
+    Ht, Vt = U.to_device(np.float32(h), kept, _pitch(f)), U.to_device(np.ones((b, f), np.float32), kept, _pitch(f))
+    one = lambda r, fmt: U.to_device(np.float32(np.eye(1, 16)).repeat(r, 0), fmt)                 # rows (1, 0, 0 ..)
+    dH, dU, ws = U.empty(b, f, grad, _pitch(f)), U.empty(b, f, grad, _pitch(f)), L.new_workspace()
+    L.us_ffn_gated_bwd(fn, one(b, grad), one(f, act), 1.0, Ht, Vt, dH, dU, ws, act_in_scale=s_in)
+    assert L.us_workspace_status(ws) == 0
+    return s_in * h, dH, dU
+
+
+SIGNED = [(b, f, *types) for b, f in ((37, 336), (1300, 1808)) for types in (("bf16", "bf16", "fp16"), ("fp16", "fp16", "bf16"), ("e4m3", "e5m2", "e4m3"), ("e4m3", "e5m2", "fp16"))]
+
+
+@pytest.mark.parametrize("fn", ["sigmoid", "tanh"])
+@pytest.mark.parametrize("s_in", [1.0, 0.625])
+@pytest.mark.parametrize("case", SIGNED)
+def test_slopes_near_zero_and_far_from_it(case, s_in, fn):
+    """Errors relative to the slope s (1 - s) itself (tanh: 4 s (1 - s) of 2 z).  In units of 2^-24: e = 2^(-z log2 e) (tanh: of 2 z) is off by 5 |z| from the rounded product and
+    4 from ex2; s = 1 / (1 + e) by 3 and e / (1 + e) of that; 1 - s = e s by what is left of it, 1 / (1 + e), 3 and 1; so with its products the slope by
+    5 |z| + 17; 6 |z| + 32 is taken."""
+    z, dH, _ = _gradients_of_both_signs(*case, s_in, fn)
+    slope = s_in * _gate_and_slope(fn, z)[1]
+    _close(dH, slope, (6 * np.abs(z) + 32) * 2.0 ** -24 * slope, case[3], "dH")
