@@ -105,6 +105,15 @@ __device__ __forceinline__ void sigmoid_both2(f32x2 x, f32x2 nl2, f32x2& s, f32x
   s = pack2(rcp_approx(p0), rcp_approx(p1));
   c = mul2(e, s);
 }
+// tanh(z) = 2 s - 1 with s = sigmoid(2 z), which cancels near zero: there z - z^3 / 3 + 2 z^5 / 15, whose next term is 2^-22 of it at 1/8.
+__device__ __forceinline__ f32x2 tanh2(f32x2 z, f32x2 s) {
+  float z0, z1, f0, f1, n0, n1;
+  const f32x2 zz = mul2(z, z);
+  unpack2(mul2(z, fma2(zz, fma2(zz, splat2(2.0f / 15.0f), splat2(-1.0f / 3.0f)), splat2(1.0f))), n0, n1);
+  unpack2(fma2(s, splat2(2.0f), splat2(-1.0f)), f0, f1);
+  unpack2(z, z0, z1);
+  return pack2(fabsf(z0) < 0.125f ? n0 : f0, fabsf(z1) < 0.125f ? n1 : f1);
+}
 __device__ __forceinline__ f32x2 normal_cdf2(f32x2 z) {
   float z0, z1, q0, q1;
   unpack2(z, z0, z1);
@@ -116,7 +125,7 @@ template <int FN>
 __device__ __forceinline__ f32x2 gate_value2(f32x2 x, f32x2 in2, f32x2 nl2) {
   if (FN == US_FN_SILU) return mul2(mul2(x, in2), sigmoid2(x, nl2));
   if (FN == US_FN_SIGMOID) return sigmoid2(x, nl2);
-  if (FN == US_FN_TANH) return fma2(sigmoid2(x, add2(nl2, nl2)), splat2(2.0f), splat2(-1.0f));      // tanh z = 2 sigmoid(2 z) - 1
+  if (FN == US_FN_TANH) return tanh2(mul2(x, in2), sigmoid2(x, add2(nl2, nl2)));
   const f32x2 z = mul2(x, in2);
   if (FN == US_FN_GELU) return mul2(z, normal_cdf2(z));
   float z0, z1;
@@ -138,10 +147,10 @@ __device__ __forceinline__ void gate_grads2(f32x2 x, f32x2 u, f32x2 d, float act
     f32x2 c;
     sigmoid_both2(x, nl2, f, c);
     df = mul2(f, c);
-  } else if (FN == US_FN_TANH) {                          // tanh z = 2 sigmoid(2 z) - 1
+  } else if (FN == US_FN_TANH) {
     f32x2 s, c;
     sigmoid_both2(x, add2(nl2, nl2), s, c);
-    f = fma2(s, splat2(2.0f), splat2(-1.0f));
+    f = tanh2(mul2(x, in2), s);
     df = mul2(mul2(s, splat2(4.0f)), c);
   } else {
     const f32x2 z = mul2(x, in2);

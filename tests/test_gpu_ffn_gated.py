@@ -301,3 +301,26 @@ def test_slopes_near_zero_and_far_from_it(case, s_in, fn):
     z, dH, _ = _gradients_of_both_signs(*case, s_in, fn)
     slope = s_in * _gate_and_slope(fn, z)[1]
     _close(dH, slope, (6 * np.abs(z) + 32) * 2.0 ** -24 * slope, case[3], "dH")
+
+
+@pytest.mark.parametrize("fn", ["sigmoid", "tanh"])
+@pytest.mark.parametrize("s_in", [1.0, 0.625])
+@pytest.mark.parametrize("case", SIGNED)
+def test_values_near_zero_and_far_from_it(case, s_in, fn):
+    """The gate's values, in dU and in A, with errors relative to the value itself.  In units of 2^-24: s = sigmoid(z) is off by 5 |z| + 7 (as above); tanh from 1/8 on, as 2 s - 1
+    with s of 2 z, by 2 s (3 + (1 - s) (5 |z| + 4)) and 1, 9 at 1/8, where that is 8 times as much of the value, and 5 where |z| is large; below 1/8, as a polynomial, by the term left out, 4, and
+    five roundings; products 5.  6 |z| + 96 is taken."""
+    b, f, act, grad, kept = case
+    L, _ = _lib()
+    z, _, dU = _gradients_of_both_signs(*case, s_in, fn)
+    value = _gate_and_slope(fn, z)[0]
+    _close(dU, value, (6 * np.abs(z) + 96) * 2.0 ** -24 * np.abs(value), grad, "dU")
+    h = np.float32(2.0 ** np.linspace(-12, np.log2(15), f // 2))
+    h = U.values_of(np.concatenate([h, -h])[None], act)
+    rows = lambda r: U.to_device(np.float32(np.concatenate([r, np.zeros((15, f))])), act, _pitch(f))
+    X, A, ws = U.to_device(np.float32(np.eye(1, 16)).repeat(b, 0), act), U.empty(b, f, act, _pitch(f)), L.new_workspace()
+    L.us_ffn_gated_fwd(fn, X, rows(h), rows(np.ones((1, f))), 1.0, A, ws, act_in_scale=s_in)
+    assert L.us_workspace_status(ws) == 0
+    z = s_in * h
+    value = _gate_and_slope(fn, z)[0].repeat(b, 0)
+    _close(A, value, (6 * np.abs(z) + 96) * 2.0 ** -24 * np.abs(value), act, "A")
