@@ -360,7 +360,8 @@ us_status us_test_ffn_gated_bwd_starved(const us_mat* G, const us_mat* W2, const
  *                  skip = incoming gradient, branch = gradient at the branch entry.
  * us_activation_fwd  A  = alpha * f(s_in * H) for f = relu(x) = max(x, 0), tanh, sigmoid(x) = (1 + e^-x)^-1,
  *                  silu(x) = x sigmoid(x) or gelu (table rows relu / gelu / tanh / sigmoid: alpha = 1 / std f(Z), Z ~ N(0,1));
- * us_activation_bwd  dH = beta * s_in * f'(s_in * H) * dA (beta = 1 / rms f'(Z)); relu'(0) = 0.
+ * us_activation_bwd  dH = beta * s_in * f'(s_in * H) * dA (beta = 1 / rms f'(Z)); relu'(0) = 0.  A NaN of H is one of A for every f, and one of dH but
+ *                  for relu, whose slope is 0 there (so in the epilogues of linear ops; us_ffn_gated_bwd keeps it for relu too).
  *                  US_FN_GELU gives the same values as us_gelu_fwd / us_gelu_bwd.
  * us_weighted_add  out = alpha * sum_i gamma_i * src_i over count (1..8) tensors of one shape (table row
  *                  weighted_add: alpha = (sum_i gamma_i^2)^-1/2 keeps unit scale; each input's gradient

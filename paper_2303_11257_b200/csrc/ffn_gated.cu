@@ -163,7 +163,7 @@ __device__ __forceinline__ void gate_grads2(f32x2 x, f32x2 u, f32x2 d, float act
     } else {
       unpack2(z, z0, z1);
       f = pack2(act_value(US_FN_RELU, z0), act_value(US_FN_RELU, z1));
-      df = pack2(act_slope(US_FN_RELU, z0), act_slope(US_FN_RELU, z1));
+      df = pack2(z0 > 0.f ? 1.0f : z0 <= 0.f ? 0.f : z0, z1 > 0.f ? 1.0f : z1 <= 0.f ? 0.f : z1);          // NaN of NaN
     }
   }
   yh = mul2(mul2(mul2(c1, df), u), d);

@@ -174,3 +174,43 @@ def test_low_precision_gradient_exchange_arithmetic_on_device(transport, world):
     res = torch.empty(rows, cols, device="cuda")
     dp.exchange_weight_grads([torch.from_numpy(parts[0]).cuda()], [res], transport=transport)
     assert np.abs(res.cpu().numpy() - F.decode(F.quantise_codes(parts[0].astype(np.float64), fmt), fmt)).max() <= 1e-6
+
+
+@pytest.mark.parametrize("fn", ["relu", "tanh", "sigmoid", "gelu", "silu"])
+@pytest.mark.parametrize("in_fmt,out_fmt", [("f32", "f32"), ("bf16", "bf16"), ("fp16", "e4m3"), ("bf16", "e5m2")])
+@pytest.mark.parametrize("shape,ld", [((5, 1000), None), ((3, 33), 64)])
+def test_activations_keep_a_nan(fn, in_fmt, out_fmt, shape, ld):
+    """A NaN of the pre-activation is one of the result and (but for relu, whose slope there is 0) of the gradient, and of no other element."""
+    L, synth = _lib()
+    h = U.to_device(synth.normal(8, 0, shape), in_fmt, ld)
+    h[1, 7] = float("nan")
+    g = U.to_device(np.ones(shape, np.float32), in_fmt, ld)
+    out = U.empty(shape[0], shape[1], out_fmt, ld)
+    L.us_activation_fwd(fn, h, 0.875, 1.5, out)
+    nan = torch.isnan(out.float())
+    assert nan[1, 7] and int(nan.sum()) == 1
+    L.us_activation_bwd(fn, h, g, 0.875, 1.5, out)
+    nan = torch.isnan(out.float())
+    assert int(nan.sum()) == (fn != "relu") and (out[1, 7] == 0 if fn == "relu" else nan[1, 7])
+
+
+@pytest.mark.parametrize("act", ["RELU", "TANH", "SIGMOID", "GELU"])
+@pytest.mark.parametrize("fmt,out_fmt", [("bf16", "bf16"), ("bf16", "f32"), ("e4m3", "e4m3")])
+def test_epilogues_keep_a_nan(act, fmt, out_fmt):
+    """The same of the activation that is fused into a linear op, forward and backward."""
+    L, synth = _lib()
+    b, m, n = 200, 80, 160
+    X, W = (U.to_device(synth.normal(9, i, s), fmt) for i, s in enumerate(((b, m), (m, n))))
+    if fmt == "e4m3":
+        X.view(torch.uint8)[3, 2] = 0x7f
+    else:
+        X[3, 2] = float("nan")
+    aux, out, ws = U.empty(b, n, "bf16"), U.empty(b, n, out_fmt), L.new_workspace()
+    L.us_linear_fwd(X, W, m ** -0.5, out, ws, L.epilogue(act=getattr(L, "US_ACT_" + act), act_in_scale=0.875, act_out_scale=1.5, aux=aux))
+    nan = torch.isnan(out.float())
+    assert nan[3].all() and int(nan.sum()) == n and torch.isnan(aux[3]).all()
+    dX, G = U.empty(b, n, out_fmt), U.to_device(synth.normal(9, 2, (b, m)), fmt)
+    Wt = U.to_device(synth.normal(9, 3, (n, m)), fmt)
+    L.us_linear_bwd_x(G, Wt, m ** -0.5, dX, ws, L.epilogue(act=getattr(L, f"US_ACT_{act}_GRAD"), act_in_scale=0.875, act_out_scale=1.5, aux=aux))
+    nan = torch.isnan(dX.float())
+    assert int(nan.sum()) == (0 if act == "RELU" else n) and ((dX[3].float() == 0).all() if act == "RELU" else nan[3].all()) and L.us_workspace_status(ws) == 0

@@ -324,3 +324,21 @@ def test_values_near_zero_and_far_from_it(case, s_in, fn):
     z = s_in * h
     value = _gate_and_slope(fn, z)[0].repeat(b, 0)
     _close(A, value, (6 * np.abs(z) + 96) * 2.0 ** -24 * np.abs(value), act, "A")
+
+
+@pytest.mark.parametrize("fn", ["gelu", "relu", "tanh", "sigmoid", "silu"])
+@pytest.mark.parametrize("shape", ["token", "pair"])
+def test_every_gate_keeps_a_nan(fn, shape):
+    L, synth = _lib()
+    b, m, f, n = SHAPES[shape]
+    bf = lambda i, r, c: U.to_device(synth.normal(17, i, (r, c)), "bf16", _pitch(c))
+    X, Wg, Wu, G, W2, H, V = bf(0, b, m), bf(1, m, f), bf(2, m, f), bf(3, b, n), bf(4, f, n), bf(5, b, f), bf(6, b, f)
+    Wg[0, 5] = H[0, 3] = float("nan")
+    A, dH, dU = (U.empty(b, f, "bf16", _pitch(f)) for _ in range(3))
+    ws = L.new_workspace()
+    L.us_ffn_gated_fwd(fn, X, Wg, Wu, m ** -0.5, A, ws)
+    L.us_ffn_gated_bwd(fn, G, W2, n ** -0.5, H, V, dH, dU, ws)
+    assert L.us_workspace_status(ws) == 0
+    nan = torch.isnan(A)
+    assert nan[:, 5].all() and int(nan.sum()) == b
+    assert all(torch.isnan(t[0, 3]) and int(torch.isnan(t).sum()) == 1 for t in (dH, dU))
