@@ -857,7 +857,7 @@ def us_qk_norm_fwd(X, w, Y, head_width, eps, table=None, positions=None, start=0
     if len(Y) != n or (w is not None and len(w) != n):
         raise ValueError("one entry per matrix is wanted")
     if positions is not None:
-        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == X[0].size(0)
+        assert positions.is_cuda and positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == X[0].size(0)
     _check("us_qk_norm_fwd", _entry("us_qk_norm_fwd")(n, X, w, Y, head_width, eps, table, positions, start, period, neighbours, _stream(stream)))
     return Y
 
@@ -873,7 +873,7 @@ def us_qk_norm_bwd(X, w, G, dX, dw, head_width, eps, ws, beta_x=1.0, beta_w=None
     if len(G) != n or len(dX) != n or (w is not None and len(w) != n) or (dw is not None and len(dw) != n) or (beta_w is not None and len(beta_w) != n):
         raise ValueError("one entry per matrix is wanted")
     if positions is not None:
-        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == X[0].size(0)
+        assert positions.is_cuda and positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == X[0].size(0)
     _check("us_qk_norm_bwd", _entry("us_qk_norm_bwd")(
         n, X, w, G, dX, dw, beta_w, head_width, eps, beta_x, table, positions, start, period, neighbours, ws, ws if ws is not None else 0, _stream(stream)))
     return dX, dw

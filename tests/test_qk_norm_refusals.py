@@ -97,3 +97,12 @@ def test_starts_near_the_end_of_64_bits():
     assert fwd(period=last) == 5 and fwd(period=last, start=24) == 5 and fwd(period=last, start=25) == 1
     # where the positions are on the device, or nothing is turned, start is not read
     assert fwd(start=last, pos=0x40000) == 5 and fwd(start=last, table=None) == 5
+
+
+def test_positions_in_host_memory():
+    """The kernels would read them through an address that is none on the device."""
+    x, at = torch.zeros(4, 128, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        L.us_qk_norm_fwd([x], None, [x], 64, 0.0, positions=at, stream=0)
+    with pytest.raises(AssertionError):
+        L.us_qk_norm_bwd([x], None, [x], [x], None, 64, 0.0, None, positions=at, stream=0)
