@@ -71,8 +71,7 @@ struct GatedShape {
   // Forward: B is N-major, in chunks of rows of K: 128 bytes wide, or the columns of one projection where they are fewer
   static constexpr int kChunkRow = CG == 2 || HC * ES >= 128 ? 128 : HC * ES;
   static constexpr int kChunkBytes = (kStageKBytes / ES) * kChunkRow;
-  static constexpr int kWarpCols = HC / (kEW / 4);    // hidden columns of an epilogue warp, worked in slices
-  static constexpr int kSlice = kWarpCols < 32 ? kWarpCols : 32;
+  static constexpr int kWarpCols = HC / (kEW / 4);    // hidden columns of an epilogue warp
 };
 
 // ---------------------------------------------------------------- the gate
@@ -170,14 +169,12 @@ __device__ __forceinline__ void gate_grads2(f32x2 x, f32x2 u, f32x2 d, float act
   yu = mul2(mul2(c0, f), d);
 }
 
-// What is computed from v[FROM .. FROM + COUNT - 1] is computed behind this, and behind the stores before it: a slice is worked on in groups of
-// columns, because all of it at once does not fit the registers.
-template <int FROM, int COUNT, class T, int N>
-__device__ __forceinline__ void from_here(T (&v)[N]) {
+// What is computed from v is computed behind this, and behind the stores before it: of the halves of a unit one after the other, because both at once do not
+// fit the registers.
+template <int N>
+__device__ __forceinline__ void from_here(uint32_t (&v)[N]) {
 #pragma unroll
-  for (int i = FROM; i < FROM + COUNT; ++i) {
-    if constexpr (std::is_same_v<T, float>) asm volatile("" : "+f"(v[i])); else asm volatile("" : "+r"(v[i]));
-  }
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(v[i]));
 }
 template <int N, class G>
 __device__ __forceinline__ void unrolled(G g) {              // g(0) .. g(N - 1), the argument as a constant
@@ -195,7 +192,7 @@ __device__ __forceinline__ void with_gate(int fn, G g) {
   else if (fn == US_FN_GELU) g(std::integral_constant<int, US_FN_GELU>());
   else g(std::integral_constant<int, US_FN_RELU>());
 }
-// ---------------------------------------------------------------- a lane's S columns of a row
+// ---------------------------------------------------------------- a lane's S columns of a row (16 or 32)
 // S results rounded to dt, packed.
 template <int S>
 __device__ __forceinline__ void pack_row(int dt, const float (&y)[S], uint32_t (&w)[S / 2]) {
@@ -294,7 +291,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
              const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_dh,
              const __grid_constant__ CUtensorMap tm_du, const GatedParams p) {
   using S = GatedShape<BWD, ES, HC, CG, BOXED>;
-  constexpr int kEW = S::kEW, kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN, kSl = S::kSlice, kSlices = S::kWarpCols / kSl;
+  constexpr int kEW = S::kEW, kBK = kStageKBytes / ES, kTileM = kBM * CG, kN = S::kN;
   constexpr uint32_t kTmemCols = 2 * kN;
   const uint32_t a_bytes = CG == 2 ? (uint32_t)(kBM * kStageKBytes) : p.a_bytes, stage_bytes = a_bytes + S::kBBytes;
   const int stages = CG == 2 ? S::kStages : p.stages;
@@ -463,6 +460,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
     bool ok = true;
     if constexpr (BOXED) {
       // A warp has 32 hidden columns of a tile; A and the copies leave through a box each.
+      static_assert(S::kWarpCols == 32, "a box holds 32 columns");
       const uint32_t box_a = smem_base + (uint32_t)(kRoom - S::kEpiBytes + (warp - 2) * S::kEpiBytes / kEW), box_h = box_a + 1024u * out_es, box_u = box_h + 1024u * kept_es;
       const uint32_t out_sw = out_es == 2 ? (uint32_t)((lane >> 1) & 3) : 0u, kept_sw = kept_es == 2 ? (uint32_t)((lane >> 1) & 3) : 0u;
       for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
@@ -528,46 +526,45 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
       if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();
       __syncwarp();
     } else if constexpr (!BWD) {
+      constexpr int kCols = S::kWarpCols;                        // of a warp: all at once in its registers
+      static_assert(kCols <= 32, "a lane's columns of both projections would not fit its registers");
       for (int tile = unit; ok && tile < num_tiles; tile += num_units, ++local) {
-        int row, col0;
-        place(tile, row, col0);
+        int row, col;
+        place(tile, row, col);
         const uint32_t acc = local & 1u, acc_phase = (local >> 1) & 1u;
         ok = wait_bounded(acc_full_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         ptx::tc_fence_after_sync();
         const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * kN + part * S::kWarpCols;
-#pragma unroll 1
-        for (int sl = 0; sl < kSlices; ++sl) {
-          const int col = col0 + sl * kSl, cols = row < p.M ? p.N - col : 0;
-          uint32_t r0[kSl], r1[kSl];
-          ptx::tmem_ld_32x32_issue(t_row + sl * kSl, r0);
-          ptx::tmem_ld_32x32_issue(t_row + HC + sl * kSl, r1);
-          ptx::tmem_ld_fence(r0);
-          ptx::tmem_ld_fence(r1);
-          if (sl + 1 == kSlices) release_acc(acc, tile);          // the values are in registers
-          float a[kSl], b[kSl];
-          uint32_t w[kSl / 2];
+        const int cols = row < p.M ? p.N - col : 0;
+        uint32_t r0[kCols], r1[kCols];
+        ptx::tmem_ld_32x32_issue(t_row, r0);
+        ptx::tmem_ld_32x32_issue(t_row + HC, r1);
+        ptx::tmem_ld_fence(r0);
+        ptx::tmem_ld_fence(r1);
+        release_acc(acc, tile);                                  // the values are in registers
+        float a[kCols], b[kCols];
+        uint32_t w[kCols / 2];
 #pragma unroll
-          for (int i = 0; i < kSl; i += 2) {
-            unpack2(mul2(scale2, pack2(__uint_as_float(r0[i]), __uint_as_float(r0[i + 1]))), a[i], a[i + 1]);
-            unpack2(mul2(scale2, pack2(__uint_as_float(r1[i]), __uint_as_float(r1[i + 1]))), b[i], b[i + 1]);
-          }
-          if (p.h) {
-            pack_row<kSl>(p.kept_dt, a, w);
-            put_row<kSl>(p.h + (row * p.h_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
-            pack_row<kSl>(p.kept_dt, b, w);
-            put_row<kSl>(p.u + (row * p.u_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
-          }
-          float y[kSl];
-          with_gate(p.fn, [&](auto fn) {
-#pragma unroll
-            for (int i = 0; i < kSl; i += 2)
-              unpack2(mul2(mul2(gate_value2<decltype(fn)::value>(pack2(a[i], a[i + 1]), in2, nl2), c0), pack2(b[i], b[i + 1])), y[i], y[i + 1]);
-          });
-          pack_row<kSl>(p.out_dt, y, w);
-          put_row<kSl>(p.o0 + (row * p.o0_ld + col) * out_es, out_es, w, cols, p.out_sectors);
+        for (int i = 0; i < kCols; i += 2) {
+          unpack2(mul2(scale2, pack2(__uint_as_float(r0[i]), __uint_as_float(r0[i + 1]))), a[i], a[i + 1]);
+          unpack2(mul2(scale2, pack2(__uint_as_float(r1[i]), __uint_as_float(r1[i + 1]))), b[i], b[i + 1]);
         }
+        if (p.h) {
+          pack_row<kCols>(p.kept_dt, a, w);
+          put_row<kCols>(p.h + (row * p.h_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
+          pack_row<kCols>(p.kept_dt, b, w);
+          put_row<kCols>(p.u + (row * p.u_ld + col) * kept_es, kept_es, w, cols, p.kept_sectors);
+        }
+        float y[kCols];
+        with_gate(p.fn, [&](auto fn) {
+#pragma unroll
+          for (int i = 0; i < kCols; i += 2)
+            unpack2(mul2(mul2(gate_value2<decltype(fn)::value>(pack2(a[i], a[i + 1]), in2, nl2), c0), pack2(b[i], b[i + 1])), y[i], y[i + 1]);
+        });
+        pack_row<kCols>(p.out_dt, y, w);
+        put_row<kCols>(p.o0 + (row * p.o0_ld + col) * out_es, out_es, w, cols, p.out_sectors);
       }
     } else {
       // Units of 32 columns, whose copies arrive in a slot's boxes ahead of the accumulator.  A lane's row of a box is read and written by that lane, 16-byte chunk c at c ^ the
@@ -641,7 +638,7 @@ gated_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ C
                 ptx::tmem_ld_fence(r0);
                 if (decltype(half)::value == 1 && at + 32 >= end) release_acc(acc, tile);            // the values are in registers
                 f32x2 yh[8], yu[8];
-                from_here<0, 16>(r0);
+                from_here(r0);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                   gate_grads2<decltype(fn)::value>(widen2<decltype(kept)::value>(rh, i), widen2<decltype(kept)::value>(ru, i),

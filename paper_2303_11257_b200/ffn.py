@@ -450,7 +450,8 @@ class UnitScaledGatedFFN(UnitScaledFFN):
 
     W1 = [Wg Wu] is one [d x 2 f] matrix, and dW1 its gradient.  kept: the type in which h and u wait for the backward pass, "bf16",
     "fp16", or "e4m3": checkpoints of 8 bits, half the bytes, which at unit scale need no factor.  f must be a multiple of 16.  step(), forward() and
-    backward() are used as those of UnitScaledFFN; a step is four launches (three GEMMs of the second layer and the first layer's gradients are one)."""
+    backward() are used as those of UnitScaledFFN.  A step is four launches: the casts, the hidden layer forward and backward, and the four GEMMs that remain, which
+    are two launches where they share contractions (launches_per_step)."""
 
     def __init__(self, T: int, d: int, f: int, scales: GatedScales | None = None, operand: str = "fp8", gate: str = "silu", kept: str = "bf16",
                  io_dtype=torch.bfloat16, device="cuda", tau: float = 0.5):
