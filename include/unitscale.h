@@ -328,7 +328,8 @@ typedef enum { US_FN_GELU = 0, US_FN_RELU = 1, US_FN_TANH = 2, US_FN_SIGMOID = 3
  *              dU = beta_u * f(act_in_scale * H) * dA
  *              dH = beta_h * act_in_scale * f'(act_in_scale * H) * U * dA
  *
- * A is formed from the unrounded h and u; the gradients take H and U as stored, and dA is never rounded.  The unit-scaling values
+ * A is formed from the unrounded h and u; the gradients take H and U as stored, and dA is never rounded.  The values and
+ * slopes of sigmoid and tanh and the values of silu are right to a few 2^-22 (1 + |z|) of themselves, gelu and slopes near their zeros to about 3e-7.  The unit-scaling values
  * are act_out_scale = beta_u = 1 / rms f(Z) and beta_h = 1 / rms f'(Z) (us_scales_gated).  Wg and Wu may be the halves of one [m x 2 f] matrix, dH and dU those of one [b x 2 f]
  * gradient: the rest of the backward pass is then us_linear_bwd_x and us_linear_bwd_w on these.
  *
@@ -362,6 +363,7 @@ us_status us_test_ffn_gated_bwd_starved(const us_mat* G, const us_mat* W2, const
  *                  silu(x) = x sigmoid(x) or gelu (table rows relu / gelu / tanh / sigmoid: alpha = 1 / std f(Z), Z ~ N(0,1));
  * us_activation_bwd  dH = beta * s_in * f'(s_in * H) * dA (beta = 1 / rms f'(Z)); relu'(0) = 0.  A NaN of H is one of A for every f, and one of dH but
  *                  for relu, whose slope is 0 there (so in the epilogues of linear ops; us_ffn_gated_bwd keeps it for relu too).
+ *                  tanh, sigmoid, gelu and their slopes are off by up to about 3e-7 absolutely, tanh near zero and gelu's tail too.
  *                  US_FN_GELU gives the same values as us_gelu_fwd / us_gelu_bwd.
  * us_weighted_add  out = alpha * sum_i gamma_i * src_i over count (1..8) tensors of one shape (table row
  *                  weighted_add: alpha = (sum_i gamma_i^2)^-1/2 keeps unit scale; each input's gradient

@@ -10,9 +10,10 @@
 // Wu's.)  Neither projection is written unless the caller wants the copies the backward pass reads; those are 16-bit or, at unit scale, E4M3
 // without a factor.  Backward, a tile is HC columns of dA, from which the epilogue makes both gradients with the copies it has fetched.
 //
-// Bound: forward the tensor pipe and, over seconds, power: 8192 x 1024 x 4096 BF16 with copies 125 us (1.10 PFLOP/s; 98 in a burst), 16384 x 2048 x 8192 FP8 with E4M3
-// copies 440 us (2.5 PFLOP/s).  Backward, BF16 85 us (268 MB of copies and gradients beside 69 GFLOP: the SM's memory path), FP8 from E4M3 copies 53 us (the epilogue's
-// instructions).  One token of 1024 x 4096 in BF16 5.4 us.
+// Bound, us from one GPU to another, launches over seconds (power cap) / in a burst: forward the tensor pipe and power: 8192 x 1024 x 4096 BF16 with copies 120 to 133 / 98 to 110
+// (F16 140 / 115), FP8 with copies in BF16 79 / 65, 16384 x 2048 x 8192 FP8 with copies in E4M3 429 to 478 / 407 (2.3 to 2.7 PFLOP/s).  Backward, BF16 85 to 90 / 75 (268 MB of copies and gradients beside
+// 69 GFLOP: the SM's memory path), FP8 from E4M3 copies 53 to 56 / 46, from BF16 copies 63 / 54: the epilogue, by the latency of its chain (no unit above 55 %; a warp waits for fixed latencies, the
+// accumulator's loads and other warps in turn).  One token of 1024 x 4096 in BF16 5.3, FP8 4.1 in a graph; 64 tokens the same.
 //
 // Every wait is bounded as in the other GEMM kernels.
 #include <cuda.h>
@@ -28,6 +29,7 @@ namespace {
 
 // Epilogue warps.  Of a CTA pair's tiles sixteen a CTA, whose arithmetic is the longest part of an FP8 tile; backward with 16-bit operands, where the MMAs
 // take twice as long, eight.  (8192 x 1024 x 4096 backward, us, sixteen / eight: FP8 54.0 / 57.5, BF16 90.9 / 88.3.)
+// (With sixteen the forward kernel whose results leave by the lanes spills 28 bytes at the 96 registers that a thread has; with 60 bytes it took the same time.)
 __host__ __device__ constexpr bool gated_few(bool bwd, int es, int cg) { return cg == 1 || (bwd && es == 2); }
 __host__ __device__ constexpr int gated_ew(bool bwd, int es, int cg) { return gated_few(bwd, es, cg) ? 8 : 16; }
 constexpr int kRoom = 229376;                 // shared memory for stages and the epilogue's boxes
@@ -35,7 +37,8 @@ constexpr int kMostStages = 16;
 // Backward, an epilogue warp has slots for the copies of h and u that arrive and the dH and dU that leave, in boxes of 32 rows x 32 columns.  Where copies and gradients have one
 // width a gradient leaves from the box of its copy, and there are three slots: a store has a unit's time to read one before it is filled again (8192 x 1024 x 4096, two / three / four slots, the last in a stage's room:
 // BF16 92.7 / 84.7 / 91.8 us, FP8 56.8 / 53.3 / 54.8).  Elsewhere a slot has
-// boxes for both (6144 bytes), in as many slots as fit.
+// boxes for both (6144 bytes), in as many slots as fit: two of eight warps, one of sixteen (FP8 from 16-bit copies, 63 us at that size, where the bytes take 33: the copies of
+// a unit are asked for when the one before has been stored).
 constexpr int kMostSlots = 3;
 __host__ __device__ constexpr int epi_room(int ew) { return ew == 16 ? 6144 : 12288; }      // bytes of a warp
 

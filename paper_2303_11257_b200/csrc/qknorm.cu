@@ -4,14 +4,16 @@
 //   forward    r = 1 / sqrt(mean x^2 + eps),  n = w x r,  y = R n          R: each pair (a, b) of the rotated features -> (a c - b s, b c + a s)
 //   backward   n' = R^T g,  u = w n',  dx = beta_x r (u - x r mean(u x r)),  dw = beta_w sum n' x r
 //
-// Every element is read once and written once; the kernels are bound by the instructions they issue before they are by HBM (11 to 14 a value).  8192 tokens of 16 + 16 heads of 64
-// in BF16: forward 13.5 us (5.0 TB/s), backward 22.0 (4.6 TB/s); 16384 tokens of 32 + 8 heads of 128 into E4M3 58 us (4.5 TB/s).
+// Every element is read once and written once.  The kernels are bound by the latency of what they issue (11 to 14 instructions a value) before they are by HBM: 59 % of the issue slots are used, with 16 warps
+// an SM that wait for results of fixed latency, then for shared memory and shuffles, hardly for global memory.  8192 tokens of 16 + 16 heads of 64
+// in BF16: forward 13.5 us (5.0 TB/s), backward 22.0 (4.6 TB/s), in float32 34.4 and 54.6 (3.9 and 3.7 TB/s); 16384 tokens of 32 + 8 heads of 128 into E4M3 58 us (4.5 TB/s).
 // A head is held by a group of G lanes (a power of two), each with two chunks of eight features that hold whole pairs -- features i .. i + 7 and their partners half a
 // rotation further, or sixteen neighbours -- so that the rotation needs no exchange and one group sum (forward) or two (backward) are all that lanes tell one another.  A warp's
 // unit is some steps of 32 / G heads of one row, whose cosines and sines it holds in registers over all of them; the norm's weight it holds for the whole launch,
 // since a CTA works for one part (queries or keys) only.  Weight gradients are summed in the registers of the lane that has the feature, then over groups, warps and, in a second
 // launch, CTAs, in a fixed order without atomics.
-// Rows that are not on 16-byte boundaries, and widths that are no multiple of eight, take the general kernels: a warp a head, through shared memory.
+// Rows that are not on 16-byte boundaries, widths that are no multiple of eight, matrices of several types and turns of a number of features that is no multiple of 16 (neighbours: 8) take the general kernels: a warp a head,
+// through shared memory, one value a lane at a time (8192 tokens of 16 + 16 heads of 72 in BF16, all turned: forward 294 us, backward 430; with neighbouring pairs, which the vector kernels take, 26 and 43).
 #include <cuda.h>
 
 #include <algorithm>
@@ -623,7 +625,9 @@ us_status prepare(Call& c, int count, const us_mat* X, const us_mat* w, const us
   return US_OK;
 }
 
-// Deals the CTAs to the parts by their heads; returns the grid.
+// Deals the CTAs to the parts by their heads; returns the grid.  A part's work is its units, per_block heads each, so that parts get what they need where their heads fill units; one whose
+// heads do not (a unit holds heads of one row only) has more units than its heads say, and ends last.  (8192 tokens in BF16, heads of 64, forward / backward us: 16 + 16 heads 13.4 / 22.2,
+// 16 + 4 19.2 / 31.1, 16 + 1 54.7 / 82.9; of 128: 32 + 8 30.9 / 50.5, 32 + 4 37.9 / 59.8.)
 int deal(QkArgs& a, int per_block, int most) {
   int64_t all = 0;
   for (int k = 0; k < a.count; ++k) {
