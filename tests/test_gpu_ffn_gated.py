@@ -342,3 +342,24 @@ def test_every_gate_keeps_a_nan(fn, shape):
     nan = torch.isnan(A)
     assert nan[:, 5].all() and int(nan.sum()) == b
     assert all(torch.isnan(t[0, 3]) and int(torch.isnan(t).sum()) == 1 for t in (dH, dU))
+
+
+@pytest.mark.parametrize("fn", ["sigmoid", "tanh"])
+@pytest.mark.parametrize("act,grad", [("bf16", "bf16"), ("e4m3", "e5m2")])
+def test_limits_of_sigmoid_and_tanh(fn, act, grad):
+    """Arguments of +-100, +-1e30 and infinity: the limits, with slopes of nothing, and no NaN."""
+    L, _ = _lib()
+    b, f, ws = 40, 96, L.new_workspace()
+    h = torch.tensor([100.0, 1e30, float("inf")] * 16, device="cuda")
+    H = torch.cat([h, -h]).expand(b, f).contiguous().bfloat16()
+    one = lambda r, fmt: U.to_device(np.float32(np.eye(1, 16)).repeat(r, 0), fmt)
+    dH, dU = U.empty(b, f, grad), U.empty(b, f, grad)
+    L.us_ffn_gated_bwd(fn, one(b, grad), one(f, act), 1.0, H, torch.ones_like(H), dH, dU, ws)
+    low = 0.0 if fn == "sigmoid" else -1.0
+    assert (dH.float() == 0).all() and (dU.float()[:, :48] == 1).all() and (dU.float()[:, 48:] == low).all()
+    if act == "bf16":                                             # (8-bit operands have no infinities)
+        X, Wg, Wu, A = one(b, act), U.empty(16, f, act), U.empty(16, f, act), U.empty(b, f, act)
+        Wg[0], Wu[0] = H[0].clamp(-1e38, 1e38), 1.0
+        L.us_ffn_gated_fwd(fn, X, Wg, Wu, 10.0, A, ws)             # (infinities by the scale: an infinite weight times a zero of X is NaN)
+        assert (A.float()[:, :48] == 10).all() and (A.float()[:, 48:] == 10 * low).all()          # u = 10, too
+    assert L.us_workspace_status(ws) == 0
