@@ -608,6 +608,61 @@ us_status us_qk_norm_bwd(int count, const us_mat* X, const us_mat* w, const us_m
                          int64_t period, int neighbours, void* ws, size_t ws_bytes, void* stream);
 us_status us_rotary_table(const us_mat* table, double base, double scale, int64_t first, void* stream);
 
+/* ------------------------------------------------------------ gradients of biases
+ *
+ * us_bias_grad: db_j = beta * sum over rows of G_ij, the gradient of a bias added to every row (us_linear_fwd_bias; a bias is a cut-edge
+ * and takes its own factor, beta = b^-1/2 for b rows), for count (1..8) matrices in one launch.  G [b x n]: any us_dtype, any ld >= n, any
+ * number of rows (none: db = 0); db (1 x n): F32, BF16 or F16; beta: NULL = ones.  G, beta, db: host arrays of count elements.  Pointers
+ * need the natural alignment of their elements (rows on 16-byte boundaries are read in 16-byte pieces).  Sums are float32, formed without
+ * atomics in an order that depends on the sizes alone.  Outputs must not overlap one another or an input.
+ */
+us_status us_bias_grad(int count, const us_mat* G, const float* beta, const us_mat* db, void* stream);
+
+/* ------------------------------------------------------------ optimiser
+ *
+ * us_grad_norm: out[0] = norm = sqrt(sum of the squares of all elements of all matrices), out[1] = min(1, max_norm / norm), the factor that
+ * clips them to max_norm (positive; INFINITY: no clipping); where the norm is not finite, out[1] is NaN.  grads: host array of count (any
+ * number from 1 on) F32, BF16 or F16 matrices, any ld >= cols, natural alignment.  out: two float32 in device memory.  Squares are added
+ * in float32 eight at a time, then in float64, in an order that depends on the sizes and the device alone.  ws: device workspace of
+ * us_grad_norm_workspace_bytes() bytes, 16-byte aligned, zeroed once by the caller before its first use, that no call at the same time
+ * uses.  One launch for up to 640 matrices.
+ */
+size_t us_grad_norm_workspace_bytes(void);
+us_status us_grad_norm(int count, const us_mat* grads, float max_norm, float* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * us_adamw: one step of AdamW (Adam with decoupled weight decay) over count tensors (any number from 1 on) at once, in place:
+ *
+ *   g = grad_factor * grad,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   param = param - lr' weight_decay param - lr' (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),    lr' = lr * *lr_factor * tensor's lr_factor
+ *   copy  = copy_scale * param rounded to the copy's format (FP8 saturates): the operand that the next step's matmuls read (us_cast_multi)
+ *
+ * param [rows x cols]: F32; grad of that shape: F32, BF16 or F16; copy (ptr NULL: none) of that shape: any us_dtype; any ld >= cols.
+ * m and v hold rows * cols elements in row-major order without padding, in any shape, and are alike:
+ *   F32    as in the formula (zeros before the first step)
+ *   E4M3   states in 8 bits.  Every 256 consecutive elements are a block, the last one shorter, with a scale of its own: m = m_scale * code
+ *          and sqrt(v) = v_scale * code.  After a step a block's scale is its largest |m| (sqrt(v)) / 448 and codes are the nearest ones,
+ *          but a v above 0 has at least the smallest code, so that no step is divided by eps alone.  A block whose largest |m| or
+ *          sqrt(v) is at most 2^-100 becomes zeros.  A step is made from the unrounded m and v.  m_scale, v_scale: F32, one element a
+ *          block, without padding.  All zeros before the first step.
+ * Tensors of one call may differ in all of this; none may be named twice or overlap another.
+ *
+ * t = step[0] + 1.  step: two 64-bit integers in device memory, the number of steps made and a zero that the library uses; the call raises
+ * step[0] at its end, so that a captured call counts on when it is replayed.  Calls that share it must not run at the same time.
+ * lr_factor, grad_factor: NULL (1), or a float32 in device memory (a schedule; out[1] of us_grad_norm).  Where *grad_factor is not finite the
+ * call changes nothing, step included.  A NaN or infinite gradient makes NaN of its own element (of its block of 8-bit states).
+ *
+ * lr >= 0, 0 <= beta < 1, eps > 0 (also once rounded to float32).  Arithmetic in float32; 1 - beta and log(beta) are formed in float64.  Pointers
+ * need the natural alignment of their elements; F32 tensors on 16-byte boundaries (copies, gradients and codes: of four elements), with rows that are dense
+ * or of a multiple of four columns and so padded, are the fast ones.  One launch for up to 240 tensors; tensors without elements are skipped.
+ */
+typedef struct {
+  us_mat param, grad, m, v, m_scale, v_scale, copy;
+  float copy_scale, lr_factor, weight_decay;
+} us_adamw_tensor;
+us_status us_adamw(int count, const us_adamw_tensor* tensors, double lr, double beta1, double beta2, double eps, const float* lr_factor,
+                   const float* grad_factor, int64_t* step, void* stream);
+
 /* ------------------------------------------------------------ quantisation diagnostics
  *
  * us_quant_stats: for v = scale * src (one float32 multiply per element) and a storage format fmt

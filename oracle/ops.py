@@ -490,3 +490,62 @@ def gated_ffn_block(X, W1, W2, G, gate: str, tau: float = 0.5, operand: str = "f
     r.dX, _, _ = apply_epilogue(linear_bwd_x(r.dHq, r.W1q, (2 * f) ** -0.5), ep5, io_dtype)
     r.dW1, _, _ = apply_epilogue(linear_bwd_w(r.Xq, r.dHq, T ** -0.5), None, "f32")
     return r
+
+
+# --------------------------------------------------------------------------- biases and the optimiser's step
+
+def linear_bias_fwd(X, W, alpha, bias):
+    """alpha * X W + bias, the bias added to every row."""
+    return linear_fwd(X, W, alpha) + np.asarray(bias, np.float64).reshape(1, -1)
+
+
+def bias_grad(G, beta):
+    """Gradient of a bias added to every row: beta * the column sums of G."""
+    return _f32(beta) * np.asarray(G, np.float64).sum(axis=0)
+
+
+def grad_norm(grads, max_norm):
+    """(norm, factor): 2-norm of all gradients together and the factor that clips them to max_norm; NaN where the norm is not finite."""
+    norm = math.sqrt(sum(float((np.asarray(g, np.float64) ** 2).sum()) for g in grads))
+    if not math.isfinite(norm):
+        return norm, math.nan
+    return norm, min(1.0, _f32(max_norm) / norm) if norm > 0 else 1.0
+
+
+@dataclass
+class AdamWStep:
+    p: np.ndarray
+    m: np.ndarray
+    v: np.ndarray
+    update: np.ndarray         # what the gradient's part of the step took off p
+    decayed: np.ndarray        # what weight decay took off p
+    denominator: np.ndarray
+
+
+def adamw_step(p, g, m, v, t, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, factor=1.0) -> AdamWStep:
+    """Step number t (from 1 on) of AdamW in float64, from the moments m and v as they are held."""
+    p, g, m, v = (np.asarray(x, np.float64) for x in (p, g, m, v))
+    b1, b2 = betas
+    g = factor * g
+    m = b1 * m + (1.0 - b1) * g
+    v = b2 * v + (1.0 - b2) * g * g
+    den = np.sqrt(v / (1.0 - b2 ** t)) + eps
+    update, decayed = lr * (m / (1.0 - b1 ** t)) / den, lr * weight_decay * p
+    return AdamWStep(p - decayed - update, m, v, update, decayed, den)
+
+
+def block_codes(x, block: int = 256, positive: bool = False):
+    """(codes, scales) of x in blocks of E4M3 values: scale = largest magnitude / 448, nearest codes (as the values they stand for); positive: a
+    value above 0 has at least the smallest code.  Blocks whose largest magnitude is at most 2^-100 are zeros."""
+    x = np.asarray(x, np.float64).ravel()
+    codes, scales = np.zeros_like(x), []
+    for i in range(0, x.size, block):
+        b = x[i:i + block]
+        most = np.abs(b).max()
+        scales.append(most / 448.0)
+        if most > 2.0 ** -100:
+            c = b * (448.0 / most)
+            if positive:
+                c = np.where(c > 0, np.maximum(c, 2.0 ** -9), c)
+            codes[i:i + block] = F.quantise(c, F.FORMATS["e4m3"])
+    return codes, np.array(scales)

@@ -1,0 +1,177 @@
+// us_bias_grad: gradients of biases, the column sums of the gradients of linear layers' outputs, for several matrices in one launch.
+//
+// Bound by the bytes of G, which the matmuls around it have just written or read.  A cluster of CTAs shares a strip of columns 128 bytes
+// wide: each CTA sums its part of the rows (a thread 16 bytes of every 32nd row), the CTAs' sums meet in shared memory, and
+// every CTA finishes some of the strip's columns.  One launch, no workspace and no atomics.
+#include <algorithm>
+
+#include "common.cuh"
+#include "host.h"
+#include "sm100.cuh"
+
+namespace us {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMostParts = 8, kStripBytes = 128;
+constexpr int kAhead = 8;                    // rows that a thread has in flight
+
+struct BiasPart {
+  const void* g;
+  void* out;
+  int64_t rows, ld;
+  int cols, strip_end;                       // strips up to and including this matrix
+  int g_dt, out_dt, wide;                    // wide: rows start on 16-byte boundaries
+  float beta;
+};
+struct BiasArgs {
+  BiasPart part[kMostParts];
+  int count;
+};
+
+template <int DT>
+__device__ __forceinline__ void add16(const uint4& t, float* acc) {
+  const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (DT == US_F32) {
+      acc[j] += __uint_as_float(w[j]);
+    } else if (DT == US_BF16 || DT == US_F16) {
+      const float2 f = DT == US_BF16 ? unpack_bf16x2(w[j]) : unpack_f16x2(w[j]);
+      acc[2 * j] += f.x; acc[2 * j + 1] += f.y;
+    } else {
+      const float2 lo = unpack_fp8x2((uint16_t)(w[j] & 0xffffu), DT == US_E5M2), hi = unpack_fp8x2((uint16_t)(w[j] >> 16), DT == US_E5M2);
+      acc[4 * j] += lo.x; acc[4 * j + 1] += lo.y; acc[4 * j + 2] += hi.x; acc[4 * j + 3] += hi.y;
+    }
+  }
+}
+
+// Sums of a strip's columns over rows first .. end - 1, one line of `sums` (kStripBytes / element size columns) per warp.
+template <int DT>
+__device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t first, int64_t end, float (*sums)[kStripBytes]) {
+  constexpr int kEs = DT == US_F32 ? 4 : DT == US_BF16 || DT == US_F16 ? 2 : 1, kCols = kStripBytes / kEs, kChunk = 16 / kEs;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (p.wide) {
+    const int chunk = lane & 7, col = strip * kCols + chunk * kChunk, cols = p.cols - col;
+    float acc[kChunk] = {};
+    if (cols > 0) {
+      // The last piece of a row may be cut by the matrix's last column.  It is read whole where a row follows.
+      const bool cut = cols < kChunk;
+      const int64_t whole = cut ? min(end, p.rows - 1) : end;
+      const char* g = static_cast<const char*>(p.g) + (int64_t)col * kEs;
+      const int64_t pitch = p.ld * kEs;
+      int64_t r = first + warp * 4 + (lane >> 3);
+      for (; r + 32 * (kAhead - 1) < whole; r += 32 * kAhead) {
+        uint4 t[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) t[k] = __ldg(reinterpret_cast<const uint4*>(g + (r + 32 * k) * pitch));
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) add16<DT>(t[k], acc);
+      }
+      for (; r < whole; r += 32) add16<DT>(__ldg(reinterpret_cast<const uint4*>(g + r * pitch)), acc);
+      if (r < end) {                                           // the matrix's last row
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+          if (i < cols) acc[i] += load_one(p.g, DT, r * p.ld + col + i);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) {
+      acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 8);
+      acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 16);
+    }
+    if (lane < 8) {
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i) sums[warp][chunk * kChunk + i] = acc[i];
+    }
+  } else {
+    float acc[kCols / 32] = {};
+    for (int64_t r = first + warp; r < end; r += kWarps) {
+#pragma unroll
+      for (int j = 0; j < kCols / 32; ++j) {
+        const int col = strip * kCols + 32 * j + lane;
+        if (col < p.cols) acc[j] += load_one(p.g, DT, r * p.ld + col);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kCols / 32; ++j) sums[warp][32 * j + lane] = acc[j];
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) bias_grad_kernel(const __grid_constant__ BiasArgs a) {
+  __shared__ float sums[kWarps][kStripBytes];
+  __shared__ float mine[kStripBytes];
+  ptx::grid_sync_previous();
+  const int parts = (int)ptx::cluster_nctarank(), rank = (int)ptx::cluster_ctarank();
+  int strip = blockIdx.x / parts, k = 0;
+  while (strip >= a.part[k].strip_end) ++k;
+  const BiasPart& p = a.part[k];
+  if (k > 0) strip -= a.part[k - 1].strip_end;
+  const int64_t first = p.rows * rank / parts, end = p.rows * (rank + 1) / parts;
+  switch (p.g_dt) {
+    case US_F32: strip_sums<US_F32>(p, strip, first, end, sums); break;
+    case US_BF16: strip_sums<US_BF16>(p, strip, first, end, sums); break;
+    case US_F16: strip_sums<US_F16>(p, strip, first, end, sums); break;
+    case US_E4M3: strip_sums<US_E4M3>(p, strip, first, end, sums); break;
+    default: strip_sums<US_E5M2>(p, strip, first, end, sums); break;
+  }
+  __syncthreads();
+  const int cols = kStripBytes / dtype_size(p.g_dt), i = threadIdx.x, col = strip * cols + i;
+  float s = 0.f;
+  if (i < cols) {
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) s += sums[w][i];
+    mine[i] = s;
+  }
+  if (parts > 1) {
+    ptx::cluster_sync();
+    const int share = cols / parts;                            // columns that a CTA finishes
+    if (i < cols && i / share == rank) {
+      s = 0.f;
+      for (int r = 0; r < parts; ++r) s += ptx::ld_cluster(ptx::in_cta(ptx::smem_addr(&mine[i]), (uint32_t)r));
+    }
+    if (i < cols && i / share == rank && col < p.cols) store_one(p.out, p.out_dt, col, p.beta * s);
+    ptx::cluster_meet();                                       // nobody leaves while its sums are being read
+  } else if (i < cols && col < p.cols) {
+    store_one(p.out, p.out_dt, col, p.beta * s);
+  }
+}
+
+us_status check(const us_mat& G, const us_mat& db) {
+  for (const us_mat* m : {&G, &db})
+    if (m->dtype < US_F32 || m->dtype > US_E5M2 || m->rows < 0 || m->cols < 0 || m->rows >= (1ll << 31) || m->cols >= (1ll << 31) - kStripBytes) return US_ERR_INVALID_ARG;
+  if (db.rows != 1 || db.cols != G.cols) return US_ERR_INVALID_ARG;
+  if (db.dtype == US_E4M3 || db.dtype == US_E5M2) return US_ERR_UNSUPPORTED;
+  if (G.cols == 0) return US_OK;
+  if (!db.ptr || (G.rows > 0 && (!G.ptr || G.ld < G.cols))) return US_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(db.ptr) % dtype_size(db.dtype) || (G.rows > 0 && reinterpret_cast<uintptr_t>(G.ptr) % dtype_size(G.dtype))) return US_ERR_ALIGNMENT;
+  return US_OK;
+}
+
+}  // namespace
+}  // namespace us
+
+using namespace us;
+
+extern "C" us_status us_bias_grad(int count, const us_mat* G, const float* beta, const us_mat* db, void* stream) {
+  if (count < 1 || count > kMostParts || !G || !db) return US_ERR_INVALID_ARG;
+  BiasArgs a{};
+  int64_t strips = 0, rows = 0;
+  for (int k = 0; k < count; ++k) {
+    const us_status s = check(G[k], db[k]);
+    if (s != US_OK) return s;
+    BiasPart& p = a.part[k];
+    const int es = dtype_size(G[k].dtype);
+    p.g = G[k].ptr; p.out = db[k].ptr; p.rows = G[k].rows; p.ld = G[k].ld; p.cols = (int)G[k].cols;
+    p.g_dt = G[k].dtype; p.out_dt = db[k].dtype; p.beta = beta ? beta[k] : 1.f;
+    p.wide = reinterpret_cast<uintptr_t>(p.g) % 16 == 0 && (p.rows <= 1 || p.ld * es % 16 == 0);
+    strips += (G[k].cols * es + kStripBytes - 1) / kStripBytes;
+    if (strips * 8 >= (1ll << 31)) return US_ERR_UNSUPPORTED;
+    p.strip_end = (int)strips;
+    rows = std::max(rows, G[k].rows);
+  }
+  if (strips == 0) return US_OK;
+  a.count = count;
+  const int parts = rows <= 64 ? 1 : rows <= 128 ? 2 : rows <= 256 ? 4 : 8;
+  return host::launch(bias_grad_kernel, nullptr, (int)strips * parts, kThreads, 0, parts, static_cast<cudaStream_t>(stream), a);
+}

@@ -120,7 +120,7 @@ T* structure(PyObject* o, size_t count) {
 
 // Pointers to device memory (and handles) are given as addresses or tensors, those to structures and to arrays on the host are not.
 template <class T>
-constexpr bool kAddress = std::is_same_v<T, void*> || std::is_same_v<T, float*> || std::is_same_v<T, const float*> || std::is_same_v<T, const int32_t*>;
+constexpr bool kAddress = std::is_same_v<T, void*> || std::is_same_v<T, float*> || std::is_same_v<T, const float*> || std::is_same_v<T, const int32_t*> || std::is_same_v<T, int64_t*>;
 
 // ARRAY: a pointer to `count` elements in host memory.
 template <class T, bool ARRAY>
@@ -252,7 +252,7 @@ const Known kKnown[] = {
     US_CALL(us_activation_bwd), US_ARRAYS(us_weighted_add, 2), US_CALL(us_softmax_fwd), US_CALL(us_softmax_bwd), US_CALL(us_softmax_xent_fwd),
     US_CALL(us_softmax_xent_bwd), US_CALL(us_layer_norm_fwd), US_CALL(us_layer_norm_bwd), US_CALL(us_linear_fwd_cast), US_ARRAYS(us_linear_group_cast, 2),
     US_CALL(us_layer_norm_fwd_cast), US_CALL(us_layer_norm_bwd_cast), US_ARRAYS(us_qk_norm_fwd, 3), US_ARRAYS(us_qk_norm_bwd, 6), US_CALL(us_rotary_table),
-    US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd),
+    US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd), US_ARRAYS(us_bias_grad, 3), US_ARRAYS(us_grad_norm, 1), US_ARRAYS(us_adamw, 1),
 };
 constexpr size_t kCount = sizeof(kKnown) / sizeof(kKnown[0]);
 PyMethodDef g_calls[kCount];
@@ -392,7 +392,7 @@ PyObject* unchanged(PyObject*, PyObject* const* o, Py_ssize_t n) {
 }
 
 // register_types((us_mat, us_epilogue, us_batch, us_attention_batch, us_attention_bwd_batch, us_attention_bwd_all_batch, us_linear_call,
-// c_float)): the ctypes types of the parameters; every argument is checked against its own
+// us_adamw_tensor, c_float)): the ctypes types of the parameters; every argument is checked against its own
 template <class... T>
 void keep_types(PyObject* types) {
   Py_ssize_t i = 0;
@@ -402,8 +402,8 @@ void keep_types(PyObject* types) {
 }
 PyObject* register_types(PyObject*, PyObject* const* o, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    if (n != 1 || !PyTuple_Check(o[0]) || PyTuple_GET_SIZE(o[0]) != 8) fail(PyExc_TypeError, "register_types((eight types))");
-    keep_types<us_mat, us_epilogue, us_batch, us_attention_batch, us_attention_bwd_batch, us_attention_bwd_all_batch, us_linear_call, float>(o[0]);
+    if (n != 1 || !PyTuple_Check(o[0]) || PyTuple_GET_SIZE(o[0]) != 9) fail(PyExc_TypeError, "register_types((nine types))");
+    keep_types<us_mat, us_epilogue, us_batch, us_attention_batch, us_attention_bwd_batch, us_attention_bwd_all_batch, us_linear_call, us_adamw_tensor, float>(o[0]);
     Py_RETURN_NONE;
   });
 }

@@ -61,6 +61,11 @@ class us_linear_call(C.Structure):
     _fields_ = [("op", C.c_int32), ("a", us_mat), ("b", us_mat), ("scale", C.c_float), ("ep", us_epilogue), ("out", us_mat)]
 
 
+class us_adamw_tensor(C.Structure):
+    _fields_ = [(n, us_mat) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + \
+               [(n, C.c_float) for n in ("copy_scale", "lr_factor", "weight_decay")]
+
+
 US_OP_FWD, US_OP_BWD_X, US_OP_BWD_W = 0, 1, 2
 
 
@@ -162,6 +167,12 @@ def _load() -> C.CDLL:
     lib.us_qk_norm_fwd.restype = lib.us_qk_norm_bwd.restype = lib.us_rotary_table.restype = C.c_int
     lib.us_qk_norm_bwd_workspace_bytes.argtypes = [C.c_int64]
     lib.us_qk_norm_bwd_workspace_bytes.restype = SZ
+    lib.us_bias_grad.argtypes = [C.c_int, MP, C.POINTER(F), MP, V]
+    lib.us_grad_norm.argtypes = [C.c_int, MP, F, V, V, SZ, V]
+    lib.us_adamw.argtypes = [C.c_int, C.POINTER(us_adamw_tensor)] + [C.c_double] * 4 + [V] * 4
+    lib.us_bias_grad.restype = lib.us_grad_norm.restype = lib.us_adamw.restype = C.c_int
+    lib.us_grad_norm_workspace_bytes.argtypes = []
+    lib.us_grad_norm_workspace_bytes.restype = SZ
     lib.us_quant_stats_workspace_bytes.argtypes = []
     lib.us_quant_stats_workspace_bytes.restype = SZ
     lib.us_quant_stats.argtypes = [MP, F, C.c_int, C.c_int, C.c_int, V, V, V, SZ, V]
@@ -196,7 +207,7 @@ except ImportError as e:
     raise ImportError(f"the Python binding is missing or was built for another Python or torch ({e}): build it with "
                       "`python -m paper_2303_11257_b200.build`") from e
 
-_binding.register_types((us_mat, us_epilogue, us_batch, us_attention_batch, us_attention_bwd_batch, us_attention_bwd_all_batch, us_linear_call, C.c_float))
+_binding.register_types((us_mat, us_epilogue, us_batch, us_attention_batch, us_attention_bwd_batch, us_attention_bwd_all_batch, us_linear_call, us_adamw_tensor, C.c_float))
 
 
 def _entry(name: str):
@@ -877,6 +888,71 @@ def us_qk_norm_bwd(X, w, G, dX, dw, head_width, eps, ws, beta_x=1.0, beta_w=None
     _check("us_qk_norm_bwd", _entry("us_qk_norm_bwd")(
         n, X, w, G, dX, dw, beta_w, head_width, eps, beta_x, table, positions, start, period, neighbours, ws, ws if ws is not None else 0, _stream(stream)))
     return dX, dw
+
+
+def us_bias_grad(G, beta, db, stream=None):
+    """db[i] = beta[i] * the column sums of G[i], in one launch: lists of matrices, factors (or None: ones) and bias gradients."""
+    if len(db) != len(G) or (beta is not None and len(beta) != len(G)):
+        raise ValueError("one entry per matrix is wanted")
+    _check("us_bias_grad", _entry("us_bias_grad")(len(G), G, beta, db, _stream(stream)))
+    return db
+
+
+def mats(tensors):
+    """An array of us_mat for us_grad_norm, laid out once for tensors that stay where they are; 1-D tensors are rows."""
+    arr = (us_mat * len(tensors))(*[_vec(t) if t.dim() == 1 else mat(t) for t in tensors])
+    arr._keep_alive = tuple(tensors)
+    return arr
+
+
+def us_grad_norm_workspace_bytes() -> int:
+    return int(_lib.us_grad_norm_workspace_bytes())
+
+
+def us_grad_norm(grads, max_norm, out, ws, stream=None):
+    """out (float32 CUDA tensor of two) = 2-norm of all gradients and the factor that clips them to max_norm; grads: a list of tensors, or what
+    mats() made of it; ws: a uint8 CUDA tensor of us_grad_norm_workspace_bytes() bytes, zeroed before its first use."""
+    assert out.is_cuda and out.dtype is torch.float32 and out.numel() >= 2 and out.is_contiguous()
+    if not isinstance(grads, C.Array):
+        grads = mats(grads)
+    _check("us_grad_norm", _entry("us_grad_norm")(len(grads), grads, max_norm, out, ws, ws, _stream(stream)))
+    return out
+
+
+ADAMW_BLOCK = 256                                             # elements that share a scale of states in 8 bits
+
+
+def adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, copy_scale=1.0, weight_decay=0.0, lr_factor=1.0):
+    """The tensors of a us_adamw call, laid out once: lists with an entry per tensor (1-D tensors are rows).  m_scale, v_scale: for states in 8 bits, else
+    None or a list with Nones; copies: None, or a list with Nones; copy_scale, weight_decay, lr_factor: numbers or lists."""
+    n = len(params)
+    each = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n
+    columns = [list(params), list(grads), list(m), list(v), each(m_scale), each(v_scale), each(copies)]
+    numbers = [each(copy_scale), each(lr_factor), each(weight_decay)]
+    if any(len(c) != n for c in columns + numbers):
+        raise ValueError("one entry per tensor is wanted")
+    if any(t is not None and not t.is_cuda for c in columns for t in c):
+        raise ValueError("expected CUDA tensors")
+    arr = (us_adamw_tensor * n)()
+    for a, ts, ns in zip(arr, zip(*columns), zip(*numbers)):
+        for name, t in zip(("param", "grad", "m", "v", "m_scale", "v_scale", "copy"), ts):
+            if t is not None:
+                setattr(a, name, _vec(t) if t.dim() == 1 else mat(t))
+        a.copy_scale, a.lr_factor, a.weight_decay = ns
+    arr._keep_alive = columns
+    return arr
+
+
+def new_adamw_step(made: int = 0, device="cuda") -> torch.Tensor:
+    """The count of steps that us_adamw keeps on the device: the first element is the number of steps made."""
+    return torch.tensor([made, 0], dtype=torch.int64, device=device)
+
+
+def us_adamw(tensors, step, lr, betas=(0.9, 0.999), eps=1e-8, lr_factor=None, grad_factor=None, stream=None):
+    """One AdamW step over what adamw_tensors() laid out; step: new_adamw_step(); lr_factor, grad_factor: float32 CUDA tensors (one element is read), or None."""
+    assert step.is_cuda and step.dtype is torch.int64 and step.numel() == 2 and step.is_contiguous()
+    assert all(t is None or (t.is_cuda and t.dtype is torch.float32) for t in (lr_factor, grad_factor))
+    _check("us_adamw", _entry("us_adamw")(len(tensors), tensors, lr, betas[0], betas[1], eps, lr_factor, grad_factor, step, _stream(stream)))
 
 
 def us_scales_linear(b: int, m: int, n: int, constrained: bool = False):
