@@ -110,6 +110,8 @@ typedef struct {
  * both US_F16.  Output dtype: any us_dtype.  Every dimension must be >= 1; rows
  * and columns need not be multiples of the tile sizes.  Alignment rule: see
  * us_mat (violations return US_ERR_ALIGNMENT).
+ * Outputs are written in pieces of 16 bytes: where a row does not end on such a boundary, the bytes from its
+ * last element to the boundary (row padding) are written too.
  *
  * Where an output has few tiles and the contraction is long (more than 2432 bytes of an operand's K, for
  * weight gradients 6016) without a fused activation, up to eight SMs may share a tile: each sums a part of the
@@ -136,6 +138,17 @@ us_status us_linear_bwd_w(const us_mat* X, const us_mat* G, float beta_w, const 
  * US_ERR_UNSUPPORTED for other epilogues and formats. */
 us_status us_linear_fwd_cast(const us_mat* X, const us_mat* W, float alpha, const us_epilogue* ep, const us_mat* Y, const us_mat* Yq,
                              void* ws, size_t ws_bytes, void* stream);
+
+/* us_linear_fwd for a layer with a bias (1 x n, US_F32, US_BF16 or US_F16, on a 16-byte boundary), which is added to every row of the scaled
+ * product before anything else of the epilogue:
+ *
+ *   v = alpha * acc + bias      in float32, rounded once; then aux, activation, skip and Y as us_epilogue says
+ *
+ * Forward activations (or none), with a kept pre-activation and with a skip tensor or without; Yq: NULL, or the FP8 copy of us_linear_fwd_cast
+ * under its conditions.  With a bias the pre-activation that aux keeps holds it, so the backward pass is that of a layer without one
+ * (us_linear_bwd_x, us_linear_bwd_w) and us_bias_grad.  The US_ACT_*_GRAD activations: US_ERR_UNSUPPORTED; everything else as for us_linear_fwd. */
+us_status us_linear_fwd_bias(const us_mat* X, const us_mat* W, float alpha, const us_mat* bias, const us_epilogue* ep, const us_mat* Y,
+                             const us_mat* Yq, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Batched forms: count[0] x count[1] independent problems of one shape in a single launch, e.g. the

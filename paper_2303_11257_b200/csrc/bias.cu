@@ -64,11 +64,11 @@ __device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t
       for (; r + 32 * (kAhead - 1) < whole; r += 32 * kAhead) {
         uint4 t[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) t[k] = __ldg(reinterpret_cast<const uint4*>(g + (r + 32 * k) * pitch));
+        for (int k = 0; k < kAhead; ++k) t[k] = *reinterpret_cast<const uint4*>(g + (r + 32 * k) * pitch);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) add16<DT>(t[k], acc);
       }
-      for (; r < whole; r += 32) add16<DT>(__ldg(reinterpret_cast<const uint4*>(g + r * pitch)), acc);
+      for (; r < whole; r += 32) add16<DT>(*reinterpret_cast<const uint4*>(g + r * pitch), acc);
       if (r < end) {                                           // the matrix's last row
 #pragma unroll
         for (int i = 0; i < kChunk; ++i)

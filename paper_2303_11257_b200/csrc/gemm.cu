@@ -35,7 +35,8 @@ struct WaitTest {
 // A, B: the two operands in call order; out [M x N].
 static us_status linear(Op op, const us_mat* A, const us_mat* B, float scale, const us_epilogue* ep, const us_mat* out,
                         void* ws, size_t ws_bytes, void* stream, const us_batch* batch = nullptr,
-                        const WaitTest* wt = nullptr, bool validate_only = false, const us_mat* copy = nullptr, Tiling* tiling = nullptr) {
+                        const WaitTest* wt = nullptr, bool validate_only = false, const us_mat* copy = nullptr, Tiling* tiling = nullptr,
+                        const us_mat* bias = nullptr) {
   if (!valid_mat(A) || !valid_mat(B) || !valid_mat(out)) return US_ERR_INVALID_ARG;
   int64_t M, N, K;
   bool shapes_ok;
@@ -81,6 +82,13 @@ static us_status linear(Op op, const us_mat* A, const us_mat* B, float scale, co
       p.skip = ep->skip.ptr; p.skip_dt = ep->skip.dtype; p.skip_ld = ep->skip.ld;
       p.skip_coef = ep->skip_coef; p.out_coef = ep->out_coef;
     }
+  }
+  if (bias) {
+    if (!valid_mat(bias) || bias->rows != 1 || bias->cols != N) return US_ERR_INVALID_ARG;
+    if (bias->dtype != US_F32 && bias->dtype != US_BF16 && bias->dtype != US_F16) return US_ERR_UNSUPPORTED;
+    if (p.act == US_ACT_GELU_GRAD) return US_ERR_UNSUPPORTED;         // (a backward op)
+    if (reinterpret_cast<uintptr_t>(bias->ptr) % 16) return US_ERR_ALIGNMENT;
+    p.bias = bias->ptr; p.bias_dt = bias->dtype;
   }
   if (copy) {
     const us_status s = check_copy(copy, out, p.skip != nullptr && p.act == US_ACT_NONE);
@@ -149,6 +157,10 @@ extern "C" us_status us_linear_fwd(const us_mat* X, const us_mat* W, float alpha
 extern "C" us_status us_linear_fwd_cast(const us_mat* X, const us_mat* W, float alpha, const us_epilogue* ep, const us_mat* Y,
                                         const us_mat* Yq, void* ws, size_t ws_bytes, void* stream) {
   return Yq ? us::linear(us::kFwd, X, W, alpha, ep, Y, ws, ws_bytes, stream, nullptr, nullptr, false, Yq) : US_ERR_INVALID_ARG;
+}
+extern "C" us_status us_linear_fwd_bias(const us_mat* X, const us_mat* W, float alpha, const us_mat* bias, const us_epilogue* ep, const us_mat* Y,
+                                        const us_mat* Yq, void* ws, size_t ws_bytes, void* stream) {
+  return bias ? us::linear(us::kFwd, X, W, alpha, ep, Y, ws, ws_bytes, stream, nullptr, nullptr, false, Yq, nullptr, bias) : US_ERR_INVALID_ARG;
 }
 extern "C" us_status us_linear_bwd_x(const us_mat* G, const us_mat* W, float beta_x, const us_epilogue* ep,
                                      const us_mat* dX, void* ws, size_t ws_bytes, void* stream) {

@@ -34,7 +34,7 @@ static bool make_tmap(CUtensorMap* tm, const us_mat* m, int es, int box_rows, in
             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int ES, bool A_MN, bool B_MN, int BN, int CG, int EPI, int EW, bool BATCHED = false>
+template <int ES, bool A_MN, bool B_MN, int BN, int CG, int EPI, int EW, bool BATCHED = false, bool BIAS = false>
 static us_status launch(const us_mat* A, const us_mat* B, const GemmParams& p, const EpiMats& em, cudaStream_t stream,
                         const BatchDesc* bd = nullptr) {
   constexpr int kBK = kStageKBytes / ES;
@@ -51,7 +51,7 @@ static us_status launch(const us_mat* A, const us_mat* B, const GemmParams& p, c
   const int aux_row = EPI == kEpiGeluGrad ? (EW == 16 ? 64 : 128) : out_row_bytes(BN, 2);
   if (EPI != kEpiLegacy && em.aux && !make_tmap(&t_aux, em.aux, dtype_size(em.aux->dtype), 32, aux_row)) return US_ERR_CUDA;
   if (EPI != kEpiLegacy && em.skip && !make_tmap(&t_skip, em.skip, dtype_size(em.skip->dtype), 32)) return US_ERR_CUDA;
-  auto kern = gemm_kernel<ES, A_MN, B_MN, BN, CG, EPI, EW, BATCHED>;
+  auto kern = gemm_kernel<ES, A_MN, B_MN, BN, CG, EPI, EW, BATCHED, BIAS>;
   constexpr int smem = GemmSmem<BN, CG, EW, EPI == kEpiPlain16>::kTotal;
   const int sms = host::sm_count();
   if (sms <= 0) return US_ERR_CUDA;
@@ -62,21 +62,28 @@ static us_status launch(const us_mat* A, const us_mat* B, const GemmParams& p, c
   return host::launch(kern, &smem_set, grid, gemm_threads(EW), smem, CG, stream, ta, tb, t_out, t_aux, t_skip, p);
 }
 
-template <int ES, bool A_MN, bool B_MN, int BN, int CG>
+template <int ES, bool A_MN, bool B_MN, int BN, int CG, bool BIAS = false>
 static us_status pick_epilogue(const us_mat* A, const us_mat* B, const GemmParams& p, const EpiMats& em, int epi,
                                const BatchDesc& bd, cudaStream_t stream) {
-  if (bd.batched()) {                                  // batched problems: plain epilogue only (checked by the caller)
-    return launch<ES, A_MN, B_MN, BN, CG, kEpiPlain, 8, true>(A, B, p, em, stream, &bd);
+  if constexpr (!A_MN && B_MN && !BIAS) {
+    if (p.bias) return pick_epilogue<ES, A_MN, B_MN, BN, CG, true>(A, B, p, em, epi, bd, stream);
+  }
+  if constexpr (!BIAS) {
+    if (bd.batched()) {                                  // batched problems: plain epilogue only (checked by the caller)
+      return launch<ES, A_MN, B_MN, BN, CG, kEpiPlain, 8, true>(A, B, p, em, stream, &bd);
+    }
   }
   // The GELU epilogues with an FP8 output (the FFN's forward and backward hidden layer) are ALU
   // bound with eight epilogue warps; they run with sixteen.
   const bool fp8_out = (em.out->dtype == US_E4M3 || em.out->dtype == US_E5M2) && p.fn == US_FN_GELU;   // the 16-warp epilogue is the GELU pair's
   if constexpr (BN != 64) {                            // (a warp has 32 columns of a narrow tile: eight are enough there)
-    if (fp8_out && epi == kEpiGelu) return launch<ES, A_MN, B_MN, BN, CG, kEpiGelu, 16>(A, B, p, em, stream);
-    if (fp8_out && epi == kEpiGeluGrad) return launch<ES, A_MN, B_MN, BN, CG, kEpiGeluGrad, 16>(A, B, p, em, stream);
+    if (fp8_out && epi == kEpiGelu) return launch<ES, A_MN, B_MN, BN, CG, kEpiGelu, 16, false, BIAS>(A, B, p, em, stream);
+    if constexpr (!BIAS) {
+      if (fp8_out && epi == kEpiGeluGrad) return launch<ES, A_MN, B_MN, BN, CG, kEpiGeluGrad, 16>(A, B, p, em, stream);
+    }
   }
   if constexpr (!A_MN && B_MN) {
-    if (epi == kEpiSkipCopy) return launch<ES, A_MN, B_MN, BN, CG, kEpiSkipCopy, 8>(A, B, p, em, stream);
+    if (epi == kEpiSkipCopy) return launch<ES, A_MN, B_MN, BN, CG, kEpiSkipCopy, 8, false, BIAS>(A, B, p, em, stream);
   }
   switch (epi) {
     case kEpiPlain:
@@ -85,16 +92,18 @@ static us_status pick_epilogue(const us_mat* A, const us_mat* B, const GemmParam
         // whose tiles are bound by the bytes they write (FP8 operands into BF16, eight / sixteen warps, us: 8192 x 128 x 3072 12.1 / 11.3,
         // x 1024 x 3072 22.6 / 23.8, 2048 x 1024 x 30528 57.6 / 60.2).
         if ((em.out->dtype == US_E4M3 || em.out->dtype == US_E5M2) && (long long)p.K * ES <= 4096)
-          return launch<ES, A_MN, B_MN, BN, CG, kEpiPlain16, 16>(A, B, p, em, stream);
+          return launch<ES, A_MN, B_MN, BN, CG, kEpiPlain16, 16, false, BIAS>(A, B, p, em, stream);
       }
-      return em.out->dtype == US_F32 ? launch<ES, A_MN, B_MN, BN, CG, kEpiPlainF32, 8>(A, B, p, em, stream)
-                                     : launch<ES, A_MN, B_MN, BN, CG, kEpiPlain, 8>(A, B, p, em, stream);
-    case kEpiGelu:     return launch<ES, A_MN, B_MN, BN, CG, kEpiGelu, 8>(A, B, p, em, stream);
-    case kEpiGeluGrad: return launch<ES, A_MN, B_MN, BN, CG, kEpiGeluGrad, 8>(A, B, p, em, stream);
+      return em.out->dtype == US_F32 ? launch<ES, A_MN, B_MN, BN, CG, kEpiPlainF32, 8, false, BIAS>(A, B, p, em, stream)
+                                     : launch<ES, A_MN, B_MN, BN, CG, kEpiPlain, 8, false, BIAS>(A, B, p, em, stream);
+    case kEpiGelu:     return launch<ES, A_MN, B_MN, BN, CG, kEpiGelu, 8, false, BIAS>(A, B, p, em, stream);
+    case kEpiGeluGrad:
+      if constexpr (BIAS) return US_ERR_UNSUPPORTED;   // (checked by the caller)
+      else return launch<ES, A_MN, B_MN, BN, CG, kEpiGeluGrad, 8>(A, B, p, em, stream);
     case kEpiSkip:
-      return em.out->dtype == US_F32 ? launch<ES, A_MN, B_MN, BN, CG, kEpiSkipF32, 8>(A, B, p, em, stream)
-                                     : launch<ES, A_MN, B_MN, BN, CG, kEpiSkip, 8>(A, B, p, em, stream);
-    default:           return launch<ES, A_MN, B_MN, BN, CG, kEpiLegacy, 8>(A, B, p, em, stream);
+      return em.out->dtype == US_F32 ? launch<ES, A_MN, B_MN, BN, CG, kEpiSkipF32, 8, false, BIAS>(A, B, p, em, stream)
+                                     : launch<ES, A_MN, B_MN, BN, CG, kEpiSkip, 8, false, BIAS>(A, B, p, em, stream);
+    default:           return launch<ES, A_MN, B_MN, BN, CG, kEpiLegacy, 8, false, BIAS>(A, B, p, em, stream);
   }
 }
 
@@ -169,7 +178,7 @@ us_status launch_gemm(const us_mat* A, const us_mat* B, GemmParams& p, const Epi
   }
   const int bn = t.bn, cg = t.cg;
   if (t.splits > 1) {
-    const SplitCall call{A, B, em.out, em.skip, em.copy, A_MN, B_MN, p.scale, p.skip_coef, p.out_coef};
+    const SplitCall call{A, B, em.out, em.skip, em.copy, A_MN, B_MN, p.scale, p.skip_coef, p.out_coef, p.bias, p.bias_dt};
     return launch_split(1, &call, t, p.status, p.wait_limit, p.served ? 0 : p.starved, stream);
   }
   p.tiles_m = (p.M + kBM * cg - 1) / (kBM * cg);

@@ -46,6 +46,7 @@ struct GemmParams {
   void* aux; int aux_dt; int64_t aux_ld;   // pre-activation; kEpiSkipCopy: the FP8 copy of the output
   int aux_sectors;                          // the copy's rows start on 32-byte boundaries
   const void* skip; int skip_dt; int64_t skip_ld; float skip_coef, out_coef;
+  const void* bias; int bias_dt;            // one value per output column
   unsigned int* status;
   uint32_t wait_limit;                      // polls a bounded wait makes before it gives up (kWaitLimit unless a test shortens it)
   int starved, served;                      // test hook (starved_cta)
@@ -146,6 +147,38 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
   *abort_flag = 1;
   if (status) atomicExch(status, kStatusTimeout);
   return false;
+}
+
+// The bias of COLS columns from `col` on (a multiple of 8), two to a register; zeros behind the last of n.  Every lane reads the same: one
+// access of a warp takes 16 bytes.
+template <int COLS>
+__device__ __forceinline__ void bias_columns(const void* bias, int dt, int col, int n, f32x2 (&b)[COLS / 2]) {
+  if (col + COLS <= n) {
+    if (dt == US_F32) {
+      const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(bias) + col);
+#pragma unroll
+      for (int i = 0; i < COLS / 4; ++i) {
+        const float4 t = q[i];
+        b[2 * i] = pack2(t.x, t.y); b[2 * i + 1] = pack2(t.z, t.w);
+      }
+    } else {
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(bias) + col);
+#pragma unroll
+      for (int i = 0; i < COLS / 8; ++i) {
+        const uint4 t = q[i];
+        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = dt == US_BF16 ? unpack_bf16x2(w[j]) : unpack_f16x2(w[j]);
+          b[4 * i + j] = pack2(f.x, f.y);
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < COLS / 2; ++i)
+      b[i] = pack2(col + 2 * i < n ? load_one(bias, dt, col + 2 * i) : 0.f, col + 2 * i + 1 < n ? load_one(bias, dt, col + 2 * i + 1) : 0.f);
+  }
 }
 
 // Operands of the fused epilogue for one 32-column slice of one row, fetched as raw 16-byte
@@ -343,7 +376,7 @@ __host__ __device__ constexpr int out_row_bytes(int bn, int es) { return bn / 2 
 // edges, so ragged shapes need no special path.  No cross-warp synchronisation is involved.
 // (128 x 128 tiles: with four warps of 128 columns instead of eight of 64 the exposed epilogue made 256 x 128 x 512 4.8 us
 // and, with a residual, 6.7 us; now 4.0 and 5.1.)
-template <int BN, int CG, int EPI, int EW, bool BATCHED>
+template <int BN, int CG, int EPI, int EW, bool BATCHED, bool BIAS>
 __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUtensorMap* tm_out, const CUtensorMap* tm_aux,
                                                 const CUtensorMap* tm_skip, const EpiCtx& c) {
   constexpr int kWarpCols = BN / 2;                         // columns of the tile one warp handles
@@ -457,6 +490,8 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
           }
           __syncwarp();
         }
+        f32x2 bias[BIAS ? 16 : 1];
+        if constexpr (BIAS) bias_columns<32>(p.bias, p.bias_dt, col, p.N, bias);
         float v[32];
         ptx::tmem_ld_32x32(t_row + 32 * sl, v);
         if (last_slice) { release_acc(acc, tile); released = true; }   // the MMA warp may refill it while this slice is worked on
@@ -471,7 +506,10 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
         // 4096 with GELU 5.9 -> 4.5; plain, 16 x 8192 x 8192 weight gradient in BF16 31.5 -> 23.9, 2048 x 128 x 8192 10.9 -> 8.9).
         float y[32];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) unpack2(mul2(pack2(v[2 * k], v[2 * k + 1]), scale2), y[2 * k], y[2 * k + 1]);
+        for (int k = 0; k < 16; ++k) {
+          const f32x2 x = pack2(v[2 * k], v[2 * k + 1]);
+          unpack2(BIAS ? fma2(x, scale2, bias[BIAS ? k : 0]) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
+        }
         if (EPI == kEpiGelu) {
           if (aux_out) {
             uint32_t w[16];
@@ -561,7 +599,7 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
 // swizzle), [4096, 6144) output; GELU gradient: [0, 2048) and [2048, 4096) the input boxes,
 // [4096, 6144) output; 64-byte rows use the 64-byte swizzle: 16-byte chunk c of row r sits at
 // chunk c ^ ((r >> 1) & 3).
-template <int BN, int CG, int EPI, bool OUT_E5, bool AUX_BF16>
+template <int BN, int CG, int EPI, bool OUT_E5, bool AUX_BF16, bool BIAS>
 __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtensorMap* tm_out, const CUtensorMap* tm_aux,
                                                const EpiCtx& c, uint32_t in_bar1) {
   static_assert(EPI == kEpiGelu || EPI == kEpiGeluGrad, "GELU kinds only");
@@ -596,15 +634,18 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       else ptx::mbar_arrive(c.acc_empty0 + 8u * a);
     }
   };
-  // One 32-column slice: scale, (kept pre-activation,) activation, rounding, staging stores.
-  auto slice = [&](const uint32_t (&r)[32], int s) {
+  // One 32-column slice: scale, (bias,) (kept pre-activation,) activation, rounding, staging stores.
+  auto slice = [&](const uint32_t (&r)[32], int s, int col) {
     uint32_t held[2];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      f32x2 x[4];
+      f32x2 x[4], bias[4];
+      if constexpr (BIAS) bias_columns<8>(p.bias, p.bias_dt, col + 8 * g, p.N, bias);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        x[k] = mul2(pack2(__uint_as_float(r[8 * g + 2 * k]), __uint_as_float(r[8 * g + 2 * k + 1])), scale2);
+      for (int k = 0; k < 4; ++k) {
+        x[k] = pack2(__uint_as_float(r[8 * g + 2 * k]), __uint_as_float(r[8 * g + 2 * k + 1]));
+        x[k] = BIAS ? fma2(x[k], scale2, bias[k]) : mul2(x[k], scale2);
+      }
       float y[8];
       if (EPI == kEpiGelu) {
         if (aux_out) {
@@ -675,7 +716,7 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       pending[0] = false;
       ph0 ^= 1u;
     }
-    if (active) slice(r0, 0);
+    if (active) slice(r0, 0, n_w);
     if (kIn) {
       __syncwarp();                                           // every lane has read the first input box
       if (next < c.num_tiles) {
@@ -692,7 +733,7 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       pending[1] = false;
       ph1 ^= 1u;
     }
-    if (active) slice(r1, 1);
+    if (active) slice(r1, 1, n_w + 32);
     if (kIn) {
       __syncwarp();
       if (next < c.num_tiles) {
@@ -726,16 +767,24 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
 // first is rounded, and a tile is one box and one store per warp.  With eight warps of 128 columns a tile's epilogue takes longer
 // than the main loop of a short contraction.  us, FP8 operands and outputs: 8192 x 128 x 3072 16.2 -> 8.8, 8192 x 512 x 4096 22.1 -> 15.6, 8192 x 1024
 // x 3072 21.7 -> 20.3, 8192 x 2048 x 4096 45.4 -> 44.0, 8192 x 8192 x 4096 186 -> 186; weight gradient 512 x 8192 x 8192 38.9 -> 27.0.
-template <int BN, int CG>
+template <int BN, int CG, bool BIAS>
 __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUtensorMap* tm_out, const EpiCtx& c) {
   const int q = c.warp & 3, part = (c.warp - 2) >> 2, lane = c.lane;
   const uint32_t out_sw = (uint32_t)((lane >> 1) & 3), dst = c.buf0 + (uint32_t)lane * 64u;
   const f32x2 scale2 = splat2(p.scale);
-  auto slice = [&](const uint32_t (&r)[32], uint32_t chunk) {
+  auto slice = [&](const uint32_t (&r)[32], uint32_t chunk, int col) {
     float y[32];
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-      unpack2(mul2(pack2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1])), scale2), y[2 * k], y[2 * k + 1]);
+    for (int g = 0; g < 4; ++g) {
+      f32x2 bias[4];
+      if constexpr (BIAS) bias_columns<8>(p.bias, p.bias_dt, col + 8 * g, p.N, bias);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = 4 * g + i;
+        const f32x2 x = pack2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+        unpack2(BIAS ? fma2(x, scale2, bias[i]) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
+      }
+    }
     uint32_t w[8];
     if (p.out_dt == US_E5M2) {
 #pragma unroll
@@ -766,7 +815,7 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
       __syncwarp();
       ptx::tmem_ld_fence(r0);
       ptx::tmem_ld_32x32_issue(t_row + 32, r1);
-      slice(r0, 0);
+      slice(r0, 0, n_w);
       ptx::tmem_ld_fence(r1);
     }
     ptx::tc_fence_before_sync();
@@ -776,7 +825,7 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
       else ptx::mbar_arrive(c.acc_empty0 + 8u * acc);
     }
     if (active) {
-      slice(r1, 2);
+      slice(r1, 2, n_w + 32);
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (ptx::elect_one()) { ptx::tma_store_2d(tm_out, c.buf0, n_w, row0); ptx::bulk_commit_group(); }
@@ -792,13 +841,15 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
 // EPI: the fused epilogue (EpiKind).  EW: number of epilogue warps (8 or 16).
 // CG: 1 = every CTA computes its own 128 x BN tiles; 2 = clusters of two CTAs compute 256 x BN
 //     tiles with tcgen05.mma.cta_group::2 (the even CTA issues, both load and both run an epilogue).
-template <int ES, bool A_MN, bool B_MN, int BN, int CG, int EPI, int EW, bool BATCHED>
+// BIAS: p.bias is added to every row (forward layout only).  It takes the place of the scaling's multiply: one fused multiply-add.
+template <int ES, bool A_MN, bool B_MN, int BN, int CG, int EPI, int EW, bool BATCHED, bool BIAS>
 __global__ void __launch_bounds__(gemm_threads(EW), 1)
 gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
             const __grid_constant__ CUtensorMap tmap_out, const __grid_constant__ CUtensorMap tmap_aux,
             const __grid_constant__ CUtensorMap tmap_skip, const GemmParams p) {
   using S = GemmSmem<BN, CG, EW, EPI == kEpiPlain16>;
   static_assert(!BATCHED || EPI == kEpiPlain, "batched problems take the plain epilogue");
+  static_assert(!BIAS || (!BATCHED && !A_MN && B_MN && EPI != kEpiGeluGrad), "biases: single forward problems");
   static_assert(EW == 8 || (EW == 16 && (EPI == kEpiGelu || EPI == kEpiGeluGrad || EPI == kEpiPlain16)), "16 epilogue warps: GELU and plain");
   constexpr int kBK = kStageKBytes / ES;            // K elements per stage
   constexpr int kChunkElems = 128 / ES;             // MN elements per 128-byte row of an MN-major tile
@@ -980,16 +1031,16 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     c.abort_flag = abort_flag; c.warp = warp; c.lane = lane; c.rank = rank;
     c.group = group; c.num_groups = num_groups; c.num_tiles = num_tiles;
     if constexpr (EPI == kEpiPlain16) {
-      epilogue_plain16<BN, CG>(p, &tmap_out, c);
+      epilogue_plain16<BN, CG, BIAS>(p, &tmap_out, c);
     } else if constexpr (EW == 16) {
       const uint32_t in_bar1 = epi_in_bar(2 * (warp - 2) + 1);
       const bool e5 = p.out_dt == US_E5M2, bf = p.aux_dt == US_BF16;
-      if (e5 && bf) epilogue_act16<BN, CG, EPI, true, true>(p, &tmap_out, &tmap_aux, c, in_bar1);
-      else if (e5) epilogue_act16<BN, CG, EPI, true, false>(p, &tmap_out, &tmap_aux, c, in_bar1);
-      else if (bf) epilogue_act16<BN, CG, EPI, false, true>(p, &tmap_out, &tmap_aux, c, in_bar1);
-      else epilogue_act16<BN, CG, EPI, false, false>(p, &tmap_out, &tmap_aux, c, in_bar1);
+      if (e5 && bf) epilogue_act16<BN, CG, EPI, true, true, BIAS>(p, &tmap_out, &tmap_aux, c, in_bar1);
+      else if (e5) epilogue_act16<BN, CG, EPI, true, false, BIAS>(p, &tmap_out, &tmap_aux, c, in_bar1);
+      else if (bf) epilogue_act16<BN, CG, EPI, false, true, BIAS>(p, &tmap_out, &tmap_aux, c, in_bar1);
+      else epilogue_act16<BN, CG, EPI, false, false, BIAS>(p, &tmap_out, &tmap_aux, c, in_bar1);
     } else {
-      epilogue_staged<BN, CG, EPI, EW, BATCHED>(p, &tmap_out, &tmap_aux, &tmap_skip, c);
+      epilogue_staged<BN, CG, EPI, EW, BATCHED, BIAS>(p, &tmap_out, &tmap_aux, &tmap_skip, c);
     }
   } else {
     // ------------------------------------------------------------ epilogue warps, direct global accesses
@@ -1015,10 +1066,17 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
 #pragma unroll 1
       for (int c = c_first; c < BN; c += 64) {
         if (n0 + c >= p.N) break;                    // warp-uniform
+        f32x2 bias[BIAS ? 16 : 1];
+        if constexpr (BIAS) bias_columns<32>(p.bias, p.bias_dt, n0 + c, p.N, bias);
         float v[32];
         ptx::tmem_ld_32x32(t_row + c, v);
+        if constexpr (BIAS) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= p.scale;
+          for (int i = 0; i < 16; ++i) unpack2(fma2(pack2(v[2 * i], v[2 * i + 1]), splat2(p.scale), bias[i]), v[2 * i], v[2 * i + 1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] *= p.scale;
+        }
         const int ncols = min(32, p.N - (n0 + c));
         if (row_ok) {
           if (ncols == 32) epilogue_chunk_full(p, v, pf, row, n0 + c);

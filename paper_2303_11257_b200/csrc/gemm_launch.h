@@ -31,11 +31,13 @@ struct BatchDesc {
 // How an output is tiled: columns of a tile, CTAs that cooperate on it as a pair (1: none), CTAs (pairs) that share its contraction.
 struct Tiling { int bn, cg, splits; };
 
-// One GEMM of a launch with shared contractions (gemm_split.cu); skip and copy may be NULL.
+// One GEMM of a launch with shared contractions (gemm_split.cu); skip and copy may be NULL, and bias, which only a launch of one takes.
 struct SplitCall {
   const us_mat *a, *b, *out, *skip, *copy;
   bool a_mn, b_mn;
   float scale, skip_coef, out_coef;
+  const void* bias = nullptr;
+  int bias_dt = US_F32;
 };
 // Tiles of the calls' outputs all t; t.splits is 2, 4 or 8 and t.splits * t.cg at most 8.
 us_status launch_split(int count, const SplitCall* calls, const Tiling& t, unsigned int* status, uint32_t wait_limit, int starved, cudaStream_t stream);

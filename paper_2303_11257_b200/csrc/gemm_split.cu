@@ -15,6 +15,12 @@ using host::make_tmap;
 template <int ES, int BN, int CG, int PROBLEMS>
 us_status launch(const SplitParams<PROBLEMS>& p, int tiles, cudaStream_t stream) {
   static std::atomic<uint64_t> smem_set{0};
+  if constexpr (PROBLEMS == 1) {
+    static std::atomic<uint64_t> smem_set_bias{0};
+    if (p.prob[0].bias)
+      return host::launch(gemm_split_kernel<ES, BN, CG, false, true>, &smem_set_bias, CG * p.splits * tiles, gemm_threads(8), GemmSmem<BN, CG, 8>::kTotal,
+                          CG * p.splits, stream, p);
+  }
   return host::launch(gemm_split_kernel<ES, BN, CG, (PROBLEMS > 1)>, &smem_set, CG * p.splits * tiles, gemm_threads(8), GemmSmem<BN, CG, 8>::kTotal,
                       CG * p.splits, stream, p);
 }
@@ -45,6 +51,7 @@ us_status launch_problems(int count, const SplitCall* calls, const Tiling& t, un
     P.copy_ld = c.copy ? c.copy->ld : 0;
     P.copy_dt = c.copy ? c.copy->dtype : US_E4M3;
     P.copy_sectors = reinterpret_cast<uintptr_t>(P.copy) % 32 == 0 && P.copy_ld % 32 == 0;
+    s.bias = c.bias; s.bias_dt = c.bias_dt;
     s.a_bytes = (uint32_t)us::split_a_bytes(t.bn, c.a_mn, c.out->rows);
     using Narrow = GemmSmem<64, 1, 8>;
     s.stages = t.bn == 64    ? std::min((int)Narrow::kMaxStages, Narrow::kStages * Narrow::kStageBytes / ((int)s.a_bytes + Narrow::kBBytes))

@@ -17,6 +17,7 @@ namespace us {
 struct SplitProblem {
   GroupProblem g;                           // out boxes: 32 rows x 32 columns
   int tiles_m, tile_end;                    // tile rows; tiles of the problems up to and including this one
+  const void* bias; int bias_dt;            // BIAS: one value per output column
   uint32_t a_bytes; int stages;             // bytes of A in a stage (narrow tiles of few rows: those that exist), and the stages that fit
 };
 template <int PROBLEMS>
@@ -29,7 +30,7 @@ struct SplitParams {
 };
 
 // MULTI: several problems; the parameters of one alone are at fixed addresses and need not be fetched ahead.
-template <int ES, int BN, int CG, bool MULTI>
+template <int ES, int BN, int CG, bool MULTI, bool BIAS = false>
 __global__ void __launch_bounds__(gemm_threads(8), 1)
 gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems : 1> p) {
   using S = GemmSmem<BN, CG, 8>;
@@ -258,6 +259,8 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
           issue_in(sl + 1);
         }
       }
+      f32x2 bias[BIAS ? 16 : 1];
+      if constexpr (BIAS) bias_columns<32>(sp.bias, sp.bias_dt, col, cols, bias);
       float y[32];
       ptx::tmem_ld_32x32(t_row + 32 * sl, y);
       uint32_t at = smem_base + (uint32_t)(block(sl) % run) * kBlockBytes + (uint32_t)lane * 16u;
@@ -273,7 +276,10 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
         }
       }
 #pragma unroll
-      for (int k = 0; k < 16; ++k) unpack2(mul2(pack2(y[2 * k], y[2 * k + 1]), scale2), y[2 * k], y[2 * k + 1]);
+      for (int k = 0; k < 16; ++k) {
+        const f32x2 x = pack2(y[2 * k], y[2 * k + 1]);
+        unpack2(BIAS ? fma2(x, scale2, bias[BIAS ? k : 0]) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
+      }
       if (skip) residual_row32(skip_dt, raw, skip2, oc2, y);
       if (P.copy && row0 + lane < rows) {             // an FP8 copy of the result
         uint32_t copy[8];

@@ -167,6 +167,8 @@ def _load() -> C.CDLL:
     lib.us_qk_norm_fwd.restype = lib.us_qk_norm_bwd.restype = lib.us_rotary_table.restype = C.c_int
     lib.us_qk_norm_bwd_workspace_bytes.argtypes = [C.c_int64]
     lib.us_qk_norm_bwd_workspace_bytes.restype = SZ
+    lib.us_linear_fwd_bias.argtypes = [MP, MP, F, MP, EP, MP, MP, V, SZ, V]
+    lib.us_linear_fwd_bias.restype = C.c_int
     lib.us_bias_grad.argtypes = [C.c_int, MP, C.POINTER(F), MP, V]
     lib.us_grad_norm.argtypes = [C.c_int, MP, F, V, V, SZ, V]
     lib.us_adamw.argtypes = [C.c_int, C.POINTER(us_adamw_tensor)] + [C.c_double] * 4 + [V] * 4
@@ -463,6 +465,12 @@ def _linear(name, a, b, scale, ep, out, ws, stream):
 
 def us_linear_fwd(X, W, alpha, Y, ws, ep=None, stream=None):
     return _linear("us_linear_fwd", X, W, alpha, ep, Y, ws, stream)
+
+
+def us_linear_fwd_bias(X, W, alpha, bias, Y, ws, ep=None, Yq=None, stream=None):
+    """us_linear_fwd of a layer with a bias (a vector), which is added to the scaled product; Yq: an FP8 copy of a residual's result."""
+    _check("us_linear_fwd_bias", _entry("us_linear_fwd_bias")(X, W, alpha, bias.view(1, -1) if bias.dim() == 1 else bias, ep, Y, Yq, ws, ws, _stream(stream)))
+    return Y
 
 
 def us_linear_bwd_x(G, W, beta_x, dX, ws, ep=None, stream=None):
