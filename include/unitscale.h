@@ -139,7 +139,7 @@ us_status us_linear_bwd_w(const us_mat* X, const us_mat* G, float beta_w, const 
 us_status us_linear_fwd_cast(const us_mat* X, const us_mat* W, float alpha, const us_epilogue* ep, const us_mat* Y, const us_mat* Yq,
                              void* ws, size_t ws_bytes, void* stream);
 
-/* us_linear_fwd for a layer with a bias (1 x n, US_F32, US_BF16 or US_F16, on a 16-byte boundary), which is added to every row of the scaled
+/* us_linear_fwd for a layer with a bias (1 x n, US_F32, US_BF16 or US_F16, natural alignment), which is added to every row of the scaled
  * product before anything else of the epilogue:
  *
  *   v = alpha * acc + bias      in float32, rounded once; then aux, activation, skip and Y as us_epilogue says

@@ -87,7 +87,7 @@ static us_status linear(Op op, const us_mat* A, const us_mat* B, float scale, co
     if (!valid_mat(bias) || bias->rows != 1 || bias->cols != N) return US_ERR_INVALID_ARG;
     if (bias->dtype != US_F32 && bias->dtype != US_BF16 && bias->dtype != US_F16) return US_ERR_UNSUPPORTED;
     if (p.act == US_ACT_GELU_GRAD) return US_ERR_UNSUPPORTED;         // (a backward op)
-    if (reinterpret_cast<uintptr_t>(bias->ptr) % 16) return US_ERR_ALIGNMENT;
+    if (reinterpret_cast<uintptr_t>(bias->ptr) % dtype_size(bias->dtype)) return US_ERR_ALIGNMENT;
     p.bias = bias->ptr; p.bias_dt = bias->dtype;
   }
   if (copy) {
@@ -108,6 +108,7 @@ static us_status linear(Op op, const us_mat* A, const us_mat* B, float scale, co
   else if (p.act == US_ACT_NONE) epi = copy ? kEpiSkipCopy : kEpiSkip;
   else if (p.act == US_ACT_GELU && !p.skip) epi = kEpiGelu;
   else if (p.act == US_ACT_GELU_GRAD && !p.skip) epi = kEpiGeluGrad;
+  else if (bias) epi = kEpiActSkip;
   BatchDesc bd;
   if (batch) {
     if (ep) return US_ERR_UNSUPPORTED;                  // batched problems take no fused epilogue

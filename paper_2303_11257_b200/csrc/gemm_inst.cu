@@ -103,7 +103,12 @@ static us_status pick_epilogue(const us_mat* A, const us_mat* B, const GemmParam
     case kEpiSkip:
       return em.out->dtype == US_F32 ? launch<ES, A_MN, B_MN, BN, CG, kEpiSkipF32, 8, false, BIAS>(A, B, p, em, stream)
                                      : launch<ES, A_MN, B_MN, BN, CG, kEpiSkip, 8, false, BIAS>(A, B, p, em, stream);
-    default:           return launch<ES, A_MN, B_MN, BN, CG, kEpiLegacy, 8, false, BIAS>(A, B, p, em, stream);
+    case kEpiActSkip:
+      if constexpr (BIAS) return launch<ES, A_MN, B_MN, BN, CG, kEpiActSkip, 8, false, true>(A, B, p, em, stream);
+      else return US_ERR_UNSUPPORTED;                  // (with a bias only)
+    default:
+      if constexpr (BIAS) return US_ERR_UNSUPPORTED;   // (every combination has an epilogue of its own)
+      else return launch<ES, A_MN, B_MN, BN, CG, kEpiLegacy, 8>(A, B, p, em, stream);
   }
 }
 

@@ -75,6 +75,7 @@ enum EpiKind {
   kEpiSkip = 3,      // + weighted skip tensor (residual)
   kEpiSkipF32 = 8,   // the same with float32 output (beside the code of the other types 160 x 512 x 288 with a float32 skip tensor takes 3.43 us instead of 3.35)
   kEpiSkipCopy = 5,  // the same and an FP8 copy of the output (forward layout only: its code, never taken, costs kEpiSkip 3 %)
+  kEpiActSkip = 9,   // with a bias: activation (a kept pre-activation leaves by plain stores) and weighted skip tensor
   kEpiLegacy = 4     // any other combination: direct global accesses, runtime switches
 };
 constexpr uint32_t kWaitLimit = 1u << 22;
@@ -149,37 +150,12 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
   return false;
 }
 
-// The bias of COLS columns from `col` on (a multiple of 8), two to a register; zeros behind the last of n.  Every lane reads the same: one
-// access of a warp takes 16 bytes.
-template <int COLS>
-__device__ __forceinline__ void bias_columns(const void* bias, int dt, int col, int n, f32x2 (&b)[COLS / 2]) {
-  if (col + COLS <= n) {
-    if (dt == US_F32) {
-      const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(bias) + col);
-#pragma unroll
-      for (int i = 0; i < COLS / 4; ++i) {
-        const float4 t = q[i];
-        b[2 * i] = pack2(t.x, t.y); b[2 * i + 1] = pack2(t.z, t.w);
-      }
-    } else {
-      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(bias) + col);
-#pragma unroll
-      for (int i = 0; i < COLS / 8; ++i) {
-        const uint4 t = q[i];
-        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 f = dt == US_BF16 ? unpack_bf16x2(w[j]) : unpack_f16x2(w[j]);
-          b[4 * i + j] = pack2(f.x, f.y);
-        }
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < COLS / 2; ++i)
-      b[i] = pack2(col + 2 * i < n ? load_one(bias, dt, col + 2 * i) : 0.f, col + 2 * i + 1 < n ? load_one(bias, dt, col + 2 * i + 1) : 0.f);
-  }
-}
+// Column col's bias (0 behind the last), and two columns' of a slice of which lane i has column i's.  A lane's values are a register per slice, fetched
+// ahead; handed round they take as many cycles of the path to the registers as the same loads by every lane would (us, FP8 8192 x 1024 -> 4096 with
+// GELU: 43.7 with 16-byte loads of every lane in front of each group of columns, 38.4 so, 36.3 without a bias).
+template <class P>
+__device__ __forceinline__ float bias_lane(const P& p, int col, int n) { return col < n ? load_one(p.bias, p.bias_dt, col) : 0.f; }
+__device__ __forceinline__ f32x2 bias_pair(float mine, int i) { return pack2(__shfl_sync(0xffffffffu, mine, i), __shfl_sync(0xffffffffu, mine, i + 1)); }
 
 // Operands of the fused epilogue for one 32-column slice of one row, fetched as raw 16-byte
 // vectors before the accumulator is read so that their latency overlaps the TMEM load.
@@ -364,6 +340,18 @@ __device__ __forceinline__ void residual_row32(int skip_dt, const uint4 (&raw)[8
   }
 }
 
+// A lane's 32 pre-activations to its row of the 16-bit copy that the backward pass reads.
+__device__ __forceinline__ void keep_row32(const GemmParams& p, const float (&y)[32], int row, int col) {
+  char* dst = static_cast<char*>(p.aux) + ((int64_t)row * p.aux_ld + col) * 2;
+  if (col + 32 <= p.N) {
+    store_vec<32>(dst, p.aux_dt, y);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (col + i < p.N) store_one(dst, p.aux_dt, i, y[i]);
+  }
+}
+
 // Bytes per row of an output box of the eight-warp epilogue.
 __host__ __device__ constexpr int out_row_bytes(int bn, int es) { return bn / 2 * es < 128 ? bn / 2 * es : 128; }
 
@@ -383,7 +371,7 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
   const int q = c.warp & 3, half = (c.warp - 2) >> 2;       // lane quarter; which group of kWarpCols columns
   if (half >= BN / kWarpCols) return;                       // more warps than column groups: the rest sit out
   const int lane = c.lane;
-  constexpr int in_kind = EPI == kEpiGeluGrad ? 1 : (EPI == kEpiSkip || EPI == kEpiSkipF32 || EPI == kEpiSkipCopy ? 2 : 0);
+  constexpr int in_kind = EPI == kEpiGeluGrad ? 1 : (EPI == kEpiSkip || EPI == kEpiSkipF32 || EPI == kEpiSkipCopy || EPI == kEpiActSkip ? 2 : 0);
   const int in_dt = in_kind == 1 ? p.aux_dt : p.skip_dt;
   const int in_es = in_kind ? dtype_size(in_dt) : 4;
   const CUtensorMap* tm_in = in_kind == 1 ? tm_aux : tm_skip;
@@ -434,6 +422,11 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
     if (t0 < c.num_tiles) issue_in(tile_cols(t0), tile_rows(t0));
   }
 
+  float next_bias = 0.f;                                     // of the slice to come, a column a lane, fetched a slice ahead
+  if constexpr (BIAS) {
+    const int t0 = next_active_tile(c.group);
+    if (t0 < c.num_tiles) next_bias = bias_lane(p, tile_cols(t0) + lane, p.N);
+  }
   uint32_t local = 0;
   bool ok = true;
   for (int tile = c.group; ok && tile < c.num_tiles; tile += c.num_groups, ++local) {
@@ -490,8 +483,15 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
           }
           __syncwarp();
         }
-        f32x2 bias[BIAS ? 16 : 1];
-        if constexpr (BIAS) bias_columns<32>(p.bias, p.bias_dt, col, p.N, bias);
+        const float bias = next_bias;
+        if constexpr (BIAS) {
+          int nc = col + 32;
+          if (last_slice) {
+            const int tn = next_active_tile(tile + c.num_groups);
+            nc = tn < c.num_tiles ? tile_cols(tn) : p.N;
+          }
+          next_bias = bias_lane(p, nc + lane, p.N);
+        }
         float v[32];
         ptx::tmem_ld_32x32(t_row + 32 * sl, v);
         if (last_slice) { release_acc(acc, tile); released = true; }   // the MMA warp may refill it while this slice is worked on
@@ -508,9 +508,10 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           const f32x2 x = pack2(v[2 * k], v[2 * k + 1]);
-          unpack2(BIAS ? fma2(x, scale2, bias[BIAS ? k : 0]) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
+          unpack2(BIAS ? fma2(x, scale2, bias_pair(bias, 2 * k)) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
         }
-        if (EPI == kEpiGelu) {
+        if (EPI == kEpiActSkip && p.aux && row0 + lane < p.M) keep_row32(p, y, row0 + lane, col);
+        if (EPI == kEpiGelu || EPI == kEpiActSkip) {
           if (aux_out) {
             uint32_t w[16];
             if (p.aux_dt == US_BF16) {
@@ -547,9 +548,8 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
 #pragma unroll
             for (int k = 0; k < 32; ++k) y[k] = act_grad_scaled(p.fn, h[k], y[k], p.act_in, p.act_out);
           }
-        } else if (in_kind == 2) {
-          residual_row32(in_dt, raw, skip2, oc2, y);
         }
+        if (in_kind == 2) residual_row32(in_dt, raw, skip2, oc2, y);
         if (EPI == kEpiSkipCopy) copy_codes32(p.out_dt, p.aux_dt, y, copy);
         // ---- rounding to the output format and staging stores
         stage_row32<(EPI != kEpiPlain && EPI != kEpiSkip) || BATCHED>(out_dt, y, dst, out_cb, out_sw);
@@ -634,17 +634,16 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       else ptx::mbar_arrive(c.acc_empty0 + 8u * a);
     }
   };
-  // One 32-column slice: scale, (bias,) (kept pre-activation,) activation, rounding, staging stores.
-  auto slice = [&](const uint32_t (&r)[32], int s, int col) {
+  // One 32-column slice: scale, (bias, of which lane i has column i's,) (kept pre-activation,) activation, rounding, staging stores.
+  auto slice = [&](const uint32_t (&r)[32], int s, float bias) {
     uint32_t held[2];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      f32x2 x[4], bias[4];
-      if constexpr (BIAS) bias_columns<8>(p.bias, p.bias_dt, col + 8 * g, p.N, bias);
+      f32x2 x[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         x[k] = pack2(__uint_as_float(r[8 * g + 2 * k]), __uint_as_float(r[8 * g + 2 * k + 1]));
-        x[k] = BIAS ? fma2(x[k], scale2, bias[k]) : mul2(x[k], scale2);
+        x[k] = BIAS ? fma2(x[k], scale2, bias_pair(bias, 8 * g + 2 * k)) : mul2(x[k], scale2);
       }
       float y[8];
       if (EPI == kEpiGelu) {
@@ -681,8 +680,10 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
 
   int row0 = 0, n_w = 0;
   bool pending[2] = {false, false};                          // an input box load is in flight
+  float bias0 = 0.f, bias1 = 0.f;
   if (tile < c.num_tiles) {
     coords(tile, row0, n_w);
+    if constexpr (BIAS) { bias0 = bias_lane(p, n_w + lane, p.N); bias1 = bias_lane(p, n_w + 32 + lane, p.N); }
     if (kIn) {
       if (ptx::elect_one()) { issue_in(0, n_w, row0); issue_in(1, n_w, row0); }
       pending[0] = pending[1] = true;
@@ -702,7 +703,11 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
     if (active) ptx::tmem_ld_32x32_issue(t_row, r0);
     const int next = tile + c.num_groups;
     int next_row0 = 0, next_n_w = 0;
-    if (next < c.num_tiles) coords(next, next_row0, next_n_w);
+    float next_bias0 = 0.f, next_bias1 = 0.f;
+    if (next < c.num_tiles) {
+      coords(next, next_row0, next_n_w);
+      if constexpr (BIAS) { next_bias0 = bias_lane(p, next_n_w + lane, p.N); next_bias1 = bias_lane(p, next_n_w + 32 + lane, p.N); }
+    }
     if (active) {
       if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();          // the previous tile's stores have read the staging boxes
       __syncwarp();
@@ -716,7 +721,7 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       pending[0] = false;
       ph0 ^= 1u;
     }
-    if (active) slice(r0, 0, n_w);
+    if (active) slice(r0, 0, bias0);
     if (kIn) {
       __syncwarp();                                           // every lane has read the first input box
       if (next < c.num_tiles) {
@@ -733,7 +738,7 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       pending[1] = false;
       ph1 ^= 1u;
     }
-    if (active) slice(r1, 1, n_w + 32);
+    if (active) slice(r1, 1, bias1);
     if (kIn) {
       __syncwarp();
       if (next < c.num_tiles) {
@@ -751,6 +756,7 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       }
     }
     tile = next; row0 = next_row0; n_w = next_n_w;
+    if constexpr (BIAS) { bias0 = next_bias0; bias1 = next_bias1; }
   }
   // Leaving early (a wait ran out somewhere in the CTA): let tensor-memory loads and input boxes
   // that are still in flight land before the CTA may give up its resources.
@@ -772,18 +778,12 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
   const int q = c.warp & 3, part = (c.warp - 2) >> 2, lane = c.lane;
   const uint32_t out_sw = (uint32_t)((lane >> 1) & 3), dst = c.buf0 + (uint32_t)lane * 64u;
   const f32x2 scale2 = splat2(p.scale);
-  auto slice = [&](const uint32_t (&r)[32], uint32_t chunk, int col) {
+  auto slice = [&](const uint32_t (&r)[32], uint32_t chunk, float bias) {
     float y[32];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      f32x2 bias[4];
-      if constexpr (BIAS) bias_columns<8>(p.bias, p.bias_dt, col + 8 * g, p.N, bias);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = 4 * g + i;
-        const f32x2 x = pack2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
-        unpack2(BIAS ? fma2(x, scale2, bias[i]) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
-      }
+    for (int k = 0; k < 16; ++k) {
+      const f32x2 x = pack2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+      unpack2(BIAS ? fma2(x, scale2, bias_pair(bias, 2 * k)) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
     }
     uint32_t w[8];
     if (p.out_dt == US_E5M2) {
@@ -802,6 +802,8 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
     int tm, tn;
     tile_mn(p, tile, tm, tn);
     const int row0 = tm * (kBM * CG) + c.rank * kBM + q * 32, n_w = tn * BN + part * 64;
+    float bias0 = 0.f, bias1 = 0.f;
+    if constexpr (BIAS) { bias0 = bias_lane(p, n_w + lane, p.N); bias1 = bias_lane(p, n_w + 32 + lane, p.N); }
     bool ok = wait_bounded(c.acc_full0 + 8u * acc, acc_phase, c.abort_flag, p.status, p.wait_limit);
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) break;
@@ -815,7 +817,7 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
       __syncwarp();
       ptx::tmem_ld_fence(r0);
       ptx::tmem_ld_32x32_issue(t_row + 32, r1);
-      slice(r0, 0, n_w);
+      slice(r0, 0, bias0);
       ptx::tmem_ld_fence(r1);
     }
     ptx::tc_fence_before_sync();
@@ -825,7 +827,7 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
       else ptx::mbar_arrive(c.acc_empty0 + 8u * acc);
     }
     if (active) {
-      slice(r1, 2, n_w + 32);
+      slice(r1, 2, bias1);
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (ptx::elect_one()) { ptx::tma_store_2d(tm_out, c.buf0, n_w, row0); ptx::bulk_commit_group(); }
@@ -849,7 +851,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             const __grid_constant__ CUtensorMap tmap_skip, const GemmParams p) {
   using S = GemmSmem<BN, CG, EW, EPI == kEpiPlain16>;
   static_assert(!BATCHED || EPI == kEpiPlain, "batched problems take the plain epilogue");
-  static_assert(!BIAS || (!BATCHED && !A_MN && B_MN && EPI != kEpiGeluGrad), "biases: single forward problems");
+  static_assert(!BIAS || (!BATCHED && !A_MN && B_MN && EPI != kEpiGeluGrad && EPI != kEpiLegacy), "biases: single forward problems");
+  static_assert(BIAS || EPI != kEpiActSkip, "activation and skip tensor without a bias: the general epilogue");
   static_assert(EW == 8 || (EW == 16 && (EPI == kEpiGelu || EPI == kEpiGeluGrad || EPI == kEpiPlain16)), "16 epilogue warps: GELU and plain");
   constexpr int kBK = kStageKBytes / ES;            // K elements per stage
   constexpr int kChunkElems = 128 / ES;             // MN elements per 128-byte row of an MN-major tile
@@ -1066,17 +1069,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
 #pragma unroll 1
       for (int c = c_first; c < BN; c += 64) {
         if (n0 + c >= p.N) break;                    // warp-uniform
-        f32x2 bias[BIAS ? 16 : 1];
-        if constexpr (BIAS) bias_columns<32>(p.bias, p.bias_dt, n0 + c, p.N, bias);
         float v[32];
         ptx::tmem_ld_32x32(t_row + c, v);
-        if constexpr (BIAS) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) unpack2(fma2(pack2(v[2 * i], v[2 * i + 1]), splat2(p.scale), bias[i]), v[2 * i], v[2 * i + 1]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] *= p.scale;
-        }
+        for (int i = 0; i < 32; ++i) v[i] *= p.scale;
         const int ncols = min(32, p.N - (n0 + c));
         if (row_ok) {
           if (ncols == 32) epilogue_chunk_full(p, v, pf, row, n0 + c);

@@ -115,6 +115,7 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
   };
   int first = 0;                                     // this warp's first block of its own
   while (first < kSlices && !mine(first)) ++first;
+  float bias = 0.f;                                  // of a block's columns, a column a lane
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (every CTA)
@@ -209,6 +210,7 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
   } else {
     ptx::grid_wait_previous();
     if (first < kSlices && skip) issue_in(first);
+    if constexpr (BIAS) bias = bias_lane(sp, n_w + 32 * first + lane, first < kSlices ? cols : 0);
     ok = wait_bounded(acc_full_bar, 0, abort_flag, p.status, p.wait_limit);
     ok = __all_sync(0xffffffffu, ok);
   }
@@ -259,8 +261,9 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
           issue_in(sl + 1);
         }
       }
-      f32x2 bias[BIAS ? 16 : 1];
-      if constexpr (BIAS) bias_columns<32>(sp.bias, sp.bias_dt, col, cols, bias);
+      if constexpr (BIAS) {
+        if (sl > first) bias = bias_lane(sp, col + lane, cols);
+      }
       float y[32];
       ptx::tmem_ld_32x32(t_row + 32 * sl, y);
       uint32_t at = smem_base + (uint32_t)(block(sl) % run) * kBlockBytes + (uint32_t)lane * 16u;
@@ -278,7 +281,7 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
         const f32x2 x = pack2(y[2 * k], y[2 * k + 1]);
-        unpack2(BIAS ? fma2(x, scale2, bias[BIAS ? k : 0]) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
+        unpack2(BIAS ? fma2(x, scale2, bias_pair(bias, 2 * k)) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
       }
       if (skip) residual_row32(skip_dt, raw, skip2, oc2, y);
       if (P.copy && row0 + lane < rows) {             // an FP8 copy of the result

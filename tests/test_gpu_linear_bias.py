@@ -50,7 +50,8 @@ def _normal(rows, cols, fmt, seed):
 def _make(shape, fmt, bias_fmt):
     b, m, n = shape
     (X, x), (W, w) = _normal(b, m, fmt, 1), _normal(m, n, fmt, 2)
-    bias = (_normal(1, n, "f32", 3)[0] + (0.01 * torch.arange(n, device="cuda")) % 3).to(U.TORCH_OF[bias_fmt])
+    bias = torch.zeros((1, n + 1), dtype=U.TORCH_OF[bias_fmt], device="cuda")[:, 1:]          # an element behind a boundary
+    bias.copy_(_normal(1, n, "f32", 3)[0] + (0.01 * torch.arange(n, device="cuda")) % 3)
     return (X, W, bias), (x @ w) * float(torch.tensor(m ** -0.5)) + bias.double()
 
 

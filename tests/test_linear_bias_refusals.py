@@ -50,6 +50,5 @@ def test_what_is_refused():
         assert call(ep=ep(act, aux=M(0x50000, BF, 8, 48))) == 2
     assert call(Yq=Q) == 2 and call(ep=ep(L.US_ACT_GELU, skip=SKIP), Yq=Q) == 2 and call(ep=ep(skip=SKIP), Yq=M(0x60000, BF, 8, 48)) == 2
     assert call(X=M(0x10000, F16, 8, 64)) == 2
-    for off in (2, 4, 8):
-        assert call(bias=M(0x30000 + off, F32 if off > 2 else BF, 1, 48)) == 3
+    assert call(bias=M(0x30002, F32, 1, 48)) == 3 and call(bias=M(0x30001, BF, 1, 48)) == 3 and call(bias=M(0x30004, F32, 1, 48)) == 5 and call(bias=M(0x30002, F16, 1, 48)) == 5
     assert call(ws=None) == 4 and call(size=255) == 4 and call(ws=0x70008) == 3
