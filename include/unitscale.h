@@ -663,7 +663,7 @@ us_status us_grad_norm(int count, const us_mat* grads, float max_norm, float* ou
  * t = step[0] + 1.  step: two 64-bit integers in device memory, the number of steps made and a zero that the library uses; the call raises
  * step[0] at its end, so that a captured call counts on when it is replayed.  Calls that share it must not run at the same time.
  * lr_factor, grad_factor: NULL (1), or a float32 in device memory (a schedule; out[1] of us_grad_norm).  Where *grad_factor is not finite the
- * call changes nothing, step included.  A NaN or infinite gradient makes NaN of its own element (of its block of 8-bit states).
+ * call changes nothing, step included.  A NaN gradient makes NaN of its own element, an infinite one too, and of its block of 8-bit states.
  *
  * lr >= 0, 0 <= beta < 1, eps > 0 (also once rounded to float32).  Arithmetic in float32; 1 - beta and log(beta) are formed in float64.  Pointers
  * need the natural alignment of their elements; F32 tensors on 16-byte boundaries (copies, gradients and codes: of four elements), with rows that are dense

@@ -8,6 +8,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "host.h"
@@ -17,6 +18,7 @@ namespace us {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+__host__ __device__ constexpr int adam_ctas(bool eight) { return eight ? 4 : 3; }             // CTAs per SM
 constexpr int kUnit = 256;                   // elements of a unit, and of a block of states in 8 bits
 constexpr int kFew = 30, kMany = 240;        // tensors that a launch describes: in 4 KB of parameters, or in 32 KB
 constexpr float kTiny = 0x1p-100f;           // blocks whose largest magnitude is not above this are stored as zeros
@@ -34,12 +36,12 @@ struct AdamTensor {
   FastDiv by_cols;
   float copy_scale, lr_factor, decay;
   uint8_t g_dt, copy_dt;
-  uint8_t wide, dense;                       // groups of four are 16-byte accesses; p and g have no padded rows
+  uint8_t wide, dense;                       // p and g have no padded rows; and groups of four of all are aligned
   uint8_t copy_wide, copy_dense;
 };
 template <int MOST>
 struct AdamArgs {
-  float lr, beta1, beta2, rest1, rest2, eps;  // rest = 1 - beta, rounded once
+  float lr, beta1, beta2, root_beta2, rest1, root_rest2, eps;   // rest1 = 1 - beta1, root_rest2 = sqrt(1 - beta2); each rounded once
   float ln_beta1, ln_beta2;
   const float *lr_factor, *grad_factor;
   int64_t* step;
@@ -48,43 +50,81 @@ struct AdamArgs {
   AdamTensor t[MOST];
 };
 
+// (Numbers below 2^-126 count as zero in both.)
 __device__ __forceinline__ float sqrt_approx(float x) {
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
-__device__ __forceinline__ void load4(const void* base, int dt, int64_t i, float* v) {
-  if (dt == US_F32) {
+// Four elements of a gradient.
+template <int DT>
+__device__ __forceinline__ void load4(const void* base, int64_t i, float* v) {
+  if (DT == US_F32) {
     const float4 t = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + i);
     v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
   } else {
     const uint2 t = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + i);
-    const float2 a = dt == US_BF16 ? unpack_bf16x2(t.x) : unpack_f16x2(t.x), b = dt == US_BF16 ? unpack_bf16x2(t.y) : unpack_f16x2(t.y);
+    const float2 a = DT == US_BF16 ? unpack_bf16x2(t.x) : unpack_f16x2(t.x), b = DT == US_BF16 ? unpack_bf16x2(t.y) : unpack_f16x2(t.y);
     v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
   }
 }
-__device__ __forceinline__ void store4(void* base, int dt, int64_t i, const float* v) {
-  if (dt == US_F32) *reinterpret_cast<float4*>(static_cast<float*>(base) + i) = make_float4(v[0], v[1], v[2], v[3]);
-  else if (dt == US_BF16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + i) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-  else if (dt == US_F16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + i) = make_uint2(pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3]));
-  else *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(base) + i) = dt == US_E5M2 ? cvt_fp8x4<true>(v[0], v[1], v[2], v[3]) : cvt_fp8x4<false>(v[0], v[1], v[2], v[3]);
+template <int DT>
+__device__ __forceinline__ void store4(void* base, int64_t i, const float* v) {
+  if (DT == US_F32) *reinterpret_cast<float4*>(static_cast<float*>(base) + i) = make_float4(v[0], v[1], v[2], v[3]);
+  else if (DT == US_BF16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + i) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  else if (DT == US_F16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + i) = make_uint2(pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3]));
+  else *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(base) + i) = cvt_fp8x4<DT == US_E5M2>(v[0], v[1], v[2], v[3]);
 }
-__device__ __forceinline__ void load_codes4(const void* base, int64_t i, float scale, float* v) {
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(base) + i);
+// Four elements as they were fetched.
+__device__ __forceinline__ void four(const float4& t, int, float* v) { v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w; }
+__device__ __forceinline__ void four(const uint2& t, int dt, float* v) {
+  const float2 a = dt == US_BF16 ? unpack_bf16x2(t.x) : unpack_f16x2(t.x), b = dt == US_BF16 ? unpack_bf16x2(t.y) : unpack_f16x2(t.y);
+  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+__device__ __forceinline__ void four(uint32_t w, int, float* v) {
   const float2 a = unpack_fp8x2((uint16_t)w, false), b = unpack_fp8x2((uint16_t)(w >> 16), false);
-  v[0] = scale * a.x; v[1] = scale * a.y; v[2] = scale * b.x; v[3] = scale * b.y;
+  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+// f(std::integral_constant<int, dtype>()): the choice of a type is taken once, not for every element.
+template <class F>
+__device__ __forceinline__ void with_grad_type(int dt, F f) {
+  if (dt == US_F32) f(std::integral_constant<int, US_F32>());
+  else if (dt == US_BF16) f(std::integral_constant<int, US_BF16>());
+  else f(std::integral_constant<int, US_F16>());
+}
+template <class F>
+__device__ __forceinline__ void with_type(int dt, F f) {
+  if (dt == US_E4M3) f(std::integral_constant<int, US_E4M3>());
+  else if (dt == US_E5M2) f(std::integral_constant<int, US_E5M2>());
+  else with_grad_type(dt, f);
 }
 
-// Largest magnitude of the warp's values; a NaN is the largest.
+// Largest magnitude of the warp's values; a NaN is none.
 __device__ __forceinline__ float warp_most(const float (&x)[8]) {
-  uint32_t most = 0;
+  float most = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-  return __uint_as_float(__reduce_max_sync(0xffffffffu, most));
+  for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
 }
 
-// Where an element of a matrix with padded rows is: element `off` counted from (row0, col0).
+// Four codes of roots above or at zero; one that is above zero has at least the smallest code.
+__device__ __forceinline__ uint32_t root_codes4(const float* x) {
+  uint32_t w = cvt_fp8x4<false>(x[0], x[1], x[2], x[3]);
+  if ((w - 0x01010101u) & ~w & 0x80808080u) {                // a byte of zeros
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (x[i] > 0.f && !(w >> 8 * i & 0xffu)) w |= 1u << 8 * i;
+  }
+  return w;
+}
+
+// Where element `off` behind (row0, col0) of a matrix with padded rows is.
 struct Place {
   int64_t row0;
   int col0;
@@ -94,134 +134,288 @@ __device__ __forceinline__ Place place_of(const AdamTensor& t, int64_t e) {
   return {row, (int)(e - row * t.cols)};
 }
 __device__ __forceinline__ int64_t at(const AdamTensor& t, const Place& w, int off, int64_t ld) {
-  const int q = t.by_cols.div(w.col0 + off);
-  return (w.row0 + q) * ld + (w.col0 + off - q * t.cols);
+  const int rows = t.cols >= kUnit ? (int)(w.col0 + off >= t.cols) : t.by_cols.div(w.col0 + off);   // that lie between
+  return w.row0 * ld + w.col0 + off + rows * (ld - t.cols);
 }
 
-template <int MOST>
-__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constant__ AdamArgs<MOST> a) {
-  ptx::grid_sync_previous();
-  const float gf = a.grad_factor ? *a.grad_factor : 1.0f;
-  if (!(fabsf(gf) < INFINITY)) return;                       // the gradients were not finite: no step
-  const int64_t step = *a.step + 1;
-  // 1 - beta^t without cancellation at small t
-  const float fix1 = -expm1f((float)step * a.ln_beta1), fix2 = -expm1f((float)step * a.ln_beta2);
-  const float root_factor = 1.0f / sqrtf(fix2), lr = a.lr * (a.lr_factor ? *a.lr_factor : 1.0f), rate = lr / fix1;
-  const int lane = threadIdx.x & 31;
-  const uint32_t stride = gridDim.x * kWarps;
-  uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  int cur = 0;
-  if (unit < a.units) {                                      // the first tensor whose units end behind this one
-    int lo = 0, hi = a.count - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (unit < a.t[mid].unit_end) hi = mid; else lo = mid + 1;
-    }
-    cur = lo;
-  }
-  for (; unit < a.units; unit += stride) {
-    while (unit >= a.t[cur].unit_end) ++cur;
-    const AdamTensor& t = a.t[cur];
-    const uint32_t block = unit - (cur ? a.t[cur - 1].unit_end : 0u);
-    const int64_t base = (int64_t)block * kUnit;
-    const int here = (int)min((int64_t)kUnit, t.n - base);   // elements of this unit
-    const bool small = t.m_scale != nullptr, wide = t.wide && here == kUnit;
-    const bool padded = !t.dense || (t.copy && !t.copy_dense);
-    const Place w = padded ? place_of(t, base) : Place{0, 0};
-    float p[8], g[8], m[8], v[8];                            // v: the root of v where states are in 8 bits
-    const float sm = small ? t.m_scale[block] : 0.f, sv = small ? t.v_scale[block] : 0.f;
-    // element i of a lane: groups of four, or one of every 32
-    auto offset = [&](int i) { return wide ? 128 * (i >> 2) + 4 * lane + (i & 3) : 32 * i + lane; };
-    if (wide) {
+// What all units of a launch share.
+//   m = beta1 m + gm g,   v = beta2 v + (gv g)^2,   p = p - lr wd p - rate m / (sqrt(v) + eps)
+// with gm = (1 - beta1) grad_factor, gv = sqrt(1 - beta2) grad_factor, and sqrt(1 - beta2^t) taken out of the denominator into rate and eps.
+struct AdamStep {
+  float beta1, beta2, root_beta2, gm, gv, eps, lr, rate;
+};
+
+// The step of a lane's eight elements; sm, sv: the scales of states in 8 bits, whose codes m and v are (v's root).  Afterwards m is what is stored, and v, or where EIGHT root,
+// codes before their rounding; the block's scales are written.
+template <bool EIGHT>
+__device__ __forceinline__ void step8(const AdamStep& a, const AdamTensor& t, uint32_t block, int lane, float sm, float sv, float (&p)[8], const float (&g)[8], float (&m)[8],
+                                      float (&v)[8], float (&root)[8]) {
+  const f32x2 rate = splat2(-(a.rate * t.lr_factor)), decay = splat2(-(a.lr * t.lr_factor * t.decay));
+  const f32x2 keep_m = splat2(EIGHT ? a.beta1 * sm : a.beta1), keep_v = splat2(EIGHT ? a.root_beta2 * sv : a.beta2), gm = splat2(a.gm), gv = splat2(a.gv), eps = splat2(a.eps);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int off = 128 * k + 4 * lane;
-        load4(t.p, US_F32, t.dense ? base + off : at(t, w, off, t.p_ld), &p[4 * k]);
-        load4(t.g, t.g_dt, t.dense ? base + off : at(t, w, off, t.g_ld), &g[4 * k]);
-        if (small) {
-          load_codes4(t.m, base + off, sm, &m[4 * k]);
-          load_codes4(t.v, base + off, sv, &v[4 * k]);
-        } else {
-          load4(t.m, US_F32, base + off, &m[4 * k]);
-          load4(t.v, US_F32, base + off, &v[4 * k]);
-        }
+  for (int i = 0; i < 8; i += 2) {
+    const f32x2 gg = pack2(g[i], g[i + 1]), x = mul2(gv, gg), x2 = mul2(x, x);
+    const f32x2 mm = fma2(keep_m, pack2(m[i], m[i + 1]), mul2(gm, gg));
+    f32x2 vv = pack2(v[i], v[i + 1]);
+    if (EIGHT) {
+      vv = mul2(keep_v, vv);
+      vv = fma2(vv, vv, x2);
+    } else {
+      vv = fma2(keep_v, vv, x2);
+    }
+    unpack2(mm, m[i], m[i + 1]);
+    unpack2(vv, v[i], v[i + 1]);
+    root[i] = sqrt_approx(v[i]);
+    root[i + 1] = sqrt_approx(v[i + 1]);
+    float d0, d1;
+    unpack2(add2(pack2(root[i], root[i + 1]), eps), d0, d1);
+    const f32x2 pp = pack2(p[i], p[i + 1]);                  // (rounded once: what comes off it is formed first)
+    unpack2(add2(pp, fma2(decay, pp, mul2(rate, mul2(mm, pack2(rcp_approx(d0), rcp_approx(d1)))))), p[i], p[i + 1]);
+  }
+  if (EIGHT) {
+    const float most_m = warp_most(m), most_v = warp_most(root);
+    const f32x2 inv_m = splat2(most_m > kTiny ? __fdividef(kMostE4, most_m) : 0.f), inv_v = splat2(most_v > kTiny ? __fdividef(kMostE4, most_v) : 0.f);
+    if (lane == 0) { t.m_scale[block] = most_m * (1.0f / kMostE4); t.v_scale[block] = most_v * (1.0f / kMostE4); }
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      unpack2(mul2(pack2(m[i], m[i + 1]), inv_m), m[i], m[i + 1]);
+      unpack2(mul2(pack2(root[i], root[i + 1]), inv_v), root[i], root[i + 1]);
+    }
+  }
+}
+
+// A unit's copies whose rows cut groups of four: one element a lane, 32 neighbours at a time.
+__device__ __noinline__ void store_row(const AdamTensor& t, int64_t base, int lane, const float* row) {
+  __syncwarp();
+  const Place w = place_of(t, base);
+  char* first = static_cast<char*>(t.copy) + (w.row0 * t.copy_ld + w.col0) * dtype_size(t.copy_dt);
+  const int left = t.cols - w.col0;
+  const int64_t between = t.copy_ld - t.cols;                  // columns of the first row, and what lies between two rows
+  with_type(t.copy_dt, [&](auto dt) {
+    if (t.cols >= kUnit) {                                     // two rows at most
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int off = 32 * i + lane;
+        store_one(first, decltype(dt)::value, off + (off >= left ? between : 0), row[off]);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int off = 32 * i + lane;
-        p[i] = g[i] = m[i] = v[i] = 0.f;
-        if (off < here) {
-          p[i] = t.p[t.dense ? base + off : at(t, w, off, t.p_ld)];
-          g[i] = load_one(t.g, t.g_dt, t.dense ? base + off : at(t, w, off, t.g_ld));
-          m[i] = small ? sm * load_one(t.m, US_E4M3, base + off) : static_cast<const float*>(t.m)[base + off];
-          v[i] = small ? sv * load_one(t.v, US_E4M3, base + off) : static_cast<const float*>(t.v)[base + off];
-        }
+        store_one(first, decltype(dt)::value, off + t.by_cols.div(w.col0 + off) * between, row[off]);
       }
     }
-    const float my_rate = rate * t.lr_factor, decay = lr * t.lr_factor * t.decay;
-    float root[8];
+  });
+  __syncwarp();
+}
+
+// Whole units of a tensor whose groups of four are aligned.  With states in 8 bits a unit is more work for fewer bytes: it comes through shared memory while
+// the warp works on the unit before.  A lane copies what it will read itself, so that nothing but its own copies has to be waited for.  A warp's slot: rows of
+// 32 lanes' pieces, two of param, grad and the codes of m and v each, and one of each scale.
+constexpr int kGradAt = 1024, kMAt = 2048, kVAt = 2304, kScaleAt = 2560, kSlotBytes = 2816;
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+__device__ __forceinline__ void fetch_unit(const AdamTensor& t, uint32_t block, int lane, uint32_t slot) {
+  const int64_t base = (int64_t)block * kUnit;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = gf * g[i];
-      if (small) v[i] *= v[i];
-      m[i] = fmaf(a.beta1, m[i], a.rest1 * x);
-      v[i] = fmaf(a.beta2, v[i], a.rest2 * x * x);
-      root[i] = sqrt_approx(v[i]);
-      // p - (lr wd p + rate m / (root / sqrt(1 - beta2^t) + eps)): p is rounded once
-      p[i] -= fmaf(decay, p[i], my_rate * __fdividef(m[i], fmaf(root[i], root_factor, a.eps)));
-    }
-    float inv_m = 0.f, inv_v = 0.f;
-    if (small) {
-      const float most_m = warp_most(m), most_v = warp_most(root);
-      inv_m = most_m > kTiny ? kMostE4 / most_m : 0.f;
-      inv_v = most_v > kTiny ? kMostE4 / most_v : 0.f;
-      if (lane == 0) { t.m_scale[block] = most_m / kMostE4; t.v_scale[block] = most_v / kMostE4; }
+  for (int k = 0; k < 2; ++k) {
+    const int off = 128 * k + 4 * lane;
+    copy16(slot + 512 * k + 16 * lane, t.p + base + off);
+    if (t.g_dt == US_F32) copy16(slot + kGradAt + 512 * k + 16 * lane, static_cast<const float*>(t.g) + base + off);
+    else copy8(slot + kGradAt + 256 * k + 8 * lane, static_cast<const uint16_t*>(t.g) + base + off);
+    copy4(slot + kMAt + 128 * k + 4 * lane, static_cast<const uint8_t*>(t.m) + base + off);
+    copy4(slot + kVAt + 128 * k + 4 * lane, static_cast<const uint8_t*>(t.v) + base + off);
+  }
+  copy4(slot + kScaleAt + 4 * lane, t.m_scale + block);
+  copy4(slot + kScaleAt + 128 + 4 * lane, t.v_scale + block);
+}
+
+// The step of a unit, from its tensor or (EIGHT) from the slot; `refill` starts the copies that take the slot next, once this lane has read what is there.
+template <bool EIGHT, int GRAD, class F>
+__device__ __forceinline__ void unit_step(const AdamStep& a, const AdamTensor& t, uint32_t block, int lane, const char* slot, float* row, F refill) {
+  const int64_t base = (int64_t)block * kUnit;
+  using States = std::conditional_t<EIGHT, uint32_t, float4>;
+  using Grads = std::conditional_t<GRAD == US_F32, float4, uint2>;
+  float4 p4[2];
+  Grads g4[2];
+  States m4[2], v4[2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        m[i] *= inv_m;
-        v[i] = root[i] * inv_v;
-        v[i] = v[i] > 0.f ? fmaxf(v[i], 0x1p-9f) : v[i];     // the smallest code: no denominator is lost
-      }
+  for (int k = 0; k < 2; ++k) {
+    if (EIGHT) {
+      p4[k] = reinterpret_cast<const float4*>(slot)[32 * k + lane];
+      g4[k] = reinterpret_cast<const Grads*>(slot + kGradAt)[32 * k + lane];
+      m4[k] = reinterpret_cast<const States*>(slot + kMAt)[32 * k + lane];
+      v4[k] = reinterpret_cast<const States*>(slot + kVAt)[32 * k + lane];
+    } else {
+      const int off = 128 * k + 4 * lane;
+      p4[k] = *reinterpret_cast<const float4*>(t.p + base + off);
+      g4[k] = *reinterpret_cast<const Grads*>(static_cast<const char*>(t.g) + (base + off) * (GRAD == US_F32 ? 4 : 2));
+      m4[k] = *reinterpret_cast<const States*>(static_cast<const float*>(t.m) + base + off);
+      v4[k] = *reinterpret_cast<const States*>(static_cast<const float*>(t.v) + base + off);
     }
-    const int state_dt = small ? US_E4M3 : US_F32;
+  }
+  const float sm = EIGHT ? reinterpret_cast<const float*>(slot + kScaleAt)[lane] : 0.f, sv = EIGHT ? reinterpret_cast<const float*>(slot + kScaleAt + 128)[lane] : 0.f;
+  float p[8], g[8], m[8], v[8], root[8];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    four(p4[k], US_F32, &p[4 * k]);
+    four(g4[k], GRAD, &g[4 * k]);
+    four(m4[k], EIGHT ? US_E4M3 : US_F32, &m[4 * k]);
+    four(v4[k], EIGHT ? US_E4M3 : US_F32, &v[4 * k]);
+  }
+  refill();
+  step8<EIGHT>(a, t, block, lane, sm, sv, p, g, m, v, root);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int off = 128 * k + 4 * lane;
+    store4<US_F32>(t.p, base + off, &p[4 * k]);
+    store4<EIGHT ? US_E4M3 : US_F32>(t.m, base + off, &m[4 * k]);
+    if (EIGHT) *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + base + off) = root_codes4(&root[4 * k]);
+    else store4<US_F32>(t.v, base + off, &v[4 * k]);
+  }
+  if (t.copy) {
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = t.copy_scale * p[i];
-    if (wide) {
+    if (t.copy_wide) {
+      const Place w = t.copy_dense ? Place{0, 0} : place_of(t, base);
+      with_type(t.copy_dt, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int off = 128 * k + 4 * lane;
-        store4(t.p, US_F32, t.dense ? base + off : at(t, w, off, t.p_ld), &p[4 * k]);
-        store4(t.m, state_dt, base + off, &m[4 * k]);
-        store4(t.v, state_dt, base + off, &v[4 * k]);
-        if (t.copy && t.copy_wide) store4(t.copy, t.copy_dt, t.copy_dense ? base + off : at(t, w, off, t.copy_ld), &y[4 * k]);
-      }
-      if (t.copy && !t.copy_wide) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) store_one(t.copy, t.copy_dt, t.copy_dense ? base + offset(i) : at(t, w, offset(i), t.copy_ld), y[i]);
-      }
+        for (int k = 0; k < 2; ++k) {
+          const int off = 128 * k + 4 * lane;
+          store4<DT>(t.copy, t.copy_dense ? base + off : at(t, w, off, t.copy_ld), &y[4 * k]);
+        }
+      });
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int off = 32 * i + lane;
-        if (off < here) {
-          t.p[t.dense ? base + off : at(t, w, off, t.p_ld)] = p[i];
-          store_one(t.m, state_dt, base + off, m[i]);
-          store_one(t.v, state_dt, base + off, v[i]);
-          if (t.copy) store_one(t.copy, t.copy_dt, t.copy_dense ? base + off : at(t, w, off, t.copy_ld), y[i]);
-        }
+      for (int k = 0; k < 2; ++k) *reinterpret_cast<float4*>(row + 128 * k + 4 * lane) = make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+      store_row(t, base, lane, row);
+    }
+  }
+}
+
+// Any unit: a lane has every 32nd element.
+template <bool EIGHT>
+__device__ __noinline__ void unit_step_any(AdamStep a, const AdamTensor& t, uint32_t block, int lane) {
+  const int64_t base = (int64_t)block * kUnit;
+  const int here = (int)min((int64_t)kUnit, t.n - base);     // elements of this unit
+  const Place w = !t.dense || (t.copy && !t.copy_dense) ? place_of(t, base) : Place{0, 0};
+  float p[8], g[8], m[8], v[8];
+  const float sm = EIGHT ? t.m_scale[block] : 0.f, sv = EIGHT ? t.v_scale[block] : 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int off = 32 * i + lane;
+    p[i] = g[i] = m[i] = v[i] = 0.f;
+    if (off < here) {
+      p[i] = t.p[t.dense ? base + off : at(t, w, off, t.p_ld)];
+      g[i] = load_one(t.g, t.g_dt, t.dense ? base + off : at(t, w, off, t.g_ld));
+      m[i] = load_one(t.m, EIGHT ? US_E4M3 : US_F32, base + off);
+      v[i] = load_one(t.v, EIGHT ? US_E4M3 : US_F32, base + off);
+    }
+  }
+  float root[8];
+  step8<EIGHT>(a, t, block, lane, sm, sv, p, g, m, v, root);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int off = 32 * i + lane;
+    if (off < here) {
+      t.p[t.dense ? base + off : at(t, w, off, t.p_ld)] = p[i];
+      store_one(t.m, EIGHT ? US_E4M3 : US_F32, base + off, m[i]);
+      store_one(t.v, EIGHT ? US_E4M3 : US_F32, base + off, EIGHT && root[i] > 0.f ? fmaxf(root[i], 0x1p-9f) : EIGHT ? root[i] : v[i]);
+      if (t.copy) store_one(t.copy, t.copy_dt, t.copy_dense ? base + off : at(t, w, off, t.copy_ld), t.copy_scale * p[i]);
+    }
+  }
+}
+
+// EIGHT: tensors with states in 8 bits, else those in 32.
+template <bool EIGHT, int MOST>
+__global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const __grid_constant__ AdamArgs<MOST> a) {
+  __shared__ __align__(16) float rows[kWarps][kUnit];        // (units whose copies have rows that cut groups of four)
+  __shared__ __align__(16) char slots[kWarps][EIGHT ? kSlotBytes : 16];
+  __shared__ int64_t made;
+  __shared__ uint32_t taken[2];
+  ptx::grid_sync_previous();
+  if (threadIdx.x == 0) made = *a.step;
+  const float grad_factor = a.grad_factor ? *a.grad_factor : 1.0f, lr_factor = a.lr_factor ? *a.lr_factor : 1.0f;
+  __syncthreads();
+  if (!(fabsf(grad_factor) < INFINITY)) return;              // the gradients were not finite: no step
+  const int64_t step = made + 1;
+  // 1 - beta^t without cancellation at small t
+  const float fix1 = -expm1f((float)step * a.ln_beta1), root_fix2 = sqrtf(-expm1f((float)step * a.ln_beta2));
+  AdamStep s;
+  s.beta1 = a.beta1; s.beta2 = a.beta2; s.root_beta2 = a.root_beta2;
+  s.gm = a.rest1 * grad_factor; s.gv = a.root_rest2 * grad_factor;
+  s.eps = a.eps * root_fix2;
+  s.lr = a.lr * lr_factor;
+  s.rate = s.lr * root_fix2 / fix1;
+  // (handed round from one lane, the warp's number is known to be the same in all of them: what depends on it alone -- which tensor, where its
+  // fields and addresses are -- is worked out once for the warp, by the uniform datapath)
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0);
+  unsigned int* count = reinterpret_cast<unsigned int*>(a.step + 1);
+  const uint32_t chunks = (a.units + kWarps - 1) / kWarps;
+  int cur = 0, ahead = 0;                                    // tensors of the unit at hand, and of the one fetched
+  {                                                          // the first tensor whose units end behind this CTA's first
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (blockIdx.x * kWarps < a.t[mid].unit_end) hi = mid; else lo = mid + 1;
+    }
+    cur = ahead = lo;
+  }
+  auto block_of = [&](uint32_t unit, int k) { return unit - (k ? a.t[k - 1].unit_end : 0u); };
+  auto whole = [&](const AdamTensor& t, uint32_t block) { return t.wide && (int64_t)(block + 1) * kUnit <= t.n; };
+  auto fetch = [&](uint32_t unit) {
+    if (EIGHT && unit < a.units) {
+      while (unit >= a.t[ahead].unit_end) ++ahead;
+      const uint32_t block = block_of(unit, ahead);
+      if (whole(a.t[ahead], block)) fetch_unit(a.t[ahead], block, lane, ptx::smem_addr(slots[warp]));
+    }
+  };
+  // A CTA's first chunks (one unit a warp) are set, the others are taken as it comes to them, so that chunks are worked on in their order and what all SMs read
+  // and write at a time stays close together (us, 201 million parameters, states in 32 bits: 943 where every CTA walks with a fixed stride and SMs drift apart,
+  // 845 so; two chunks at a time 857, four 862).  What is fetched ahead has to be taken one chunk sooner.
+  constexpr uint32_t kSet = EIGHT ? 2 : 1;
+  uint32_t chunk = blockIdx.x, after = gridDim.x + blockIdx.x;
+  fetch(chunk * kWarps + warp);
+  for (int turn = 0; chunk < chunks; turn ^= 1) {
+    uint32_t next = 0;
+    if (threadIdx.x == 0) next = atomicAdd(count, 1u);       // (needed only once the chunk is done)
+    const uint32_t unit = chunk * kWarps + warp;
+    if (EIGHT) copies_wait();
+    auto refill = [&] { fetch(after * kWarps + warp); };
+    if (unit < a.units) {
+      while (unit >= a.t[cur].unit_end) ++cur;
+      const AdamTensor& t = a.t[cur];
+      const uint32_t block = block_of(unit, cur);
+      if (whole(t, block)) {
+        with_grad_type(t.g_dt, [&](auto dt) { unit_step<EIGHT, decltype(dt)::value>(s, t, block, lane, slots[warp], rows[warp], refill); });
+      } else {
+        refill();
+        unit_step_any<EIGHT>(s, t, block, lane);
       }
     }
-  }
-  // Every CTA has read the count of steps; the last one to end raises it.
-  if (a.last) {
-    __syncthreads();
     if (threadIdx.x == 0) {
-      unsigned int* ended = reinterpret_cast<unsigned int*>(a.step + 1);
-      if (atomicAdd(ended, 1u) == gridDim.x - 1) { *a.step = step; *ended = 0; }
+      taken[turn] = kSet * gridDim.x + next;
+      // As many have counted as there are chunks: none will, and all CTAs have read the count of steps.
+      if (next == chunks - 1) {
+        if (a.last) *a.step = step;
+        *count = 0;
+      }
     }
+    __syncthreads();
+    chunk = EIGHT ? after : taken[turn];
+    after = taken[turn];
   }
+}
+
+// The step of a call whose tensors have no elements.
+__global__ void count_step_kernel(int64_t* step, const float* grad_factor) {
+  ptx::grid_sync_previous();
+  if (threadIdx.x == 0 && (!grad_factor || fabsf(*grad_factor) < INFINITY)) *step += 1;
 }
 
 // ---------------------------------------------------------------- norm
@@ -272,16 +466,18 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     const int here = (int)min((int64_t)kNormUnit, t.n - base);
     // sums of 8 squares in float32, then in float64
     if (t.wide && here == kNormUnit) {
-      float x[32];
+      with_grad_type(t.dt, [&](auto dt) {
+        float x[32];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) load4(t.g, t.dt, base + 128 * k + 4 * lane, &x[4 * k]);
+        for (int k = 0; k < 8; ++k) load4<decltype(dt)::value>(t.g, base + 128 * k + 4 * lane, &x[4 * k]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float s = 0.f;
+        for (int k = 0; k < 4; ++k) {
+          float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(x[8 * k + i], x[8 * k + i], s);
-        sum += (double)s;
-      }
+          for (int i = 0; i < 8; ++i) s = fmaf(x[8 * k + i], x[8 * k + i], s);
+          sum += (double)s;
+        }
+      });
     } else {
       const int64_t row0 = t.dense ? 0 : base / t.cols;
       const int col0 = t.dense ? 0 : (int)(base - row0 * t.cols);
@@ -395,15 +591,13 @@ AdamTensor describe(const us_adamw_tensor& t) {
   d.copy_scale = t.copy_scale; d.lr_factor = t.lr_factor; d.decay = t.weight_decay;
   d.g_dt = (uint8_t)t.grad.dtype; d.copy_dt = (uint8_t)t.copy.dtype;
   d.dense = dense(t.param) && dense(t.grad);
-  // (a matrix without padded rows beside one with them is walked as those are)
-  const bool rows_of_four = d.dense || t.param.cols % 4 == 0;
-  d.wide = fours(t.param) && fours(t.grad) && fours(t.m) && fours(t.v) && rows_of_four;
+  d.wide = d.dense && fours(t.param) && fours(t.grad) && fours(t.m) && fours(t.v);
   d.copy_dense = t.copy.ptr && dense(t.copy);
   d.copy_wide = t.copy.ptr && fours(t.copy);
   return d;
 }
 
-template <int MOST>
+template <bool EIGHT, int MOST>
 us_status launch_adamw(AdamArgs<MOST>& a, const us_adamw_tensor* const* ts, int count, cudaStream_t stream) {
   const int sms = host::sm_count();
   if (sms <= 0) return US_ERR_CUDA;
@@ -416,14 +610,14 @@ us_status launch_adamw(AdamArgs<MOST>& a, const us_adamw_tensor* const* ts, int 
   }
   a.count = count;
   a.units = (uint32_t)units;
-  const int grid = (int)std::max<uint64_t>(1, std::min<uint64_t>((units + kWarps - 1) / kWarps, (uint64_t)sms * 4));
-  return host::launch(adamw_kernel<MOST>, nullptr, grid, kThreads, 0, 1, stream, a);
+  const int grid = (int)std::min<uint64_t>((units + kWarps - 1) / kWarps, (uint64_t)(sms * adam_ctas(EIGHT)));
+  return host::launch(adamw_kernel<EIGHT, MOST>, nullptr, grid, kThreads, 0, 1, stream, a);
 }
 
 template <class A>
 void set_options(A& a, double lr, double beta1, double beta2, double eps, const float* lr_factor, const float* grad_factor, int64_t* step) {
   a.lr = (float)lr; a.beta1 = (float)beta1; a.beta2 = (float)beta2; a.eps = (float)eps;
-  a.rest1 = (float)(1.0 - beta1); a.rest2 = (float)(1.0 - beta2);
+  a.rest1 = (float)(1.0 - beta1); a.root_rest2 = (float)sqrt(1.0 - beta2); a.root_beta2 = (float)sqrt(beta2);
   a.ln_beta1 = (float)log(beta1); a.ln_beta2 = (float)log(beta2);
   a.lr_factor = lr_factor; a.grad_factor = grad_factor; a.step = step;
 }
@@ -444,8 +638,9 @@ us_status launch_norm(NormArgs<MOST>& a, const us_mat* const* ms, int count, cud
   }
   a.count = count;
   a.units = (uint32_t)units;
-  // the same grid for every launch of a call: a CTA's sum is carried on by the CTA of that number
-  const int grid = std::min(sms * 4, kMostCtas);
+  // where there are several launches, all have one grid: a CTA's sum is carried on by the CTA of that number
+  const uint64_t want = a.first && a.last ? std::max<uint64_t>(1, (units + kWarps - 1) / kWarps) : kMostCtas;
+  const int grid = (int)std::min<uint64_t>({want, (uint64_t)sms * 4, (uint64_t)kMostCtas});
   return host::launch(norm_kernel<MOST>, nullptr, grid, kThreads, 0, 1, stream, a);
 }
 
@@ -464,30 +659,39 @@ extern "C" us_status us_adamw(int count, const us_adamw_tensor* tensors, double 
     if (s != US_OK) return s;
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const us_adamw_tensor* ts[kMany];
-  auto go = [&](auto& a, int n, bool last) {
+  // Launches: the tensors with states in 32 bits, then those in 8, as many to one as its table holds.  The last launch counts the step.
+  auto go = [&](auto& a, auto eight, const us_adamw_tensor* const* ts, int n, bool last) {
     set_options(a, lr, beta1, beta2, eps, lr_factor, grad_factor, step);
     a.last = last;
-    return launch_adamw(a, ts, n, st);
+    return launch_adamw<decltype(eight)::value>(a, ts, n, st);
   };
-  int n = 0;
-  for (int i = 0; i < count; ++i) {
-    if (elements(tensors[i].param) > 0) {
-      if (n == kMany) {                                      // the table is full, and there is more
-        AdamArgs<kMany> a;
-        const us_status s = go(a, n, false);
-        if (s != US_OK) return s;
-        n = 0;
-      }
+  auto table = [&](auto eight, const us_adamw_tensor* const* ts, int n, bool last) {
+    if (n <= kFew) {
+      AdamArgs<kFew> a;
+      return go(a, eight, ts, n, last);
+    }
+    AdamArgs<kMany> a;
+    return go(a, eight, ts, n, last);
+  };
+  auto is_eight = [](const us_adamw_tensor& t) { return t.m.dtype == US_E4M3; };
+  int64_t left[2] = {0, 0};                                  // tensors with elements, not launched yet
+  for (int i = 0; i < count; ++i)
+    if (elements(tensors[i].param) > 0) ++left[is_eight(tensors[i])];
+  if (left[0] + left[1] == 0) return us::host::launch(count_step_kernel, nullptr, 1, 32, 0, 1, st, step, grad_factor);
+  const us_adamw_tensor* ts[kMany];
+  for (int eight = 0; eight < 2; ++eight) {
+    for (int i = 0, n = 0; left[eight] > 0; ++i) {
+      if (elements(tensors[i].param) == 0 || is_eight(tensors[i]) != (eight == 1)) continue;
       ts[n++] = &tensors[i];
+      if (n < kMany && n < left[eight]) continue;
+      left[eight] -= n;
+      const bool last = left[0] + left[1] == 0;
+      const us_status s = eight ? table(std::true_type(), ts, n, last) : table(std::false_type(), ts, n, last);
+      if (s != US_OK) return s;
+      n = 0;
     }
   }
-  if (n <= kFew) {
-    AdamArgs<kFew> a;
-    return go(a, n, true);
-  }
-  AdamArgs<kMany> a;
-  return go(a, n, true);
+  return US_OK;
 }
 
 extern "C" size_t us_grad_norm_workspace_bytes(void) { return 64 + kMostCtas * sizeof(double); }
