@@ -512,6 +512,23 @@ def grad_norm(grads, max_norm):
     return norm, min(1.0, _f32(max_norm) / norm) if norm > 0 else 1.0
 
 
+def bias_ffn_block(X, W1, b1, W2, b2, G, sc: FFNScales, operand: str = "fp8", h_dtype: str = "bf16", io_dtype: str = "bf16"):
+    """ffn_block with a bias in each linear layer: (results, db1, db2); operand, h_dtype and io_dtype may be "f64" (nothing is rounded)."""
+    act_fmt, grad_fmt = ("e4m3", "e5m2") if operand == "fp8" else (operand, operand)
+    r = FFNResult()
+    r.Xq, r.W1q, r.W2q, r.Gq = (store(np.asarray(t), f)[0] for t, f in ((X, act_fmt), (W1, act_fmt), (W2, act_fmt), (G, grad_fmt)))
+    c_skip, c_branch = S.residual_coefficients(sc.tau)
+    ep1 = Epilogue(act="gelu", act_in_scale=sc.s_in, act_out_scale=sc.alpha_g, aux_dtype=h_dtype)
+    r.Aq, r.Aq_codes, r.H = apply_epilogue(linear_bias_fwd(r.Xq, r.W1q, sc.alpha1, b1), ep1, act_fmt)
+    r.R, _, _ = apply_epilogue(linear_bias_fwd(r.Aq, r.W2q, sc.alpha2, b2), Epilogue(skip=np.asarray(X, np.float64), skip_coef=c_skip, out_coef=c_branch), io_dtype)
+    r.dHq, r.dHq_codes, _ = apply_epilogue(linear_bwd_x(r.Gq, r.W2q, sc.beta_x2), Epilogue(act="gelu_grad", act_in_scale=sc.s_in, act_out_scale=sc.beta_g, aux=r.H), grad_fmt)
+    full = "f64" if operand == "f64" else "f32"
+    r.dW2, _ = store(linear_bwd_w(r.Aq, r.Gq, sc.beta_w), full)
+    r.dW1, _ = store(linear_bwd_w(r.Xq, r.dHq, sc.beta_w), full)
+    r.dX, _, _ = apply_epilogue(linear_bwd_x(r.dHq, r.W1q, sc.beta_x1), Epilogue(skip=np.asarray(G, np.float64), skip_coef=c_skip, out_coef=c_branch), io_dtype)
+    return r, bias_grad(r.dHq, sc.beta_w), bias_grad(r.Gq, sc.beta_w)
+
+
 @dataclass
 class AdamWStep:
     p: np.ndarray

@@ -391,6 +391,24 @@ PyObject* unchanged(PyObject*, PyObject* const* o, Py_ssize_t n) {
   });
 }
 
+// fill(address, stride, tensors): descriptions of the tensors of a list (1-D ones are rows, None: nothing is written), `stride` bytes apart.
+PyObject* fill(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 3 || !PyList_Check(o[2])) fail(PyExc_TypeError, "fill(address, stride, list)");
+    char* at = static_cast<char*>(PyLong_AsVoidPtr(o[0]));
+    const size_t stride = PyLong_AsSize_t(o[1]);
+    if (PyErr_Occurred()) throw Failed();
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(o[2]); ++i, at += stride) {
+      PyObject* t = PyList_GET_ITEM(o[2], i);
+      if (t == Py_None) continue;
+      if (!THPVariable_Check(t)) fail(PyExc_TypeError, "expected tensors");
+      if (!THPVariable_Unpack(t).is_cuda()) fail(PyExc_ValueError, "expected CUDA tensors");
+      *reinterpret_cast<us_mat*>(at) = describe(t, true);
+    }
+    Py_RETURN_NONE;
+  });
+}
+
 // register_types((us_mat, us_epilogue, us_batch, us_attention_batch, us_attention_bwd_batch, us_attention_bwd_all_batch, us_linear_call,
 // us_adamw_tensor, c_float)): the ctypes types of the parameters; every argument is checked against its own
 template <class... T>
@@ -410,6 +428,7 @@ PyObject* register_types(PyObject*, PyObject* const* o, Py_ssize_t n) {
 
 PyMethodDef g_methods[] = {
     {"register_types", (PyCFunction)(void (*)(void))register_types, METH_FASTCALL, nullptr},
+    {"fill", (PyCFunction)(void (*)(void))fill, METH_FASTCALL, nullptr},
     {"unchanged", (PyCFunction)(void (*)(void))unchanged, METH_FASTCALL, nullptr},
     {"prepare", (PyCFunction)(void (*)(void))prepare, METH_FASTCALL, nullptr},
     {"program", (PyCFunction)(void (*)(void))program, METH_FASTCALL, nullptr},

@@ -415,6 +415,82 @@ class UnitScaledFFN:
         return 12.0 * T * d * f
 
 
+class UnitScaledBiasFFN(UnitScaledFFN):
+    """An FFN block whose linear layers have biases (b1 [f], b2 [d], float32, zeros at first, the block's own as their gradients db1, db2 are):
+
+        H = alpha1 q(X) q(W1) + b1 ; A = q(alpha_g gelu(s_in H)), H kept            us_linear_fwd_bias + GELU epilogue
+        R = sqrt(1-tau) X + sqrt(tau) (alpha2 A W2q + b2)                           us_linear_fwd_bias + residual epilogue
+        dH = q(beta_g s_in gelu'(s_in H) * beta_x2 Gq W2q^T)                        us_linear_bwd_x + GELU-grad epilogue
+        db1 = beta_w sum over rows of dH ; db2 = beta_w sum over rows of Gq         us_bias_grad
+        dW2, dW1 and dX as for the block without biases                             us_linear_group_any
+
+    A bias is a cut-edge as a weight is: its gradient takes beta_w = b^-1/2.  step(), forward() and backward() are used as those of UnitScaledFFN.  W1 and
+    W2 may be None where self.W1q and self.W2q hold the weights already, as an optimiser that writes them does (optim.AdamW)."""
+
+    def __init__(self, T: int, d: int, f: int, scales: FFNScales | None = None, operand: str = "fp8", h_dtype=torch.bfloat16, io_dtype=torch.bfloat16, device="cuda"):
+        super().__init__(T, d, f, scales, operand, h_dtype, io_dtype, device, keep_h=True)
+        zeros = lambda n: torch.zeros(n, dtype=torch.float32, device=device)
+        self.b1, self.b2, self.db1, self.db2 = zeros(f), zeros(d), zeros(f), zeros(d)
+
+    def _owned(self):
+        return super()._owned() + (self.b1, self.b2, self.db1, self.db2)
+
+    def _plan_linear(self, p, a, w, scale, bias, ep, out):
+        return L.Call("us_linear_fwd_bias", p.mat(a), p.mat(w), scale, p.mat(bias.view(1, -1)), ep, p.mat(out), None, self.ws.data_ptr(), self.ws.numel())
+
+    def _plan_step_of_operands(self, p):
+        yield p.cast_multi(["X", "G"], [self.Xq, self.Gq], padded=self.operand != "fp8")
+        yield from self.plan_gemms(p, "X", "G")
+
+    def plan_gemms(self, p, X, G, dX_copy=None):
+        yield from self.plan_forward(p, X, cast_x=False)
+        yield from self.plan_backward(p, G, cast_g=False, dX_copy=dX_copy)
+
+    def plan_forward(self, p, X, cast_x=True):
+        sc = self.sc
+        if cast_x:
+            yield self._plan_cast(p, X, self.Xq)
+        yield self._plan_linear(p, self.Xq, self.W1q, sc.alpha1, self.b1, L.epilogue(act=L.US_ACT_GELU, act_in_scale=sc.s_in, act_out_scale=sc.alpha_g, aux=self.H), self.Aq)
+        yield self._plan_linear(p, self.Aq, self.W2q, sc.alpha2, self.b2, p.residual(X, self._c), self.R)
+
+    def plan_backward(self, p, G, cast_g=True, dX_copy=None):
+        sc = self.sc
+        if cast_g:
+            yield self._plan_cast(p, G, self.Gq)
+        yield p.linear("us_linear_bwd_x", self.Gq, self.W2q, sc.beta_x2, self.dHq, self.ws,
+                       L.epilogue(act=L.US_ACT_GELU_GRAD, act_in_scale=sc.s_in, act_out_scale=sc.beta_g, aux=self.H))
+        yield p.bias_grad([self.dHq, self.Gq], [sc.beta_w] * 2, [self.db1, self.db2])
+        yield p.group(self._plan_backward_entries(G), self.ws, {2: dX_copy} if dX_copy is not None else None)
+
+    @property
+    def gemm_launches(self) -> int:
+        """Launches of a step without its casts: the two forward GEMMs, the GELU-gradient GEMM, the biases' gradients and the grouped launch (two where it
+        shares contractions)."""
+        return 4 + self._group_launches(forward=False)
+
+    @property
+    def launches_per_step(self) -> int:
+        return 1 + self.gemm_launches
+
+    def backward(self, G, stream=None, cast_g: bool = True):
+        self._run("backward" if cast_g else "backward_from_cast", stream, G=G)
+        return self.dX, self.dW1, self.dW2
+
+    def step(self, X, W1, W2, G, stream=None):
+        if (W1 is None) != (W2 is None):
+            raise ValueError("both weights, or neither")
+        if W1 is None:
+            self._run("step_of_operands", stream, X=X, G=G)
+        else:
+            self._run("step", stream, X=X, W1=W1, W2=W2, G=G)
+        return self.dX, self.dW1, self.dW2
+
+    def stages(self, *args, **kwargs):
+        raise NotImplementedError("a block with biases has no other launches")
+
+    step_launches = step_from_casts = group_calls = backward_calls = stages
+
+
 @dataclass
 class GatedScales:
     alpha1: float

@@ -421,6 +421,11 @@ class Plan:
     def linear(self, name, a, b, scale, out, ws, ep=None):
         return Call(name, self.mat(a), self.mat(b), scale, ep, self.mat(out), ws.data_ptr(), ws.numel())
 
+    def bias_grad(self, grads, beta, db):
+        """us_bias_grad; db: vectors."""
+        n = len(grads)
+        return Call("us_bias_grad", n, (us_mat * n)(*[self.mat(g) for g in grads]), (C.c_float * n)(*beta), (us_mat * n)(*[_vec(t) for t in db]))
+
     def batched(self, name, a, b, scale, out, bt, ws):
         return Call(name, self.mat(a), self.mat(b), scale, self.mat(out), bt, ws.data_ptr(), ws.numel())
 
@@ -906,10 +911,17 @@ def us_bias_grad(G, beta, db, stream=None):
     return db
 
 
+def _fill(arr, column: int, tensors) -> None:
+    """Descriptions of CUDA tensors (1-D ones are rows; None: left empty) into the us_mat number `column` of every structure of an array."""
+    _binding.fill(C.addressof(arr) + column * C.sizeof(us_mat), C.sizeof(arr._type_), tensors)
+
+
 def mats(tensors):
     """An array of us_mat for us_grad_norm, laid out once for tensors that stay where they are; 1-D tensors are rows."""
-    arr = (us_mat * len(tensors))(*[_vec(t) if t.dim() == 1 else mat(t) for t in tensors])
-    arr._keep_alive = tuple(tensors)
+    tensors = list(tensors)
+    arr = (us_mat * len(tensors))()
+    _fill(arr, 0, tensors)
+    arr._keep_alive = tensors
     return arr
 
 
@@ -939,14 +951,11 @@ def adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, 
     numbers = [each(copy_scale), each(lr_factor), each(weight_decay)]
     if any(len(c) != n for c in columns + numbers):
         raise ValueError("one entry per tensor is wanted")
-    if any(t is not None and not t.is_cuda for c in columns for t in c):
-        raise ValueError("expected CUDA tensors")
     arr = (us_adamw_tensor * n)()
-    for a, ts, ns in zip(arr, zip(*columns), zip(*numbers)):
-        for name, t in zip(("param", "grad", "m", "v", "m_scale", "v_scale", "copy"), ts):
-            if t is not None:
-                setattr(a, name, _vec(t) if t.dim() == 1 else mat(t))
-        a.copy_scale, a.lr_factor, a.weight_decay = ns
+    for k, c in enumerate(columns):
+        _fill(arr, k, c)
+    for a, *a_numbers in zip(arr, *numbers):
+        a.copy_scale, a.lr_factor, a.weight_decay = a_numbers
     arr._keep_alive = columns
     return arr
 

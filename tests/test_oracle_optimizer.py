@@ -58,3 +58,24 @@ def test_bias_gradient_against_differences():
     # with a unit-normal gradient of b rows, b^-1/2 makes a unit-normal gradient of the bias
     G = rng.standard_normal((4096, 512))
     assert abs(O.bias_grad(G, 4096 ** -0.5).std() - 1) < 0.1
+
+
+def test_block_with_biases_against_differences():
+    """Nothing rounded: both bias gradients are the loss's true ones times constants (a bias is a cut-edge), with L = sum(R * G)."""
+    rng = np.random.default_rng(2)
+    T, d, f = 7, 5, 6
+    X, W1, W2, G = (rng.standard_normal(s) for s in ((T, d), (d, f), (f, d), (T, d)))
+    b1, b2 = rng.standard_normal(f), rng.standard_normal(d)
+    sc = O.FFNScales.unconstrained(T, d, f)
+    run = lambda b1, b2: O.bias_ffn_block(X, W1, b1, W2, b2, G, sc, "f64", "f64", "f64")
+    loss = lambda b1, b2: float((run(b1, b2)[0].R * G).sum())
+    _, db1, db2 = run(b1, b2)
+    h = 1e-5
+    d1 = [(loss(b1 + e, b2) - loss(b1 - e, b2)) / (2 * h) for e in h * np.eye(f)]
+    d2 = [(loss(b1, b2 + e) - loss(b1, b2 - e)) / (2 * h) for e in h * np.eye(d)]
+    branch = math.sqrt(sc.tau)
+    assert np.allclose(d2, db2 * branch / sc.beta_w, rtol=1e-6)
+    assert np.allclose(d1, db1 * branch / sc.beta_w * (np.float32(sc.alpha2) / np.float32(sc.beta_x2)) * (np.float32(sc.alpha_g) / np.float32(sc.beta_g)), rtol=1e-5)
+    plain = O.ffn_block(X, W1, W2, G, sc, operand="f64", h_dtype="f64", io_dtype="f64")
+    zero, _, _ = O.bias_ffn_block(X, W1, np.zeros(f), W2, np.zeros(d), G, sc, "f64", "f64", "f64")
+    assert np.allclose(plain.R, zero.R) and np.allclose(plain.dW1, zero.dW1, atol=1e-6) and np.allclose(plain.dX, zero.dX)
