@@ -398,11 +398,15 @@ PyObject* fill(PyObject*, PyObject* const* o, Py_ssize_t n) {
     char* at = static_cast<char*>(PyLong_AsVoidPtr(o[0]));
     const size_t stride = PyLong_AsSize_t(o[1]);
     if (PyErr_Occurred()) throw Failed();
+    int device = -1;
     for (Py_ssize_t i = 0; i < PyList_GET_SIZE(o[2]); ++i, at += stride) {
       PyObject* t = PyList_GET_ITEM(o[2], i);
       if (t == Py_None) continue;
       if (!THPVariable_Check(t)) fail(PyExc_TypeError, "expected tensors");
-      if (!THPVariable_Unpack(t).is_cuda()) fail(PyExc_ValueError, "expected CUDA tensors");
+      const at::Tensor& tensor = THPVariable_Unpack(t);
+      if (!tensor.is_cuda()) fail(PyExc_ValueError, "expected CUDA tensors");
+      if (device >= 0 && tensor.get_device() != device) fail(PyExc_ValueError, "expected tensors of one device");
+      device = (int)tensor.get_device();
       *reinterpret_cast<us_mat*>(at) = describe(t, true);
     }
     Py_RETURN_NONE;

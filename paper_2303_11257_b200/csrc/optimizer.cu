@@ -1,10 +1,16 @@
 // us_adamw: one AdamW step over many tensors in one launch, with states in 32 or 8 bits and the matmul operands of the next step;
 // us_grad_norm: the 2-norm of all gradients and the factor that clips them.
 //
-// Both are bound by the bytes of their tensors.  The tensors are cut into units of 256 consecutive elements, which are dealt to the warps
-// of a grid that is resident at once; a lane has two groups of four elements, so that every access is 16 bytes wide and a warp's accesses
-// are whole lines.  The descriptions of the tensors travel as a kernel parameter: no table in device memory has to be kept or written,
-// and a captured launch holds its own.
+// Both are bound by the bytes of their tensors.  These are cut into blocks of 256 consecutive elements, of which a warp steps one at a time: a lane has two groups of
+// four, so that its accesses are 16 bytes wide and the warp's are whole lines.  The descriptions of the tensors travel as a kernel parameter: no table in device
+// memory has to be kept or written, and a captured launch holds its own.
+//
+// Measured on 201 million parameters (a copy moves 6.46 TB/s on the same card): states in 32 bits, FP8 operands written, 29 bytes an element, 845 us = 6.9 TB/s; states
+// in 8 bits, BF16 gradients and operands, 16 bytes, 495 us = 6.5 TB/s, 540 under a load that holds the clock down: this one is bound by its instructions as
+// well, about 50 a lane and element.  What made the difference, in us (32 bits, 8 bits): the type of gradients and copies chosen once a block instead of for every
+// element (984 -> 974, 823 -> 599); a warp number that the compiler knows to be uniform, so that fields and addresses are worked out once a warp (974 -> 943);
+// chunks taken in order (943 -> 845; 599 -> 566); 8-bit blocks fetched ahead through shared memory, no register spilled (566 -> 501), in pairs and in pieces of 16
+// bytes (501 -> 495, under load 578 -> 540).  Gradient norms: 124 us for 806 MB, 64 in BF16.
 #include <math.h>
 
 #include <algorithm>
@@ -19,7 +25,8 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 __host__ __device__ constexpr int adam_ctas(bool eight) { return eight ? 4 : 3; }             // CTAs per SM
-constexpr int kUnit = 256;                   // elements of a unit, and of a block of states in 8 bits
+constexpr int kUnit = 256;                   // elements that a warp steps at a time, and of a block of states in 8 bits
+__host__ __device__ constexpr int blocks_of_unit(bool eight) { return eight ? 2 : 1; }
 constexpr int kFew = 30, kMany = 240;        // tensors that a launch describes: in 4 KB of parameters, or in 32 KB
 constexpr float kTiny = 0x1p-100f;           // blocks whose largest magnitude is not above this are stored as zeros
 constexpr float kMostE4 = 448.0f;
@@ -36,7 +43,7 @@ struct AdamTensor {
   FastDiv by_cols;
   float copy_scale, lr_factor, decay;
   uint8_t g_dt, copy_dt;
-  uint8_t wide, dense;                       // p and g have no padded rows; and groups of four of all are aligned
+  uint8_t wide, dense;                       // dense: p and g have no padded rows; wide: and the pieces in which all are fetched are aligned
   uint8_t copy_wide, copy_dense;
 };
 template <int MOST>
@@ -209,65 +216,38 @@ __device__ __noinline__ void store_row(const AdamTensor& t, int64_t base, int la
   __syncwarp();
 }
 
-// Whole units of a tensor whose groups of four are aligned.  With states in 8 bits a unit is more work for fewer bytes: it comes through shared memory while
-// the warp works on the unit before.  A lane copies what it will read itself, so that nothing but its own copies has to be waited for.  A warp's slot: rows of
-// 32 lanes' pieces, two of param, grad and the codes of m and v each, and one of each scale.
-constexpr int kGradAt = 1024, kMAt = 2048, kVAt = 2304, kScaleAt = 2560, kSlotBytes = 2816;
+// With states in 8 bits a block is more work for fewer bytes: a unit of two comes through shared memory while the warp works on the unit before, in pieces of 16 bytes
+// a lane.  A warp's slot: param, grad, the codes of m and of v, and the four scales.
+constexpr int kPair = 2 * kUnit, kGradAt = 4 * kPair, kMAt = 8 * kPair, kVAt = 9 * kPair, kScaleAt = 10 * kPair, kSlotBytes = 10 * kPair + 16;
+__host__ __device__ constexpr int warp_bytes(bool eight) { return kUnit * 4 + (eight ? kSlotBytes : 0); }   // of shared memory: a block's copies, and the slot
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
-__device__ __forceinline__ void copy8(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-__device__ __forceinline__ void fetch_unit(const AdamTensor& t, uint32_t block, int lane, uint32_t slot) {
-  const int64_t base = (int64_t)block * kUnit;
+__device__ __forceinline__ void fetch_unit(const AdamTensor& t, uint32_t unit, int lane, uint32_t slot) {
+  const int64_t base = (int64_t)unit * kPair;
+  const uint32_t at = slot + 16 * lane;
+  const float* p = t.p + base + 4 * lane;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int off = 128 * k + 4 * lane;
-    copy16(slot + 512 * k + 16 * lane, t.p + base + off);
-    if (t.g_dt == US_F32) copy16(slot + kGradAt + 512 * k + 16 * lane, static_cast<const float*>(t.g) + base + off);
-    else copy8(slot + kGradAt + 256 * k + 8 * lane, static_cast<const uint16_t*>(t.g) + base + off);
-    copy4(slot + kMAt + 128 * k + 4 * lane, static_cast<const uint8_t*>(t.m) + base + off);
-    copy4(slot + kVAt + 128 * k + 4 * lane, static_cast<const uint8_t*>(t.v) + base + off);
+  for (int k = 0; k < 4; ++k) copy16(at + 512 * k, p + 128 * k);
+  if (t.g_dt == US_F32) {
+    const float* g = static_cast<const float*>(t.g) + base + 4 * lane;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) copy16(at + kGradAt + 512 * k, g + 128 * k);
+  } else {
+    const uint16_t* g = static_cast<const uint16_t*>(t.g) + base + 8 * lane;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) copy16(at + kGradAt + 512 * k, g + 256 * k);
   }
-  copy4(slot + kScaleAt + 4 * lane, t.m_scale + block);
-  copy4(slot + kScaleAt + 128 + 4 * lane, t.v_scale + block);
+  copy16(at + kMAt, static_cast<const uint8_t*>(t.m) + base + 16 * lane);
+  copy16(at + kVAt, static_cast<const uint8_t*>(t.v) + base + 16 * lane);
+  if (lane < 4) copy4(slot + kScaleAt + 4 * lane, (lane < 2 ? t.m_scale : t.v_scale) + (int64_t)unit * 2 + (lane & 1));
 }
 
-// The step of a unit, from its tensor or (EIGHT) from the slot; `refill` starts the copies that take the slot next, once this lane has read what is there.
-template <bool EIGHT, int GRAD, class F>
-__device__ __forceinline__ void unit_step(const AdamStep& a, const AdamTensor& t, uint32_t block, int lane, const char* slot, float* row, F refill) {
-  const int64_t base = (int64_t)block * kUnit;
-  using States = std::conditional_t<EIGHT, uint32_t, float4>;
-  using Grads = std::conditional_t<GRAD == US_F32, float4, uint2>;
-  float4 p4[2];
-  Grads g4[2];
-  States m4[2], v4[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    if (EIGHT) {
-      p4[k] = reinterpret_cast<const float4*>(slot)[32 * k + lane];
-      g4[k] = reinterpret_cast<const Grads*>(slot + kGradAt)[32 * k + lane];
-      m4[k] = reinterpret_cast<const States*>(slot + kMAt)[32 * k + lane];
-      v4[k] = reinterpret_cast<const States*>(slot + kVAt)[32 * k + lane];
-    } else {
-      const int off = 128 * k + 4 * lane;
-      p4[k] = *reinterpret_cast<const float4*>(t.p + base + off);
-      g4[k] = *reinterpret_cast<const Grads*>(static_cast<const char*>(t.g) + (base + off) * (GRAD == US_F32 ? 4 : 2));
-      m4[k] = *reinterpret_cast<const States*>(static_cast<const float*>(t.m) + base + off);
-      v4[k] = *reinterpret_cast<const States*>(static_cast<const float*>(t.v) + base + off);
-    }
-  }
-  const float sm = EIGHT ? reinterpret_cast<const float*>(slot + kScaleAt)[lane] : 0.f, sv = EIGHT ? reinterpret_cast<const float*>(slot + kScaleAt + 128)[lane] : 0.f;
-  float p[8], g[8], m[8], v[8], root[8];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    four(p4[k], US_F32, &p[4 * k]);
-    four(g4[k], GRAD, &g[4 * k]);
-    four(m4[k], EIGHT ? US_E4M3 : US_F32, &m[4 * k]);
-    four(v4[k], EIGHT ? US_E4M3 : US_F32, &v[4 * k]);
-  }
-  refill();
-  step8<EIGHT>(a, t, block, lane, sm, sv, p, g, m, v, root);
+// What a block's step leaves, to its tensor.
+template <bool EIGHT>
+__device__ __forceinline__ void store_block(const AdamTensor& t, int64_t base, int lane, float* row, const float (&p)[8], const float (&m)[8], const float (&v)[8],
+                                            const float (&root)[8]) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int off = 128 * k + 4 * lane;
@@ -276,33 +256,82 @@ __device__ __forceinline__ void unit_step(const AdamStep& a, const AdamTensor& t
     if (EIGHT) *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + base + off) = root_codes4(&root[4 * k]);
     else store4<US_F32>(t.v, base + off, &v[4 * k]);
   }
-  if (t.copy) {
-    float y[8];
+  if (!t.copy) return;
+  float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = t.copy_scale * p[i];
-    if (t.copy_wide) {
-      const Place w = t.copy_dense ? Place{0, 0} : place_of(t, base);
-      with_type(t.copy_dt, [&](auto dt) {
-        constexpr int DT = decltype(dt)::value;
+  for (int i = 0; i < 8; ++i) y[i] = t.copy_scale * p[i];
+  if (t.copy_wide) {
+    const Place w = t.copy_dense ? Place{0, 0} : place_of(t, base);
+    with_type(t.copy_dt, [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int off = 128 * k + 4 * lane;
-          store4<DT>(t.copy, t.copy_dense ? base + off : at(t, w, off, t.copy_ld), &y[4 * k]);
-        }
-      });
-    } else {
+      for (int k = 0; k < 2; ++k) {
+        const int off = 128 * k + 4 * lane;
+        store4<DT>(t.copy, t.copy_dense ? base + off : at(t, w, off, t.copy_ld), &y[4 * k]);
+      }
+    });
+  } else {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) *reinterpret_cast<float4*>(row + 128 * k + 4 * lane) = make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
-      store_row(t, base, lane, row);
-    }
+    for (int k = 0; k < 2; ++k) *reinterpret_cast<float4*>(row + 128 * k + 4 * lane) = make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+    store_row(t, base, lane, row);
   }
 }
 
-// Any unit: a lane has every 32nd element.
+// A whole unit of a tensor whose pieces are aligned, from its tensor or (EIGHT) from the slot; `refill` starts the copies that take the slot next, once the warp
+// has read what is there.
+template <bool EIGHT, int GRAD, class F>
+__device__ __forceinline__ void unit_step(const AdamStep& a, const AdamTensor& t, uint32_t unit, int lane, const char* slot, float* row, F refill) {
+  using Grads = std::conditional_t<GRAD == US_F32, float4, uint2>;
+  if constexpr (EIGHT) {
+#pragma unroll 1
+    for (int j = 0; j < 2; ++j) {
+      float p[8], g[8], m[8], v[8], root[8];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int i = 64 * j + 32 * k + lane;
+        four(reinterpret_cast<const float4*>(slot)[i], US_F32, &p[4 * k]);
+        four(reinterpret_cast<const Grads*>(slot + kGradAt)[i], GRAD, &g[4 * k]);
+        four(reinterpret_cast<const uint32_t*>(slot + kMAt)[i], US_E4M3, &m[4 * k]);
+        four(reinterpret_cast<const uint32_t*>(slot + kVAt)[i], US_E4M3, &v[4 * k]);
+      }
+      const float sm = reinterpret_cast<const float*>(slot + kScaleAt)[j], sv = reinterpret_cast<const float*>(slot + kScaleAt)[2 + j];
+      if (j == 1) {
+        __syncwarp();
+        refill();
+      }
+      step8<true>(a, t, 2 * unit + j, lane, sm, sv, p, g, m, v, root);
+      store_block<true>(t, (int64_t)unit * kPair + kUnit * j, lane, row, p, m, v, root);
+    }
+  } else {
+    const int64_t base = (int64_t)unit * kUnit;
+    float4 p4[2], m4[2], v4[2];
+    Grads g4[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int off = 128 * k + 4 * lane;
+      p4[k] = *reinterpret_cast<const float4*>(t.p + base + off);
+      g4[k] = *reinterpret_cast<const Grads*>(static_cast<const char*>(t.g) + (base + off) * (GRAD == US_F32 ? 4 : 2));
+      m4[k] = *reinterpret_cast<const float4*>(static_cast<const float*>(t.m) + base + off);
+      v4[k] = *reinterpret_cast<const float4*>(static_cast<const float*>(t.v) + base + off);
+    }
+    float p[8], g[8], m[8], v[8], root[8];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      four(p4[k], US_F32, &p[4 * k]);
+      four(g4[k], GRAD, &g[4 * k]);
+      four(m4[k], US_F32, &m[4 * k]);
+      four(v4[k], US_F32, &v[4 * k]);
+    }
+    step8<false>(a, t, unit, lane, 0.f, 0.f, p, g, m, v, root);
+    store_block<false>(t, base, lane, row, p, m, v, root);
+  }
+}
+
+// Any block: a lane has every 32nd element.
 template <bool EIGHT>
-__device__ __noinline__ void unit_step_any(AdamStep a, const AdamTensor& t, uint32_t block, int lane) {
+__device__ __noinline__ void block_step_any(AdamStep a, const AdamTensor& t, uint32_t block, int lane) {
   const int64_t base = (int64_t)block * kUnit;
-  const int here = (int)min((int64_t)kUnit, t.n - base);     // elements of this unit
+  const int here = (int)min((int64_t)kUnit, t.n - base);     // elements of this block
   const Place w = !t.dense || (t.copy && !t.copy_dense) ? place_of(t, base) : Place{0, 0};
   float p[8], g[8], m[8], v[8];
   const float sm = EIGHT ? t.m_scale[block] : 0.f, sv = EIGHT ? t.v_scale[block] : 0.f;
@@ -334,8 +363,7 @@ __device__ __noinline__ void unit_step_any(AdamStep a, const AdamTensor& t, uint
 // EIGHT: tensors with states in 8 bits, else those in 32.
 template <bool EIGHT, int MOST>
 __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const __grid_constant__ AdamArgs<MOST> a) {
-  __shared__ __align__(16) float rows[kWarps][kUnit];        // (units whose copies have rows that cut groups of four)
-  __shared__ __align__(16) char slots[kWarps][EIGHT ? kSlotBytes : 16];
+  extern __shared__ __align__(16) char smem[];
   __shared__ int64_t made;
   __shared__ uint32_t taken[2];
   ptx::grid_sync_previous();
@@ -355,6 +383,8 @@ __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const
   // (handed round from one lane, the warp's number is known to be the same in all of them: what depends on it alone -- which tensor, where its
   // fields and addresses are -- is worked out once for the warp, by the uniform datapath)
   const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0);
+  float* row = reinterpret_cast<float*>(smem + warp * warp_bytes(EIGHT));
+  char* slot = smem + warp * warp_bytes(EIGHT) + kUnit * 4;
   unsigned int* count = reinterpret_cast<unsigned int*>(a.step + 1);
   const uint32_t chunks = (a.units + kWarps - 1) / kWarps;
   int cur = 0, ahead = 0;                                    // tensors of the unit at hand, and of the one fetched
@@ -366,13 +396,14 @@ __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const
     }
     cur = ahead = lo;
   }
-  auto block_of = [&](uint32_t unit, int k) { return unit - (k ? a.t[k - 1].unit_end : 0u); };
-  auto whole = [&](const AdamTensor& t, uint32_t block) { return t.wide && (int64_t)(block + 1) * kUnit <= t.n; };
+  constexpr int kBlocks = blocks_of_unit(EIGHT);
+  auto in_tensor = [&](uint32_t unit, int k) { return unit - (k ? a.t[k - 1].unit_end : 0u); };
+  auto whole = [&](const AdamTensor& t, uint32_t unit) { return t.wide && (int64_t)(unit + 1) * (kBlocks * kUnit) <= t.n; };
   auto fetch = [&](uint32_t unit) {
     if (EIGHT && unit < a.units) {
       while (unit >= a.t[ahead].unit_end) ++ahead;
-      const uint32_t block = block_of(unit, ahead);
-      if (whole(a.t[ahead], block)) fetch_unit(a.t[ahead], block, lane, ptx::smem_addr(slots[warp]));
+      const uint32_t i = in_tensor(unit, ahead);
+      if (whole(a.t[ahead], i)) fetch_unit(a.t[ahead], i, lane, ptx::smem_addr(slot));
     }
   };
   // A CTA's first chunks (one unit a warp) are set, the others are taken as it comes to them, so that chunks are worked on in their order and what all SMs read
@@ -385,17 +416,20 @@ __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const
     uint32_t next = 0;
     if (threadIdx.x == 0) next = atomicAdd(count, 1u);       // (needed only once the chunk is done)
     const uint32_t unit = chunk * kWarps + warp;
-    if (EIGHT) copies_wait();
+    if (EIGHT) {
+      copies_wait();
+      __syncwarp();
+    }
     auto refill = [&] { fetch(after * kWarps + warp); };
     if (unit < a.units) {
       while (unit >= a.t[cur].unit_end) ++cur;
       const AdamTensor& t = a.t[cur];
-      const uint32_t block = block_of(unit, cur);
-      if (whole(t, block)) {
-        with_grad_type(t.g_dt, [&](auto dt) { unit_step<EIGHT, decltype(dt)::value>(s, t, block, lane, slots[warp], rows[warp], refill); });
+      const uint32_t i = in_tensor(unit, cur);
+      if (whole(t, i)) {
+        with_grad_type(t.g_dt, [&](auto dt) { unit_step<EIGHT, decltype(dt)::value>(s, t, i, lane, slot, row, refill); });
       } else {
         refill();
-        unit_step_any<EIGHT>(s, t, block, lane);
+        for (uint32_t block = i * kBlocks; block < (i + 1) * kBlocks && (int64_t)block * kUnit < t.n; ++block) block_step_any<EIGHT>(s, t, block, lane);
       }
     }
     if (threadIdx.x == 0) {
@@ -591,7 +625,8 @@ AdamTensor describe(const us_adamw_tensor& t) {
   d.copy_scale = t.copy_scale; d.lr_factor = t.lr_factor; d.decay = t.weight_decay;
   d.g_dt = (uint8_t)t.grad.dtype; d.copy_dt = (uint8_t)t.copy.dtype;
   d.dense = dense(t.param) && dense(t.grad);
-  d.wide = d.dense && fours(t.param) && fours(t.grad) && fours(t.m) && fours(t.v);
+  const auto aligned16 = [](const us_mat& m) { return reinterpret_cast<uintptr_t>(m.ptr) % 16 == 0; };
+  d.wide = d.dense && (small ? aligned16(t.param) && aligned16(t.grad) && aligned16(t.m) && aligned16(t.v) : fours(t.param) && fours(t.grad) && fours(t.m) && fours(t.v));
   d.copy_dense = t.copy.ptr && dense(t.copy);
   d.copy_wide = t.copy.ptr && fours(t.copy);
   return d;
@@ -604,14 +639,16 @@ us_status launch_adamw(AdamArgs<MOST>& a, const us_adamw_tensor* const* ts, int 
   uint64_t units = 0;
   for (int i = 0; i < count; ++i) {
     a.t[i] = describe(*ts[i]);
-    units += (uint64_t)((a.t[i].n + kUnit - 1) / kUnit);
+    constexpr int kElements = kUnit * blocks_of_unit(EIGHT);
+    units += (uint64_t)((a.t[i].n + kElements - 1) / kElements);
     if (units >= (1ull << 31)) return US_ERR_UNSUPPORTED;
     a.t[i].unit_end = (uint32_t)units;
   }
   a.count = count;
   a.units = (uint32_t)units;
   const int grid = (int)std::min<uint64_t>((units + kWarps - 1) / kWarps, (uint64_t)(sms * adam_ctas(EIGHT)));
-  return host::launch(adamw_kernel<EIGHT, MOST>, nullptr, grid, kThreads, 0, 1, stream, a);
+  static std::atomic<uint64_t> smem_set{0};
+  return host::launch(adamw_kernel<EIGHT, MOST>, &smem_set, grid, kThreads, kWarps * warp_bytes(EIGHT), 1, stream, a);
 }
 
 template <class A>

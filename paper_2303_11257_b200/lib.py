@@ -474,6 +474,7 @@ def us_linear_fwd(X, W, alpha, Y, ws, ep=None, stream=None):
 
 def us_linear_fwd_bias(X, W, alpha, bias, Y, ws, ep=None, Yq=None, stream=None):
     """us_linear_fwd of a layer with a bias (a vector), which is added to the scaled product; Yq: an FP8 copy of a residual's result."""
+    _here(Y)
     _check("us_linear_fwd_bias", _entry("us_linear_fwd_bias")(X, W, alpha, bias.view(1, -1) if bias.dim() == 1 else bias, ep, Y, Yq, ws, ws, _stream(stream)))
     return Y
 
@@ -903,8 +904,20 @@ def us_qk_norm_bwd(X, w, G, dX, dw, head_width, eps, ws, beta_x=1.0, beta_w=None
     return dX, dw
 
 
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _here(t: torch.Tensor) -> None:
+    """A launch goes to the current device, whose own tensors it takes."""
+    if t.is_cuda and t.device.index != _current_device():
+        raise ValueError(f"a tensor of {t.device} in a call on cuda:{_current_device()}")
+
+
 def us_bias_grad(G, beta, db, stream=None):
     """db[i] = beta[i] * the column sums of G[i], in one launch: lists of matrices, factors (or None: ones) and bias gradients."""
+    for t in db:
+        _here(t)
     if len(db) != len(G) or (beta is not None and len(beta) != len(G)):
         raise ValueError("one entry per matrix is wanted")
     _check("us_bias_grad", _entry("us_bias_grad")(len(G), G, beta, db, _stream(stream)))
@@ -933,6 +946,7 @@ def us_grad_norm(grads, max_norm, out, ws, stream=None):
     """out (float32 CUDA tensor of two) = 2-norm of all gradients and the factor that clips them to max_norm; grads: a list of tensors, or what
     mats() made of it; ws: a uint8 CUDA tensor of us_grad_norm_workspace_bytes() bytes, zeroed before its first use."""
     assert out.is_cuda and out.dtype is torch.float32 and out.numel() >= 2 and out.is_contiguous()
+    _here(out)
     if not isinstance(grads, C.Array):
         grads = mats(grads)
     _check("us_grad_norm", _entry("us_grad_norm")(len(grads), grads, max_norm, out, ws, ws, _stream(stream)))
@@ -951,6 +965,9 @@ def adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, 
     numbers = [each(copy_scale), each(lr_factor), each(weight_decay)]
     if any(len(c) != n for c in columns + numbers):
         raise ValueError("one entry per tensor is wanted")
+    written = [t.data_ptr() for i in (0, 2, 3, 4, 5, 6) for t in columns[i] if t is not None and t.numel()]
+    if len(set(written)) != len(written):
+        raise ValueError("a tensor that a step writes is named twice")
     arr = (us_adamw_tensor * n)()
     for k, c in enumerate(columns):
         _fill(arr, k, c)
@@ -969,6 +986,7 @@ def us_adamw(tensors, step, lr, betas=(0.9, 0.999), eps=1e-8, lr_factor=None, gr
     """One AdamW step over what adamw_tensors() laid out; step: new_adamw_step(); lr_factor, grad_factor: float32 CUDA tensors (one element is read), or None."""
     assert step.is_cuda and step.dtype is torch.int64 and step.numel() == 2 and step.is_contiguous()
     assert all(t is None or (t.is_cuda and t.dtype is torch.float32) for t in (lr_factor, grad_factor))
+    _here(step)
     _check("us_adamw", _entry("us_adamw")(len(tensors), tensors, lr, betas[0], betas[1], eps, lr_factor, grad_factor, step, _stream(stream)))
 
 

@@ -24,7 +24,7 @@ from . import lib as L
 
 
 class AdamW:
-    """params: float32 CUDA tensors, updated in place; grads: their gradients (float32, bfloat16 or float16), the same tensors in every step; copies: None or a
+    """params: float32 CUDA matrices and vectors, updated in place; grads: their gradients (float32, bfloat16 or float16), the same tensors in every step; copies: None or a
     list of operands (or Nones) of the parameters' shapes; weight_decay: a number or one per tensor; states: "32bit" or "8bit"."""
 
     def __init__(self, params, grads, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, copies=None, states: str = "32bit",
@@ -43,7 +43,7 @@ class AdamW:
             raise ValueError("one entry per parameter is wanted")
         self.lr, self.betas, self.eps, self.max_norm, self.states, self.lr_factor = lr, tuple(betas), eps, max_norm, states, lr_factor
         eight = states == "8bit"
-        state = lambda p: torch.zeros(p.numel(), dtype=torch.uint8 if eight else torch.float32, device=p.device).view(torch.float8_e4m3fn if eight else torch.float32)
+        state = lambda p: torch.zeros(p.shape, dtype=torch.uint8 if eight else torch.float32, device=p.device).view(torch.float8_e4m3fn if eight else torch.float32)
         scale = lambda p: torch.zeros(-(-p.numel() // L.ADAMW_BLOCK), dtype=torch.float32, device=p.device) if eight else None
         self.m, self.v = [state(p) for p in self.params], [state(p) for p in self.params]
         self.m_scale, self.v_scale = [scale(p) for p in self.params], [scale(p) for p in self.params]

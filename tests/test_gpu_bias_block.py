@@ -98,12 +98,12 @@ def test_training_steps(states, operand):
             assert np.abs(U.host_values(p).ravel() - w.p).max() <= 2e-6 * np.abs(w.p).max(), (t, i)
             if states == "8bit":
                 scale = lambda s: np.repeat(s.double().cpu().numpy(), 256)[:g.size]
-                m[i] = scale(opt.m_scale[i]) * U.host_values(opt.m[i].view(1, -1)).ravel()
-                v[i] = (scale(opt.v_scale[i]) * U.host_values(opt.v[i].view(1, -1)).ravel()) ** 2
+                m[i] = scale(opt.m_scale[i]) * U.host_values(opt.m[i]).ravel()
+                v[i] = (scale(opt.v_scale[i]) * U.host_values(opt.v[i]).ravel()) ** 2
                 # half a step of E4M3 in its last binade, 16 of 448 = 0.0357 of a block's largest value; of v, (1 + 0.0357)^2 - 1 = 0.0727
                 assert np.abs(m[i] - w.m).max() <= 0.0358 * np.abs(w.m).max() and np.abs(v[i] - w.v).max() <= 0.0728 * np.abs(w.v).max()
             else:
-                m[i], v[i] = U.host_values(opt.m[i].view(1, -1)).ravel(), U.host_values(opt.v[i].view(1, -1)).ravel()
+                m[i], v[i] = U.host_values(opt.m[i]).ravel(), U.host_values(opt.v[i]).ravel()
         for p, q in ((opt.params[0], block.W1q), (opt.params[1], block.W2q)):
             assert torch.equal(q.float(), p.clamp(-448, 448).to(q.dtype).float() if operand == "fp8" else p.to(q.dtype).float())
     assert opt.count.tolist() == [3, 0] and not any(torch.equal(a, b) for a, b in zip(first, opt.params))
@@ -165,6 +165,24 @@ def test_states_travel_to_another_optimiser():
         assert all(torch.equal(x, y) for x, y in zip(a.params, b.params)) and a.count.tolist() == b.count.tolist() == [2, 0]
     with pytest.raises(ValueError):
         b.load_state_dict(optim.AdamW(p, g).state_dict())
+
+
+def test_calls_on_another_device_and_tensors_named_twice_are_refused(monkeypatch):
+    from paper_2303_11257_b200 import lib as L
+    from paper_2303_11257_b200 import optim
+    p, q, g = (torch.ones(40, 64, device="cuda") for _ in range(3))
+    opt, twice = optim.AdamW([p, q], [g, g], max_norm=1.0), optim.AdamW([p, p], [g, g])
+    with pytest.raises(ValueError):
+        twice.step()
+    opt.step()
+    before = p.clone()
+    ws, out = L.new_workspace(), torch.empty(40, 64, dtype=torch.bfloat16, device="cuda")
+    x = torch.ones(40, 64, device="cuda").bfloat16()
+    monkeypatch.setattr(L, "_current_device", lambda: 7)
+    for call in (opt.step, optim.AdamW([p], [g]).step, lambda: L.us_bias_grad([x], None, [q[0]]), lambda: L.us_linear_fwd_bias(x, x[:, :64], 1.0, q[0], out, ws)):
+        with pytest.raises(ValueError):
+            call()
+    assert torch.equal(p, before) and opt.count.tolist() == [1, 0]
 
 
 def test_other_tensors_are_laid_out_anew_and_lr_follows_the_schedule():
