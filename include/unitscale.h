@@ -627,7 +627,7 @@ us_status us_rotary_table(const us_mat* table, double base, double scale, int64_
  * and takes its own factor, beta = b^-1/2 for b rows), for count (1..8) matrices in one launch.  G [b x n]: any us_dtype, any ld >= n, any
  * number of rows (none: db = 0); db (1 x n): F32, BF16 or F16; beta: NULL = ones.  G, beta, db: host arrays of count elements.  Pointers
  * need the natural alignment of their elements (rows on 16-byte boundaries are read in 16-byte pieces).  Sums are float32, formed without
- * atomics in an order that depends on the sizes alone.  Outputs must not overlap one another or an input.
+ * atomics in an order that depends on the sizes and the device alone.  Outputs must not overlap one another or an input.
  */
 us_status us_bias_grad(int count, const us_mat* G, const float* beta, const us_mat* db, void* stream);
 

@@ -150,11 +150,35 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
   return false;
 }
 
-// Column col's bias (0 behind the last), and two columns' of a slice of which lane i has column i's.  A lane's values are a register per slice, fetched
-// ahead; handed round they take as many cycles of the path to the registers as the same loads by every lane would (us, FP8 8192 x 1024 -> 4096 with
-// GELU: 43.7 with 16-byte loads of every lane in front of each group of columns, 38.4 so, 36.3 without a bias).
+// Column col's bias (0 behind the last), and two columns' of a slice of which lane i has column i's: a register per slice, fetched ahead and handed round (us, FP8 8192 x 1024 ->
+// 4096 with GELU: 43.7 with 16-byte loads of every lane in front of each group of columns, 38.4 so; through shared memory, below, 1.04 times the 36.3 to 38.2 that the
+// op takes without a bias, before 1.06; into FP8 without an activation, 8192 x 1024 -> 1024, 1.01 before 1.06).
 template <class P>
 __device__ __forceinline__ float bias_lane(const P& p, int col, int n) { return col < n ? load_one(p.bias, p.bias_dt, col) : 0.f; }
+// The sixteen-warp epilogues keep the bias of a warp's 64 columns in shared memory, four columns to a cell: IN_BOX in the warp's box of 128-byte rows, slice s's in
+// rows 0 .. 7 where chunk 4 s + 3 goes, the last of the slice to be staged; else one behind the other.
+template <bool IN_BOX>
+__device__ __forceinline__ uint32_t bias_cell(uint32_t at, int s, int j) { return IN_BOX ? at + (uint32_t)(j * 128 + (((4 * s + 3) ^ j) << 4)) : at + (uint32_t)(128 * s + 16 * j); }
+// Lanes 0 .. 15: a tile's, from global memory and to the cells.
+__device__ __forceinline__ void bias_fetch(const GemmParams& p, int col, int lane, float (&b)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = bias_lane(p, col + 4 * lane + i, lane < 16 ? p.N : 0);
+}
+template <bool IN_BOX>
+__device__ __forceinline__ void bias_keep(uint32_t at, int lane, const float (&b)[4]) {
+  if (lane < 16)
+    ptx::sts128(bias_cell<IN_BOX>(at, lane >> 3, lane & 7), make_uint4(__float_as_uint(b[0]), __float_as_uint(b[1]), __float_as_uint(b[2]), __float_as_uint(b[3])));
+  __syncwarp();
+}
+// Every lane: those of group g of eight columns of slice s.
+template <bool IN_BOX>
+__device__ __forceinline__ void bias_cells(uint32_t at, int s, int g, f32x2 (&b)[4]) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const uint4 t = ptx::lds128(bias_cell<IN_BOX>(at, s, 2 * g + half));
+    b[2 * half] = pack2(__uint_as_float(t.x), __uint_as_float(t.y)); b[2 * half + 1] = pack2(__uint_as_float(t.z), __uint_as_float(t.w));
+  }
+}
 __device__ __forceinline__ f32x2 bias_pair(float mine, int i) { return pack2(__shfl_sync(0xffffffffu, mine, i), __shfl_sync(0xffffffffu, mine, i + 1)); }
 
 // Operands of the fused epilogue for one 32-column slice of one row, fetched as raw 16-byte
@@ -634,16 +658,20 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       else ptx::mbar_arrive(c.acc_empty0 + 8u * a);
     }
   };
-  // One 32-column slice: scale, (bias, of which lane i has column i's,) (kept pre-activation,) activation, rounding, staging stores.
-  auto slice = [&](const uint32_t (&r)[32], int s, float bias) {
+  // One 32-column slice: scale, (bias,) (kept pre-activation,) activation, rounding, staging stores.
+  auto slice = [&](const uint32_t (&r)[32], int s) {
     uint32_t held[2];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      f32x2 x[4];
+      f32x2 x[4], bias[4];
+      if constexpr (BIAS) {
+        bias_cells<true>(buf_aux, s, g, bias);
+        if (g == 3) __syncwarp();                             // (lanes 0 .. 7 stage theirs in the cells' place now)
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         x[k] = pack2(__uint_as_float(r[8 * g + 2 * k]), __uint_as_float(r[8 * g + 2 * k + 1]));
-        x[k] = BIAS ? fma2(x[k], scale2, bias_pair(bias, 8 * g + 2 * k)) : mul2(x[k], scale2);
+        x[k] = BIAS ? fma2(x[k], scale2, bias[k]) : mul2(x[k], scale2);
       }
       float y[8];
       if (EPI == kEpiGelu) {
@@ -680,10 +708,10 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
 
   int row0 = 0, n_w = 0;
   bool pending[2] = {false, false};                          // an input box load is in flight
-  float bias0 = 0.f, bias1 = 0.f;
+  float bias[4];                                             // lanes 0 .. 15: the tile's, four columns each
   if (tile < c.num_tiles) {
     coords(tile, row0, n_w);
-    if constexpr (BIAS) { bias0 = bias_lane(p, n_w + lane, p.N); bias1 = bias_lane(p, n_w + 32 + lane, p.N); }
+    if constexpr (BIAS) bias_fetch(p, n_w, lane, bias);
     if (kIn) {
       if (ptx::elect_one()) { issue_in(0, n_w, row0); issue_in(1, n_w, row0); }
       pending[0] = pending[1] = true;
@@ -703,16 +731,16 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
     if (active) ptx::tmem_ld_32x32_issue(t_row, r0);
     const int next = tile + c.num_groups;
     int next_row0 = 0, next_n_w = 0;
-    float next_bias0 = 0.f, next_bias1 = 0.f;
-    if (next < c.num_tiles) {
-      coords(next, next_row0, next_n_w);
-      if constexpr (BIAS) { next_bias0 = bias_lane(p, next_n_w + lane, p.N); next_bias1 = bias_lane(p, next_n_w + 32 + lane, p.N); }
-    }
+    if (next < c.num_tiles) coords(next, next_row0, next_n_w);
     if (active) {
       if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();          // the previous tile's stores have read the staging boxes
       __syncwarp();
+      if constexpr (BIAS) bias_keep<true>(buf_aux, lane, bias);
       ptx::tmem_ld_fence(r0);
       ptx::tmem_ld_32x32_issue(t_row + 32, r1);
+    }
+    if constexpr (BIAS) {
+      if (next < c.num_tiles) bias_fetch(p, next_n_w, lane, bias);
     }
     if (kIn) {
       ok = wait_bounded(c.in_bar, ph0, c.abort_flag, p.status, p.wait_limit);
@@ -721,7 +749,7 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       pending[0] = false;
       ph0 ^= 1u;
     }
-    if (active) slice(r0, 0, bias0);
+    if (active) slice(r0, 0);
     if (kIn) {
       __syncwarp();                                           // every lane has read the first input box
       if (next < c.num_tiles) {
@@ -738,7 +766,7 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       pending[1] = false;
       ph1 ^= 1u;
     }
-    if (active) slice(r1, 1, bias1);
+    if (active) slice(r1, 1);
     if (kIn) {
       __syncwarp();
       if (next < c.num_tiles) {
@@ -756,7 +784,6 @@ __device__ __forceinline__ void epilogue_act16(const GemmParams& p, const CUtens
       }
     }
     tile = next; row0 = next_row0; n_w = next_n_w;
-    if constexpr (BIAS) { bias0 = next_bias0; bias1 = next_bias1; }
   }
   // Leaving early (a wait ran out somewhere in the CTA): let tensor-memory loads and input boxes
   // that are still in flight land before the CTA may give up its resources.
@@ -778,12 +805,19 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
   const int q = c.warp & 3, part = (c.warp - 2) >> 2, lane = c.lane;
   const uint32_t out_sw = (uint32_t)((lane >> 1) & 3), dst = c.buf0 + (uint32_t)lane * 64u;
   const f32x2 scale2 = splat2(p.scale);
-  auto slice = [&](const uint32_t (&r)[32], uint32_t chunk, float bias) {
+  const uint32_t spare = c.buf0 + 2048u;                     // (behind the box of 2 KB)
+  auto slice = [&](const uint32_t (&r)[32], uint32_t chunk) {
     float y[32];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      const f32x2 x = pack2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
-      unpack2(BIAS ? fma2(x, scale2, bias_pair(bias, 2 * k)) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
+    for (int g = 0; g < 4; ++g) {
+      f32x2 bias[4];
+      if constexpr (BIAS) bias_cells<false>(spare, (int)chunk / 2, g, bias);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = 4 * g + i;
+        const f32x2 x = pack2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+        unpack2(BIAS ? fma2(x, scale2, bias[i]) : mul2(x, scale2), y[2 * k], y[2 * k + 1]);
+      }
     }
     uint32_t w[8];
     if (p.out_dt == US_E5M2) {
@@ -802,8 +836,12 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
     int tm, tn;
     tile_mn(p, tile, tm, tn);
     const int row0 = tm * (kBM * CG) + c.rank * kBM + q * 32, n_w = tn * BN + part * 64;
-    float bias0 = 0.f, bias1 = 0.f;
-    if constexpr (BIAS) { bias0 = bias_lane(p, n_w + lane, p.N); bias1 = bias_lane(p, n_w + 32 + lane, p.N); }
+    if constexpr (BIAS) {                                     // (every lane is done with the last tile's)
+      float bias[4];
+      bias_fetch(p, n_w, lane, bias);
+      __syncwarp();
+      bias_keep<false>(spare, lane, bias);
+    }
     bool ok = wait_bounded(c.acc_full0 + 8u * acc, acc_phase, c.abort_flag, p.status, p.wait_limit);
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) break;
@@ -817,7 +855,7 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
       __syncwarp();
       ptx::tmem_ld_fence(r0);
       ptx::tmem_ld_32x32_issue(t_row + 32, r1);
-      slice(r0, 0, bias0);
+      slice(r0, 0);
       ptx::tmem_ld_fence(r1);
     }
     ptx::tc_fence_before_sync();
@@ -827,7 +865,7 @@ __device__ __forceinline__ void epilogue_plain16(const GemmParams& p, const CUte
       else ptx::mbar_arrive(c.acc_empty0 + 8u * acc);
     }
     if (active) {
-      slice(r1, 2, bias1);
+      slice(r1, 2);
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (ptx::elect_one()) { ptx::tma_store_2d(tm_out, c.buf0, n_w, row0); ptx::bulk_commit_group(); }
