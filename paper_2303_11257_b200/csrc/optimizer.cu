@@ -6,11 +6,11 @@
 // memory has to be kept or written, and a captured launch holds its own.
 //
 // Measured on 201 million parameters (a copy moves 6.46 TB/s on the same card): states in 32 bits, FP8 operands written, 29 bytes an element, 845 us = 6.9 TB/s; states
-// in 8 bits, BF16 gradients and operands, 16 bytes, 495 us = 6.5 TB/s, 519 under a load that holds the clock down: this one is bound by its instructions as
+// in 8 bits, BF16 gradients and operands, 16 bytes, 495 us = 6.5 TB/s, 527 under a load that holds the clock down: this one is bound by its instructions as
 // well, about 50 a lane and element.  What made the difference, in us (32 bits, 8 bits): the type of gradients and copies chosen once a block instead of for every
 // element (984 -> 974, 823 -> 599); a warp number that the compiler knows to be uniform, so that fields and addresses are worked out once a warp (974 -> 943);
 // chunks taken in order (943 -> 845; 599 -> 566); 8-bit blocks fetched ahead through shared memory, no register spilled (566 -> 501), in pairs and in pieces of 16
-// bytes (501 -> 495, under load 578 -> 519).  Gradient norms: 124 us for 806 MB, 64 in BF16.
+// bytes (501 -> 495, under load 578 -> 519; with m rounded as the formula says 527).  Gradient norms: 124 us for 806 MB, 64 in BF16.
 #include <math.h>
 
 #include <algorithm>
@@ -150,6 +150,7 @@ __device__ __forceinline__ int64_t at(const AdamTensor& t, const Place& w, int o
 // with gm = (1 - beta1) grad_factor, gv = sqrt(1 - beta2) grad_factor, and sqrt(1 - beta2^t) taken out of the denominator into rate and eps.
 struct AdamStep {
   float beta1, beta2, root_beta2, gm, gv, eps, lr, rate;
+  float grad_factor, rest1;
 };
 
 // The step of a lane's eight elements; sm, sv: the scales of states in 8 bits, whose codes m and v are (v's root).  Afterwards m is what is stored, and v, or where EIGHT root,
@@ -158,11 +159,22 @@ template <bool EIGHT>
 __device__ __forceinline__ void step8(const AdamStep& a, const AdamTensor& t, uint32_t block, int lane, float sm, float sv, float (&p)[8], const float (&g)[8], float (&m)[8],
                                       float (&v)[8], float (&root)[8]) {
   const f32x2 rate = splat2(-(a.rate * t.lr_factor)), decay = splat2(-(a.lr * t.lr_factor * t.decay));
-  const f32x2 keep_m = splat2(EIGHT ? a.beta1 * sm : a.beta1), keep_v = splat2(EIGHT ? a.root_beta2 * sv : a.beta2), gm = splat2(a.gm), gv = splat2(a.gv), eps = splat2(a.eps);
+  const f32x2 keep_v = splat2(EIGHT ? a.root_beta2 * sv : a.beta2), gm = splat2(a.gm), gv = splat2(a.gv), eps = splat2(a.eps);
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     const f32x2 gg = pack2(g[i], g[i + 1]), x = mul2(gv, gg), x2 = mul2(x, x);
-    const f32x2 mm = fma2(keep_m, pack2(m[i], m[i + 1]), mul2(gm, gg));
+    // In 8 bits the operations of m are rounded one by one, as the formula has them: a code that falls the other way, because a fused form is off by 2^-24, is a block's largest
+    // value in a later step every now and then, and moves all of its codes.  (The root, of which a step moves a thousandth, is not as sensitive.)  Scalar: the compiler makes
+    // packed products and sums one operation again.
+    f32x2 mm = mul2(EIGHT ? splat2(a.grad_factor) : gm, gg);
+    if (EIGHT) {
+      float m0, m1, g0, g1;
+      unpack2(mul2(splat2(sm), pack2(m[i], m[i + 1])), m0, m1);
+      unpack2(mul2(splat2(a.rest1), mm), g0, g1);
+      mm = pack2(__fadd_rn(__fmul_rn(a.beta1, m0), g0), __fadd_rn(__fmul_rn(a.beta1, m1), g1));
+    } else {
+      mm = fma2(splat2(a.beta1), pack2(m[i], m[i + 1]), mm);
+    }
     f32x2 vv = pack2(v[i], v[i + 1]);
     if (EIGHT) {
       vv = mul2(keep_v, vv);
@@ -181,7 +193,7 @@ __device__ __forceinline__ void step8(const AdamStep& a, const AdamTensor& t, ui
   }
   if (EIGHT) {
     const float most_m = warp_most(m), most_v = warp_most(root);
-    const f32x2 inv_m = splat2(most_m > kTiny ? __fdividef(kMostE4, most_m) : 0.f), inv_v = splat2(most_v > kTiny ? __fdividef(kMostE4, most_v) : 0.f);
+    const f32x2 inv_m = splat2(most_m > kTiny ? __frcp_rn(most_m) * kMostE4 : 0.f), inv_v = splat2(most_v > kTiny ? __fdividef(kMostE4, most_v) : 0.f);
     if (lane == 0) { t.m_scale[block] = most_m * (1.0f / kMostE4); t.v_scale[block] = most_v * (1.0f / kMostE4); }
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
@@ -377,6 +389,7 @@ __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const
   AdamStep s;
   s.beta1 = a.beta1; s.beta2 = a.beta2; s.root_beta2 = a.root_beta2;
   s.gm = a.rest1 * grad_factor; s.gv = a.root_rest2 * grad_factor;
+  s.grad_factor = grad_factor; s.rest1 = a.rest1;
   s.eps = a.eps * root_fix2;
   s.lr = a.lr * lr_factor;
   s.rate = s.lr * root_fix2 / fix1;

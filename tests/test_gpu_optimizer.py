@@ -251,6 +251,26 @@ def test_blocks_of_zeros_and_of_far_apart_values():
     assert (c.scales[0][0] == 0) and (c.scales[1][0] == 0) and (U.host_values(c.state[1]).ravel()[256:512] > 0).all()
 
 
+def test_first_moments_in_8_bits_round_as_the_formula_says():
+    """Operation by operation in float32, to the bit: codes and scales of m do not depend on fused forms."""
+    L = _lib()
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    n = 256 * 4000
+    normal = lambda: torch.randn(n, generator=gen, device="cuda")
+    p, g = normal(), (normal() * torch.exp(normal())).bfloat16()
+    m = (normal() * torch.exp(normal())).view(-1, 256)
+    sm = m.abs().amax(1) / 448.0
+    cm = (m * ((1 / m.abs().amax(1)) * 448.0)[:, None]).to(torch.float8_e4m3fn).flatten()
+    cv, sv = torch.ones(n, device="cuda").to(torch.float8_e4m3fn), torch.ones(n // 256, device="cuda")
+    factor = torch.tensor([0.7], device="cuda")
+    for _ in range(3):
+        x = 0.9 * (cm.float().view(-1, 256) * sm[:, None]) + (1 - 0.9) * (g.float() * factor).view(-1, 256)
+        most = x.abs().amax(1)
+        want_scale, want = most * torch.tensor(1 / 448, device="cuda"), (x * ((1 / most) * 448.0)[:, None]).to(torch.float8_e4m3fn).flatten()
+        L.us_adamw(L.adamw_tensors([p], [g], [cm], [cv], [sm], [sv]), L.new_adamw_step(5), 1e-3, grad_factor=factor)
+        assert torch.equal(sm, want_scale) and torch.equal(cm.view(torch.uint8), want.view(torch.uint8))
+
+
 def test_captured_steps_count_on_and_agree():
     L = _lib()
     make = lambda: [Case(20, 100, copy="e4m3", decay=0.1), Case(10, 777, eight=True)] + [Case(1, 9, seed=i) for i in range(250)]
