@@ -214,6 +214,9 @@ us_status us_linear_group_any(int count, const us_linear_call* calls, void* ws, 
 /* us_linear_group_any with FP8 copies as in us_linear_fwd_cast: copies[i] (ptr NULL: none) of the output of call i, which has a skip
  * tensor. */
 us_status us_linear_group_cast(int count, const us_linear_call* calls, const us_mat* copies, void* ws, size_t ws_bytes, void* stream);
+/* us_linear_group_any with biases as in us_linear_fwd_bias: biases[i] (ptr NULL: none) of call i, which is a US_OP_FWD (another op's:
+ * US_ERR_INVALID_ARG). */
+us_status us_linear_group_bias(int count, const us_linear_call* calls, const us_mat* biases, void* ws, size_t ws_bytes, void* stream);
 /* Number of kernels that us_linear_group_any launches for these calls on the current device (1 or 2); host only, nothing is launched.
  * Errors as there. */
 us_status us_linear_group_launches(int count, const us_linear_call* calls, int* launches);
@@ -248,6 +251,11 @@ us_status us_ffn_hidden(const us_mat* X, const us_mat* W1, float alpha, const us
 us_status us_ffn_hidden_any(const us_mat* X, const us_mat* W1, float alpha, const us_mat* G, const us_mat* W2, float beta_x,
                             float act_in_scale, float act_out_scale, float grad_out_scale, int32_t h_dtype, const us_mat* H,
                             const us_mat* A, const us_mat* dH, void* ws, size_t ws_bytes, void* stream);
+
+/* us_ffn_hidden_any of a first layer with a bias (1 x f, as in us_linear_fwd_bias): H = alpha * X W1 + bias, all else as above. */
+us_status us_ffn_hidden_bias(const us_mat* X, const us_mat* W1, float alpha, const us_mat* bias, const us_mat* G, const us_mat* W2, float beta_x,
+                             float act_in_scale, float act_out_scale, float grad_out_scale, int32_t h_dtype, const us_mat* H,
+                             const us_mat* A, const us_mat* dH, void* ws, size_t ws_bytes, void* stream);
 
 /* us_test_ffn_hidden_starved: us_test_linear_fwd_starved for the kernel of us_ffn_hidden (no operand loads, every
  * device-side wait gives up after `wait_limit` polls, 1 .. 65536): the kernel raises the status word, frees its

@@ -253,6 +253,7 @@ const Known kKnown[] = {
     US_CALL(us_softmax_xent_bwd), US_CALL(us_layer_norm_fwd), US_CALL(us_layer_norm_bwd), US_CALL(us_linear_fwd_cast), US_ARRAYS(us_linear_group_cast, 2),
     US_CALL(us_layer_norm_fwd_cast), US_CALL(us_layer_norm_bwd_cast), US_ARRAYS(us_qk_norm_fwd, 3), US_ARRAYS(us_qk_norm_bwd, 6), US_CALL(us_rotary_table),
     US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd), US_ARRAYS(us_bias_grad, 3), US_ARRAYS(us_grad_norm, 1), US_ARRAYS(us_adamw, 1), US_CALL(us_linear_fwd_bias),
+    US_CALL(us_ffn_hidden_bias), US_ARRAYS(us_linear_group_bias, 2),
 };
 constexpr size_t kCount = sizeof(kKnown) / sizeof(kKnown[0]);
 PyMethodDef g_calls[kCount];

@@ -62,6 +62,7 @@ struct HiddenParams {
   float act_in, act_out, grad_out;  // s_in, alpha_g, beta_g
   uint8_t* h_ptr; long long h_ld;   // optional copy of the rounded pre-activation (NULL: none); ld in elements
   int h_sectors;                    // its rows start on 32-byte boundaries
+  const void* bias; int bias_dt;    // BIAS: one value per hidden unit
   uint8_t *a_ptr, *d_ptr; long long a_ld, d_ld;   // A and dH, for SPLIT > 1 (otherwise reached by TMA)
   unsigned int* status;
   uint32_t wait_limit;
@@ -76,7 +77,8 @@ struct HiddenParams {
 // longest part of the launch while most SMs are idle.  With all 128 columns computed by each they fetched a third more bytes (32 KB a K block
 // instead of 24, with few rows twice as many): captured steps, us, 48 x 1024 x 4096 30.7 -> 28.7, 16 x 1024 x 4096 32.4 -> 29.1, 512 x 512 x 1456 15.0 -> 14.8.
 // OUT_A, OUT_D: output formats of A and dH (us_dtype).  H_BF16: pre-activation rounded to BF16 (else F16).
-template <int ES, int BN, int CG, int SPLIT, int OUT_A, int OUT_D, bool H_BF16>
+// BIAS: H = alpha X W1 + b, in the place of the scaling's multiply one fused multiply-add.
+template <int ES, int BN, int CG, int SPLIT, int OUT_A, int OUT_D, bool H_BF16, bool BIAS>
 __global__ void __launch_bounds__(gemm_threads(kHidEW), 1)
 ffn_hidden_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w1,
                   const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_w2,
@@ -298,17 +300,33 @@ ffn_hidden_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
         put((uint32_t)(4 * s + g), make_uint4(w[0], w[1], w[2], w[3]), 2);
       }
     };
+    // BIAS: the cells of a tile's bias (four columns each, cell j of slice s) lie in rows 0 .. 7 of the staging box where the slice's last piece goes, which
+    // is staged when every cell has been read; one behind the other where nothing is staged.
+    auto cell = [&](int s, int j) {
+      constexpr int kLast = 2 * kOes - 1;
+      const int sw = S::kRowBytes == 128 ? j : S::kRowBytes == 64 ? j >> 1 : 0;
+      return SPLIT > 1 ? buf_out + 16u * j : buf_out + (uint32_t)(j * S::kRowBytes + (((s * 2 * kOes + kLast) ^ sw) << 4));
+    };
     uint32_t hst[kSliceCols / 2 * kSlices];
     // One 32-column slice s of accumulator 0: scale, keep round16(H), GELU, round, stage.
     auto slice_fwd = [&](const uint32_t (&r)[kSliceCols], int s) {
       uint32_t held[2];
 #pragma unroll
       for (int g = 0; g < kSliceCols / 8; ++g) {
-        f32x2 x[4];
+        f32x2 x[4], bias[4];
         float y[8];
+        if constexpr (BIAS) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const uint4 t = ptx::lds128(cell(s, 2 * g + half));
+            bias[2 * half] = pack2(__uint_as_float(t.x), __uint_as_float(t.y)); bias[2 * half + 1] = pack2(__uint_as_float(t.z), __uint_as_float(t.w));
+          }
+          if (SPLIT == 1 && g == kSliceCols / 8 - 1) __syncwarp();    // every lane has read the slice's cells
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          x[k] = mul2(pack2(__uint_as_float(r[8 * g + 2 * k]), __uint_as_float(r[8 * g + 2 * k + 1])), s1);
+          x[k] = pack2(__uint_as_float(r[8 * g + 2 * k]), __uint_as_float(r[8 * g + 2 * k + 1]));
+          x[k] = BIAS ? fma2(x[k], s1, bias[k]) : mul2(x[k], s1);
           float a, b;
           unpack2(x[k], a, b);
           hst[kSliceCols / 2 * s + 4 * g + k] = H_BF16 ? pack_bf16x2(a, b) : pack_f16x2(a, b);
@@ -342,6 +360,8 @@ ffn_hidden_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
       const int row0 = tm * kTileM + rank * 128 + q * 32, n_w = tn * BN + split_col + part * kWarpCols;
       const bool active = n_w < p.N;                            // warp-uniform
       const uint32_t acc_phase = local & 1u;
+      float bias[4];
+      if constexpr (BIAS) bias_fetch<kWarpCols / 4>(p, n_w, lane, bias);
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
         ok = wait_bounded(acc_full_bar(sub), acc_phase, abort_flag, p.status, p.wait_limit);
@@ -359,6 +379,11 @@ ffn_hidden_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constan
           ptx::tmem_ld_32x32_issue(t_row, r0);
           if (SPLIT == 1) {
             if (ptx::elect_one()) ptx::bulk_wait_group_read<0>();      // earlier stores have read the staging boxes
+            __syncwarp();
+          }
+          if (BIAS && sub == 0) {
+            if (lane < kWarpCols / 4)
+              ptx::sts128(cell(lane >> 3, lane & 7), make_uint4(__float_as_uint(bias[0]), __float_as_uint(bias[1]), __float_as_uint(bias[2]), __float_as_uint(bias[3])));
             __syncwarp();
           }
           ptx::tmem_ld_fence(r0);
@@ -438,12 +463,16 @@ bool valid_mat(const us_mat* m) {
 }
 bool is_fp8(int dt) { return dt == US_E4M3 || dt == US_E5M2; }
 
-template <int ES, int BN, int CG, int SPLIT, int OUT_A, int OUT_D, bool H_BF16>
-us_status launch_hidden(const CUtensorMap* t, const HiddenParams& p, int units, cudaStream_t stream) {
-  auto kern = ffn_hidden_kernel<ES, BN, CG, SPLIT, OUT_A, OUT_D, H_BF16>;
+template <int ES, int BN, int CG, int SPLIT, int OUT_A, int OUT_D, bool H_BF16, bool BIAS>
+us_status launch_variant(const CUtensorMap* t, const HiddenParams& p, int units, cudaStream_t stream) {
+  auto kern = ffn_hidden_kernel<ES, BN, CG, SPLIT, OUT_A, OUT_D, H_BF16, BIAS>;
   constexpr int smem = HidSmem<BN, OUT_A == US_E4M3 || OUT_A == US_E5M2 ? 1 : 2, (SPLIT > 1 ? 64 : BN)>::kTotal;
   static std::atomic<uint64_t> smem_set{0};
   return host::launch(kern, &smem_set, CG * SPLIT * units, gemm_threads(kHidEW), smem, CG, stream, t[0], t[1], t[2], t[3], t[4], t[5], p);
+}
+template <int ES, int BN, int CG, int SPLIT, int OUT_A, int OUT_D, bool H_BF16>
+us_status launch_hidden(const CUtensorMap* t, const HiddenParams& p, int units, cudaStream_t stream) {
+  return p.bias ? launch_variant<ES, BN, CG, SPLIT, OUT_A, OUT_D, H_BF16, true>(t, p, units, stream) : launch_variant<ES, BN, CG, SPLIT, OUT_A, OUT_D, H_BF16, false>(t, p, units, stream);
 }
 template <int ES, int OUT_A, int OUT_D, bool H_BF16>
 us_status pick_tile(bool pair, int split, const CUtensorMap* t, const HiddenParams& p, int units, cudaStream_t st) {
@@ -461,9 +490,10 @@ us_status pick_hidden(bool pair, int split, bool h_bf16, const CUtensorMap* t, c
 us_status hidden_impl(const us_mat* X, const us_mat* W1, float alpha, const us_mat* G, const us_mat* W2, float beta_x,
                       float act_in_scale, float act_out_scale, float grad_out_scale, int h_dtype, const us_mat* H,
                       const us_mat* A, const us_mat* dH, void* ws, size_t ws_bytes, void* stream, uint32_t wait_limit,
-                      int starved, int served, bool any) {
+                      int starved, int served, bool any, const us_mat* bias = nullptr) {
   if (!valid_mat(X) || !valid_mat(W1) || !valid_mat(G) || !valid_mat(W2) || !valid_mat(A) || !valid_mat(dH)) return US_ERR_INVALID_ARG;
   const bool keep_h = H && H->ptr;
+  if (bias && (!valid_mat(bias) || bias->rows != 1 || bias->cols != W1->cols)) return US_ERR_INVALID_ARG;
   if (keep_h && !valid_mat(H)) return US_ERR_INVALID_ARG;
   if (h_dtype != US_BF16 && h_dtype != US_F16) return US_ERR_INVALID_ARG;
   const int64_t M = X->rows, K1 = X->cols, N = W1->cols, K2 = G->cols;
@@ -480,6 +510,8 @@ us_status hidden_impl(const us_mat* X, const us_mat* W1, float alpha, const us_m
   for (const us_mat* m : ms) { f8 = f8 && is_fp8(m->dtype); h16 = h16 && m->dtype == X->dtype; }
   if (!f8 && !(any && h16)) return US_ERR_UNSUPPORTED;
   if (!any && (M <= 128 || N <= 128)) return US_ERR_UNSUPPORTED;
+  if (bias && bias->dtype != US_F32 && bias->dtype != US_BF16 && bias->dtype != US_F16) return US_ERR_UNSUPPORTED;
+  if (bias && reinterpret_cast<uintptr_t>(bias->ptr) % dtype_size(bias->dtype)) return US_ERR_ALIGNMENT;
   const int sms = host::sm_count();
   if (sms <= 0) return US_ERR_CUDA;
 
@@ -510,6 +542,7 @@ us_status hidden_impl(const us_mat* X, const us_mat* W1, float alpha, const us_m
   p.h_ptr = keep_h ? static_cast<uint8_t*>(H->ptr) : nullptr;
   p.h_ld = keep_h ? H->ld : 0;
   p.h_sectors = keep_h && reinterpret_cast<uintptr_t>(H->ptr) % 32 == 0 && H->ld % 16 == 0;
+  if (bias) { p.bias = bias->ptr; p.bias_dt = bias->dtype; }
   p.a_ptr = static_cast<uint8_t*>(A->ptr); p.a_ld = A->ld;
   p.d_ptr = static_cast<uint8_t*>(dH->ptr); p.d_ld = dH->ld;
   p.status = static_cast<unsigned int*>(ws);
@@ -552,6 +585,13 @@ extern "C" us_status us_ffn_hidden_any(const us_mat* X, const us_mat* W1, float 
                                        size_t ws_bytes, void* stream) {
   return us::hidden_impl(X, W1, alpha, G, W2, beta_x, act_in_scale, act_out_scale, grad_out_scale, h_dtype, H, A, dH, ws,
                          ws_bytes, stream, us::kWaitLimit, 0, 0, true);
+}
+
+extern "C" us_status us_ffn_hidden_bias(const us_mat* X, const us_mat* W1, float alpha, const us_mat* bias, const us_mat* G, const us_mat* W2,
+                                        float beta_x, float act_in_scale, float act_out_scale, float grad_out_scale, int32_t h_dtype,
+                                        const us_mat* H, const us_mat* A, const us_mat* dH, void* ws, size_t ws_bytes, void* stream) {
+  return bias ? us::hidden_impl(X, W1, alpha, G, W2, beta_x, act_in_scale, act_out_scale, grad_out_scale, h_dtype, H, A, dH, ws,
+                                ws_bytes, stream, us::kWaitLimit, 0, 0, true, bias) : US_ERR_INVALID_ARG;
 }
 
 extern "C" us_status us_test_ffn_hidden_starved(const us_mat* X, const us_mat* W1, const us_mat* G, const us_mat* W2,

@@ -171,23 +171,24 @@ unsigned shared_calls(const us_linear_call* calls, const Shape* sh, int count, i
   return pick;
 }
 
-template <int ES, int BN, int CG, int SPLIT, bool COPY>
+template <int ES, int BN, int CG, int SPLIT, bool COPY, bool BIAS>
 us_status launch_variant(const GroupParams& g, cudaStream_t stream) {
-  auto kern = gemm_group_kernel<ES, BN, CG, SPLIT, COPY>;
+  auto kern = gemm_group_kernel<ES, BN, CG, SPLIT, COPY, BIAS>;
   constexpr int smem = GemmSmem<BN, CG, kGroupEW>::kTotal;
   static std::atomic<uint64_t> smem_set{0};
   return host::launch(kern, &smem_set, CG * g.units, gemm_threads(kGroupEW), smem, CG, stream, g);
 }
 template <int ES, int BN, int CG, int SPLIT>
-us_status launch_group(const GroupParams& g, bool copy, cudaStream_t stream) {
-  return copy ? launch_variant<ES, BN, CG, SPLIT, true>(g, stream) : launch_variant<ES, BN, CG, SPLIT, false>(g, stream);
+us_status launch_group(const GroupParams& g, bool copy, bool bias, cudaStream_t stream) {
+  if (bias) return launch_variant<ES, BN, CG, SPLIT, false, true>(g, stream);
+  return copy ? launch_variant<ES, BN, CG, SPLIT, true, false>(g, stream) : launch_variant<ES, BN, CG, SPLIT, false, false>(g, stream);
 }
 
-// copies: NULL, or for each call the FP8 copy of its output (ptr NULL: none).
+// copies: NULL, or for each call the FP8 copy of its output (ptr NULL: none).  biases: NULL, or for each call its bias (ptr NULL: none); not with copies.
 // test: NULL, or a short wait limit and which CTAs get no operands.  launches: NULL, or receives the number of kernels, and nothing is launched.
 struct GroupTest { uint32_t wait_limit; int starved, served; };
 us_status group_impl(int count, const us_linear_call* calls, const us_mat* copies, bool any, void* ws, size_t ws_bytes, void* stream,
-                     const GroupTest* test = nullptr, int* launches = nullptr) {
+                     const GroupTest* test = nullptr, int* launches = nullptr, const us_mat* biases = nullptr) {
   if (count < 1 || count > kGroupMaxProblems || !calls) return count >= 1 && calls ? US_ERR_UNSUPPORTED : US_ERR_INVALID_ARG;
   if (!launches && (!ws || ws_bytes < us_workspace_bytes())) return US_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(ws) % 16) return US_ERR_ALIGNMENT;
@@ -201,6 +202,12 @@ us_status group_impl(int count, const us_linear_call* calls, const us_mat* copie
       s = check_copy(&copies[i], &calls[i].out, calls[i].ep.skip.ptr != nullptr);
       if (s != US_OK) return s;
     }
+    if (biases && biases[i].ptr) {
+      const us_mat* b = &biases[i];
+      if (!valid_mat(b) || b->rows != 1 || b->cols != sh[i].N || calls[i].op != US_OP_FWD) return US_ERR_INVALID_ARG;
+      if (b->dtype != US_F32 && b->dtype != US_BF16 && b->dtype != US_F16) return US_ERR_UNSUPPORTED;
+      if (reinterpret_cast<uintptr_t>(b->ptr) % dtype_size(b->dtype)) return US_ERR_ALIGNMENT;
+    }
   }
   const int sms = host::sm_count();
   if (sms <= 0) return US_ERR_CUDA;
@@ -213,18 +220,20 @@ us_status group_impl(int count, const us_linear_call* calls, const us_mat* copie
   SplitCall split_calls[kGroupMaxProblems];
   int splits = 0, left = 0, at[kGroupMaxProblems];
   int64_t pair_tiles = 0;
-  bool copy = false;
+  bool copy = false, bias = false;
   for (int i = 0; i < count; ++i) {
     const us_linear_call& c = calls[i];
     const us_mat* q = copies && copies[i].ptr ? &copies[i] : nullptr;
+    const us_mat* b = biases && biases[i].ptr ? &biases[i] : nullptr;
     if (shared >> i & 1) {
       const bool skip = c.ep.skip.ptr != nullptr;
       split_calls[splits++] = SplitCall{&c.a, &c.b, &c.out, skip ? &c.ep.skip : nullptr, q, c.op == US_OP_BWD_W, c.op != US_OP_BWD_X, c.scale,
-                                        skip ? c.ep.skip_coef : 0.f, skip ? c.ep.out_coef : 1.f};
+                                        skip ? c.ep.skip_coef : 0.f, skip ? c.ep.out_coef : 1.f, b ? b->ptr : nullptr, b ? b->dtype : US_F32};
       continue;
     }
     at[left++] = i;
     copy = copy || q;
+    bias = bias || b;
     pair_tiles += ((sh[i].M + 255) / 256) * ((sh[i].N + 255) / 256);
   }
   if (launches) *launches = (splits > 0) + (left > 0);
@@ -256,6 +265,8 @@ us_status group_impl(int count, const us_linear_call* calls, const us_mat* copie
     P.copy_ld = P.copy ? copies[i].ld : 0;
     P.copy_dt = P.copy ? copies[i].dtype : US_E4M3;
     P.copy_sectors = reinterpret_cast<uintptr_t>(P.copy) % 32 == 0 && P.copy_ld % 32 == 0;
+    P.bias = biases ? biases[i].ptr : nullptr;
+    P.bias_dt = P.bias ? biases[i].dtype : US_F32;
     if (launches) continue;
     if (!make_tmap(&P.ta, &c.a, es, P.a_mn ? 128 / es : 128) || !make_tmap(&P.tb, &c.b, es, P.b_mn ? 128 / es : 128)) return US_ERR_CUDA;
     const int oes = dtype_size(c.out.dtype);
@@ -271,8 +282,8 @@ us_status group_impl(int count, const us_linear_call* calls, const us_mat* copie
     const us_status s = launch_split(splits, split_calls, t, static_cast<unsigned int*>(ws), tt.wait_limit, starved, st);
     if (s != US_OK) return s;
   }
-  if (es == 1) return pair ? launch_group<1, 256, 2, 1>(g, copy, st) : split == 2 ? launch_group<1, 128, 1, 2>(g, copy, st) : launch_group<1, 128, 1, 1>(g, copy, st);
-  return pair ? launch_group<2, 256, 2, 1>(g, copy, st) : split == 2 ? launch_group<2, 128, 1, 2>(g, copy, st) : launch_group<2, 128, 1, 1>(g, copy, st);
+  if (es == 1) return pair ? launch_group<1, 256, 2, 1>(g, copy, bias, st) : split == 2 ? launch_group<1, 128, 1, 2>(g, copy, bias, st) : launch_group<1, 128, 1, 1>(g, copy, bias, st);
+  return pair ? launch_group<2, 256, 2, 1>(g, copy, bias, st) : split == 2 ? launch_group<2, 128, 1, 2>(g, copy, bias, st) : launch_group<2, 128, 1, 1>(g, copy, bias, st);
 }
 
 }  // namespace
@@ -286,6 +297,9 @@ extern "C" us_status us_linear_group_any(int count, const us_linear_call* calls,
 }
 extern "C" us_status us_linear_group_cast(int count, const us_linear_call* calls, const us_mat* copies, void* ws, size_t ws_bytes, void* stream) {
   return copies ? us::group_impl(count, calls, copies, true, ws, ws_bytes, stream) : US_ERR_INVALID_ARG;
+}
+extern "C" us_status us_linear_group_bias(int count, const us_linear_call* calls, const us_mat* biases, void* ws, size_t ws_bytes, void* stream) {
+  return biases ? us::group_impl(count, calls, nullptr, true, ws, ws_bytes, stream, nullptr, nullptr, biases) : US_ERR_INVALID_ARG;
 }
 extern "C" us_status us_linear_group_launches(int count, const us_linear_call* calls, int* launches) {
   if (!launches) return US_ERR_INVALID_ARG;

@@ -45,6 +45,7 @@ struct GroupProblem {
   float skip_coef, out_coef;
   uint8_t* copy; int64_t copy_ld;       // an FP8 copy of the output (null: none)
   int copy_dt, copy_sectors;            // its rows start on 32-byte boundaries
+  const void* bias; int bias_dt;        // one value per output column (null: none)
 };
 
 struct GroupParams {
@@ -67,8 +68,8 @@ constexpr int kGroupEW = 8;
 // small that half of the SMs would be idle: the epilogue of a tile takes longer than a short main loop.
 //
 // COPY: some problem's output is also written as FP8 codes.  A variant of its own, because the code of the copy, never taken,
-// cost the launches without one 3 to 4 % (1000 x 528 x 2096: 15.3 to 16.0 us).
-template <int ES, int BN, int CG, int SPLIT, bool COPY>
+// cost the launches without one 3 to 4 % (1000 x 528 x 2096: 15.3 to 16.0 us).  BIAS: some problem has a bias.
+template <int ES, int BN, int CG, int SPLIT, bool COPY, bool BIAS>
 __global__ void __launch_bounds__(gemm_threads(kGroupEW), 1)
 gemm_group_kernel(const __grid_constant__ GroupParams g) {
   using S = GemmSmem<BN, CG, kGroupEW>;
@@ -279,6 +280,9 @@ gemm_group_kernel(const __grid_constant__ GroupParams g) {
       const int out_row = min(128, kWarpCols * out_es);
       const int in_box_cols = 128 / in_es, out_box_cols = out_row / out_es;
       const uint32_t out_sw = out_row == 128 ? sw : out_row == 64 ? (uint32_t)((lane >> 1) & 3) : 0u;
+      const int bias_cols = BIAS && P.bias != nullptr ? cols : 0;
+      float bias = 0.f;                                        // of the slice to come, a column a lane
+      if constexpr (BIAS) bias = bias_lane(P, n_w + lane, bias_cols);
       next = look(r + 1);
       ok = wait_bounded(acc_full_bar(acc), acc_phase, abort_flag, g.status, g.wait_limit);
       ok = __all_sync(0xffffffffu, ok);
@@ -335,8 +339,14 @@ gemm_group_kernel(const __grid_constant__ GroupParams g) {
           uint32_t copy[8];
           float y[32];
           // The choices of a tile are taken once per slice, not once per eight columns.
+          if (BIAS && bias_cols) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k) unpack2(mul2(pack2(v[2 * k], v[2 * k + 1]), scale2), y[2 * k], y[2 * k + 1]);
+            for (int k = 0; k < 16; ++k) unpack2(fma2(pack2(v[2 * k], v[2 * k + 1]), scale2, bias_pair(bias, 2 * k)), y[2 * k], y[2 * k + 1]);
+            bias = bias_lane(P, col + 32 + lane, last_slice ? 0 : bias_cols);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) unpack2(mul2(pack2(v[2 * k], v[2 * k + 1]), scale2), y[2 * k], y[2 * k + 1]);
+          }
           if (skip) {
             residual_row32(skip_dt, raw, skip2, oc2, y);
             if (COPY && P.copy) copy_codes32(out_dt, P.copy_dt, y, copy);

@@ -159,10 +159,11 @@ __device__ __forceinline__ float bias_lane(const P& p, int col, int n) { return 
 // rows 0 .. 7 where chunk 4 s + 3 goes, the last of the slice to be staged; else one behind the other.
 template <bool IN_BOX>
 __device__ __forceinline__ uint32_t bias_cell(uint32_t at, int s, int j) { return IN_BOX ? at + (uint32_t)(j * 128 + (((4 * s + 3) ^ j) << 4)) : at + (uint32_t)(128 * s + 16 * j); }
-// Lanes 0 .. 15: a tile's, from global memory and to the cells.
-__device__ __forceinline__ void bias_fetch(const GemmParams& p, int col, int lane, float (&b)[4]) {
+// Lanes 0 .. 15 (the first CELLS): a tile's, from global memory and to the cells.
+template <int CELLS = 16, class P>
+__device__ __forceinline__ void bias_fetch(const P& p, int col, int lane, float (&b)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) b[i] = bias_lane(p, col + 4 * lane + i, lane < 16 ? p.N : 0);
+  for (int i = 0; i < 4; ++i) b[i] = bias_lane(p, col + 4 * lane + i, lane < CELLS ? p.N : 0);
 }
 template <bool IN_BOX>
 __device__ __forceinline__ void bias_keep(uint32_t at, int lane, const float (&b)[4]) {

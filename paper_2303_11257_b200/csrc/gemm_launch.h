@@ -31,7 +31,7 @@ struct BatchDesc {
 // How an output is tiled: columns of a tile, CTAs that cooperate on it as a pair (1: none), CTAs (pairs) that share its contraction.
 struct Tiling { int bn, cg, splits; };
 
-// One GEMM of a launch with shared contractions (gemm_split.cu); skip and copy may be NULL, and bias, which only a launch of one takes.
+// One GEMM of a launch with shared contractions (gemm_split.cu); skip, copy and bias may be NULL.
 struct SplitCall {
   const us_mat *a, *b, *out, *skip, *copy;
   bool a_mn, b_mn;

@@ -13,13 +13,12 @@ namespace {
 using host::make_tmap;
 
 template <int ES, int BN, int CG, int PROBLEMS>
-us_status launch(const SplitParams<PROBLEMS>& p, int tiles, cudaStream_t stream) {
+us_status launch(const SplitParams<PROBLEMS>& p, int tiles, bool bias, cudaStream_t stream) {
   static std::atomic<uint64_t> smem_set{0};
-  if constexpr (PROBLEMS == 1) {
+  if (bias) {
     static std::atomic<uint64_t> smem_set_bias{0};
-    if (p.prob[0].bias)
-      return host::launch(gemm_split_kernel<ES, BN, CG, false, true>, &smem_set_bias, CG * p.splits * tiles, gemm_threads(8), GemmSmem<BN, CG, 8>::kTotal,
-                          CG * p.splits, stream, p);
+    return host::launch(gemm_split_kernel<ES, BN, CG, (PROBLEMS > 1), true>, &smem_set_bias, CG * p.splits * tiles, gemm_threads(8), GemmSmem<BN, CG, 8>::kTotal,
+                        CG * p.splits, stream, p);
   }
   return host::launch(gemm_split_kernel<ES, BN, CG, (PROBLEMS > 1)>, &smem_set, CG * p.splits * tiles, gemm_threads(8), GemmSmem<BN, CG, 8>::kTotal,
                       CG * p.splits, stream, p);
@@ -35,6 +34,7 @@ us_status launch_problems(int count, const SplitCall* calls, const Tiling& t, un
   p.splits = t.splits; p.status = status; p.wait_limit = wait_limit; p.starved = starved;
   const int es = dtype_size(calls[0].a->dtype), one = es == 1 ? US_E5M2 : US_BF16;      // the format the descriptor numbers 1
   int tiles = 0;
+  bool bias = false;
   for (int i = 0; i < count; ++i) {
     const SplitCall& c = calls[i];
     SplitProblem& s = p.prob[i];
@@ -51,7 +51,8 @@ us_status launch_problems(int count, const SplitCall* calls, const Tiling& t, un
     P.copy_ld = c.copy ? c.copy->ld : 0;
     P.copy_dt = c.copy ? c.copy->dtype : US_E4M3;
     P.copy_sectors = reinterpret_cast<uintptr_t>(P.copy) % 32 == 0 && P.copy_ld % 32 == 0;
-    s.bias = c.bias; s.bias_dt = c.bias_dt;
+    P.bias = c.bias; P.bias_dt = c.bias_dt;
+    bias = bias || c.bias;
     s.a_bytes = (uint32_t)us::split_a_bytes(t.bn, c.a_mn, c.out->rows);
     using Narrow = GemmSmem<64, 1, 8>;
     s.stages = t.bn == 64    ? std::min((int)Narrow::kMaxStages, Narrow::kStages * Narrow::kStageBytes / ((int)s.a_bytes + Narrow::kBBytes))
@@ -67,8 +68,8 @@ us_status launch_problems(int count, const SplitCall* calls, const Tiling& t, un
     if (c.skip && !make_tmap(&P.tskip, c.skip, dtype_size(c.skip->dtype), 32)) return US_ERR_CUDA;
   }
   for (int i = count; i < PROBLEMS; ++i) p.prob[i].tile_end = tiles;
-  if (es == 1) return t.bn == 64 ? launch<1, 64, 1>(p, tiles, stream) : t.bn == 128 ? launch<1, 128, 1>(p, tiles, stream) : launch<1, 256, 2>(p, tiles, stream);
-  return t.bn == 64 ? launch<2, 64, 1>(p, tiles, stream) : t.bn == 128 ? launch<2, 128, 1>(p, tiles, stream) : launch<2, 256, 2>(p, tiles, stream);
+  if (es == 1) return t.bn == 64 ? launch<1, 64, 1>(p, tiles, bias, stream) : t.bn == 128 ? launch<1, 128, 1>(p, tiles, bias, stream) : launch<1, 256, 2>(p, tiles, bias, stream);
+  return t.bn == 64 ? launch<2, 64, 1>(p, tiles, bias, stream) : t.bn == 128 ? launch<2, 128, 1>(p, tiles, bias, stream) : launch<2, 256, 2>(p, tiles, bias, stream);
 }
 
 }  // namespace

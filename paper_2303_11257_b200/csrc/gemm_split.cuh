@@ -17,7 +17,6 @@ namespace us {
 struct SplitProblem {
   GroupProblem g;                           // out boxes: 32 rows x 32 columns
   int tiles_m, tile_end;                    // tile rows; tiles of the problems up to and including this one
-  const void* bias; int bias_dt;            // BIAS: one value per output column
   uint32_t a_bytes; int stages;             // bytes of A in a stage (narrow tiles of few rows: those that exist), and the stages that fit
 };
 template <int PROBLEMS>
@@ -29,7 +28,7 @@ struct SplitParams {
   int starved;                              // test hook (starved_cta)
 };
 
-// MULTI: several problems; the parameters of one alone are at fixed addresses and need not be fetched ahead.
+// MULTI: several problems; the parameters of one alone are at fixed addresses and need not be fetched ahead.  BIAS: some problem has a bias.
 template <int ES, int BN, int CG, bool MULTI, bool BIAS = false>
 __global__ void __launch_bounds__(gemm_threads(8), 1)
 gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems : 1> p) {
@@ -116,6 +115,8 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
   int first = 0;                                     // this warp's first block of its own
   while (first < kSlices && !mine(first)) ++first;
   float bias = 0.f;                                  // of a block's columns, a column a lane
+  // (-0 where a problem among others has none: a product plus -0 is the product, zeros and their signs included)
+  auto fetch_bias = [&](int col, int n) { return MULTI && P.bias == nullptr ? -0.f : bias_lane(P, col, n); };
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (every CTA)
@@ -210,7 +211,7 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
   } else {
     ptx::grid_wait_previous();
     if (first < kSlices && skip) issue_in(first);
-    if constexpr (BIAS) bias = bias_lane(sp, n_w + 32 * first + lane, first < kSlices ? cols : 0);
+    if constexpr (BIAS) bias = fetch_bias(n_w + 32 * first + lane, first < kSlices ? cols : 0);
     ok = wait_bounded(acc_full_bar, 0, abort_flag, p.status, p.wait_limit);
     ok = __all_sync(0xffffffffu, ok);
   }
@@ -262,7 +263,7 @@ gemm_split_kernel(const __grid_constant__ SplitParams<MULTI ? kGroupMaxProblems 
         }
       }
       if constexpr (BIAS) {
-        if (sl > first) bias = bias_lane(sp, col + lane, cols);
+        if (sl > first) bias = fetch_bias(col + lane, cols);
       }
       float y[32];
       ptx::tmem_ld_32x32(t_row + 32 * sl, y);

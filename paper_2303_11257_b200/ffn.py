@@ -418,17 +418,19 @@ class UnitScaledFFN:
 class UnitScaledBiasFFN(UnitScaledFFN):
     """An FFN block whose linear layers have biases (b1 [f], b2 [d], float32, zeros at first, the block's own as their gradients db1, db2 are):
 
-        H = alpha1 q(X) q(W1) + b1 ; A = q(alpha_g gelu(s_in H)), H kept            us_linear_fwd_bias + GELU epilogue
+        H = alpha1 q(X) q(W1) + b1 ; A = q(alpha_g gelu(s_in H))                    us_linear_fwd_bias + GELU epilogue
         R = sqrt(1-tau) X + sqrt(tau) (alpha2 A W2q + b2)                           us_linear_fwd_bias + residual epilogue
         dH = q(beta_g s_in gelu'(s_in H) * beta_x2 Gq W2q^T)                        us_linear_bwd_x + GELU-grad epilogue
         db1 = beta_w sum over rows of dH ; db2 = beta_w sum over rows of Gq         us_bias_grad
         dW2, dW1 and dX as for the block without biases                             us_linear_group_any
 
-    A bias is a cut-edge as a weight is: its gradient takes beta_w = b^-1/2.  step(), forward() and backward() are used as those of UnitScaledFFN.  W1 and
+    A bias is a cut-edge as a weight is: its gradient takes beta_w = b^-1/2.  forward() and backward() issue these calls; step() those of the block without biases,
+    us_ffn_hidden_bias and us_linear_group_bias, with us_bias_grad between them.  All are used as UnitScaledFFN's are, and keep_h is the same; W1 and
     W2 may be None where self.W1q and self.W2q hold the weights already, as an optimiser that writes them does (optim.AdamW)."""
 
-    def __init__(self, T: int, d: int, f: int, scales: FFNScales | None = None, operand: str = "fp8", h_dtype=torch.bfloat16, io_dtype=torch.bfloat16, device="cuda"):
-        super().__init__(T, d, f, scales, operand, h_dtype, io_dtype, device, keep_h=True)
+    def __init__(self, T: int, d: int, f: int, scales: FFNScales | None = None, operand: str = "fp8", h_dtype=torch.bfloat16, io_dtype=torch.bfloat16, device="cuda",
+                 keep_h: bool = False):
+        super().__init__(T, d, f, scales, operand, h_dtype, io_dtype, device, keep_h)
         zeros = lambda n: torch.zeros(n, dtype=torch.float32, device=device)
         self.b1, self.b2, self.db1, self.db2 = zeros(f), zeros(d), zeros(f), zeros(d)
 
@@ -442,9 +444,21 @@ class UnitScaledBiasFFN(UnitScaledFFN):
         yield p.cast_multi(["X", "G"], [self.Xq, self.Gq], padded=self.operand != "fp8")
         yield from self.plan_gemms(p, "X", "G")
 
-    def plan_gemms(self, p, X, G, dX_copy=None):
-        yield from self.plan_forward(p, X, cast_x=False)
-        yield from self.plan_backward(p, G, cast_g=False, dX_copy=dX_copy)
+    def plan_gemms(self, p, X, G):
+        if not self.fused_hidden:
+            yield from self.plan_forward(p, X, cast_x=False)
+            yield from self.plan_backward(p, G, cast_g=False)
+            return
+        sc = self.sc
+        yield L.Call("us_ffn_hidden_bias", p.mat(self.Xq), p.mat(self.W1q), sc.alpha1, p.mat(self.b1.view(1, -1)), p.mat(self.Gq), p.mat(self.W2q), sc.beta_x2,
+                     sc.s_in, sc.alpha_g, sc.beta_g, L._TORCH_DTYPES[self.H.dtype], p.mat(self.H) if self._writes_h() else None,
+                     p.mat(self.Aq), p.mat(self.dHq), self.ws.data_ptr(), self.ws.numel())
+        yield self._plan_bias_grad(p)
+        w2, w1, x1 = self._plan_backward_entries(G)
+        yield p.group([w2, w1, (L.US_OP_FWD, self.Aq, self.W2q, sc.alpha2, self.R, X, self._c), x1], self.ws, biases={2: self.b2})
+
+    def _plan_bias_grad(self, p):
+        return p.bias_grad([self.dHq, self.Gq], [self.sc.beta_w] * 2, [self.db1, self.db2])
 
     def plan_forward(self, p, X, cast_x=True):
         sc = self.sc
@@ -453,20 +467,19 @@ class UnitScaledBiasFFN(UnitScaledFFN):
         yield self._plan_linear(p, self.Xq, self.W1q, sc.alpha1, self.b1, L.epilogue(act=L.US_ACT_GELU, act_in_scale=sc.s_in, act_out_scale=sc.alpha_g, aux=self.H), self.Aq)
         yield self._plan_linear(p, self.Aq, self.W2q, sc.alpha2, self.b2, p.residual(X, self._c), self.R)
 
-    def plan_backward(self, p, G, cast_g=True, dX_copy=None):
+    def plan_backward(self, p, G, cast_g=True):
         sc = self.sc
         if cast_g:
             yield self._plan_cast(p, G, self.Gq)
         yield p.linear("us_linear_bwd_x", self.Gq, self.W2q, sc.beta_x2, self.dHq, self.ws,
                        L.epilogue(act=L.US_ACT_GELU_GRAD, act_in_scale=sc.s_in, act_out_scale=sc.beta_g, aux=self.H))
-        yield p.bias_grad([self.dHq, self.Gq], [sc.beta_w] * 2, [self.db1, self.db2])
-        yield p.group(self._plan_backward_entries(G), self.ws, {2: dX_copy} if dX_copy is not None else None)
+        yield self._plan_bias_grad(p)
+        yield p.group(self._plan_backward_entries(G), self.ws)
 
     @property
     def gemm_launches(self) -> int:
-        """Launches of a step without its casts: the two forward GEMMs, the GELU-gradient GEMM, the biases' gradients and the grouped launch (two where it
-        shares contractions)."""
-        return 4 + self._group_launches(forward=False)
+        """Launches of a step without its casts: the hidden layer's, the biases' gradients and the grouped launch (two where it shares contractions)."""
+        return 2 + self._group_launches(forward=True) if self.fused_hidden else 4 + self._group_launches(forward=False)
 
     @property
     def launches_per_step(self) -> int:

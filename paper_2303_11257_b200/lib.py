@@ -115,6 +115,9 @@ def _load() -> C.CDLL:
     lib.us_test_linear_tiling.restype = C.c_int
     lib.us_linear_group_launches.argtypes = [C.c_int, C.POINTER(us_linear_call), C.POINTER(C.c_int)]
     lib.us_linear_group_launches.restype = C.c_int
+    lib.us_linear_group_bias.argtypes = [C.c_int, C.POINTER(us_linear_call), MP, V, SZ, V]
+    lib.us_ffn_hidden_bias.argtypes = [MP, MP, F, MP, MP, MP, F, F, F, F, C.c_int32, MP, MP, MP, V, SZ, V]
+    lib.us_linear_group_bias.restype = lib.us_ffn_hidden_bias.restype = C.c_int
     lib.us_linear_fwd_cast.argtypes = [MP, MP, F, EP, MP, MP, V, SZ, V]
     lib.us_linear_group_cast.argtypes = [C.c_int, C.POINTER(us_linear_call), MP, V, SZ, V]
     lib.us_layer_norm_fwd_cast.argtypes = [MP, MP, MP, F, MP, MP, V]
@@ -391,9 +394,10 @@ class Plan:
             ep.skip = self.mat(skip)
         return ep
 
-    def group(self, entries, ws, copies=None):
+    def group(self, entries, ws, copies=None, biases=None):
         """us_linear_group_any over (op, a, b, scale, out, skip or None, (skip_coef, out_coef)); as single launches where
-        there are more tiles than its work list holds.  copies: FP8 copies of the outputs (us_linear_group_cast), by entry."""
+        there are more tiles than its work list holds.  copies: FP8 copies of the outputs (us_linear_group_cast), biases: vectors
+        (us_linear_group_bias), by entry; one or the other."""
         arr = (us_linear_call * len(entries))()
         for c, (op, a, b, scale, out, skip, coef) in zip(arr, entries):
             c.op, c.a, c.b, c.scale, c.out, c.ep.out_coef = op, self.mat(a), self.mat(b), scale, self.mat(out), 1.0
@@ -404,6 +408,12 @@ class Plan:
                     self.slot(skip, c.ep.skip)
                 else:
                     c.ep.skip = self.mat(skip)
+        if biases:
+            bs = (us_mat * len(entries))()
+            for i, t in biases.items():
+                bs[i] = self.mat(t.view(1, -1))
+            return Call("us_linear_group_bias", len(entries), arr, bs, ws.data_ptr(), ws.numel(),
+                        instead=((US_ERR_UNSUPPORTED,), lambda stream: linear_each(arr, ws, stream, bs)))
         if not copies:
             return Call("us_linear_group_any", len(entries), arr, ws.data_ptr(), ws.numel(),
                         instead=((US_ERR_UNSUPPORTED,), lambda stream: linear_each(arr, ws, stream)))
@@ -510,6 +520,15 @@ def us_linear_group_any(calls, ws, stream=None):
     us_linear_group(calls, ws, stream, "us_linear_group_any")
 
 
+def us_linear_group_bias(calls, biases, ws, stream=None):
+    """us_linear_group_any with a bias (a vector) or None for each call; biases belong to forward ops."""
+    _here(ws)
+    if len(biases) != len(calls):
+        raise ValueError("a bias or None for each call")
+    rows = [us_mat() if b is None else mat(b.view(1, -1) if b.dim() == 1 else b) for b in biases]
+    _check("us_linear_group_bias", _entry("us_linear_group_bias")(len(calls), (us_linear_call * len(calls))(*calls), (us_mat * len(calls))(*rows), ws, ws, _stream(stream)))
+
+
 def us_linear_group_launches(calls) -> int:
     """Number of kernels us_linear_group_any launches for these calls; one each where it refuses them (linear_together)."""
     n = C.c_int()
@@ -520,9 +539,12 @@ def us_linear_group_launches(calls) -> int:
     return n.value
 
 
-def linear_each(calls, ws, stream=None):
+def linear_each(calls, ws, stream=None, biases=None):
     """The same ops as single launches, in order (for a group with more tiles than the grouped form's work list holds)."""
-    for c in calls:
+    for i, c in enumerate(calls):
+        if biases is not None and biases[i].ptr:
+            _check("us_linear_fwd_bias", _entry("us_linear_fwd_bias")(c.a, c.b, c.scale, biases[i], c.ep, c.out, None, ws, ws, _stream(stream)))
+            continue
         name = ("us_linear_fwd", "us_linear_bwd_x", "us_linear_bwd_w")[c.op]
         _check(name, _entry(name)(c.a, c.b, c.scale, c.ep, c.out, ws, ws, _stream(stream)))
 
@@ -654,6 +676,15 @@ def us_ffn_hidden(X, W1, alpha, G, W2, beta_x, act_in_scale, act_out_scale, grad
 def us_ffn_hidden_any(*args, **kwargs):
     """us_ffn_hidden for 16-bit operands and any number of rows and hidden units, too."""
     return us_ffn_hidden(*args, **kwargs, name="us_ffn_hidden_any")
+
+
+def us_ffn_hidden_bias(X, W1, alpha, bias, G, W2, beta_x, act_in_scale, act_out_scale, grad_out_scale, A, dH, ws,
+                       H=None, h_dtype=torch.bfloat16, stream=None):
+    """us_ffn_hidden_any of a first layer with a bias (a vector)."""
+    _here(A)
+    _check("us_ffn_hidden_bias", _entry("us_ffn_hidden_bias")(X, W1, alpha, bias.view(1, -1) if bias.dim() == 1 else bias, G, W2, beta_x, act_in_scale, act_out_scale,
+                                                              grad_out_scale, _TORCH_DTYPES[h_dtype], H, A, dH, ws, ws, _stream(stream)))
+    return A, dH
 
 
 def us_test_ffn_hidden_starved(X, W1, G, W2, A, dH, ws, wait_limit: int, stream=None):

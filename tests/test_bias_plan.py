@@ -18,7 +18,8 @@ def test_calls_of_a_step(monkeypatch, operand):
     block, x = _ffn(operand=operand)
     rec = _Recorder()
     monkeypatch.setattr(L, "_lib", rec)
-    gemms = ["linear_fwd_bias", "linear_fwd_bias", "linear_bwd_x", "bias_grad", "linear_group_any"]
+    gemms = ["ffn_hidden_bias", "bias_grad", "linear_group_bias"]
+    apart = ["linear_fwd_bias", "linear_fwd_bias", "linear_bwd_x", "bias_grad", "linear_group_any"]
     block.step(*x, stream=0)
     assert rec.names() == ["cast_multi"] + gemms
     assert rec.calls[0][1][0] == 4
@@ -30,7 +31,28 @@ def test_calls_of_a_step(monkeypatch, operand):
     block.backward(x[3], stream=0)
     block.backward(x[3], stream=0, cast_g=False)
     cast = "cast_fp8" if operand == "fp8" else "residual_add"
-    assert rec.names() == [cast] + gemms[:2] + [cast] + gemms[2:] + gemms[2:]
+    assert rec.names() == [cast] + apart[:2] + [cast] + apart[2:] + apart[2:]
+
+
+def test_a_step_whose_pre_activation_has_32_bits(monkeypatch):
+    block, x = _ffn(operand="bf16", h_dtype=torch.float32)
+    rec = _Recorder()
+    monkeypatch.setattr(L, "_lib", rec)
+    block.step(*x, stream=0)
+    assert rec.names() == ["cast_multi", "linear_fwd_bias", "linear_fwd_bias", "linear_bwd_x", "bias_grad", "linear_group_any"]
+
+
+def test_a_refused_group_adds_the_bias_in_single_launches(monkeypatch):
+    class Refuses(_Recorder):
+        def __getattr__(self, name):
+            call = super().__getattr__(name)
+            return (lambda *args: call(*args) or L.US_ERR_UNSUPPORTED) if name == "us_linear_group_bias" else call
+    block, x = _ffn()
+    rec = Refuses()
+    monkeypatch.setattr(L, "_lib", rec)
+    block.step(*x, stream=0)
+    assert rec.names()[3:] == ["linear_group_bias", "linear_bwd_w", "linear_bwd_w", "linear_fwd_bias", "linear_bwd_x"]
+    assert rec.calls[6][1][3].ptr == block.b2.data_ptr()
 
 
 def test_a_copy_has_its_own_buffers(monkeypatch):

@@ -52,3 +52,47 @@ def test_what_is_refused():
     assert call(X=M(0x10000, F16, 8, 64)) == 2
     assert call(bias=M(0x30002, F32, 1, 48)) == 3 and call(bias=M(0x30001, BF, 1, 48)) == 3 and call(bias=M(0x30004, F32, 1, 48)) == 5 and call(bias=M(0x30002, F16, 1, 48)) == 5
     assert call(ws=None) == 4 and call(size=255) == 4 and call(ws=0x70008) == 3
+
+
+def hidden(bias=M(0x30000, F32, 1, 48), X=M(0x10000, E4, 200, 64), H=None, h_dtype=BF, ws=0x70000):
+    ref = lambda m: None if m is None else C.byref(m)
+    T = X.rows
+    fmt = X.dtype
+    return L.raw().us_ffn_hidden_bias(ref(X), ref(M(0x20000, fmt, 64, 48)), 0.5, ref(bias), ref(M(0x80000, fmt, T, 32)), ref(M(0x90000, fmt, 48, 32)), 0.5, 1.0, 1.0, 1.0,
+                                      h_dtype, ref(H), ref(M(0xa0000, fmt, T, 48)), ref(M(0xb0000, fmt, T, 48)), ws, 256, None)
+
+
+def test_hidden_layer():
+    for dt in (F32, BF, F16):
+        for fmt in (E4, BF, F16):
+            assert hidden(bias=M(0x30000, dt, 1, 48, 50), X=M(0x10000, fmt, 200, 64)) == 5
+    for bad in (None, M(None, F32, 1, 48), M(0x30000, F32, 1, 47), M(0x30000, F32, 2, 48), M(0x30000, F32, 48, 1), M(0x30000, 9, 1, 48), M(0x30000, F32, 1, 48, 47)):
+        assert hidden(bias=bad) == 1
+    assert hidden(h_dtype=F32) == 1 and hidden(H=M(0xc0000, F16, 200, 48)) == 1
+    for bad in (E4, E5):
+        assert hidden(bias=M(0x30000, bad, 1, 48)) == 2
+    assert hidden(X=M(0x10000, F32, 200, 64)) == 2
+    assert hidden(bias=M(0x30002, F32, 1, 48)) == 3 and hidden(bias=M(0x30001, BF, 1, 48)) == 3 and hidden(bias=M(0x30002, BF, 1, 48)) == 5
+    assert hidden(ws=None) == 4 and hidden(ws=0x70008) == 3
+
+
+def group(biases, op=L.US_OP_FWD, count=2, act=0):
+    calls = (L.us_linear_call * 2)()
+    for c in calls:
+        c.op, c.a, c.b, c.scale, c.out, c.ep = L.US_OP_FWD, M(0x10000, BF, 48, 48), M(0x20000, BF, 48, 48), 0.5, M(0x40000, BF, 48, 48), ep(act)
+    calls[1].op = op
+    return L.raw().us_linear_group_bias(count, calls, None if biases is None else (L.us_mat * 2)(*biases), 0x70000, 256, None)
+
+
+def test_group():
+    none, good = L.us_mat(), M(0x30000, F32, 1, 48)
+    for biases in ([none, none], [none, good], [good, good], [M(0x30002, BF, 1, 48), none]):
+        assert group(biases) == 5
+    assert group([good, none], op=L.US_OP_BWD_X) == 5 and group([good, none], op=L.US_OP_BWD_W) == 5
+    for op in (L.US_OP_BWD_X, L.US_OP_BWD_W):
+        assert group([none, good], op=op) == 1
+    for bad in (M(0x30000, F32, 1, 47), M(0x30000, F32, 48, 1), M(0x30000, 9, 1, 48)):
+        assert group([none, bad]) == 1
+    assert group(None) == 1 and group([none, good], count=0) == 1 and group([none, good], count=5) == 2
+    assert group([none, M(0x30000, E4, 1, 48)]) == 2 and group([none, good], act=L.US_ACT_GELU) == 2
+    assert group([none, M(0x30002, F32, 1, 48)]) == 3
