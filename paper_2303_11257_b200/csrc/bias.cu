@@ -15,7 +15,8 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostParts = 8, kStripBytes = 128;
 constexpr int kStep = kThreads / 8;          // rows that a CTA has side by side
-constexpr int kAhead = 16;                   // rows that a thread has in flight
+constexpr int kAhead = 16;                   // rows that a thread has in flight,
+constexpr int kRest = 8;                     // and where fewer are left
 
 struct BiasPart {
   const void* g;
@@ -84,11 +85,17 @@ __device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) add16<DT>(t[k], acc);
       }
-      for (; r < whole; r += kStep) add16<DT>(*reinterpret_cast<const uint4*>(g + r * pitch), acc);
-      if (r < end) {                                           // the matrix's last row
+      for (; r < whole; r += kStep * kRest) {                  // (of rows that are not there, zeros)
+        uint4 t[kRest];
+#pragma unroll
+        for (int k = 0; k < kRest; ++k) t[k] = r + kStep * k < whole ? *reinterpret_cast<const uint4*>(g + (r + kStep * k) * pitch) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < kRest; ++k) add16<DT>(t[k], acc);
+      }
+      if (cut && end == p.rows && (p.rows - 1 - first) % kStep == warp * 4 + (lane >> 3)) {    // the matrix's last row
 #pragma unroll
         for (int i = 0; i < kChunk; ++i)
-          if (i < cols) acc[i] += load_one(p.g, DT, r * p.ld + col + i);
+          if (i < cols) acc[i] += load_one(p.g, DT, (p.rows - 1) * p.ld + col + i);
       }
     }
 #pragma unroll
@@ -101,12 +108,27 @@ __device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t
       for (int i = 0; i < kChunk; ++i) sums[warp][chunk * kChunk + i] = acc[i];
     }
   } else {
+    // A lane has every 32nd column of every 8th row, kRest of them at a time (behind the last row, that one and not added); lanes behind the last column have that
+    // one's too.
     float acc[kCols / 32] = {};
-    for (int64_t r = first + warp; r < end; r += kWarps) {
+    int col[kCols / 32];
 #pragma unroll
-      for (int j = 0; j < kCols / 32; ++j) {
-        const int col = strip * kCols + 32 * j + lane;
-        if (col < p.cols) acc[j] += load_one(p.g, DT, r * p.ld + col);
+    for (int j = 0; j < kCols / 32; ++j) col[j] = min(strip * kCols + 32 * j + lane, p.cols - 1);
+    const char* g = static_cast<const char*>(p.g);
+    const int64_t pitch = p.ld * kEs;
+    for (int64_t r = first + warp; r < end; r += kWarps * kRest) {
+      const int left = (int)min((end - 1 - r) / kWarps, (int64_t)kRest - 1);
+      float x[kRest][kCols / 32];
+#pragma unroll
+      for (int k = 0; k < kRest; ++k) {
+        const char* row = g + (r + kWarps * min(k, left)) * pitch;
+#pragma unroll
+        for (int j = 0; j < kCols / 32; ++j) x[k][j] = load_one(row, DT, col[j]);
+      }
+#pragma unroll
+      for (int k = 0; k < kRest; ++k) {
+#pragma unroll
+        for (int j = 0; j < kCols / 32; ++j) acc[j] += k <= left ? x[k][j] : 0.f;
       }
     }
 #pragma unroll
