@@ -37,8 +37,8 @@ __device__ __forceinline__ void add_halves(uint32_t w, float& a, float& b) {
   if (BF16) asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}" : "+f"(a), "+f"(b) : "r"(w));
   else asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.f16 %0, l, %0;\n\tadd.rn.f32.f16 %1, h, %1;\n\t}" : "+f"(a), "+f"(b) : "r"(w));
 }
-// Two FP8 codes as F16 numbers; a code of E5M2 is the upper half of one.  (The additions that widen, and E5M2 codes put in their places instead of converted, take an
-// 8192 x (4096 + 1024) E5M2 block from 12.2 to 11.4 us: beside the bytes, 6.5 us, it is bound by one addition and half a permutation per element.)
+// Two FP8 codes as F16 numbers; a code of E5M2 is the upper half of one.  (The additions that widen, and E5M2 codes put in their places instead of converted, took an
+// 8192 x (4096 + 1024) E5M2 block from 12.2 to 11.4 us: beside the bytes it costs one addition and half a permutation per element.)
 template <int DT, int HIGH>
 __device__ __forceinline__ uint32_t fp8_halves(uint32_t w) {
   if (DT == US_E5M2) return __byte_perm(w, 0u, HIGH ? 0x3424 : 0x1404);
@@ -61,6 +61,14 @@ __device__ __forceinline__ void add16(const uint4& t, float* acc) {
       add_halves<false>(fp8_halves<DT, 1>(w[j]), acc[4 * j + 2], acc[4 * j + 3]);
     }
   }
+}
+
+// 16 bytes, or zeros; a predicated load (of a conditional one the compiler makes a branch, which keeps the next load waiting).
+__device__ __forceinline__ uint4 load16_if(bool there, const void* at) {
+  uint4 t;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+               "@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}" : "=&r"(t.x), "=&r"(t.y), "=&r"(t.z), "=&r"(t.w) : "l"(at), "r"((int)there));
+  return t;
 }
 
 // Sums of a strip's columns over rows first .. end - 1, one line of `sums` (kStripBytes / element size columns) per warp.
@@ -88,7 +96,7 @@ __device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t
       for (; r < whole; r += kStep * kRest) {                  // (of rows that are not there, zeros)
         uint4 t[kRest];
 #pragma unroll
-        for (int k = 0; k < kRest; ++k) t[k] = r + kStep * k < whole ? *reinterpret_cast<const uint4*>(g + (r + kStep * k) * pitch) : make_uint4(0u, 0u, 0u, 0u);
+        for (int k = 0; k < kRest; ++k) t[k] = load16_if(r + kStep * k < whole, g + (r + kStep * k) * pitch);
 #pragma unroll
         for (int k = 0; k < kRest; ++k) add16<DT>(t[k], acc);
       }
@@ -136,7 +144,8 @@ __device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t
   }
 }
 
-__global__ void __launch_bounds__(kThreads) bias_grad_kernel(const __grid_constant__ BiasArgs a) {
+// (Registers for three CTAs an SM: with four the loads in flight do not fit, 8192 x (4096 + 1024) E5M2 9.7 us in the place of 8.0; with two 10.9.)
+__global__ void __launch_bounds__(kThreads, 3) bias_grad_kernel(const __grid_constant__ BiasArgs a) {
   __shared__ float sums[kWarps][kStripBytes];
   __shared__ float mine[kStripBytes];
   ptx::grid_sync_previous();
@@ -195,6 +204,7 @@ extern "C" us_status us_bias_grad(int count, const us_mat* G, const float* beta,
   if (count < 1 || count > kMostParts || !G || !db) return US_ERR_INVALID_ARG;
   BiasArgs a{};
   int64_t strips = 0, rows = 0;
+  bool wide = true;
   for (int k = 0; k < count; ++k) {
     const us_status s = check(G[k], db[k]);
     if (s != US_OK) return s;
@@ -207,13 +217,16 @@ extern "C" us_status us_bias_grad(int count, const us_mat* G, const float* beta,
     if (strips * 8 >= (1ll << 31)) return US_ERR_UNSUPPORTED;
     p.strip_end = (int)strips;
     rows = std::max(rows, G[k].rows);
+    wide = wide && p.wide;
   }
   if (strips == 0) return US_OK;
   a.count = count;
-  // Some two CTAs an SM, of at least 128 rows each: more of them, or the cluster's barriers for few rows, cost more than they share.
+  // At most the three CTAs an SM that run at once, of at least 128 rows each, and no cluster for up to 1024 rows: more of them, or the cluster's launch and barriers, cost more
+  // than they share (us, E5M2: 1024 x (4096 + 1024) 3.6 alone, 4.1 shared by two; 1500 x (512 + 128) 4.3 alone, 3.5 by eight).  Powers of two: 8192 x (4096 + 1024) BF16 takes
+  // 15.7 with clusters of four and 18.5 with five.  Rows that are not aligned, which take longer, are shared from 129 on, 64 at least for each.
   const int sms = host::sm_count();
   if (sms <= 0) return US_ERR_CUDA;
   int parts = 1;
-  while (parts < 8 && rows > 512 && strips * parts < 2 * sms && rows >= 256 * parts) parts *= 2;
+  while (parts < 8 && rows > (wide ? 1024 : 128) && strips * parts * 2 <= (wide ? 3 : 4) * sms && rows >= (wide ? 256 : 128) * parts) parts *= 2;
   return host::launch(bias_grad_kernel, nullptr, (int)strips * parts, kThreads, 0, parts, static_cast<cudaStream_t>(stream), a);
 }
