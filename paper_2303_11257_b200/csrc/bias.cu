@@ -116,25 +116,26 @@ __device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t
       for (int i = 0; i < kChunk; ++i) sums[warp][chunk * kChunk + i] = acc[i];
     }
   } else {
-    // A lane has every 32nd column of every 8th row, kRest of them at a time (behind the last row, that one and not added); lanes behind the last column have that
+    // A lane has every 32nd column of every 8th row, kRows of them at a time (behind the last row, that one and not added); lanes behind the last column have that
     // one's too.
+    constexpr int kRows = kEs == 1 ? 8 : 16;
     float acc[kCols / 32] = {};
     int col[kCols / 32];
 #pragma unroll
     for (int j = 0; j < kCols / 32; ++j) col[j] = min(strip * kCols + 32 * j + lane, p.cols - 1);
     const char* g = static_cast<const char*>(p.g);
     const int64_t pitch = p.ld * kEs;
-    for (int64_t r = first + warp; r < end; r += kWarps * kRest) {
-      const int left = (int)min((end - 1 - r) / kWarps, (int64_t)kRest - 1);
-      float x[kRest][kCols / 32];
+    for (int64_t r = first + warp; r < end; r += kWarps * kRows) {
+      const int left = (int)min((end - 1 - r) / kWarps, (int64_t)kRows - 1);
+      float x[kRows][kCols / 32];
 #pragma unroll
-      for (int k = 0; k < kRest; ++k) {
+      for (int k = 0; k < kRows; ++k) {
         const char* row = g + (r + kWarps * min(k, left)) * pitch;
 #pragma unroll
         for (int j = 0; j < kCols / 32; ++j) x[k][j] = load_one(row, DT, col[j]);
       }
 #pragma unroll
-      for (int k = 0; k < kRest; ++k) {
+      for (int k = 0; k < kRows; ++k) {
 #pragma unroll
         for (int j = 0; j < kCols / 32; ++j) acc[j] += k <= left ? x[k][j] : 0.f;
       }
