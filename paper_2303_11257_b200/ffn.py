@@ -445,10 +445,6 @@ class UnitScaledBiasFFN(UnitScaledFFN):
         yield from self.plan_gemms(p, "X", "G")
 
     def plan_gemms(self, p, X, G):
-        if not self.fused_hidden:
-            yield from self.plan_forward(p, X, cast_x=False)
-            yield from self.plan_backward(p, G, cast_g=False)
-            return
         sc = self.sc
         yield L.Call("us_ffn_hidden_bias", p.mat(self.Xq), p.mat(self.W1q), sc.alpha1, p.mat(self.b1.view(1, -1)), p.mat(self.Gq), p.mat(self.W2q), sc.beta_x2,
                      sc.s_in, sc.alpha_g, sc.beta_g, L._TORCH_DTYPES[self.H.dtype], p.mat(self.H) if self._writes_h() else None,
@@ -479,7 +475,7 @@ class UnitScaledBiasFFN(UnitScaledFFN):
     @property
     def gemm_launches(self) -> int:
         """Launches of a step without its casts: the hidden layer's, the biases' gradients and the grouped launch (two where it shares contractions)."""
-        return 2 + self._group_launches(forward=True) if self.fused_hidden else 4 + self._group_launches(forward=False)
+        return 2 + self._group_launches(forward=True)
 
     @property
     def launches_per_step(self) -> int:

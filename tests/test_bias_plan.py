@@ -34,14 +34,6 @@ def test_calls_of_a_step(monkeypatch, operand):
     assert rec.names() == [cast] + apart[:2] + [cast] + apart[2:] + apart[2:]
 
 
-def test_a_step_whose_pre_activation_has_32_bits(monkeypatch):
-    block, x = _ffn(operand="bf16", h_dtype=torch.float32)
-    rec = _Recorder()
-    monkeypatch.setattr(L, "_lib", rec)
-    block.step(*x, stream=0)
-    assert rec.names() == ["cast_multi", "linear_fwd_bias", "linear_fwd_bias", "linear_bwd_x", "bias_grad", "linear_group_any"]
-
-
 def test_a_refused_group_adds_the_bias_in_single_launches(monkeypatch):
     class Refuses(_Recorder):
         def __getattr__(self, name):

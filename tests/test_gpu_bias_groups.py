@@ -87,3 +87,16 @@ def test_group(form, act, grad, out, bias):
         single = outs()[0]
         L.us_linear_fwd_bias(Aq, W2, f ** -0.5, B, single, ws, ep)
         assert torch.equal(_bits(got[0]), _bits(single))
+
+
+def test_a_refused_group_adds_its_biases_in_single_launches():
+    """More tiles than the work list holds: the prepared group goes out as single launches."""
+    from paper_2303_11257_b200 import lib as L, synth
+    n, k, ws = 46 * 256, 16, L.new_workspace()
+    X, W, B = U.to_device(synth.normal(60, 0, (n, k)), "e4m3"), U.to_device(synth.normal(60, 1, (k, n)), "e4m3"), torch.from_numpy(synth.normal(60, 2, (1, n))).cuda()[0]
+    Y, Y1 = U.empty(n, n, "bf16"), U.empty(n, n, "bf16")
+    call = L.Plan((), ()).group([(L.US_OP_FWD, X, W, 0.25, Y, Y, (0.0, 1.0))], ws, biases={0: B})
+    call(L.current_stream())
+    assert call.refused
+    L.us_linear_fwd_bias(X, W, 0.25, B, Y1, ws)
+    assert L.us_workspace_status(ws) == 0 and torch.equal(Y.view(torch.int16), Y1.view(torch.int16))
