@@ -58,10 +58,10 @@ struct Args {
   int used = 0, numbers_used = 0;
   bool immediate;                                            // tensors are taken only by calls that are not kept
   explicit Args(bool now) : immediate(now) {}
-  us_mat* add(PyObject* tensor) {
+  us_mat* add(PyObject* tensor, bool vector) {
     if (!immediate) fail(PyExc_TypeError, "a prepared call takes structures");
     if (used == 32) fail(PyExc_ValueError, "too many tensors");
-    mats[used] = describe(tensor);
+    mats[used] = describe(tensor, vector);
     return &mats[used++];
   }
   // `count` matrices given as a list or tuple of tensors (1-D ones are rows) and Nones
@@ -122,8 +122,8 @@ T* structure(PyObject* o, size_t count) {
 template <class T>
 constexpr bool kAddress = std::is_same_v<T, void*> || std::is_same_v<T, float*> || std::is_same_v<T, const float*> || std::is_same_v<T, const int32_t*> || std::is_same_v<T, int64_t*>;
 
-// ARRAY: a pointer to `count` elements in host memory.
-template <class T, bool ARRAY>
+// ARRAY: a pointer to `count` elements in host memory.  ROW: a 1-D tensor is taken as one row.
+template <class T, bool ARRAY, bool ROW>
 T convert(PyObject* o, Args& a, size_t count) {
   if constexpr (std::is_floating_point_v<T>) {
     const double v = PyFloat_AsDouble(o);
@@ -138,7 +138,7 @@ T convert(PyObject* o, Args& a, size_t count) {
       }
     }
     if constexpr (std::is_same_v<T, const us_mat*>) {
-      if (THPVariable_Check(o) && count <= 1) return a.add(o);
+      if (THPVariable_Check(o) && count <= 1) return a.add(o, ROW);
     }
     if constexpr (kAddress<T> && !ARRAY) {
       if (THPVariable_Check(o)) {
@@ -181,8 +181,8 @@ struct Prepared {
   virtual int run(void* stream) = 0;
 };
 
-// ARRAYS: parameters 1 .. ARRAYS are arrays of as many elements as parameter 0 says.
-template <size_t ARRAYS, class... A>
+// ARRAYS: parameters 1 .. ARRAYS are arrays of as many elements as parameter 0 says.  ROW: the parameter (0: none) that may be a vector.
+template <size_t ARRAYS, size_t ROW, class... A>
 struct Entry {
   using Fn = us_status (*)(A...);
   static constexpr size_t kArgs = sizeof...(A);
@@ -198,7 +198,7 @@ struct Entry {
     // a workspace is given twice, for its address and for its size, which one number cannot be
     for (size_t i = 0; a.immediate && i + 1 < kArgs; ++i)
       if (o[i] == o[i + 1] && kSize[i + 1] && !THPVariable_Check(o[i])) fail(PyExc_TypeError, "a workspace is a tensor");
-    return Tuple{convert<A, (I >= 1 && I <= ARRAYS)>(o[I], a, I >= 1 && I <= ARRAYS ? count : 1)...};      // braces: left to right
+    return Tuple{convert<A, (I >= 1 && I <= ARRAYS), (I > 0 && I == ROW)>(o[I], a, I >= 1 && I <= ARRAYS ? count : 1)...};      // braces: left to right
   }
   static constexpr bool kSize[] = {std::is_same_v<A, size_t>...};
   struct Kept : Prepared {
@@ -232,17 +232,18 @@ struct Entry {
     return k.release();
   }
 };
-template <size_t ARRAYS, class... A>
-Entry<ARRAYS, A...> entry_of(us_status (*)(A...));
+template <size_t ARRAYS, size_t ROW, class... A>
+Entry<ARRAYS, ROW, A...> entry_of(us_status (*)(A...));
 
 using Keep = Prepared* (*)(PyObject* const*, Py_ssize_t);
 struct Known { const char* name; PyCFunction now; Keep keep; };
 
-template <auto F, size_t ARRAYS>
-PyObject* now(PyObject*, PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS>(F))::now(F, o, n); }
-template <auto F, size_t ARRAYS>
-Prepared* keep(PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS>(F))::keep(F, o, n); }
-#define US_ARRAYS(f, n) {#f, (PyCFunction)(void (*)(void))now<f, n>, keep<f, n>}
+template <auto F, size_t ARRAYS, size_t ROW>
+PyObject* now(PyObject*, PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS, ROW>(F))::now(F, o, n); }
+template <auto F, size_t ARRAYS, size_t ROW>
+Prepared* keep(PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS, ROW>(F))::keep(F, o, n); }
+#define US_ENTRY(f, n, row) {#f, (PyCFunction)(void (*)(void))now<f, n, row>, keep<f, n, row>}
+#define US_ARRAYS(f, n) US_ENTRY(f, n, 0)
 #define US_CALL(f) US_ARRAYS(f, 0)
 const Known kKnown[] = {
     US_CALL(us_linear_fwd), US_CALL(us_linear_bwd_x), US_CALL(us_linear_bwd_w), US_CALL(us_linear_fwd_batched), US_CALL(us_linear_bwd_x_batched),
@@ -252,8 +253,8 @@ const Known kKnown[] = {
     US_CALL(us_activation_bwd), US_ARRAYS(us_weighted_add, 2), US_CALL(us_softmax_fwd), US_CALL(us_softmax_bwd), US_CALL(us_softmax_xent_fwd),
     US_CALL(us_softmax_xent_bwd), US_CALL(us_layer_norm_fwd), US_CALL(us_layer_norm_bwd), US_CALL(us_linear_fwd_cast), US_ARRAYS(us_linear_group_cast, 2),
     US_CALL(us_layer_norm_fwd_cast), US_CALL(us_layer_norm_bwd_cast), US_ARRAYS(us_qk_norm_fwd, 3), US_ARRAYS(us_qk_norm_bwd, 6), US_CALL(us_rotary_table),
-    US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd), US_ARRAYS(us_bias_grad, 3), US_ARRAYS(us_grad_norm, 1), US_ARRAYS(us_adamw, 1), US_CALL(us_linear_fwd_bias),
-    US_CALL(us_ffn_hidden_bias), US_ARRAYS(us_linear_group_bias, 2),
+    US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd), US_ARRAYS(us_bias_grad, 3), US_ARRAYS(us_grad_norm, 1), US_ARRAYS(us_adamw, 1), US_ENTRY(us_linear_fwd_bias, 0, 3),
+    US_ENTRY(us_ffn_hidden_bias, 0, 3), US_ARRAYS(us_linear_group_bias, 2),
 };
 constexpr size_t kCount = sizeof(kKnown) / sizeof(kKnown[0]);
 PyMethodDef g_calls[kCount];

@@ -485,7 +485,7 @@ def us_linear_fwd(X, W, alpha, Y, ws, ep=None, stream=None):
 def us_linear_fwd_bias(X, W, alpha, bias, Y, ws, ep=None, Yq=None, stream=None):
     """us_linear_fwd of a layer with a bias (a vector), which is added to the scaled product; Yq: an FP8 copy of a residual's result."""
     _here(Y)
-    _check("us_linear_fwd_bias", _entry("us_linear_fwd_bias")(X, W, alpha, bias.view(1, -1) if bias.dim() == 1 else bias, ep, Y, Yq, ws, ws, _stream(stream)))
+    _check("us_linear_fwd_bias", _entry("us_linear_fwd_bias")(X, W, alpha, bias, ep, Y, Yq, ws, ws, _stream(stream)))
     return Y
 
 
@@ -682,7 +682,7 @@ def us_ffn_hidden_bias(X, W1, alpha, bias, G, W2, beta_x, act_in_scale, act_out_
                        H=None, h_dtype=torch.bfloat16, stream=None):
     """us_ffn_hidden_any of a first layer with a bias (a vector)."""
     _here(A)
-    _check("us_ffn_hidden_bias", _entry("us_ffn_hidden_bias")(X, W1, alpha, bias.view(1, -1) if bias.dim() == 1 else bias, G, W2, beta_x, act_in_scale, act_out_scale,
+    _check("us_ffn_hidden_bias", _entry("us_ffn_hidden_bias")(X, W1, alpha, bias, G, W2, beta_x, act_in_scale, act_out_scale,
                                                               grad_out_scale, _TORCH_DTYPES[h_dtype], H, A, dH, ws, ws, _stream(stream)))
     return A, dH
 
@@ -941,16 +941,17 @@ def _current_device() -> int:
 
 def _here(t: torch.Tensor) -> None:
     """A launch goes to the current device, whose own tensors it takes."""
-    if t.is_cuda and t.device.index != _current_device():
-        raise ValueError(f"a tensor of {t.device} in a call on cuda:{_current_device()}")
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        raise ValueError(f"a tensor of {t.device}, which is not the current CUDA device")
 
 
 def us_bias_grad(G, beta, db, stream=None):
     """db[i] = beta[i] * the column sums of G[i], in one launch: lists of matrices, factors (or None: ones) and bias gradients."""
-    for t in db:
-        _here(t)
     if len(db) != len(G) or (beta is not None and len(beta) != len(G)):
         raise ValueError("one entry per matrix is wanted")
+    for t in db:
+        _here(t)
     _check("us_bias_grad", _entry("us_bias_grad")(len(G), G, beta, db, _stream(stream)))
     return db
 

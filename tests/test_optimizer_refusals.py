@@ -99,6 +99,10 @@ def test_python_side():
         L.adamw_tensors([t], [t], [t], [t])                       # host memory
     with pytest.raises(ValueError):
         L.us_bias_grad([t], [1.0], [])
+    with pytest.raises(ValueError):
+        L.us_bias_grad([t.view(1, 4)], [1.0], [t])
+    with pytest.raises(ValueError):
+        L.us_linear_fwd_bias(t.view(1, 4), t.view(4, 1), 1.0, t[:1], t[:1].view(1, 1), t)
     with pytest.raises(AssertionError):
         L.us_adamw(None, torch.zeros(2, dtype=torch.int64), 1e-3)
     with pytest.raises(AssertionError):
