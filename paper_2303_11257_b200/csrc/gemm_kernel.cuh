@@ -558,7 +558,15 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
 #pragma unroll
               for (int k = 0; k < 16; ++k) gelu_scaled2<false>(pack2(y[2 * k], y[2 * k + 1]), tail_k, act_oi, y[2 * k], y[2 * k + 1]);
             }
-          } else {                                              // relu, tanh, sigmoid (table section "Activations")
+          } else if constexpr (BIAS) {                          // relu, tanh, sigmoid (table section "Activations"), this choice too once per slice
+            auto all = [&](auto fn) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) y[k] = act_scaled(decltype(fn)::value, y[k], p.act_in, p.act_out);
+            };
+            if (p.fn == US_FN_RELU) all(std::integral_constant<int, US_FN_RELU>());
+            else if (p.fn == US_FN_TANH) all(std::integral_constant<int, US_FN_TANH>());
+            else all(std::integral_constant<int, US_FN_SIGMOID>());
+          } else {
 #pragma unroll
             for (int k = 0; k < 32; ++k) y[k] = act_scaled(p.fn, y[k], p.act_in, p.act_out);
           }
