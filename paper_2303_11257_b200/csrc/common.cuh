@@ -267,6 +267,29 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
   return r;
 }
 
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Two values at a time (packed float32 arithmetic): x holds pre-activations, in2 = splat(act_in), nl2 = splat(-act_in log2 e).
+// sigmoid(act_in x) = 1 / (1 + e^-z): relative error of a few 2^-22 and |z| 2^-23, far inside a step of the 16 and 8 bits that results are rounded to.
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 x, f32x2 nl2) {
+  float p0, p1;
+  unpack2(mul2(x, nl2), p0, p1);
+  unpack2(add2(pack2(ex2_approx(p0), ex2_approx(p1)), splat2(1.0f)), p0, p1);
+  return pack2(rcp_approx(p0), rcp_approx(p1));
+}
+// tanh(z) = 2 s - 1 with s = sigmoid(2 z), which cancels near zero: there z - z^3 / 3 + 2 z^5 / 15, whose next term is 2^-22 of it at 1/8.
+__device__ __forceinline__ f32x2 tanh2(f32x2 z, f32x2 s) {
+  float z0, z1, f0, f1, n0, n1;
+  const f32x2 zz = mul2(z, z);
+  unpack2(mul2(z, fma2(zz, fma2(zz, splat2(2.0f / 15.0f), splat2(-1.0f / 3.0f)), splat2(1.0f))), n0, n1);
+  unpack2(fma2(s, splat2(2.0f), splat2(-1.0f)), f0, f1);
+  unpack2(z, z0, z1);
+  return pack2(fabsf(z0) < 0.125f ? n0 : f0, fabsf(z1) < 0.125f ? n1 : f1);
+}
+
 // q for two arguments given t = min(|z| / 7.5, 1) of each (see normal_tail).
 __device__ __forceinline__ void normal_tail2(float t0, float t1, float& q0, float& q1) {
   const f32x2 t = pack2(t0, t1);

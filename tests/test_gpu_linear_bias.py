@@ -204,3 +204,27 @@ def test_captured_with_a_bias_that_changes():
     for i in range(1, 5):
         graph.replay()
         assert float((before - 0.25 * i - Y).abs().max()) < 1e-4, i
+
+
+@pytest.mark.parametrize("rows,n", [(3, 2049), (300, 2049)])
+@pytest.mark.parametrize("act", ["relu", "tanh", "sigmoid"])
+@pytest.mark.parametrize("skip", [False, True])
+def test_activations_over_their_range(rows, n, act, skip):
+    """Products of zero, so that the activation's argument is in_scale * bias: from -100 to 100, small ones, infinities and NaN.  Sigmoid: e^-z errs by 2^-22 and, as z log2 e is
+    rounded, by |z| 2^-23 log2 e, the reciprocal by 2^-23, sum and factor by 2^-24 each.  Tanh is 2 s - 1, absolute, from 1/8 on, and below that a series whose next term
+    is 2^-22 of it, with four roundings."""
+    L = _lib()
+    z = torch.cat([torch.linspace(-100, 100, n // 2), 0.13 * torch.linspace(-1, 1, n - n // 2 - 8), torch.tensor([0.0, -0.0, 1e-20, -1e-20, 0.125, float("inf"), float("-inf"), float("nan")])])
+    X, W = torch.zeros((rows, 64), device="cuda").bfloat16(), torch.zeros((64, PAD(n)), device="cuda").bfloat16()[:, :n]
+    Y, S = U.empty(rows, n, "f32", PAD(n)), torch.zeros((rows, PAD(n)), device="cuda")[:, :n]
+    code = {"relu": L.US_ACT_RELU, "tanh": L.US_ACT_TANH, "sigmoid": L.US_ACT_SIGMOID}[act]
+    ep = L.epilogue(act=code, act_in_scale=0.5, act_out_scale=1.5, skip=S if skip else None, skip_coef=0.5 if skip else 0.0, out_coef=1.0)
+    _call(n, Y, L, X, W, 1.0, (2.0 * z).cuda(), Y, ep=ep)
+    ref, zz = 1.5 * _act(act, z.double()), z.double().abs()
+    got = Y[-1].cpu().double()
+    assert bool((Y == Y[0]).logical_or(Y.isnan()).all()) and bool(got[-1].isnan()) and bool(got[:-1].isfinite().all()) == (act != "relu")
+    tol = {"relu": 2.0 ** -23 * ref.abs(), "sigmoid": (2.0 ** -20 + zz * 2.0 ** -22) * ref.abs() + 2.0 ** -125,
+           "tanh": torch.where(zz < 0.125, 2.0 ** -21 * ref.abs(), 2.0 ** -19 * torch.ones_like(zz))}[act]
+    keep = torch.isfinite(z)
+    assert bool(((got - ref).abs() <= tol)[keep].all()), float(((got - ref).abs() / tol)[keep].nan_to_num().max())
+    assert torch.equal(got[[-3, -2]], ref[[-3, -2]])
