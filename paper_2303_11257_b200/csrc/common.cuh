@@ -272,8 +272,8 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// Two values at a time (packed float32 arithmetic): x holds pre-activations, in2 = splat(act_in), nl2 = splat(-act_in log2 e).
-// sigmoid(act_in x) = 1 / (1 + e^-z): relative error of a few 2^-22 and |z| 2^-23, far inside a step of the 16 and 8 bits that results are rounded to.
+// Two values at a time: x holds pre-activations, nl2 = splat(-act_in log2 e).
+// sigmoid(act_in x) = 1 / (1 + e^-z): relative error of a few 2^-22 and |z| 2^-23, far inside a step of 16 and 8 bits; results in 32 bits have it.
 __device__ __forceinline__ f32x2 sigmoid2(f32x2 x, f32x2 nl2) {
   float p0, p1;
   unpack2(mul2(x, nl2), p0, p1);
