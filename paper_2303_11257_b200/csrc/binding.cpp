@@ -57,10 +57,20 @@ struct Args {
   float numbers[16];
   int used = 0, numbers_used = 0;
   bool immediate;                                            // tensors are taken only by calls that are not kept
-  explicit Args(bool now) : immediate(now) {}
+  bool one_device;                                           // all of them have to be CUDA tensors of one device,
+  int device = -1;                                           // this one
+  Args(bool now, bool one) : immediate(now), one_device(one) {}
+  void check(PyObject* tensor) {
+    if (!one_device) return;
+    const at::Tensor& t = THPVariable_Unpack(tensor);
+    if (!t.is_cuda()) fail(PyExc_ValueError, "expected CUDA tensors");
+    if (device >= 0 && t.get_device() != device) fail(PyExc_ValueError, "expected tensors of one device");
+    device = (int)t.get_device();
+  }
   us_mat* add(PyObject* tensor, bool vector) {
     if (!immediate) fail(PyExc_TypeError, "a prepared call takes structures");
     if (used == 32) fail(PyExc_ValueError, "too many tensors");
+    check(tensor);
     mats[used] = describe(tensor, vector);
     return &mats[used++];
   }
@@ -74,6 +84,7 @@ struct Args {
     for (size_t i = 0; i < n; ++i) {
       PyObject* o = PySequence_Fast_GET_ITEM(list, (Py_ssize_t)i);
       if (o != Py_None && !THPVariable_Check(o)) fail(PyExc_TypeError, "expected tensors");
+      if (o != Py_None) check(o);
       mats[used++] = o == Py_None ? us_mat{} : describe(o, true);
     }
     return first;
@@ -143,6 +154,7 @@ T convert(PyObject* o, Args& a, size_t count) {
     if constexpr (kAddress<T> && !ARRAY) {
       if (THPVariable_Check(o)) {
         if (!a.immediate) fail(PyExc_TypeError, "a prepared call takes addresses");
+        a.check(o);
         return (T)THPVariable_Unpack(o).data_ptr();
       }
       if (!PyLong_Check(o)) fail(PyExc_TypeError, "expected a tensor, an address or None");
@@ -181,8 +193,9 @@ struct Prepared {
   virtual int run(void* stream) = 0;
 };
 
-// ARRAYS: parameters 1 .. ARRAYS are arrays of as many elements as parameter 0 says.  ROW: the parameter (0: none) that may be a vector.
-template <size_t ARRAYS, size_t ROW, class... A>
+// ARRAYS: parameters 1 .. ARRAYS are arrays of as many elements as parameter 0 says.  ROW: the parameter (0: none) that may be a vector.  ONE_DEVICE: a
+// tensor in host memory or of another device than the others is refused.
+template <size_t ARRAYS, size_t ROW, bool ONE_DEVICE, class... A>
 struct Entry {
   using Fn = us_status (*)(A...);
   static constexpr size_t kArgs = sizeof...(A);
@@ -212,7 +225,7 @@ struct Entry {
   static PyObject* now(Fn fn, PyObject* const* o, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
       if ((size_t)n != kArgs) fail(PyExc_TypeError, "wrong number of arguments");
-      Args a(true);
+      Args a(true, ONE_DEVICE);
       Tuple t = read(o, a, std::make_index_sequence<kArgs>());
       int status;
       Py_BEGIN_ALLOW_THREADS
@@ -225,25 +238,26 @@ struct Entry {
     if ((size_t)n + 1 != kArgs) fail(PyExc_TypeError, "wrong number of arguments");
     std::vector<PyObject*> all(o, o + n);
     all.push_back(Py_None);
-    Args a(false);
+    Args a(false, false);
     auto k = std::make_unique<Kept>();
     k->fn = fn;
     k->t = read(all.data(), a, std::make_index_sequence<kArgs>());
     return k.release();
   }
 };
-template <size_t ARRAYS, size_t ROW, class... A>
-Entry<ARRAYS, ROW, A...> entry_of(us_status (*)(A...));
+template <size_t ARRAYS, size_t ROW, bool ONE_DEVICE, class... A>
+Entry<ARRAYS, ROW, ONE_DEVICE, A...> entry_of(us_status (*)(A...));
 
 using Keep = Prepared* (*)(PyObject* const*, Py_ssize_t);
 struct Known { const char* name; PyCFunction now; Keep keep; };
 
-template <auto F, size_t ARRAYS, size_t ROW>
-PyObject* now(PyObject*, PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS, ROW>(F))::now(F, o, n); }
-template <auto F, size_t ARRAYS, size_t ROW>
-Prepared* keep(PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS, ROW>(F))::keep(F, o, n); }
-#define US_ENTRY(f, n, row) {#f, (PyCFunction)(void (*)(void))now<f, n, row>, keep<f, n, row>}
-#define US_ARRAYS(f, n) US_ENTRY(f, n, 0)
+template <auto F, size_t ARRAYS, size_t ROW, bool ONE_DEVICE>
+PyObject* now(PyObject*, PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS, ROW, ONE_DEVICE>(F))::now(F, o, n); }
+template <auto F, size_t ARRAYS, size_t ROW, bool ONE_DEVICE>
+Prepared* keep(PyObject* const* o, Py_ssize_t n) { return decltype(entry_of<ARRAYS, ROW, ONE_DEVICE>(F))::keep(F, o, n); }
+#define US_ENTRY(f, n, row, one) {#f, (PyCFunction)(void (*)(void))now<f, n, row, one>, keep<f, n, row, one>}
+#define US_ARRAYS(f, n) US_ENTRY(f, n, 0, false)
+#define US_CHECKED(f, n, row) US_ENTRY(f, n, row, true)
 #define US_CALL(f) US_ARRAYS(f, 0)
 const Known kKnown[] = {
     US_CALL(us_linear_fwd), US_CALL(us_linear_bwd_x), US_CALL(us_linear_bwd_w), US_CALL(us_linear_fwd_batched), US_CALL(us_linear_bwd_x_batched),
@@ -253,8 +267,8 @@ const Known kKnown[] = {
     US_CALL(us_activation_bwd), US_ARRAYS(us_weighted_add, 2), US_CALL(us_softmax_fwd), US_CALL(us_softmax_bwd), US_CALL(us_softmax_xent_fwd),
     US_CALL(us_softmax_xent_bwd), US_CALL(us_layer_norm_fwd), US_CALL(us_layer_norm_bwd), US_CALL(us_linear_fwd_cast), US_ARRAYS(us_linear_group_cast, 2),
     US_CALL(us_layer_norm_fwd_cast), US_CALL(us_layer_norm_bwd_cast), US_ARRAYS(us_qk_norm_fwd, 3), US_ARRAYS(us_qk_norm_bwd, 6), US_CALL(us_rotary_table),
-    US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd), US_ARRAYS(us_bias_grad, 3), US_ARRAYS(us_grad_norm, 1), US_ARRAYS(us_adamw, 1), US_ENTRY(us_linear_fwd_bias, 0, 3),
-    US_ENTRY(us_ffn_hidden_bias, 0, 3), US_ARRAYS(us_linear_group_bias, 2),
+    US_CALL(us_ffn_gated_fwd), US_CALL(us_ffn_gated_bwd), US_CHECKED(us_bias_grad, 3, 0), US_CHECKED(us_grad_norm, 1, 0), US_CHECKED(us_adamw, 1, 0),
+    US_CHECKED(us_linear_fwd_bias, 0, 3), US_CHECKED(us_ffn_hidden_bias, 0, 3), US_CHECKED(us_linear_group_bias, 2, 0),
 };
 constexpr size_t kCount = sizeof(kKnown) / sizeof(kKnown[0]);
 PyMethodDef g_calls[kCount];
@@ -393,25 +407,23 @@ PyObject* unchanged(PyObject*, PyObject* const* o, Py_ssize_t n) {
   });
 }
 
-// fill(address, stride, tensors): descriptions of the tensors of a list (1-D ones are rows, None: nothing is written), `stride` bytes apart.
+// fill(address, stride, tensors): descriptions of the tensors of a list (1-D ones are rows, None: nothing is written), `stride` bytes apart; the tensors' device, or -1
+// where there are none.
 PyObject* fill(PyObject*, PyObject* const* o, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     if (n != 3 || !PyList_Check(o[2])) fail(PyExc_TypeError, "fill(address, stride, list)");
     char* at = static_cast<char*>(PyLong_AsVoidPtr(o[0]));
     const size_t stride = PyLong_AsSize_t(o[1]);
     if (PyErr_Occurred()) throw Failed();
-    int device = -1;
+    Args a(true, true);
     for (Py_ssize_t i = 0; i < PyList_GET_SIZE(o[2]); ++i, at += stride) {
       PyObject* t = PyList_GET_ITEM(o[2], i);
       if (t == Py_None) continue;
       if (!THPVariable_Check(t)) fail(PyExc_TypeError, "expected tensors");
-      const at::Tensor& tensor = THPVariable_Unpack(t);
-      if (!tensor.is_cuda()) fail(PyExc_ValueError, "expected CUDA tensors");
-      if (device >= 0 && tensor.get_device() != device) fail(PyExc_ValueError, "expected tensors of one device");
-      device = (int)tensor.get_device();
+      a.check(t);
       *reinterpret_cast<us_mat*>(at) = describe(t, true);
     }
-    Py_RETURN_NONE;
+    return PyLong_FromLong(a.device);
   });
 }
 

@@ -525,6 +525,9 @@ def us_linear_group_bias(calls, biases, ws, stream=None):
     _here(ws)
     if len(biases) != len(calls):
         raise ValueError("a bias or None for each call")
+    for b in biases:
+        if b is not None:
+            _here(b)
     rows = [us_mat() if b is None else mat(b.view(1, -1) if b.dim() == 1 else b) for b in biases]
     _check("us_linear_group_bias", _entry("us_linear_group_bias")(len(calls), (us_linear_call * len(calls))(*calls), (us_mat * len(calls))(*rows), ws, ws, _stream(stream)))
 
@@ -956,17 +959,29 @@ def us_bias_grad(G, beta, db, stream=None):
     return db
 
 
-def _fill(arr, column: int, tensors) -> None:
-    """Descriptions of CUDA tensors (1-D ones are rows; None: left empty) into the us_mat number `column` of every structure of an array."""
-    _binding.fill(C.addressof(arr) + column * C.sizeof(us_mat), C.sizeof(arr._type_), tensors)
+def _fill(arr, columns) -> None:
+    """Descriptions of CUDA tensors of one device (1-D ones are rows; None: left empty) into the us_mats at the start of every structure of an array, a list for each;
+    the array keeps the tensors, and which device it is (-1: no tensors)."""
+    arr._keep_alive, arr._device = columns, -1
+    for i, tensors in enumerate(columns):
+        device = _binding.fill(C.addressof(arr) + i * C.sizeof(us_mat), C.sizeof(arr._type_), tensors)
+        if device >= 0 and arr._device not in (-1, device):
+            raise ValueError("expected tensors of one device")
+        arr._device = max(arr._device, device)
+
+
+def _laid_out_here(arr, t: torch.Tensor) -> None:
+    """Descriptions that are used with t have to be of its device, the current one."""
+    _here(t)
+    if getattr(arr, "_device", -1) not in (-1, t.get_device()):
+        raise ValueError(f"tensors laid out on device {arr._device}, which is not the current CUDA device")
 
 
 def mats(tensors):
     """An array of us_mat for us_grad_norm, laid out once for tensors that stay where they are; 1-D tensors are rows."""
     tensors = list(tensors)
     arr = (us_mat * len(tensors))()
-    _fill(arr, 0, tensors)
-    arr._keep_alive = tensors
+    _fill(arr, [tensors])
     return arr
 
 
@@ -978,9 +993,9 @@ def us_grad_norm(grads, max_norm, out, ws, stream=None):
     """out (float32 CUDA tensor of two) = 2-norm of all gradients and the factor that clips them to max_norm; grads: a list of tensors, or what
     mats() made of it; ws: a uint8 CUDA tensor of us_grad_norm_workspace_bytes() bytes, zeroed before its first use."""
     assert out.is_cuda and out.dtype is torch.float32 and out.numel() >= 2 and out.is_contiguous()
-    _here(out)
     if not isinstance(grads, C.Array):
         grads = mats(grads)
+    _laid_out_here(grads, out)
     _check("us_grad_norm", _entry("us_grad_norm")(len(grads), grads, max_norm, out, ws, ws, _stream(stream)))
     return out
 
@@ -1001,11 +1016,9 @@ def adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, 
     if len(set(written)) != len(written):
         raise ValueError("a tensor that a step writes is named twice")
     arr = (us_adamw_tensor * n)()
-    for k, c in enumerate(columns):
-        _fill(arr, k, c)
+    _fill(arr, columns)
     for a, *a_numbers in zip(arr, *numbers):
         a.copy_scale, a.lr_factor, a.weight_decay = a_numbers
-    arr._keep_alive = columns
     return arr
 
 
@@ -1018,7 +1031,7 @@ def us_adamw(tensors, step, lr, betas=(0.9, 0.999), eps=1e-8, lr_factor=None, gr
     """One AdamW step over what adamw_tensors() laid out; step: new_adamw_step(); lr_factor, grad_factor: float32 CUDA tensors (one element is read), or None."""
     assert step.is_cuda and step.dtype is torch.int64 and step.numel() == 2 and step.is_contiguous()
     assert all(t is None or (t.is_cuda and t.dtype is torch.float32) for t in (lr_factor, grad_factor))
-    _here(step)
+    _laid_out_here(tensors, step)
     _check("us_adamw", _entry("us_adamw")(len(tensors), tensors, lr, betas[0], betas[1], eps, lr_factor, grad_factor, step, _stream(stream)))
 
 
