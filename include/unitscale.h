@@ -673,7 +673,8 @@ us_status us_grad_norm(int count, const us_mat* grads, float max_norm, float* ou
  * lr_factor, grad_factor: NULL (1), or a float32 in device memory (a schedule; out[1] of us_grad_norm).  Where *grad_factor is not finite the
  * call changes nothing, step included.  A NaN gradient makes NaN of its own element, an infinite one too, and of its block of 8-bit states.
  *
- * lr >= 0, 0 <= beta < 1, eps > 0 (also once rounded to float32).  Arithmetic in float32; 1 - beta and log(beta) are formed in float64.  Pointers
+ * lr >= 0 and finite, 0 <= beta < 1, eps > 0 (also once rounded to float32).  Arithmetic in float32; 1 - beta and log(beta) are formed in float64;
+ * eps sqrt(1 - beta2^t) counts as 2^-126 at least.  v is a float32 too: a sqrt(v) below 2^-63 has fewer digits than 24, and one below 2^-75 is zero.  Pointers
  * need the natural alignment of their elements; F32 tensors on 16-byte boundaries (copies, gradients and codes: of four elements), with rows that are dense
  * or of a multiple of four columns and so padded, are the fast ones.  One launch for up to 240 tensors; tensors without elements are skipped.
  */

@@ -57,12 +57,13 @@ struct AdamArgs {
   AdamTensor t[MOST];
 };
 
-// (Numbers below 2^-126 count as zero in both.)
+// (A v below 2^-126 has a root too, of as many digits as it holds: gradients of 10^-19 and less are stepped by lr as others are.)
 __device__ __forceinline__ float sqrt_approx(float x) {
   float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// (Arguments below 2^-126 count as zero.)
 __device__ __forceinline__ float rcp_approx(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -421,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const
   s.beta1 = a.beta1; s.beta2 = a.beta2; s.root_beta2 = a.root_beta2;
   s.gm = a.rest1 * grad_factor; s.gv = a.root_rest2 * grad_factor;
   s.grad_factor = grad_factor; s.rest1 = a.rest1;
-  s.eps = a.eps * root_fix2;
+  s.eps = fmaxf(a.eps * root_fix2, 0x1p-126f);               // (0 x 1 / 0 where an element has had no gradient)
   s.lr = a.lr * lr_factor;
   s.rate = s.lr * root_fix2 / fix1;
   // (handed round from one lane, the warp's number is known to be the same in all of them: what depends on it alone -- which tensor, where its
@@ -742,7 +743,7 @@ using namespace us;
 extern "C" us_status us_adamw(int count, const us_adamw_tensor* tensors, double lr, double beta1, double beta2, double eps, const float* lr_factor,
                               const float* grad_factor, int64_t* step, void* stream) {
   if (count < 1 || !tensors || !step) return US_ERR_INVALID_ARG;
-  if (!(lr >= 0.0) || !isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps > 0.f) || !isfinite((float)eps)) return US_ERR_INVALID_ARG;
+  if (!(lr >= 0.0) || !isfinite((float)lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps > 0.f) || !isfinite((float)eps)) return US_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(step) % 8 || reinterpret_cast<uintptr_t>(lr_factor) % 4 || reinterpret_cast<uintptr_t>(grad_factor) % 4) return US_ERR_ALIGNMENT;
   for (int i = 0; i < count; ++i) {
     const us_status s = check_tensor(tensors[i]);
