@@ -662,10 +662,19 @@ us_status us_grad_norm(int count, const us_mat* grads, float max_norm, float* ou
  * m and v hold rows * cols elements in row-major order without padding, in any shape, and are alike:
  *   F32    as in the formula (zeros before the first step)
  *   E4M3   states in 8 bits.  Every 256 consecutive elements are a block, the last one shorter, with a scale of its own: m = m_scale * code
- *          and sqrt(v) = v_scale * code.  After a step a block's scale is its largest |m| (sqrt(v)) / 448 and codes are the nearest ones,
- *          but a v above 0 has at least the smallest code, so that no step is divided by eps alone.  A block whose largest |m| or
+ *          and sqrt(v) = v_scale * code.  After a step a block's scale is its largest |m| (sqrt(v)) / 448 and codes are rounded as `rounding`
+ *          says, but a v above 0 has at least the smallest code, so that no step is divided by eps alone.  A block whose largest |m| or
  *          sqrt(v) is at most 2^-100 becomes zeros.  A step is made from the unrounded m and v.  m_scale, v_scale: F32, one element a
  *          block, without padding.  All zeros before the first step.
+ *          US_ROUND_NEAREST  to the nearest code, which is 3 to 6 % off at most.  A state that a step changes by less than that keeps its code:
+ *                            with beta2 above 0.94 the sqrt(v) of an element whose gradients become smaller than its neighbours' does not
+ *                            fall (beta2 = 0.999 takes 0.05 % off it in a step), nor with beta1 above 0.94 its m, and its steps stay too
+ *                            small.  For a training run with such factors, and 0.999 is the usual one, it is the wrong choice.
+ *          US_ROUND_RANDOM   to one of the two codes around it, up with the probability that keeps the mean (m in steps of 2^-12, sqrt(v) in steps
+ *                            of 2^-20), so that states follow their averages however little a step changes them.  sqrt(v) is spread by
+ *                            about 15 % around its average at beta2 = 0.999.  The random bits are made of the number of the step and
+ *                            the element's place in its tensor: the same steps give the same states.
+ *          F32 states take US_ROUND_NEAREST (else US_ERR_UNSUPPORTED); they are not rounded.
  * Tensors of one call may differ in all of this; none may be named twice or overlap another.
  *
  * t = step[0] + 1.  step: two 64-bit integers in device memory, the number of steps made and a zero that the library uses; the call raises
@@ -678,9 +687,11 @@ us_status us_grad_norm(int count, const us_mat* grads, float max_norm, float* ou
  * need the natural alignment of their elements; F32 tensors on 16-byte boundaries (copies, gradients and codes: of four elements), with rows that are dense
  * or of a multiple of four columns and so padded, are the fast ones.  One launch for up to 240 tensors; tensors without elements are skipped.
  */
+typedef enum { US_ROUND_NEAREST = 0, US_ROUND_RANDOM = 1 } us_rounding;
 typedef struct {
   us_mat param, grad, m, v, m_scale, v_scale, copy;
   float copy_scale, lr_factor, weight_decay;
+  int32_t rounding;                          /* us_rounding */
 } us_adamw_tensor;
 us_status us_adamw(int count, const us_adamw_tensor* tensors, double lr, double beta1, double beta2, double eps, const float* lr_factor,
                    const float* grad_factor, int64_t* step, void* stream);

@@ -551,9 +551,30 @@ def adamw_step(p, g, m, v, t, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0
     return AdamWStep(p - decayed - update, m, v, update, decayed, den)
 
 
-def block_codes(x, block: int = 256, positive: bool = False):
+def _mix(x):
+    x = np.asarray(x, np.uint32)
+    x = x ^ (x >> np.uint32(16))
+    x = x * np.uint32(0xBB67AE85)
+    x = x ^ (x >> np.uint32(15))
+    x = x * np.uint32(0x9E3779B1)
+    return x ^ (x >> np.uint32(16))
+
+
+def rounding_bits(step: int, n: int, block: int = 256):
+    """(for m, for the root of v): the fractions in [0, 1) that step number `step` rounds the codes of n elements of a tensor with, multiples of 2^-20."""
+    with np.errstate(over="ignore"):
+        at = np.arange(n, dtype=np.uint64)
+        seed = _mix(np.uint32(step & 0xFFFFFFFF) + _mix(np.uint32(step >> 32)))
+        x = _mix(seed + (at // block).astype(np.uint32) * np.uint32(0x9E3779B9)) + (at % block).astype(np.uint32) * np.uint32(0x9E3779B9)
+        x = (x ^ (x >> np.uint32(15))) * np.uint32(0xBB67AE85)
+        x = x ^ (x >> np.uint32(16))
+    return ((x & np.uint32(0xFFF)) * 256.0 + 128.0) * 2.0 ** -20, (x >> np.uint32(12)) * 2.0 ** -20
+
+
+def block_codes(x, block: int = 256, positive: bool = False, fractions=None):
     """(codes, scales) of x in blocks of E4M3 values: scale = largest magnitude / 448, nearest codes (as the values they stand for); positive: a
-    value above 0 has at least the smallest code.  Blocks whose largest magnitude is at most 2^-100 are zeros."""
+    value above 0 has at least the smallest code.  Blocks whose largest magnitude is at most 2^-100 are zeros.  fractions: in the place of the nearest code, of the two around a
+    magnitude the upper one where the part of the way that lies behind it and its fraction are 1 or more together."""
     x = np.asarray(x, np.float64).ravel()
     codes, scales = np.zeros_like(x), []
     for i in range(0, x.size, block):
@@ -564,5 +585,9 @@ def block_codes(x, block: int = 256, positive: bool = False):
             c = b * (448.0 / most)
             if positive:
                 c = np.where(c > 0, np.maximum(c, 2.0 ** -9), c)
-            codes[i:i + block] = F.quantise(c, F.FORMATS["e4m3"])
+            if fractions is None:
+                codes[i:i + block] = F.quantise(c, F.FORMATS["e4m3"])
+            else:
+                apart = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(c), 2.0 ** -6))) - 3)
+                codes[i:i + block] = np.sign(c) * np.minimum(np.floor(np.abs(c) / apart + fractions[i:i + block]) * apart, 448.0)
     return codes, np.array(scales)

@@ -121,6 +121,33 @@ __device__ __forceinline__ float warp_most(const float (&x)[8]) {
   return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
 }
 
+// Random bits for the rounding of states in 8 bits, from the number of the step and the element's place alone: a step that is made again rounds alike, on whatever path an element is
+// stepped and whatever else the call has.  mix() spreads every bit of its argument over all (shifts and products with odd numbers, each of which can be undone); a block's seed is mixed twice,
+// and what its elements make of it is one to one in the seed, so that each element's numbers are spread evenly whatever its neighbours' are.
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0xbb67ae85u;
+  x ^= x >> 15;
+  x *= 0x9e3779b1u;
+  return x ^ x >> 16;
+}
+__device__ __forceinline__ uint32_t step_seed(uint64_t step) { return mix((uint32_t)step + mix((uint32_t)(step >> 32))); }
+__device__ __forceinline__ uint32_t block_seed(uint32_t seed, uint32_t block) { return mix(seed + block * 0x9e3779b9u); }
+__device__ __forceinline__ uint32_t element_bits(uint32_t block_seed, uint32_t element) {
+  uint32_t x = block_seed + element * 0x9e3779b9u;
+  x ^= x >> 15;
+  x *= 0xbb67ae85u;
+  return x ^ x >> 16;
+}
+// x rounded to one of the two E4M3 values around it, up where the part of the way that lies behind it and r 2^-20 (r: 20 bits) are 1 or more together.  A float32 has 20 bits more than a normal
+// code: r is added to them, and they are dropped.  2^-6 is put under smaller magnitudes, whose codes are as far apart as those from 2^-6 on.  NaN stays; what is added to 448 is
+// dropped too, or taken back by the conversion.
+__device__ __forceinline__ float round_randomly(float x, uint32_t r) {
+  const float under = fabsf(x) < 0x1p-6f ? copysignf(0x1p-6f, x) : 0.f;
+  const float y = __uint_as_float((__float_as_uint(x + under) + r) & 0xfff00000u) - under;
+  return fabsf(x) <= 512.f ? y : x;
+}
+
 // Four codes of roots above or at zero; one that is above zero has at least the smallest code.
 __device__ __forceinline__ uint32_t root_codes4(const float* x) {
   uint32_t w = cvt_fp8x4<false>(x[0], x[1], x[2], x[3]);
@@ -152,13 +179,14 @@ __device__ __forceinline__ int64_t at(const AdamTensor& t, const Place& w, int o
 struct AdamStep {
   float beta1, beta2, root_beta2, gm, gv, eps, lr, rate;
   float grad_factor, rest1;
+  uint32_t seed;                                              // of this step's roundings
 };
 
 // The step of a lane's eight elements; sm, sv: the scales of states in 8 bits, whose codes m and v are (v's root).  Afterwards m is what is stored, and v, or where EIGHT root,
-// codes before their rounding; the block's scales are written.
-template <bool EIGHT>
+// codes before their rounding (RANDOM: after it); the block's scales are written.  element(i): the place in its block of the lane's element i.
+template <bool EIGHT, bool RANDOM, class F>
 __device__ __forceinline__ void step8(const AdamStep& a, const AdamTensor& t, uint32_t block, int lane, float sm, float sv, float (&p)[8], const float (&g)[8], float (&m)[8],
-                                      float (&v)[8], float (&root)[8]) {
+                                      float (&v)[8], float (&root)[8], F element) {
   const f32x2 rate = splat2(-(a.rate * t.lr_factor)), decay = splat2(-(a.lr * t.lr_factor * t.decay));
   const f32x2 keep_v = splat2(EIGHT ? a.root_beta2 * sv : a.beta2), gm = splat2(a.gm), gv = splat2(a.gv), eps = splat2(a.eps);
 #pragma unroll
@@ -200,6 +228,15 @@ __device__ __forceinline__ void step8(const AdamStep& a, const AdamTensor& t, ui
     for (int i = 0; i < 8; i += 2) {
       unpack2(mul2(pack2(m[i], m[i + 1]), inv_m), m[i], m[i + 1]);
       unpack2(mul2(pack2(root[i], root[i + 1]), inv_v), root[i], root[i + 1]);
+    }
+    if (RANDOM) {
+      const uint32_t seed = block_seed(a.seed, block);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t r = element_bits(seed, (uint32_t)element(i));
+        m[i] = round_randomly(m[i], (r << 8 & 0xfff00u) | 0x80u);     // (12 bits are enough for what a step changes of m)
+        root[i] = root[i] > 0.f ? round_randomly(fmaxf(root[i], 0x1p-9f), r >> 12) : root[i];
+      }
     }
   }
 }
@@ -258,7 +295,7 @@ __device__ __forceinline__ void fetch_unit(const AdamTensor& t, uint32_t unit, i
 }
 
 // What a block's step leaves, to its tensor.
-template <bool EIGHT>
+template <bool EIGHT, bool RANDOM>
 __device__ __forceinline__ void store_block(const AdamTensor& t, int64_t base, int lane, float* row, const float (&p)[8], const float (&m)[8], const float (&v)[8],
                                             const float (&root)[8]) {
 #pragma unroll
@@ -266,7 +303,8 @@ __device__ __forceinline__ void store_block(const AdamTensor& t, int64_t base, i
     const int off = 128 * k + 4 * lane;
     store4<US_F32>(t.p, base + off, &p[4 * k]);
     store4<EIGHT ? US_E4M3 : US_F32>(t.m, base + off, &m[4 * k]);
-    if (EIGHT) *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + base + off) = root_codes4(&root[4 * k]);
+    if (RANDOM) store4<US_E4M3>(t.v, base + off, &root[4 * k]);
+    else if (EIGHT) *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + base + off) = root_codes4(&root[4 * k]);
     else store4<US_F32>(t.v, base + off, &v[4 * k]);
   }
   if (!t.copy) return;
@@ -292,9 +330,10 @@ __device__ __forceinline__ void store_block(const AdamTensor& t, int64_t base, i
 
 // A whole unit of a tensor whose pieces are aligned, from its tensor or (EIGHT) from the slot; `refill` starts the copies that take the slot next, once the warp
 // has read what is there.
-template <bool EIGHT, int GRAD, class F>
+template <bool EIGHT, bool RANDOM, int GRAD, class F>
 __device__ __forceinline__ void unit_step(const AdamStep& a, const AdamTensor& t, uint32_t unit, int lane, const char* slot, float* row, F refill) {
   using Grads = std::conditional_t<GRAD == US_F32, float4, uint2>;
+  const auto element = [&](int i) { return 4 * lane + (i < 4 ? i : 124 + i); };
   if constexpr (EIGHT) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -312,8 +351,8 @@ __device__ __forceinline__ void unit_step(const AdamStep& a, const AdamTensor& t
         __syncwarp();
         refill();
       }
-      step8<true>(a, t, 2 * unit + j, lane, sm, sv, p, g, m, v, root);
-      store_block<true>(t, (int64_t)unit * kPair + kUnit * j, lane, row, p, m, v, root);
+      step8<true, RANDOM>(a, t, 2 * unit + j, lane, sm, sv, p, g, m, v, root, element);
+      store_block<true, RANDOM>(t, (int64_t)unit * kPair + kUnit * j, lane, row, p, m, v, root);
     }
   } else {
     const int64_t base = (int64_t)unit * kUnit;
@@ -335,8 +374,8 @@ __device__ __forceinline__ void unit_step(const AdamStep& a, const AdamTensor& t
       four(m4[k], US_F32, &m[4 * k]);
       four(v4[k], US_F32, &v[4 * k]);
     }
-    step8<false>(a, t, unit, lane, 0.f, 0.f, p, g, m, v, root);
-    store_block<false>(t, base, lane, row, p, m, v, root);
+    step8<false, false>(a, t, unit, lane, 0.f, 0.f, p, g, m, v, root, element);
+    store_block<false, false>(t, base, lane, row, p, m, v, root);
   }
 }
 
@@ -350,7 +389,7 @@ __device__ __forceinline__ float one(uint8_t x) { return unpack_fp8x2(x, false).
 
 // Any block: a lane has every 32nd element.  All are fetched before the first is converted, since a tensor's last block is often the last to end (one by one: three vectors of
 // 1000 and one of 77 took 8.3 us, now 4.9; with states in 8 bits 14.6 and 8.7).
-template <bool EIGHT, int GRAD>
+template <bool EIGHT, bool RANDOM, int GRAD>
 __device__ __forceinline__ void block_step_any(const AdamStep& a, const AdamTensor& t, uint32_t block, int lane) {
   const int64_t base = (int64_t)block * kUnit;
   const int here = (int)min((int64_t)kUnit, t.n - base);     // elements of this block
@@ -378,7 +417,7 @@ __device__ __forceinline__ void block_step_any(const AdamStep& a, const AdamTens
     v[i] = is ? one<US_E4M3>(v1[i]) : 0.f;
   }
   float root[8];
-  step8<EIGHT>(a, t, block, lane, sm, sv, p, g, m, v, root);
+  step8<EIGHT, RANDOM>(a, t, block, lane, sm, sv, p, g, m, v, root, [&](int i) { return 32 * i + lane; });
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int off = 32 * i + lane;
@@ -393,19 +432,20 @@ __device__ __forceinline__ void block_step_any(const AdamStep& a, const AdamTens
 
 // Out of line, so that the kernel's own registers stay in place: with states in 8 bits one call, which has the choice of the type in it (a call for each type: 528 us in the
 // place of 524 for 201 million parameters), with states in 32 bits one for each type (4.9 us in the place of 5.3 for half a million).
-template <bool EIGHT, int GRAD>
+template <bool EIGHT, bool RANDOM, int GRAD>
 __device__ __noinline__ void unit_step_any(AdamStep a, const AdamTensor& t, uint32_t unit, int lane) {
   if constexpr (EIGHT) {
     with_grad_type(t.g_dt, [&](auto dt) {
-      for (uint32_t block = 2 * unit; block < 2 * unit + 2 && (int64_t)block * kUnit < t.n; ++block) block_step_any<true, decltype(dt)::value>(a, t, block, lane);
+      for (uint32_t block = 2 * unit; block < 2 * unit + 2 && (int64_t)block * kUnit < t.n; ++block) block_step_any<true, RANDOM, decltype(dt)::value>(a, t, block, lane);
     });
   } else {
-    block_step_any<false, GRAD>(a, t, unit, lane);
+    block_step_any<false, false, GRAD>(a, t, unit, lane);
   }
 }
 
-// EIGHT: tensors with states in 8 bits, else those in 32.
-template <bool EIGHT, int MOST>
+// EIGHT: tensors with states in 8 bits (RANDOM: rounded randomly, else to the nearest code), else those in 32.  (The random bits and the rounding: 201 million parameters 655 us in the
+// place of 499, bound by instructions; with three CTAs an SM and fewer spilled registers 680.)
+template <bool EIGHT, bool RANDOM, int MOST>
 __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const __grid_constant__ AdamArgs<MOST> a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ int64_t made;
@@ -422,6 +462,7 @@ __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const
   s.beta1 = a.beta1; s.beta2 = a.beta2; s.root_beta2 = a.root_beta2;
   s.gm = a.rest1 * grad_factor; s.gv = a.root_rest2 * grad_factor;
   s.grad_factor = grad_factor; s.rest1 = a.rest1;
+  s.seed = RANDOM ? step_seed((uint64_t)step) : 0u;
   s.eps = fmaxf(a.eps * root_fix2, 0x1p-126f);               // (0 x 1 / 0 where an element has had no gradient)
   s.lr = a.lr * lr_factor;
   s.rate = s.lr * root_fix2 / fix1;
@@ -471,11 +512,11 @@ __global__ void __launch_bounds__(kThreads, adam_ctas(EIGHT)) adamw_kernel(const
       const AdamTensor& t = a.t[cur];
       const uint32_t i = in_tensor(unit, cur);
       if (whole(t, i)) {
-        with_grad_type(t.g_dt, [&](auto dt) { unit_step<EIGHT, decltype(dt)::value>(s, t, i, lane, slot, row, refill); });
+        with_grad_type(t.g_dt, [&](auto dt) { unit_step<EIGHT, RANDOM, decltype(dt)::value>(s, t, i, lane, slot, row, refill); });
       } else {
         refill();
-        if constexpr (EIGHT) unit_step_any<true, 0>(s, t, i, lane);
-        else with_grad_type(t.g_dt, [&](auto dt) { unit_step_any<false, decltype(dt)::value>(s, t, i, lane); });
+        if constexpr (EIGHT) unit_step_any<true, RANDOM, 0>(s, t, i, lane);
+        else with_grad_type(t.g_dt, [&](auto dt) { unit_step_any<false, false, decltype(dt)::value>(s, t, i, lane); });
       }
     }
     if (threadIdx.x == 0) {
@@ -643,7 +684,8 @@ us_status check_tensor(const us_adamw_tensor& t) {
   if (!isfinite(t.copy_scale) || !isfinite(t.lr_factor) || !isfinite(t.weight_decay)) return US_ERR_INVALID_ARG;
   const bool small = t.m.dtype == US_E4M3;
   if (t.param.dtype != US_F32 || !is_grad(t.grad.dtype) || t.m.dtype != t.v.dtype || (!small && t.m.dtype != US_F32)) return US_ERR_UNSUPPORTED;
-  if (n > kMostElements || !dense(t.m) || !dense(t.v)) return US_ERR_UNSUPPORTED;
+  if (t.rounding != US_ROUND_NEAREST && t.rounding != US_ROUND_RANDOM) return US_ERR_INVALID_ARG;
+  if (n > kMostElements || !dense(t.m) || !dense(t.v) || (!small && t.rounding == US_ROUND_RANDOM)) return US_ERR_UNSUPPORTED;
   if (small) {
     for (const us_mat* m : {&t.m_scale, &t.v_scale}) {
       const us_status s = check_mat(*m);
@@ -686,7 +728,7 @@ AdamTensor describe(const us_adamw_tensor& t) {
   return d;
 }
 
-template <bool EIGHT, int MOST>
+template <bool EIGHT, bool RANDOM, int MOST>
 us_status launch_adamw(AdamArgs<MOST>& a, const us_adamw_tensor* const* ts, int count, cudaStream_t stream) {
   const int sms = host::sm_count();
   if (sms <= 0) return US_ERR_CUDA;
@@ -702,7 +744,7 @@ us_status launch_adamw(AdamArgs<MOST>& a, const us_adamw_tensor* const* ts, int 
   a.units = (uint32_t)units;
   const int grid = (int)std::min<uint64_t>((units + kWarps - 1) / kWarps, (uint64_t)(sms * adam_ctas(EIGHT)));
   static std::atomic<uint64_t> smem_set{0};
-  return host::launch(adamw_kernel<EIGHT, MOST>, &smem_set, grid, kThreads, kWarps * warp_bytes(EIGHT), 1, stream, a);
+  return host::launch(adamw_kernel<EIGHT, RANDOM, MOST>, &smem_set, grid, kThreads, kWarps * warp_bytes(EIGHT), 1, stream, a);
 }
 
 template <class A>
@@ -750,34 +792,36 @@ extern "C" us_status us_adamw(int count, const us_adamw_tensor* tensors, double 
     if (s != US_OK) return s;
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // Launches: the tensors with states in 32 bits, then those in 8, as many to one as its table holds.  The last launch counts the step.
-  auto go = [&](auto& a, auto eight, const us_adamw_tensor* const* ts, int n, bool last) {
+  // Launches: the tensors with states in 32 bits, then those in 8, rounded to the nearest code, then randomly; as many to one as its table holds.  The last launch counts the step.
+  auto go = [&](auto& a, auto kind, const us_adamw_tensor* const* ts, int n, bool last) {
     set_options(a, lr, beta1, beta2, eps, lr_factor, grad_factor, step);
     a.last = last;
-    return launch_adamw<decltype(eight)::value>(a, ts, n, st);
+    return launch_adamw<(decltype(kind)::value > 0), (decltype(kind)::value > 1)>(a, ts, n, st);
   };
-  auto table = [&](auto eight, const us_adamw_tensor* const* ts, int n, bool last) {
+  auto table = [&](auto kind, const us_adamw_tensor* const* ts, int n, bool last) {
     if (n <= kFew) {
       AdamArgs<kFew> a;
-      return go(a, eight, ts, n, last);
+      return go(a, kind, ts, n, last);
     }
     AdamArgs<kMany> a;
-    return go(a, eight, ts, n, last);
+    return go(a, kind, ts, n, last);
   };
-  auto is_eight = [](const us_adamw_tensor& t) { return t.m.dtype == US_E4M3; };
-  int64_t left[2] = {0, 0};                                  // tensors with elements, not launched yet
+  auto kind_of = [](const us_adamw_tensor& t) { return t.m.dtype != US_E4M3 ? 0 : t.rounding == US_ROUND_RANDOM ? 2 : 1; };
+  int64_t left[3] = {0, 0, 0};                               // tensors with elements, not launched yet
   for (int i = 0; i < count; ++i)
-    if (elements(tensors[i].param) > 0) ++left[is_eight(tensors[i])];
-  if (left[0] + left[1] == 0) return us::host::launch(count_step_kernel, nullptr, 1, 32, 0, 1, st, step, grad_factor);
+    if (elements(tensors[i].param) > 0) ++left[kind_of(tensors[i])];
+  if (left[0] + left[1] + left[2] == 0) return us::host::launch(count_step_kernel, nullptr, 1, 32, 0, 1, st, step, grad_factor);
   const us_adamw_tensor* ts[kMany];
-  for (int eight = 0; eight < 2; ++eight) {
-    for (int i = 0, n = 0; left[eight] > 0; ++i) {
-      if (elements(tensors[i].param) == 0 || is_eight(tensors[i]) != (eight == 1)) continue;
+  for (int kind = 0; kind < 3; ++kind) {
+    for (int i = 0, n = 0; left[kind] > 0; ++i) {
+      if (elements(tensors[i].param) == 0 || kind_of(tensors[i]) != kind) continue;
       ts[n++] = &tensors[i];
-      if (n < kMany && n < left[eight]) continue;
-      left[eight] -= n;
-      const bool last = left[0] + left[1] == 0;
-      const us_status s = eight ? table(std::true_type(), ts, n, last) : table(std::false_type(), ts, n, last);
+      if (n < kMany && n < left[kind]) continue;
+      left[kind] -= n;
+      const bool last = left[0] + left[1] + left[2] == 0;
+      const us_status s = kind == 0   ? table(std::integral_constant<int, 0>(), ts, n, last)
+                          : kind == 1 ? table(std::integral_constant<int, 1>(), ts, n, last)
+                                      : table(std::integral_constant<int, 2>(), ts, n, last);
       if (s != US_OK) return s;
       n = 0;
     }

@@ -63,10 +63,11 @@ class us_linear_call(C.Structure):
 
 class us_adamw_tensor(C.Structure):
     _fields_ = [(n, us_mat) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + \
-               [(n, C.c_float) for n in ("copy_scale", "lr_factor", "weight_decay")]
+               [(n, C.c_float) for n in ("copy_scale", "lr_factor", "weight_decay")] + [("rounding", C.c_int32)]
 
 
 US_OP_FWD, US_OP_BWD_X, US_OP_BWD_W = 0, 1, 2
+US_ROUND_NEAREST, US_ROUND_RANDOM = 0, 1
 
 
 class UnitScaleError(RuntimeError):
@@ -1003,13 +1004,15 @@ def us_grad_norm(grads, max_norm, out, ws, stream=None):
 ADAMW_BLOCK = 256                                             # elements that share a scale of states in 8 bits
 
 
-def adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, copy_scale=1.0, weight_decay=0.0, lr_factor=1.0):
+def adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, copy_scale=1.0, weight_decay=0.0, lr_factor=1.0,
+                  rounding=US_ROUND_NEAREST):
     """The tensors of a us_adamw call, laid out once: lists with an entry per tensor (1-D tensors are rows).  m_scale, v_scale: for states in 8 bits, else
-    None or a list with Nones; copies: None, or a list with Nones; copy_scale, weight_decay, lr_factor: numbers or lists."""
+    None or a list with Nones; copies: None, or a list with Nones; copy_scale, weight_decay, lr_factor: numbers or lists; rounding: US_ROUND_NEAREST or
+    US_ROUND_RANDOM, of states in 8 bits (US_ROUND_RANDOM for a training run), or a list."""
     n = len(params)
     each = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n
     columns = [list(params), list(grads), list(m), list(v), each(m_scale), each(v_scale), each(copies)]
-    numbers = [each(copy_scale), each(lr_factor), each(weight_decay)]
+    numbers = [each(copy_scale), each(lr_factor), each(weight_decay), each(rounding)]
     if any(len(c) != n for c in columns + numbers):
         raise ValueError("one entry per tensor is wanted")
     written = [t.data_ptr() for i in (0, 2, 3, 4, 5, 6) for t in columns[i] if t is not None and t.numel()]
@@ -1018,7 +1021,7 @@ def adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, 
     arr = (us_adamw_tensor * n)()
     _fill(arr, columns)
     for a, *a_numbers in zip(arr, *numbers):
-        a.copy_scale, a.lr_factor, a.weight_decay = a_numbers
+        a.copy_scale, a.lr_factor, a.weight_decay, a.rounding = a_numbers
     return arr
 
 

@@ -6,7 +6,7 @@ takes them as they are: step(X, None, None, G)), so that no cast of the weights 
     block = ffn.UnitScaledBiasFFN(T, d, f)
     block.cast_weights(W1, W2)
     opt = optim.AdamW([W1, W2, block.b1, block.b2], [block.dW1, block.dW2, block.db1, block.db2], lr=..., weight_decay=[0.01, 0.01, 0, 0],
-                      copies=[block.W1q, block.W2q, None, None], states="8bit", max_norm=1.0)
+                      copies=[block.W1q, block.W2q, None, None], states="8bit", rounding="random", max_norm=1.0)
     for ...:
         block.step(X, None, None, G)
         opt.step()
@@ -25,13 +25,19 @@ from . import lib as L
 
 class AdamW:
     """params: float32 CUDA matrices and vectors, updated in place; grads: their gradients (float32, bfloat16 or float16), the same tensors in every step; copies: None or a
-    list of operands (or Nones) of the parameters' shapes; weight_decay: a number or one per tensor; states: "32bit" or "8bit"."""
+    list of operands (or Nones) of the parameters' shapes; weight_decay: a number or one per tensor; states: "32bit" or "8bit".
+
+    rounding: of states in 8 bits, "nearest" or "random" (up or down with the probabilities that keep the mean, alike in every run).  Take "random" to train with usual betas: to
+    the nearest code, a state that a step changes by less than 3 to 6 % does not change at all, so that with beta2 = 0.999 an element whose gradients become ten times smaller than
+    its block's others keeps its denominator, and its steps stay many times too small."""
 
     def __init__(self, params, grads, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, copies=None, states: str = "32bit",
-                 max_norm: float | None = None, lr_factor: torch.Tensor | None = None):
+                 max_norm: float | None = None, lr_factor: torch.Tensor | None = None, rounding: str = "nearest"):
         self.params, self.grads = list(params), list(grads)
         if states not in ("32bit", "8bit"):
             raise ValueError("states: 32bit or 8bit")
+        if rounding not in ("nearest", "random") or (rounding == "random" and states != "8bit"):
+            raise ValueError("rounding of states in 8 bits: nearest or random")
         if not self.params or len(self.grads) != len(self.params) or any(g.shape != p.shape for g, p in zip(self.grads, self.params)):
             raise ValueError("one gradient of the parameter's shape per parameter is wanted")
         if any(p.dtype is not torch.float32 for p in self.params):
@@ -42,7 +48,7 @@ class AdamW:
         if len(self.copies) != n or len(self.weight_decay) != n:
             raise ValueError("one entry per parameter is wanted")
         self.lr, self.betas, self.eps, self.max_norm, self.states, self.lr_factor = lr, tuple(betas), eps, max_norm, states, lr_factor
-        eight = states == "8bit"
+        eight, self._rounding = states == "8bit", L.US_ROUND_RANDOM if rounding == "random" else L.US_ROUND_NEAREST
         state = lambda p: torch.zeros(p.shape, dtype=torch.uint8 if eight else torch.float32, device=p.device).view(torch.float8_e4m3fn if eight else torch.float32)
         scale = lambda p: torch.zeros(-(-p.numel() // L.ADAMW_BLOCK), dtype=torch.float32, device=p.device) if eight else None
         self.m, self.v = [state(p) for p in self.params], [state(p) for p in self.params]
@@ -59,7 +65,8 @@ class AdamW:
         """The descriptions of all tensors, made anew where one of them, or its decay, is another."""
         tensors, decay = self._tensors(), tuple(self.weight_decay)
         if self._laid_out is None or self._laid_out[0] != decay or not _binding.unchanged(tensors, *self._laid_out[1:3]):
-            plan = L.adamw_tensors(self.params, self.grads, self.m, self.v, self.m_scale, self.v_scale, self.copies, weight_decay=self.weight_decay)
+            plan = L.adamw_tensors(self.params, self.grads, self.m, self.v, self.m_scale, self.v_scale, self.copies, weight_decay=self.weight_decay,
+                                   rounding=self._rounding)
             self._laid_out = decay, tensors, tuple(t.data_ptr() for t in tensors), plan, L.mats(self.grads)
         return self._laid_out[3:]
 
