@@ -145,7 +145,8 @@ us_status us_linear_fwd_cast(const us_mat* X, const us_mat* W, float alpha, cons
  *   v = alpha * acc + bias      in float32, rounded once; then aux, activation, skip and Y as us_epilogue says
  *
  * Forward activations (or none), with a kept pre-activation and with a skip tensor or without; Yq: NULL, or the FP8 copy of us_linear_fwd_cast
- * under its conditions.  With a bias the pre-activation that aux keeps holds it, so the backward pass is that of a layer without one
+ * under its conditions.  tanh and sigmoid into US_F32 are those of us_linear_fwd (a last bit may differ; tanh of arguments below 1/8 has all its
+ * digits); into 16 and 8 bits they are off by 2^-20 and |z| 2^-22 of the value (tanh from 1/8 on: 2^-19) before its rounding.  With a bias the pre-activation that aux keeps holds it, so the backward pass is that of a layer without one
  * (us_linear_bwd_x, us_linear_bwd_w) and us_bias_grad.  The US_ACT_*_GRAD activations: US_ERR_UNSUPPORTED; everything else as for us_linear_fwd. */
 us_status us_linear_fwd_bias(const us_mat* X, const us_mat* W, float alpha, const us_mat* bias, const us_epilogue* ep, const us_mat* Y,
                              const us_mat* Yq, void* ws, size_t ws_bytes, void* stream);

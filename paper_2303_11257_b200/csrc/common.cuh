@@ -273,14 +273,28 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return r;
 }
 // Two values at a time: x holds pre-activations, nl2 = splat(-act_in log2 e).
-// sigmoid(act_in x) = 1 / (1 + e^-z): relative error of a few 2^-22 and |z| 2^-23, far inside a step of 16 and 8 bits; results in 32 bits have it.
+// sigmoid(act_in x) = 1 / (1 + e^-z): relative error of a few 2^-22 and |z| 2^-23 log2 e (of z = -80 2^-16), far inside a step of 16 and 8 bits.
 __device__ __forceinline__ f32x2 sigmoid2(f32x2 x, f32x2 nl2) {
   float p0, p1;
   unpack2(mul2(x, nl2), p0, p1);
   unpack2(add2(pack2(ex2_approx(p0), ex2_approx(p1)), splat2(1.0f)), p0, p1);
   return pack2(rcp_approx(p0), rcp_approx(p1));
 }
-// tanh(z) = 2 s - 1 with s = sigmoid(2 z), which cancels near zero: there z - z^3 / 3 + 2 z^5 / 15, whose next term is 2^-22 of it at 1/8.
+// sigmoid_f of two values, for results in 32 bits: 1 / (1 + e^-|z|), whose divisor is at most 2, by an approximate reciprocal and one step of Newton's iteration, r + r (1 - d r): the quotient but
+// for a last bit now and then.
+__device__ __forceinline__ f32x2 sigmoid2_full(f32x2 z) {
+  float z0, z1, d0, d1;
+  unpack2(z, z0, z1);
+  unpack2(mul2(pack2(fabsf(z0), fabsf(z1)), splat2(-1.4426950408889634f)), d0, d1);
+  const f32x2 e = pack2(ex2_approx(d0), ex2_approx(d1)), d = add2(e, splat2(1.0f));
+  unpack2(d, d0, d1);
+  const f32x2 r = pack2(rcp_approx(d0), rcp_approx(d1)), s = fma2(r, fma2(mul2(d, splat2(-1.0f)), r, splat2(1.0f)), r);
+  float s0, s1, t0, t1;
+  unpack2(s, s0, s1);
+  unpack2(mul2(e, s), t0, t1);
+  return pack2(z0 >= 0.f ? s0 : t0, z1 >= 0.f ? s1 : t1);
+}
+// tanh(z) = 2 s - 1 with s = sigmoid(2 z), whose error is one of s (of values near 1/8 up to 2^-18) and which cancels near zero: below 1/8 z - z^3 / 3 + 2 z^5 / 15, whose next term is 2^-22 of it at 1/8.
 __device__ __forceinline__ f32x2 tanh2(f32x2 z, f32x2 s) {
   float z0, z1, f0, f1, n0, n1;
   const f32x2 zz = mul2(z, z);

@@ -559,7 +559,8 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
               for (int k = 0; k < 16; ++k) gelu_scaled2<false>(pack2(y[2 * k], y[2 * k + 1]), tail_k, act_oi, y[2 * k], y[2 * k + 1]);
             }
           } else if constexpr (BIAS) {                          // relu, tanh, sigmoid (table section "Activations"), this choice too once per slice
-            // (in pairs with approximate reciprocals, a few 2^-22 of the value: BF16 8192 x 1024 -> 4096 sigmoid 98 -> 61 us)
+            // (into 16 and 8 bits in pairs with approximate reciprocals, whose errors (sigmoid2, tanh2) are far below a step of the result: BF16 8192 x 1024 -> 4096 sigmoid 98 -> 61 us.  Results in 32
+            // bits have all of their digits, as they have without a bias: F32 sigmoid 60.6 us with approximate reciprocals, 63.3 so, 88.5 with divisions.)
             const f32x2 nl2 = splat2(-1.4426950408889634f * p.act_in), out2 = splat2(p.act_out);
             auto all = [&](auto value) {
 #pragma unroll
@@ -571,6 +572,15 @@ __device__ __forceinline__ void epilogue_staged(const GemmParams& p, const CUten
                 unpack2(mul2(x, in2), a, b);
                 return pack2(relu_f(a), relu_f(b));
               });
+            } else if (out_dt == US_F32) {
+              if (p.fn == US_FN_TANH) {
+                all([&](f32x2 x) {
+                  const f32x2 z = mul2(x, in2);
+                  return tanh2(z, sigmoid2_full(add2(z, z)));
+                });
+              } else {
+                all([&](f32x2 x) { return sigmoid2_full(mul2(x, in2)); });
+              }
             } else if (p.fn == US_FN_TANH) {
               all([&](f32x2 x) { return tanh2(mul2(x, in2), sigmoid2(x, add2(nl2, nl2))); });
             } else {
