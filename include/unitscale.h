@@ -645,7 +645,7 @@ us_status us_bias_grad(int count, const us_mat* G, const float* beta, const us_m
  * us_grad_norm: out[0] = norm = sqrt(sum of the squares of all elements of all matrices), out[1] = min(1, max_norm / norm), the factor that
  * clips them to max_norm (positive; INFINITY: no clipping); where the norm is not finite, out[1] is NaN.  grads: host array of count (any
  * number from 1 on) F32, BF16 or F16 matrices, any ld >= cols, natural alignment.  out: two float32 in device memory.  Squares are added
- * in float32 eight at a time, then in float64, in an order that depends on the sizes and the device alone.  ws: device workspace of
+ * in float32 eight at a time (in float64 where they leave its range), then in float64, in an order that depends on the sizes and the device alone.  ws: device workspace of
  * us_grad_norm_workspace_bytes() bytes, 16-byte aligned, zeroed once by the caller before its first use, that no call at the same time
  * uses.  One launch for up to 640 matrices.
  */

@@ -591,12 +591,19 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
         float x[32];
 #pragma unroll
         for (int k = 0; k < 8; ++k) load4<decltype(dt)::value>(t.g, base + 128 * k + 4 * lane, &x[4 * k]);
+        float s[4] = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          float s = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s = fmaf(x[8 * k + i], x[8 * k + i], s);
-          sum += (double)s;
+          for (int i = 0; i < 8; ++i) s[k] = fmaf(x[8 * k + i], x[8 * k + i], s[k]);
+        }
+        const float all = (s[0] + s[1]) + (s[2] + s[3]);
+        if (decltype(dt)::value == US_F16 || (all >= 0x1p-80f && all < INFINITY)) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum += (double)s[k];
+        } else {                                               // squares beyond float32's range, or below it with no larger one beside them
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sum += (double)x[i] * (double)x[i];
         }
       });
     } else {
@@ -616,7 +623,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
             x[k] = load_one(t.g, decltype(dt)::value, i);
           }
 #pragma unroll
-          for (int k = 0; k < 8; ++k) sum += first + 32 * k < here ? (double)(x[k] * x[k]) : 0.0;
+          for (int k = 0; k < 8; ++k) sum += first + 32 * k < here ? (double)x[k] * (double)x[k] : 0.0;
         }
       });
     }

@@ -1,6 +1,12 @@
-"""us_adamw at the edges of float32: the smallest eps and gradients that it accepts."""
+"""us_adamw at the edges of float32: the smallest eps and gradients that it accepts; us_grad_norm of elements whose squares leave its range."""
+import math
+
+import numpy as np
 import pytest
 import torch
+
+from tests import util as U
+from tests.test_gpu_optimizer import _check_norm, _norm, _place
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +63,25 @@ def test_a_learning_rate_beyond_float32_is_refused():
     with pytest.raises(L.UnitScaleError):
         L.us_adamw(plan, step, 1e39)
     assert torch.equal(p, before) and step.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("fmt,size", [("f32", 1e20), ("bf16", 1e20), ("f32", 3e36), ("f32", 1e-22), ("bf16", 1e-30), ("f32", 1e-38), ("f32", 1e-42), ("fp16", 6e-8), ("fp16", 6e4)])
+@pytest.mark.parametrize("shape,pad,shift", [((1, 3), 0, 0), ((1, 1024), 0, 0), ((5, 1031), 0, 0), ((7, 333), 5, 0), ((64, 256), 0, 3)])
+def test_norms_of_large_and_small_gradients(shape, pad, shift, fmt, size):
+    x = size * np.random.default_rng(5).uniform(0.5, 1.0, shape)
+    t, _ = _place(x, fmt, pad, shift)
+    wide = U.host_values(t)
+    want = math.sqrt(float((wide ** 2).sum()))
+    most = float(np.float32(1e-3 * want if want > 1e-38 else 1.0))      # (a float32 of the call)
+    n, f = _norm([t], most)
+    # (as the other norms; one below 2^-126 is a multiple of 2^-149)
+    assert abs(n - want) <= 6 * 2.0 ** -24 * want + 2.0 ** -150
+    assert abs(f - min(1.0, most / want)) <= 2.0 ** -24 * min(1.0, most / want) * 1.01
+
+
+def test_large_beside_small_and_norms_beyond_float32():
+    one, tiny, huge = (torch.full((4096,), v, device="cuda") for v in (1.0, 1e-30, 1e25))
+    for ts in ([one, tiny], [huge, one, tiny], [tiny, tiny[:77], huge[:5]]):
+        _check_norm([U.host_values(t.view(1, -1)) for t in ts], ts, 2.0)
+    n, f = _norm([torch.full((1024,), 3e38, device="cuda")])       # 9.6e39
+    assert n == math.inf and math.isnan(f)
