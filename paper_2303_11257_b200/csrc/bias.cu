@@ -2,7 +2,8 @@
 //
 // Bound by the bytes of G, which the matmuls around it have just written or read.  A cluster of CTAs shares a strip of columns 128 bytes
 // wide: each CTA sums its part of the rows (a thread 16 bytes of every 32nd row), the CTAs' sums meet in shared memory, and
-// every CTA finishes some of the strip's columns.  One launch, no workspace and no atomics.
+// every CTA finishes some of the strip's columns.  One launch, no workspace and no atomics.  The next grid is not released early (several CTAs an SM): captured steps of an FFN block with biases, us,
+// 256 x 128 x 512 13.6 -> 11.9, though 1000 x 528 x 2096 26.5 -> 27.4; in a row, 8192 x 4096 E5M2 7.3 -> 6.0, BF16 9.3 -> 7.4.
 #include <algorithm>
 
 #include "common.cuh"
@@ -149,7 +150,7 @@ __device__ __forceinline__ void strip_sums(const BiasPart& p, int strip, int64_t
 __global__ void __launch_bounds__(kThreads, 3) bias_grad_kernel(const __grid_constant__ BiasArgs a) {
   __shared__ float sums[kWarps][kStripBytes];
   __shared__ float mine[kStripBytes];
-  ptx::grid_sync_previous();
+  (void)ptx::grid_wait_previous();
   const int parts = (int)ptx::cluster_nctarank(), rank = (int)ptx::cluster_ctarank();
   int strip = blockIdx.x / parts, k = 0;
   while (strip >= a.part[k].strip_end) ++k;
