@@ -971,6 +971,12 @@ def _fill(arr, columns) -> None:
         arr._device = max(arr._device, device)
 
 
+def _expect(true: bool, what: str) -> None:
+    """An assertion that stays where Python drops those."""
+    if not true:
+        raise AssertionError(what)
+
+
 def _laid_out_here(arr, t: torch.Tensor) -> None:
     """Descriptions that are used with t have to be of its device, the current one."""
     _here(t)
@@ -993,7 +999,7 @@ def us_grad_norm_workspace_bytes() -> int:
 def us_grad_norm(grads, max_norm, out, ws, stream=None):
     """out (float32 CUDA tensor of two) = 2-norm of all gradients and the factor that clips them to max_norm; grads: a list of tensors, or what
     mats() made of it; ws: a uint8 CUDA tensor of us_grad_norm_workspace_bytes() bytes, zeroed before its first use."""
-    assert out.is_cuda and out.dtype is torch.float32 and out.numel() >= 2 and out.is_contiguous()
+    _expect(out.is_cuda and out.dtype is torch.float32 and out.numel() >= 2 and out.is_contiguous(), "out: two float32 in device memory")
     if not isinstance(grads, C.Array):
         grads = mats(grads)
     _laid_out_here(grads, out)
@@ -1032,8 +1038,9 @@ def new_adamw_step(made: int = 0, device="cuda") -> torch.Tensor:
 
 def us_adamw(tensors, step, lr, betas=(0.9, 0.999), eps=1e-8, lr_factor=None, grad_factor=None, stream=None):
     """One AdamW step over what adamw_tensors() laid out; step: new_adamw_step(); lr_factor, grad_factor: float32 CUDA tensors (one element is read), or None."""
-    assert step.is_cuda and step.dtype is torch.int64 and step.numel() == 2 and step.is_contiguous()
-    assert all(t is None or (t.is_cuda and t.dtype is torch.float32) for t in (lr_factor, grad_factor))
+    _expect(step.is_cuda and step.dtype is torch.int64 and step.numel() == 2 and step.is_contiguous(), "step: two 64-bit integers in device memory")
+    for t in (lr_factor, grad_factor):                            # (an empty tensor has no address and would be taken for None)
+        _expect(t is None or (t.is_cuda and t.dtype is torch.float32 and t.numel() > 0), "factors: float32 in device memory")
     _laid_out_here(tensors, step)
     _check("us_adamw", _entry("us_adamw")(len(tensors), tensors, lr, betas[0], betas[1], eps, lr_factor, grad_factor, step, _stream(stream)))
 

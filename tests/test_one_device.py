@@ -1,4 +1,8 @@
 """Linear ops with biases, gradients of biases, gradient norms and optimiser steps take CUDA tensors of one device, the current one: every argument is looked at, on the host."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -65,11 +69,11 @@ class OnDevice:
     """What the wrappers ask of a tensor."""
     is_cuda, device = True, "cuda:0"
 
-    def __init__(self, dtype):
-        self.dtype = dtype
+    def __init__(self, dtype, n=2):
+        self.dtype, self.n = dtype, n
 
     def numel(self):
-        return 2
+        return self.n
 
     def is_contiguous(self):
         return True
@@ -104,3 +108,30 @@ def test_host_memory_beside_device_memory():
         L.adamw_tensors([on(4)], [torch.ones(4)], [on(4)], [on(4)])
     L.us_linear_fwd_bias(x, w, 1.0, b, y, ws)                      # (and all of it on the device)
     assert torch.equal(y.float(), torch.full_like(y, 65.0).float())
+
+
+WITHOUT_ASSERTIONS = """
+import torch
+from paper_2303_11257_b200 import lib as L
+from tests.test_one_device import OnDevice
+L._current_device = lambda: 0
+arr, mats, step, out = (L.us_adamw_tensor * 1)(), (L.us_mat * 1)(), OnDevice(torch.int64), OnDevice(torch.float32)
+bad = [lambda: L.us_adamw(arr, OnDevice(torch.int32), 1e-3), lambda: L.us_adamw(arr, OnDevice(torch.int64, 1), 1e-3), lambda: L.us_grad_norm(mats, 1.0, OnDevice(torch.float32, 1), None),
+       lambda: L.us_grad_norm(mats, 1.0, OnDevice(torch.float64), None), lambda: L.us_adamw(arr, step, 1e-3, lr_factor=OnDevice(torch.float32, 0)),
+       lambda: L.us_adamw(arr, step, 1e-3, grad_factor=OnDevice(torch.float64)), lambda: L.us_adamw(arr, step, 1e-3, grad_factor=OnDevice(torch.float32, 0))]
+for i, call in enumerate(bad):
+    try:
+        call()
+    except AssertionError:
+        continue
+    except Exception as e:
+        print(i, type(e).__name__, e)
+    raise SystemExit(f"call {i} was not refused")
+"""
+
+
+@pytest.mark.parametrize("options", [[], ["-O"]])
+def test_arguments_are_looked_at_without_assertions_too(options):
+    """Records of other types and sizes, and factors without an element, which would be taken for none."""
+    r = subprocess.run([sys.executable, *options, "-c", WITHOUT_ASSERTIONS], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stdout + r.stderr
