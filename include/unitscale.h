@@ -685,8 +685,9 @@ us_status us_grad_norm(int count, const us_mat* grads, float max_norm, float* ou
  *
  * lr >= 0 and finite, 0 <= beta < 1, eps > 0 (also once rounded to float32).  Arithmetic in float32; 1 - beta and log(beta) are formed in float64;
  * eps sqrt(1 - beta2^t) counts as 2^-126 at least.  v is a float32 too: a sqrt(v) below 2^-63 has fewer digits than 24, and one below 2^-75 is zero.  Pointers
- * need the natural alignment of their elements; F32 tensors on 16-byte boundaries (copies, gradients and codes: of four elements), with rows that are dense
- * or of a multiple of four columns and so padded, are the fast ones.  One launch for up to 240 tensors; tensors without elements are skipped.
+ * need the natural alignment of their elements.  Fast are param and grad without padding, with all states on 16-byte boundaries (with states in 32 bits, gradients of
+ * 16 bits on 8-byte ones), and copies on boundaries of four elements that have no padding, or rows of four times any number of columns in any such pitch.
+ * One launch for up to 240 tensors whose states are alike (in 32 bits, in 8 and rounded alike); tensors without elements are skipped.
  */
 typedef enum { US_ROUND_NEAREST = 0, US_ROUND_RANDOM = 1 } us_rounding;
 typedef struct {

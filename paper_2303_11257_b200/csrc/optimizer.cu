@@ -6,12 +6,12 @@
 // memory has to be kept or written, and a captured launch holds its own.  The next grid is not released early (several CTAs an SM): captured norm and step of a small block 8.8 -> 7.5 us in 32 bits, 10.7 ->
 // 10.0 in 8; norms of 201 million elements 126 -> 118.
 //
-// Measured on 201 million parameters (a copy moves 6.46 TB/s on the same card): states in 32 bits, FP8 operands written, 29 bytes an element, 845 us = 6.9 TB/s; states
-// in 8 bits, BF16 gradients and operands, 16 bytes, 493 us = 6.5 TB/s, 520 to 530 under a load that holds the clock down: this one is bound by its instructions as
-// well, about 50 a lane and element.  What made the difference, in us (32 bits, 8 bits): the type of gradients and copies chosen once a block instead of for every
+// Measured on 201 million parameters (a copy moves 6.46 TB/s on the same card): states in 32 bits, FP8 operands written, 29 bytes an element, 841 us = 6.9 TB/s; states
+// in 8 bits, BF16 gradients and operands, 16 bytes, 489 us = 6.6 TB/s, 526 under a load that holds the clock down: this one is bound by its instructions as
+// well, 57 a lane and element.  What made the difference, in us (32 bits, 8 bits): the type of gradients and copies chosen once a block instead of for every
 // element (984 -> 974, 823 -> 599); a warp number that the compiler knows to be uniform, so that fields and addresses are worked out once a warp (974 -> 943);
 // chunks taken in order (943 -> 845; 599 -> 566); 8-bit blocks fetched ahead through shared memory, no register spilled (566 -> 501), in pairs and in pieces of 16
-// bytes (501 -> 495, under load 578 -> 519).  Gradient norms: 124 us for 806 MB, 64 in BF16.
+// bytes (501 -> 495, under load 578 -> 519).  Gradient norms: 118 us for 806 MB, 62 in BF16.
 #include <math.h>
 
 #include <algorithm>
@@ -62,12 +62,6 @@ struct AdamArgs {
 __device__ __forceinline__ float sqrt_approx(float x) {
   float r;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-// (Arguments below 2^-126 count as zero.)
-__device__ __forceinline__ float rcp_approx(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 

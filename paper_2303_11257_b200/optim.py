@@ -14,6 +14,9 @@ takes them as they are: step(X, None, None, G)), so that no cast of the weights 
 A step makes no synchronisation, and can be captured into a CUDA graph: the count of steps is kept on the device, as are the gradients' norm and the factor
 that clips them.  A schedule that a captured step is to follow goes through lr_factor, a float32 CUDA tensor whose first element multiplies lr.  A step whose gradients'
 norm is not finite changes nothing (with max_norm; float("inf") clips nothing).
+
+The tensors are described to the library once, and again whenever one of them is another or lies elsewhere.  That takes about 0.2 ms for 96 tensors, as much as the norm of small ones saves:
+keep the gradients' tensors, as the blocks do, and write into them.
 """
 from __future__ import annotations
 
