@@ -486,6 +486,7 @@ def us_linear_fwd(X, W, alpha, Y, ws, ep=None, stream=None):
 def us_linear_fwd_bias(X, W, alpha, bias, Y, ws, ep=None, Yq=None, stream=None):
     """us_linear_fwd of a layer with a bias (a vector), which is added to the scaled product; Yq: an FP8 copy of a residual's result."""
     _here(Y)
+    _described_here(ep)
     _check("us_linear_fwd_bias", _entry("us_linear_fwd_bias")(X, W, alpha, bias, ep, Y, Yq, ws, ws, _stream(stream)))
     return Y
 
@@ -529,6 +530,8 @@ def us_linear_group_bias(calls, biases, ws, stream=None):
     for b in biases:
         if b is not None:
             _here(b)
+    for c in calls:
+        _described_here(c)
     rows = [us_mat() if b is None else mat(b.view(1, -1) if b.dim() == 1 else b) for b in biases]
     _check("us_linear_group_bias", _entry("us_linear_group_bias")(len(calls), (us_linear_call * len(calls))(*calls), (us_mat * len(calls))(*rows), ws, ws, _stream(stream)))
 
@@ -948,6 +951,15 @@ def _here(t: torch.Tensor) -> None:
     device = t.get_device()
     if device < 0 or device != _current_device():
         raise ValueError(f"a tensor of {t.device}, which is not the current CUDA device")
+
+
+def _described_here(described) -> None:
+    """The same for the tensors that an epilogue or an entry of a group was made of, where it knows them."""
+    for t in getattr(described, "_keep_alive", ()):
+        if isinstance(t, us_epilogue):
+            _described_here(t)
+        elif t is not None:
+            _here(t)
 
 
 def us_bias_grad(G, beta, db, stream=None):

@@ -91,10 +91,33 @@ def test_what_was_laid_out_on_another_device_is_refused(monkeypatch):
             call(arr)
 
 
+@pytest.mark.parametrize("which", range(6))
+def test_tensors_of_epilogues_and_groups_are_looked_at(monkeypatch, which):
+    """Those that their descriptions were made of: kept pre-activation and skip tensor, operands and results."""
+    monkeypatch.setattr(L, "_current_device", lambda: 0)
+    monkeypatch.setattr(L, "describe", lambda t: (0x10000, BF, 8, 64, 64))
+    monkeypatch.setattr(L, "_entry", lambda name: lambda *a: 0)
+    monkeypatch.setattr(L, "_stream", lambda stream: 0)
+    t = [OnDevice(BF) for _ in range(6)]
+    X, W, Y, H, S, ws = t
+
+    def calls():
+        ep = L.epilogue(act=L.US_ACT_GELU, aux=t[3], skip=t[4])
+        L.us_linear_fwd_bias(X, W, 1.0, None, t[2], ws, ep)
+        L.us_linear_group_bias([L.linear_call(L.US_OP_FWD, t[0], t[1], 1.0, t[2], L.epilogue(skip=t[4]))], [None], t[5])
+    calls()
+    t[which] = torch.zeros(8, 64)
+    with pytest.raises(ValueError, match="current CUDA device"):
+        calls()
+
+
 @pytest.mark.gpu
 def test_host_memory_beside_device_memory():
     on = lambda *s: torch.ones(*s, device="cuda")
     x, w, y, b, ws = on(8, 64).bfloat16(), on(64, 64).bfloat16(), on(8, 64).bfloat16(), on(64), L.new_workspace()
+    for ep in (L.epilogue(act=L.US_ACT_GELU, aux=y.cpu()), L.epilogue(skip=y.cpu(), skip_coef=0.5, out_coef=0.5)):
+        with pytest.raises(ValueError):
+            L.us_linear_fwd_bias(x, w, 1.0, b, y, ws, ep)
     for args in ((x.cpu(), w, 1.0, b, y, ws), (x, w.cpu(), 1.0, b, y, ws), (x, w, 1.0, b.cpu(), y, ws), (x, w, 1.0, b, y, ws.cpu())):
         with pytest.raises(ValueError):
             L.us_linear_fwd_bias(*args)
