@@ -669,8 +669,8 @@ us_status us_grad_norm(int count, const us_mat* grads, float max_norm, float* ou
  *          block, without padding.  All zeros before the first step.
  *          US_ROUND_NEAREST  to the nearest code, which is 3 to 6 % off at most.  A state that a step changes by less than that keeps its code:
  *                            with beta2 above 0.94 the sqrt(v) of an element whose gradients become smaller than its neighbours' does not
- *                            fall (beta2 = 0.999 takes 0.05 % off it in a step), nor with beta1 above 0.94 its m, and its steps stay too
- *                            small.  For a training run with such factors, and 0.999 is the usual one, it is the wrong choice.
+ *                            fall (beta2 = 0.999 takes 0.05 % off it in a step), nor with beta1 above 0.94 its m (with 0.9 one of the four
+ *                            smallest codes), and its steps stay too small.  For a training run with such factors, and 0.999 is the usual one, it is the wrong choice.
  *          US_ROUND_RANDOM   to one of the two codes around it, up with the probability that keeps the mean (m in steps of 2^-12, sqrt(v) in steps
  *                            of 2^-20), so that states follow their averages however little a step changes them.  sqrt(v) is spread by
  *                            about 15 % around its average at beta2 = 0.999.  The random bits are made of the number of the step and

@@ -383,7 +383,7 @@ template <int DT>
 __device__ __forceinline__ float one(uint8_t x) { return unpack_fp8x2(x, false).x; }
 
 // Any block: a lane has every 32nd element.  All are fetched before the first is converted, since a tensor's last block is often the last to end (one by one: three vectors of
-// 1000 and one of 77 took 8.3 us, now 4.9; with states in 8 bits 14.6 and 8.7).
+// 1000 and one of 77 took 8.3 us, now 4.6; with states in 8 bits 14.6 and 9.0).
 template <bool EIGHT, bool RANDOM, int GRAD>
 __device__ __forceinline__ void block_step_any(const AdamStep& a, const AdamTensor& t, uint32_t block, int lane) {
   const int64_t base = (int64_t)block * kUnit;
